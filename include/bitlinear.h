@@ -360,6 +360,116 @@ bl_status bitlinear_block_forward(const void* x, int batch, int seq, int heads, 
                                   const bl_block_weights* w, const bl_block_buffers* buf, void* y, void* ws,
                                   size_t ws_bytes, void* stream);
 
+/* ---- attention at inference: positions, windows, a key/value cache held in 4 bits --------------
+ * What a BitNet decoder needs around its BitLinear layers to answer token by token (Sec. 2, Fig. 2b
+ * keeps this part in high precision; Sec. 2.1 leaves its form open).  Token rows are [T, heads *
+ * head_dim] with a row stride in elements, so inputs may be column blocks of one fused buffer; query
+ * head h reads key/value head h / (heads / kv_heads).  Types are BL_F16 and BL_BF16 unless said
+ * otherwise (BL_ERR_UNSUPPORTED), row strides multiples of 8.  Indices that live in device memory
+ * (positions, slots, page numbers, lengths) cannot be checked on the host: what each kernel does with
+ * one out of range is stated, and no access leaves the buffers described by the arguments. */
+
+/* Norm of each query and key head with the position rotation, in one pass:
+ *   x^ = w . x / sqrt(mean(x^2) + eps)   over the head's head_dim values (eps < 0: no norm, no weight)
+ *   (x^_a, x^_b) -> (x^_a cos t - x^_b sin t, x^_b cos t + x^_a sin t),   t = position . inv_freq[i]
+ * for the pairs i < rot_dim / 2: a = i, b = i + rot_dim / 2, or a = 2i, b = 2i + 1 when interleaved
+ * != 0; values from rot_dim on are only normalised.  fp32 throughout, angles reduced in fp64 (so far
+ * positions lose nothing), one rounding at the end.
+ *   q [T, heads * head_dim] stride ld_q, k [T, kv_heads * head_dim] stride ld_k, dtype dt (also BL_F32).
+ *   head_dim a multiple of 16, 16..256; rot_dim a multiple of 16, 0..head_dim.
+ *   wq, wk      [head_dim] of dtype dt, or NULL (ones).
+ *   inv_freq    fp32 [rot_dim / 2];  positions int32 [T]: a negative one marks a row of padding, whose
+ *               outputs are left as they were.
+ *   q_out, k_out  strides ld_qo, ld_ko; may be q, k themselves (same strides), else must not overlap them.
+ * T = 0 is valid and does nothing.  No workspace. */
+bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int64_t T, int heads, int kv_heads,
+                                 int head_dim, int64_t ld_q, int64_t ld_k, const void* wq, const void* wk,
+                                 float eps, int rot_dim, int interleaved, const float* inv_freq,
+                                 const int32_t* positions, void* q_out, void* k_out, int64_t ld_qo, int64_t ld_ko,
+                                 void* stream);
+
+/* Attention of prompts with a sliding window and sinks (first tokens that stay visible):
+ *   o_i = sum_j p_ij v_j,   p_i = softmax over the visible j of scale . q_i . k_j
+ * where position i sees j <= i with i - j < window or j < sinks (window <= 0: every j <= i).
+ *   batch sequences.  cu_q, cu_k: int32 [batch + 1] first rows of the sequences in q / o and in k / v
+ *   (packed prompts of different lengths), or NULL: sequence b owns rows b * seq_q .. (seq_k for keys).
+ *   cu_k may be NULL with cu_q given: the key rows are then those of cu_q.  seq_q, seq_k: the common
+ *   length, or with cu_* an upper bound of the lengths (rows of a sequence beyond it are not
+ *   processed).  rows_q, rows_k: rows present in q / o and k / v; entries of cu_* are clamped to them.
+ *   A sequence with fewer query rows than key rows has its queries at the last positions (a chunk
+ *   behind tokens that are already known); with more, the first ones see nothing.  A query that sees
+ *   nothing gets zeros.  Rows of o outside every sequence are left as they were.
+ *   head_dim 64 or 128; heads a multiple of kv_heads; scale 0 means 1 / sqrt(head_dim).
+ * Values in invisible places have no influence, whatever they are (infinities and NaN included).
+ * fp32 softmax statistics and accumulators; probabilities are rounded to the type of v for the
+ * product, and one rounding on output.  batch = 0 or seq_q = 0 is valid and does nothing.  No workspace. */
+bl_status bitlinear_attention_window(const void* q, const void* k, const void* v, void* o, bl_dtype dt, int batch,
+                                     const int32_t* cu_q, const int32_t* cu_k, int64_t seq_q, int64_t seq_k,
+                                     int64_t rows_q, int64_t rows_k, int heads, int kv_heads, int head_dim,
+                                     int64_t ld_q, int64_t ld_k, int64_t ld_v, int64_t ld_o, int window, int sinks,
+                                     float scale, void* stream);
+
+/* A paged key/value cache held in 4 bits: Eq. 6 with 4-bit codes, per token and head.
+ *   eta = min x,  step = (max x - min x) / 15  (both rounded to dtype),  code = clip(round((x - eta) /
+ *   step), 0, 15),  value = eta + step . code.  step == 0 stores code 0.  A row that holds a non-finite
+ *   value is stored as NaN (step and eta) as a whole.
+ * pages: num_pages x bitlinear_kv4_page_bytes() bytes; a page holds page_size tokens (16, 32 or 64) of all
+ * heads.  Within a page, head h owns page_size * (head_dim + 8) contiguous bytes:
+ *   key codes    [page_size][head_dim / 2]: byte j of a token holds values 2j (low nibble) and 2j + 1
+ *   value codes  [page_size / 8][8][4][head_dim / 32][2][2]: octet of tokens, eighth of the row, pair of
+ *                tokens, word, token of the pair, bytes: value d of token t sits in octet t / 8, eighth
+ *                d / (head_dim / 8), pair t % 8 / 2, word d % (head_dim / 8) / 4, token t % 2, nibble d % 4
+ *   key (step, eta) [page_size][2] of dtype, then value (step, eta) likewise.
+ * (The attention kernel's operands come out of these orders with one mask per pair of values.)
+ * A slot is page * page_size + place in the page. */
+typedef struct {
+  void* pages;
+  int64_t num_pages;
+  int page_size, kv_heads, head_dim;   /* head_dim 64 or 128 */
+  bl_dtype dtype;                      /* BL_F16 or BL_BF16: type of step and eta, and of the rows in and out */
+} bl_kv4_cache;
+
+/* Bytes of one page (0 if a size is not supported). */
+size_t bitlinear_kv4_page_bytes(int page_size, int kv_heads, int head_dim);
+
+/* Quantises T tokens' key and value rows (stride ld_k, ld_v, dtype of the cache) into the cache at
+ * slots int64 [T]; a slot outside the cache (e.g. -1: padding) is skipped.  No slot may appear twice in
+ * a call.  The codes are those of exact arithmetic on the rounded step and eta.  T = 0 does nothing. */
+bl_status bitlinear_kv4_append(const bl_kv4_cache* cache, const void* k, const void* v, int64_t T, int64_t ld_k,
+                               int64_t ld_v, const int64_t* slots, void* stream);
+
+/* The values the cache holds at slots int64 [T] (in any order, repeats allowed), rounded to its dtype;
+ * rows of k, v whose slot is outside the cache are left as they were.  T = 0 does nothing. */
+bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_t T, int64_t ld_k, int64_t ld_v,
+                             const int64_t* slots, void* stream);
+
+/* Attention of the last n_q tokens of each sequence over the cache (one token per step, or a few
+ * drafted ones being checked), with the visibility rule of bitlinear_attention_window.
+ *   q, o [batch * n_q, heads * head_dim] of the cache's dtype, strides ld_q, ld_o.
+ *   block_table int32 [batch, max_pages]: page of each run of page_size tokens.  Entries whose tokens
+ *   no query sees are not read; tokens of an entry outside 0..num_pages-1 are invisible.
+ *   lens int32 [batch]: tokens of the sequence in the cache, the n_q new ones included (clamped to
+ *   0..max_pages * page_size).  Query i of n_q stands at position lens - n_q + i; one that sees nothing
+ *   (negative position, empty sequence) gets zeros.
+ *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
+ * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined by a
+ * second kernel in a fixed order (same inputs and sizes, same bits).  batch = 0 does nothing.
+ * Workspace: bitlinear_attention_kv4_ws_bytes(); calls that may overlap need workspaces of their own. */
+bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, int64_t ld_q, const bl_kv4_cache* cache,
+                                  const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
+                                  int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,
+                                  void* stream);
+size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim);
+
+/* Copies whole pages inside the cache, in every layer: for each pair (src, dst) of pairs int32 [n][2],
+ * page dst becomes a copy of page src (a forked sequence's last page, a copy on write, the moves of a
+ * compaction).  Layer l's pages start at pages + l * layer_stride bytes.  A pair with a page outside
+ * 0..num_pages-1 is skipped.  No page may be the destination of two pairs, nor the destination of one
+ * and the source of another (the order of the copies is not defined).  page_bytes and layer_stride
+ * are multiples of 16, layer_stride >= num_pages * page_bytes (any value for one layer).  n = 0 does nothing. */
+bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
+                                   const int32_t* pairs, int64_t n, void* stream);
+
 /* Synchronises `stream`, then reads the status word a previous bitlinear_forward or
  * bitlinear_matmul_i32 call left in `ws`.  BL_OK, BL_ERR_TIMEOUT, or BL_ERR_CUDA. */
 bl_status bitlinear_ws_status(const void* ws, void* stream);

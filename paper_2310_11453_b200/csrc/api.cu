@@ -1,5 +1,7 @@
 // extern "C" entry points: argument validation on the host, workspace carving, launches.
 // Nothing here allocates device memory or synchronises (bitlinear_ws_status excepted).
+#include <math.h>
+
 #include "common.cuh"
 
 namespace bl {
@@ -82,6 +84,24 @@ bl_status check_layout_for_gemm(bl_layout layout, int64_t M, int64_t K, int64_t 
   if (layout == BL_LAYOUT_CANONICAL) return BL_OK;
   if (layout == BL_LAYOUT_PREFILL) return gemm_tc_supported(M, K, N, G) ? BL_OK : BL_ERR_SHAPE;
   return BL_ERR_UNSUPPORTED;
+}
+
+// ---- checks of the attention operators ---------------------------------------------------------
+constexpr int kMaxHeads = 4096;
+constexpr int64_t kMaxRows = 1 << 30;  // tokens: row numbers and positions stay inside 32 bits in the kernels
+
+inline bool attention_dtype(int t) { return t == BL_F16 || t == BL_BF16; }
+inline bool aligned_to(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// A row stride takes the row and keeps every row 16-byte aligned.
+inline bool row_stride(int64_t ld, int heads, int head_dim) { return ld >= (int64_t)heads * head_dim && ld % 8 == 0; }
+
+bl_status check_cache(const bl_kv4_cache* c) {
+  if (!c) return BL_ERR_NULL;
+  if (!attention_dtype(c->dtype) || (c->head_dim != 64 && c->head_dim != 128)) return BL_ERR_UNSUPPORTED;
+  if (bitlinear_kv4_page_bytes(c->page_size, c->kv_heads, c->head_dim) == 0) return BL_ERR_SHAPE;
+  if (c->num_pages < 0 || c->num_pages > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  if (c->num_pages > 0 && !c->pages) return BL_ERR_NULL;
+  return aligned16(c->pages) ? BL_OK : BL_ERR_ALIGN;
 }
 
 }  // namespace
@@ -490,6 +510,128 @@ bl_status bitlinear_block_forward(const void* x, int batch, int seq, int heads, 
       && quant(buf->h, d, BL_ABSMAX) && matmul(d, ffn, w->W_up, w->beta_up, 0, buf->u, ffn, true, nullptr)
       && quant(buf->u, ffn, BL_ETA) && matmul(ffn, d, w->W_down, w->beta_down, 0, y, d, false, buf->h);
   return ok ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int64_t T, int heads, int kv_heads,
+                                 int head_dim, int64_t ld_q, int64_t ld_k, const void* wq, const void* wk,
+                                 float eps, int rot_dim, int interleaved, const float* inv_freq,
+                                 const int32_t* positions, void* q_out, void* k_out, int64_t ld_qo, int64_t ld_ko,
+                                 void* stream) {
+  if (!valid_dtype(dt)) return BL_ERR_UNSUPPORTED;
+  if (T < 0 || T > kMaxRows || heads < 1 || kv_heads < 1 || heads > kMaxHeads || kv_heads > kMaxHeads) return BL_ERR_SHAPE;
+  if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0) return BL_ERR_SHAPE;
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16 != 0) return BL_ERR_SHAPE;
+  if (!row_stride(ld_q, heads, head_dim) || !row_stride(ld_qo, heads, head_dim) || !row_stride(ld_k, kv_heads, head_dim) ||
+      !row_stride(ld_ko, kv_heads, head_dim))
+    return BL_ERR_SHAPE;
+  if (T == 0) return BL_OK;
+  if (!q || !k || !q_out || !k_out || !positions || (rot_dim > 0 && !inv_freq)) return BL_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(wq) || !aligned16(wk) ||
+      !aligned_to(inv_freq, 4) || !aligned_to(positions, 4))
+    return BL_ERR_ALIGN;
+  if ((q == q_out && ld_q != ld_qo) || (k == k_out && ld_k != ld_ko)) return BL_ERR_SHAPE;
+  NormRopeArgs a{q, k, dt, T, heads, kv_heads, head_dim, ld_q, ld_k, wq, wk, eps, rot_dim, interleaved ? 1 : 0, inv_freq,
+                 positions, q_out, k_out, ld_qo, ld_ko};
+  return launch_qk_norm_rope(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_attention_window(const void* q, const void* k, const void* v, void* o, bl_dtype dt, int batch,
+                                     const int32_t* cu_q, const int32_t* cu_k, int64_t seq_q, int64_t seq_k,
+                                     int64_t rows_q, int64_t rows_k, int heads, int kv_heads, int head_dim,
+                                     int64_t ld_q, int64_t ld_k, int64_t ld_v, int64_t ld_o, int window, int sinks,
+                                     float scale, void* stream) {
+  if (!attention_dtype(dt) || (head_dim != 64 && head_dim != 128)) return BL_ERR_UNSUPPORTED;
+  if (batch < 0 || seq_q < 0 || seq_k < 0 || rows_q < 0 || rows_k < 0) return BL_ERR_SHAPE;
+  if (seq_q > kMaxRows || seq_k > kMaxRows || rows_q > kMaxRows || rows_k > kMaxRows) return BL_ERR_SHAPE;
+  if (heads < 1 || kv_heads < 1 || heads > kMaxHeads || heads % kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
+  if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
+  if (cu_k && !cu_q) return BL_ERR_NULL;
+  if (!cu_q && ((int64_t)batch * seq_q > rows_q || (int64_t)batch * seq_k > rows_k)) return BL_ERR_SHAPE;
+  if (!row_stride(ld_q, heads, head_dim) || !row_stride(ld_o, heads, head_dim) || !row_stride(ld_k, kv_heads, head_dim) ||
+      !row_stride(ld_v, kv_heads, head_dim))
+    return BL_ERR_SHAPE;
+  if (batch == 0 || seq_q == 0 || rows_q == 0) return BL_OK;
+  if (!q || !o || (rows_k > 0 && (!k || !v))) return BL_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned_to(cu_q, 4) || !aligned_to(cu_k, 4))
+    return BL_ERR_ALIGN;
+  if ((int64_t)batch * heads * ((seq_q + 127) / 128) > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  WindowArgs a{q, k, v, o, dt, batch, cu_q, cu_k ? cu_k : cu_q, seq_q, seq_k, rows_q, rows_k, heads, kv_heads, head_dim, ld_q,
+               ld_k, ld_v, ld_o, window > 0 ? window : 0, sinks, scale};
+  if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)head_dim);
+  return launch_attention_window(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+size_t bitlinear_kv4_page_bytes(int page_size, int kv_heads, int head_dim) {
+  if (page_size != 16 && page_size != 32 && page_size != 64) return 0;
+  if (kv_heads < 1 || kv_heads > kMaxHeads || (head_dim != 64 && head_dim != 128)) return 0;
+  return (size_t)page_size * (size_t)kv_heads * (size_t)(head_dim + 8);
+}
+
+bl_status bitlinear_kv4_append(const bl_kv4_cache* cache, const void* k, const void* v, int64_t T, int64_t ld_k,
+                               int64_t ld_v, const int64_t* slots, void* stream) {
+  const bl_status st = check_cache(cache);
+  if (st != BL_OK) return st;
+  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 8 * kMaxRows) return BL_ERR_SHAPE;
+  if (!row_stride(ld_k, cache->kv_heads, cache->head_dim) || !row_stride(ld_v, cache->kv_heads, cache->head_dim))
+    return BL_ERR_SHAPE;
+  if (T == 0) return BL_OK;
+  if (!k || !v || !slots) return BL_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || !aligned_to(slots, 8)) return BL_ERR_ALIGN;
+  return launch_kv4_append(*cache, k, v, T, ld_k, ld_v, slots, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_t T, int64_t ld_k, int64_t ld_v,
+                             const int64_t* slots, void* stream) {
+  const bl_status st = check_cache(cache);
+  if (st != BL_OK) return st;
+  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 8 * kMaxRows) return BL_ERR_SHAPE;
+  if (!row_stride(ld_k, cache->kv_heads, cache->head_dim) || !row_stride(ld_v, cache->kv_heads, cache->head_dim))
+    return BL_ERR_SHAPE;
+  if (T == 0) return BL_OK;
+  if (!k || !v || !slots) return BL_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || !aligned_to(slots, 8)) return BL_ERR_ALIGN;
+  return launch_kv4_read(*cache, k, v, T, ld_k, ld_v, slots, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
+  if (batch < 0 || n_q < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0) return 0;
+  if (head_dim != 64 && head_dim != 128) return 0;
+  return round256(attention_kv4_ws_bytes(batch, n_q, heads, kv_heads, head_dim));
+}
+
+bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, int64_t ld_q, const bl_kv4_cache* cache,
+                                  const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
+                                  int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  const bl_status st = check_cache(cache);
+  if (st != BL_OK) return st;
+  if (batch < 0 || n_q < 1 || heads < 1 || heads > kMaxHeads || heads % cache->kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
+  if (max_pages < 0 || max_pages > kMaxRows / cache->page_size) return BL_ERR_SHAPE;
+  if ((int64_t)batch * n_q > kMaxRows || (int64_t)batch * n_q * heads > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
+  if (!row_stride(ld_q, heads, cache->head_dim) || !row_stride(ld_o, heads, cache->head_dim)) return BL_ERR_SHAPE;
+  if (batch == 0) return BL_OK;
+  if (!q || !o || !lens || (max_pages > 0 && !block_table)) return BL_ERR_NULL;
+  if (!aligned16(q) || !aligned16(o) || !aligned_to(block_table, 4) || !aligned_to(lens, 4)) return BL_ERR_ALIGN;
+  const size_t need = bitlinear_attention_kv4_ws_bytes(batch, n_q, heads, cache->kv_heads, cache->head_dim);
+  if (!ws || ws_bytes < need) return BL_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BL_ERR_ALIGN;
+  Kv4AttnArgs a{q, batch, n_q, heads, ld_q, *cache, block_table, max_pages, lens, window > 0 ? window : 0, sinks, scale, o, ld_o, ws};
+  if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)cache->head_dim);
+  return launch_attention_kv4(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
+                                   const int32_t* pairs, int64_t n, void* stream) {
+  if (num_pages < 0 || num_pages > 0x7FFFFFFF || layers < 0 || n < 0 || n > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  if (page_bytes == 0 || page_bytes % 16 != 0) return BL_ERR_SHAPE;
+  if (layers > 1 && (layer_stride % 16 != 0 || layer_stride / page_bytes < (size_t)num_pages)) return BL_ERR_SHAPE;
+  if (layers > 65535 || page_bytes > ((size_t)1 << 40) || n * (int64_t)((page_bytes + 16383) / 16384) > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  if (n == 0 || layers == 0 || num_pages == 0) return BL_OK;
+  if (!pages || !pairs) return BL_ERR_NULL;
+  if (!aligned16(pages) || !aligned_to(pairs, 8)) return BL_ERR_ALIGN;
+  return launch_kv4_copy_pages(pages, page_bytes, num_pages, layers, layers > 1 ? layer_stride : 0, pairs, n,
+                               (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
 }
 
 bl_status bitlinear_ws_status(const void* ws, void* stream) {

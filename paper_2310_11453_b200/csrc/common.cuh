@@ -207,6 +207,35 @@ size_t gemv_tc_ws_bytes(int64_t M, int64_t K);
 cudaError_t launch_attention_causal(const void* q, const void* k, const void* v, void* o, int batch, int S,
                                     int heads, int64_t ld, int64_t ld_o, cudaStream_t s);
 
+// Attention at inference (qk_norm_rope.cu, attention_window.cu, kv4_cache.cu, attention_kv4.cu).
+struct NormRopeArgs {
+  const void* q; const void* k; bl_dtype dt; int64_t T; int heads, kv_heads, head_dim; int64_t ld_q, ld_k;
+  const void* wq; const void* wk; float eps; int rot_dim, interleaved; const float* inv_freq; const int32_t* positions;
+  void* q_out; void* k_out; int64_t ld_qo, ld_ko;
+};
+cudaError_t launch_qk_norm_rope(const NormRopeArgs& a, cudaStream_t s);
+
+struct WindowArgs {
+  const void* q; const void* k; const void* v; void* o; bl_dtype dt; int batch; const int32_t* cu_q; const int32_t* cu_k;
+  int64_t seq_q, seq_k, rows_q, rows_k; int heads, kv_heads, head_dim; int64_t ld_q, ld_k, ld_v, ld_o;
+  int window, sinks; float scale;
+};
+cudaError_t launch_attention_window(const WindowArgs& a, cudaStream_t s);
+
+cudaError_t launch_kv4_append(const bl_kv4_cache& c, const void* k, const void* v, int64_t T, int64_t ld_k, int64_t ld_v,
+                              const int64_t* slots, cudaStream_t s);
+cudaError_t launch_kv4_read(const bl_kv4_cache& c, void* k, void* v, int64_t T, int64_t ld_k, int64_t ld_v,
+                            const int64_t* slots, cudaStream_t s);
+cudaError_t launch_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
+                                  const int32_t* pairs, int64_t n, cudaStream_t s);
+
+struct Kv4AttnArgs {
+  const void* q; int batch, n_q, heads; int64_t ld_q; bl_kv4_cache cache; const int32_t* table; int64_t max_pages;
+  const int32_t* lens; int window, sinks; float scale; void* o; int64_t ld_o; void* ws;
+};
+size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim);
+cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s);
+
 // Host-side layout maps (also exported through bitlinear_layout_index).
 int64_t prefill_bytes(int64_t N, int64_t K);
 void prefill_index(int64_t K, int64_t n, int64_t k, int64_t* byte_off, int* bit);
