@@ -607,7 +607,7 @@ bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, 
   if (st != BL_OK) return st;
   if (batch < 0 || n_q < 1 || heads < 1 || heads > kMaxHeads || heads % cache->kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
   if (max_pages < 0 || max_pages > kMaxRows / cache->page_size) return BL_ERR_SHAPE;
-  if ((int64_t)batch * n_q > kMaxRows || (int64_t)batch * n_q * heads > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  if ((int64_t)batch * n_q > kMaxRows || (int64_t)batch * n_q * heads > kMaxRows) return BL_ERR_SHAPE;
   if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
   if (!row_stride(ld_q, heads, cache->head_dim) || !row_stride(ld_o, heads, cache->head_dim)) return BL_ERR_SHAPE;
   if (batch == 0) return BL_OK;

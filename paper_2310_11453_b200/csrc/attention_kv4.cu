@@ -1,6 +1,28 @@
-// Attention of the last n_q tokens of each sequence over the 4-bit paged cache.
-// One warp per (sequence, query, head): a pass over the visible tokens with the running maximum and sum of the
-// softmax, each lane holding kDim / 32 values of the query and of the output.
+// Attention of the last n_q tokens of each sequence over the 4-bit paged cache:
+//   s_jr = scale . q_r . (eta_j + step_j c_j),  o_r = sum_j p_jr (eta'_j + step'_j c'_j) / sum_j p_jr,  p = e^(s - max).
+// Bound by reading the cache (kDim + 8 bytes per token and head); everything below serves to keep up with that.
+//
+// Products.  Codes are never turned into values: with the step and eta of a token outside the sums,
+//   s_jr = scale (step_j (q_r . c_j) + eta_j sum q_r),   o_r = sum_j (p_jr step'_j) c'_j + sum_j p_jr eta'_j,
+// both products are exact integers 0..15 times 16-bit numbers on the tensor cores (mma m16n8k16, fp32 sums).
+// A nibble becomes an fp16 operand by a mask alone: bits 0-3 of a half are the subnormal c . 2^-24, bits 4-7
+// are c . 2^-20 (undone in the query operand, or in the output); one shift serves the upper two nibbles.  So 8 codes
+// cost 5 instructions.  The tokens are the rows (16) of both products and the query rows (queries x heads of one
+// key/value head) the columns (8), so with up to 8 query rows no tensor work is idle on a padded dimension of 16;
+// the probabilities pass from the first product's layout to the second's by an 8x8 transposition in registers.
+// The cache's orders are such that a lane's operands of 8 tokens are 16 contiguous bytes.
+//
+// Precision.  The query operand is the query times a power of two that puts the row's largest value at 2^13 (exact
+// unless a value is 2^-24 of the largest and more below it).  p . step' is rounded to fp16 after scaling by a running power of two (2^13 / largest
+// step' so far), so its range is 2^-37 of the largest; the sum of the rounding errors is kept in fp32 and taken
+// out at the codes' mean 7.5, which leaves the error of a value of size 7.5 steps instead of 15.  Everything else
+// (scores, statistics, eta sums, accumulators) is fp32.
+//
+// Work.  The visible tokens of all sequences, in chunks of 64, times key/value heads (times blocks of query rows)
+// form one list that is cut into equal parts, one per warp: ragged batches and single long sequences balance
+// alike.  A warp runs on its own: its chunks stream into its part of shared memory by asynchronous copies, two
+// ahead, with no barrier between warps.  A warp that owns all chunks of a head writes the output; else its
+// unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
 #include "kv4.cuh"
 
 namespace bl {
@@ -9,65 +31,572 @@ namespace {
 
 using namespace kv4;
 
-template <typename T, int kDim>
-__global__ void __launch_bounds__(128) attention_kv4_kernel(Kv4AttnArgs a) {
-  constexpr int kVals = kDim / 32;
+constexpr int kChunk = 64;                 // tokens per work item
+constexpr int kWarps = 8;                  // per CTA, one CTA per SM
+constexpr int kStages = 3;                 // chunks of a warp in shared memory
+constexpr int kMaxSms = 160;
+constexpr int kJoinWarps = 8;
+
+struct Plan {                              // how the list is laid out; the same arithmetic in both kernels
+  int group, rows, rows_per_block, blocks; // query heads per key/value head; query rows; rows per block; blocks
+  int heads_blocks;                        // key/value heads x blocks
+};
+__host__ __device__ inline Plan make_plan(int n_q, int heads, int kv_heads) {
+  Plan p;
+  p.group = heads / kv_heads;
+  p.rows = n_q * p.group;
+  p.rows_per_block = p.rows <= 8 ? p.rows : 16;
+  p.blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
+  p.heads_blocks = kv_heads * p.blocks;
+  return p;
+}
+
+// The chunks of one sequence that hold a visible token: those of the sinks, then those from the window's begin on.
+struct Seq {
+  int len, lo;                             // tokens; first token inside the first query's window
+  int sink_chunks, first_main, chunks;
+  __device__ __forceinline__ int start(int c) const { return (c < sink_chunks ? c : first_main + c - sink_chunks) * kChunk; }
+};
+__device__ __forceinline__ Seq make_seq(const Kv4AttnArgs& a, int b) {
+  Seq s;
+  s.len = (int)min((int64_t)max(a.lens[b], 0), a.max_pages * a.cache.page_size);
+  s.lo = a.window > 0 ? max(0, max(0, s.len - a.n_q) - a.window + 1) : 0;
+  s.first_main = s.lo / kChunk;
+  s.sink_chunks = min((int)(((int64_t)min(a.sinks, s.lo) + kChunk - 1) / kChunk), s.first_main);
+  s.chunks = s.len > 0 ? s.sink_chunks + (s.len + kChunk - 1) / kChunk - s.first_main : 0;
+  return s;
+}
+
+// Chunks of all sequences (by a whole warp).
+__device__ __forceinline__ int64_t total_chunks(const Kv4AttnArgs& a) {
   const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (w >= (int64_t)a.batch * a.n_q * a.heads) return;
-  const int h = (int)(w % a.heads), hk = h / (a.heads / a.cache.kv_heads);
-  const int64_t row = w / a.heads;
-  const int b = (int)(row / a.n_q), i = (int)(row % a.n_q);
-  const int ps = a.cache.page_size;
-  const int len = (int)min((int64_t)max(a.lens[b], 0), a.max_pages * ps);
-  const int pos = len - a.n_q + i;
-  const T* q = reinterpret_cast<const T*>(a.q) + row * a.ld_q + (int64_t)h * kDim + lane * kVals;
-  float qv[kVals], acc[kVals];
+  int64_t sum = 0;
+  for (int base = 0; base < a.batch; base += 32) sum += warp_sum(base + lane < a.batch ? make_seq(a, base + lane).chunks : 0);
+  return sum;
+}
+// Chunks of the sequences before b (by a whole warp).
+__device__ __forceinline__ int64_t chunks_before(const Kv4AttnArgs& a, int b) {
+  const int lane = threadIdx.x & 31;
+  int64_t sum = 0;
+  for (int base = 0; base < b; base += 32) sum += warp_sum(base + lane < b ? make_seq(a, base + lane).chunks : 0);
+  return sum;
+}
+// The sequence that item `at` of the list falls into, and the item's place among that sequence's (by a whole warp).
+__device__ __forceinline__ int find_seq(const Kv4AttnArgs& a, int heads_blocks, int64_t at, int64_t& rest) {
+  const int lane = threadIdx.x & 31;
+  int64_t before = 0;
+  for (int base = 0; base < a.batch; base += 32) {
+    const int n = base + lane < a.batch ? make_seq(a, base + lane).chunks : 0;
+    int incl = n;
 #pragma unroll
-  for (int e = 0; e < kVals; ++e) { qv[e] = in_cast(q[e]); acc[e] = 0.f; }
-  float m = -INFINITY, l = 0.f;
-  for (int j = 0; j <= pos; ++j) {
-    if (a.window > 0 && pos - j >= a.window && j >= a.sinks) continue;
-    const int page = a.table[(int64_t)b * a.max_pages + j / ps];
-    if (page < 0 || page >= a.cache.num_pages) continue;
-    const char* block = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)page * a.cache.kv_heads + hk) * Block<kDim>::bytes(ps);
-    const int t = j % ps;
-    const float2 ks = scale_floats<T>(*reinterpret_cast<const uint32_t*>(block + Block<kDim>::k_scale(ps) + 4 * t));
-    const float2 vs = scale_floats<T>(*reinterpret_cast<const uint32_t*>(block + Block<kDim>::v_scale(ps) + 4 * t));
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < kVals; ++e) {
-      const int d = lane * kVals + e;
-      const int code = ((uint8_t)block[t * (kDim / 2) + d / 2] >> (4 * (d & 1))) & 15;
-      s = fmaf(qv[e], fmaf((float)code, ks.x, ks.y), s);
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += up;
     }
-    s = warp_sum(s) * a.scale;
-    const float top = fmaxf(m, s), c = m == -INFINITY ? 0.f : expf(m - top), p = expf(s - top);
-    m = top;
-    l = l * c + p;
-#pragma unroll
-    for (int e = 0; e < kVals; ++e) {
-      const int d = lane * kVals + e;
-      const uint8_t byte = (uint8_t)block[Block<kDim>::v_codes(ps) + Block<kDim>::v_at(t, d & ~3) + ((d & 3) >> 1)];
-      acc[e] = acc[e] * c + p * fmaf((float)((byte >> (4 * (d & 1))) & 15), vs.x, vs.y);
+    const unsigned past = __ballot_sync(0xFFFFFFFFu, (before + incl) * heads_blocks > at);
+    if (past) {
+      const int f = __ffs(past) - 1;
+      rest = at - (before + __shfl_sync(0xFFFFFFFFu, incl - n, f)) * heads_blocks;
+      return base + f;
     }
+    before += __shfl_sync(0xFFFFFFFFu, incl, 31);
   }
-  T* o = reinterpret_cast<T*>(a.o) + row * a.ld_o + (int64_t)h * kDim + lane * kVals;
+  rest = 0;
+  return a.batch;
+}
+
+// Part w of `parts` of a list of `total` items starts at item part_begin(w); item i lies in part owner(i).
+__device__ __forceinline__ int64_t part_begin(int64_t total, int parts, int w) { return total * w / parts; }
+__device__ __forceinline__ int owner(int64_t total, int parts, int64_t i) { return (int)(((i + 1) * parts - 1) / total); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// 2^e as a float, e in -126..127
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ int exponent(float x) { return ((__float_as_int(x) >> 23) & 255) - 127; }
+
+template <typename T> __device__ __forceinline__ float2 pair_floats(uint32_t w) { return scale_floats<T>(w); }
+template <typename T> __device__ __forceinline__ uint32_t pair_bits(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pair_bits<__half>(float lo, float hi) { return half2_bits(lo, hi); }
+template <> __device__ __forceinline__ uint32_t pair_bits<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Walks the items of a warp's part of the list.
+struct Walk {
+  Seq s;
+  int b, hb, c;                            // sequence, key/value head x block, chunk
+  __device__ __forceinline__ void next(const Kv4AttnArgs& a, int heads_blocks) {
+    if (++c < s.chunks) return;
+    c = 0;
+    if (++hb < heads_blocks) return;
+    hb = 0;
+    do { ++b; } while (b < a.batch && (s = make_seq(a, b)).chunks == 0);
+  }
+};
+
+// Words of shared memory read as operands: 4 words for kDim 128, 2 for kDim 64.
+template <int kWords> __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[kWords]);
+template <> __device__ __forceinline__ void load_words<4>(const char* p, uint32_t (&w)[4]) {
+  const uint4 r = *reinterpret_cast<const uint4*>(p);
+  w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
+}
+template <> __device__ __forceinline__ void load_words<2>(const char* p, uint32_t (&w)[2]) {
+  const uint2 r = *reinterpret_cast<const uint2*>(p);
+  w[0] = r.x; w[1] = r.y;
+}
+
+template <typename T, int kDim, int kNT>
+__global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a) {
+  constexpr int kWords = kDim / 32;        // words of codes per lane and 8 tokens
+  constexpr int kTiles = kChunk / 16;
+  constexpr int kStageBytes = kChunk * (kDim + 8);
+  constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
+  extern __shared__ __align__(16) char smem[];
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, qd = lane & 3;
+  const int w = blockIdx.x * kWarps + warp, parts = gridDim.x * kWarps;
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
+  const int ps = a.cache.page_size, block_bytes = Block<kDim>::bytes(ps), subs = kChunk / ps;
+  char* ring = smem + warp * (kStages * kStageBytes);
+  const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
+
+  pdl_wait();
+  const int64_t total = total_chunks(a) * plan.heads_blocks;
+  const int64_t begin = part_begin(total, parts, w), end = part_begin(total, parts, w + 1);
+  const int items = (int)(end - begin);
+  if (items == 0) return;
+  int64_t rest;
+  Walk now;
+  now.b = find_seq(a, plan.heads_blocks, begin, rest);
+  now.s = make_seq(a, now.b);
+  now.hb = (int)(rest / now.s.chunks);
+  now.c = (int)(rest % now.s.chunks);
+
+  // ---- loads: the page numbers of a chunk are fetched one chunk before its copies are issued
+  Walk ahead = now;
+  auto page_of = [&](const Walk& x) -> int {           // lane i: the page of the chunk's i-th run of tokens; -1: nothing visible, or no page
+    if (lane >= subs) return -1;
+    const int t = x.s.start(x.c) + lane * ps;
+    if (t >= x.s.len || (t + ps <= x.s.lo && t >= a.sinks)) return -1;
+    const int id = a.table[(int64_t)x.b * a.max_pages + t / ps];
+    return id >= 0 && id < a.cache.num_pages ? id : -1;
+  };
+  int issued = 0;
+  uint32_t present = 0;                                // 4 bits per chunk in flight: which of its pages are there
+  int ids = page_of(ahead);
+  auto issue = [&]() {
+    if (issued < items) {
+      const int hk = ahead.hb / plan.blocks;
+      const uint32_t dst = ring_addr + (issued % kStages) * kStageBytes;
+      present = (present << 4) | (__ballot_sync(0xFFFFFFFFu, ids >= 0) & 15u);
+      for (int i = 0; i < subs; ++i) {
+        const int id = __shfl_sync(0xFFFFFFFFu, ids, i);
+        if (id < 0) continue;
+        const char* src = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)id * a.cache.kv_heads + hk) * block_bytes;
+        for (int u = lane * 16; u < block_bytes; u += 512) copy16(dst + i * block_bytes + u, src + u);
+      }
+      if (issued + 1 < items) {
+        ahead.next(a, plan.heads_blocks);
+        ids = page_of(ahead);
+      }
+    } else {
+      present <<= 4;
+    }
+    ++issued;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 #pragma unroll
-  for (int e = 0; e < kVals; ++e) o[e] = out_cast<T>(l == 0.f ? 0.f : acc[e] / l);
+  for (int i = 0; i < kStages - 1; ++i) issue();
+
+  // ---- state of the segment (one sequence, head and block of rows) being worked on
+  uint32_t qf[kNT][kWords][4];                         // query operand: per word of codes the pairs (0,4), (1,5)/16, (2,6), (3,7)/16
+  float f[kNT][2], qsum[kNT][2];                       // per column: scale of the raw score, scaled sum of the query
+  float acc[kNT][2 * kWords][4];
+  float m[kNT][2], l[kNT][2], esum[kNT][2], dsum[kNT][2];
+  int vexp = 0, seg_first = 0;                         // 2^vexp: running size of the value steps
+  bool fresh = true;
+
+  for (int item = 0; item < items; ++item) {
+    const int rows0 = (now.hb % plan.blocks) * plan.rows_per_block, hk = now.hb / plan.blocks;
+    if (fresh) {
+      fresh = false;
+      seg_first = item;
+      vexp = -1000;
+      const float sl = a.scale * 1.4426950408889634f;
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+        const int r = rows0 + nt * 8 + g;
+        const bool on = r < plan.rows;
+        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)now.b * a.n_q + (on ? r / plan.group : 0)) * a.ld_q +
+                     (int64_t)(hk * plan.group + (on ? r % plan.group : 0)) * kDim + qd * (kDim / 4);
+        float v[kWords][8], top = 0.f, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          const uint4 x = on ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0, 0, 0, 0);
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = pair_floats<T>(xs[j]);
+            v[i][2 * j] = y.x; v[i][2 * j + 1] = y.y;
+            top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+            sum += y.x + y.y;
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1); sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+        const int e = min(13 - exponent(top), 100);    // the largest value goes to 2^13 (all zero: any scale)
+        const float up = pow2i(max(e, -114));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          qf[nt][i][0] = half2_bits(v[i][0] * up, v[i][4] * up);
+          qf[nt][i][1] = half2_bits(v[i][1] * up * 0.0625f, v[i][5] * up * 0.0625f);
+          qf[nt][i][2] = half2_bits(v[i][2] * up, v[i][6] * up);
+          qf[nt][i][3] = half2_bits(v[i][3] * up * 0.0625f, v[i][7] * up * 0.0625f);
+        }
+        const float fr = sl * pow2i(min(24 - max(e, -114), 127)), sr = sum * sl;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          f[nt][j] = __shfl_sync(0xFFFFFFFFu, fr, 4 * (2 * qd + j));
+          qsum[nt][j] = __shfl_sync(0xFFFFFFFFu, sr, 4 * (2 * qd + j));
+          m[nt][j] = -INFINITY;
+          l[nt][j] = esum[nt][j] = dsum[nt][j] = 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * kWords; ++t) acc[nt][t][0] = acc[nt][t][1] = acc[nt][t][2] = acc[nt][t][3] = 0.f;
+      }
+    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();                                      // the chunk is there, and its predecessor's stage is free
+    issue();
+    const char* stage = ring + (item % kStages) * kStageBytes;
+    const uint32_t there = (present >> (4 * (issued - 1 - item))) & 15u;
+    const int t0 = now.s.start(now.c);
+    // every query of this block sees every token of the chunk?
+    const int pos_first = now.s.len - a.n_q + rows0 / plan.group;
+    const int pos_last = now.s.len - a.n_q + (min(rows0 + plan.rows_per_block, plan.rows) - 1) / plan.group;
+    const bool clean = there == (1u << subs) - 1 && t0 + kChunk - 1 <= pos_first &&
+                       (a.window == 0 || pos_last - t0 < a.window || t0 + kChunk <= a.sinks);
+    auto tile_base = [&](int i, int& j0) -> const char* {
+      j0 = (i * 16) & (ps - 1);
+      return stage + (i * 16 / ps) * block_bytes;
+    };
+
+    // ---- scores of the chunk: tile i, row g and g + 8 (tokens), columns 2 qd and 2 qd + 1 of each 8 query rows
+    float s[kTiles][kNT][4];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      int j0;
+      const char* base = tile_base(i, j0);
+      uint32_t x[kWords], y[kWords];
+      load_words<kWords>(base + j0 * (kDim / 2) + lane * (kWords * 4), x);
+      load_words<kWords>(base + j0 * (kDim / 2) + 4 * kDim + lane * (kWords * 4), y);
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) s[i][nt][0] = s[i][nt][1] = s[i][nt][2] = s[i][nt][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) {
+        const uint32_t xs = x[k] >> 8, ys = y[k] >> 8;
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          mma16816(s[i][nt], x[k] & kLo, y[k] & kLo, x[k] & kHi, y[k] & kHi, qf[nt][k][0], qf[nt][k][1]);
+          mma16816(s[i][nt], xs & kLo, ys & kLo, xs & kHi, ys & kHi, qf[nt][k][2], qf[nt][k][3]);
+        }
+      }
+    }
+    float mx[kNT][2], vtop = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) { mx[nt][0] = m[nt][0]; mx[nt][1] = m[nt][1]; }
+    uint32_t seen = 0xFFFFFFFFu;                       // per tile 4 bits per 8 query rows, as s[i][nt]; kNT <= 2
+    if (!clean) {
+      seen = 0;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int t = t0 + i * 16 + g + (e >> 1) * 8, r = rows0 + nt * 8 + 2 * qd + (e & 1);
+            const int pos = now.s.len - a.n_q + min(r, plan.rows - 1) / plan.group;
+            const bool v = t <= pos && ((there >> (i * 16 / ps)) & 1u) && (a.window == 0 || pos - t < a.window || t < a.sinks);
+            seen |= (uint32_t)v << ((i * kNT + nt) * 4 + e);
+          }
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      int j0;
+      const char* base = tile_base(i, j0);
+      const char* kse = base + Block<kDim>::k_scale(ps) + 4 * j0;
+      const float2 k0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(kse + 4 * g));
+      const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(kse + 4 * g + 32));
+      const char* vse = base + Block<kDim>::v_scale(ps) + 4 * j0;
+      const float v0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g)).x;
+      const float v1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g + 32)).x;
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 kk = e < 2 ? k0 : k1;
+          float z = fmaf(s[i][nt][e] * f[nt][e & 1], kk.x, kk.y * qsum[nt][e & 1]);
+          if (!clean && !((seen >> ((i * kNT + nt) * 4 + e)) & 1u)) z = -INFINITY;
+          s[i][nt][e] = z;
+          mx[nt][e & 1] = fmaxf(mx[nt][e & 1], z);
+        }
+        const uint32_t any = clean ? 15u : (seen >> ((i * kNT + nt) * 4)) & 15u;
+        if (any & 3u) vtop = fmaxf(vtop, v0);
+        if (any & 12u) vtop = fmaxf(vtop, v1);
+      }
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+        mx[nt][0] = fmaxf(mx[nt][0], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][0], o));
+        mx[nt][1] = fmaxf(mx[nt][1], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][1], o));
+      }
+      vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, o));
+    }
+    if (!clean) {
+      vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, 1)); vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, 2));
+    }
+    const int ve = max(vexp, max(exponent(vtop), -100));
+    const float vshift = vexp < ve ? (vexp < ve - 100 ? 0.f : pow2i(vexp - ve)) : 1.f, vscale = pow2i(min(13 - ve, 120));
+    bool moved = ve != vexp;
+    vexp = ve;
+    float mu[kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) moved |= mx[nt][j] != m[nt][j];
+    if (__any_sync(0xFFFFFFFFu, moved)) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float c = m[nt][j] == -INFINITY ? 0.f : ex2(m[nt][j] - mx[nt][j]), cv = c * vshift;
+          m[nt][j] = mx[nt][j];
+          l[nt][j] *= c; esum[nt][j] *= c; dsum[nt][j] *= cv;
+#pragma unroll
+          for (int t = 0; t < 2 * kWords; ++t) { acc[nt][t][j] *= cv; acc[nt][t][2 + j] *= cv; }
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) mu[nt][j] = m[nt][j] == -INFINITY ? 0.f : m[nt][j];
+
+    // ---- probabilities, and their products with the value codes
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      int j0;
+      const char* base = tile_base(i, j0);
+      const char* vse = base + Block<kDim>::v_scale(ps) + 4 * j0;
+      float2 v0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g));
+      float2 v1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g + 32));
+      v0.x *= vscale; v1.x *= vscale;
+      uint32_t b0[kNT], b1[kNT];
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+        float p[4], u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = ex2(s[i][nt][e] - mu[nt][e & 1]);
+          l[nt][e & 1] += p[e];
+          const float2 vv = e < 2 ? v0 : v1;
+          u[e] = p[e] * vv.x;
+          float pe = p[e] * vv.y;
+          if (!clean && !((seen >> ((i * kNT + nt) * 4 + e)) & 1u)) u[e] = pe = 0.f;   // whatever lies there
+          esum[nt][e & 1] += pe;
+        }
+        b0[nt] = half2_bits(u[0], u[1]);
+        b1[nt] = half2_bits(u[2], u[3]);
+        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&b0[nt])), r1 = __half22float2(*reinterpret_cast<const __half2*>(&b1[nt]));
+        dsum[nt][0] += (r0.x - u[0]) + (r1.x - u[2]);
+        dsum[nt][1] += (r0.y - u[1]) + (r1.y - u[3]);
+        b0[nt] = transpose8x8(b0[nt]);
+        b1[nt] = transpose8x8(b1[nt]);
+      }
+      uint32_t x[kWords], y[kWords];
+      load_words<kWords>(base + Block<kDim>::v_codes(ps) + j0 * (kDim / 2) + lane * (kWords * 4), x);
+      load_words<kWords>(base + Block<kDim>::v_codes(ps) + j0 * (kDim / 2) + 4 * kDim + lane * (kWords * 4), y);
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) {
+        const uint32_t xs = x[k] >> 8, ys = y[k] >> 8;
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          mma16816(acc[nt][2 * k], x[k] & kLo, x[k] & kHi, y[k] & kLo, y[k] & kHi, b0[nt], b1[nt]);
+          mma16816(acc[nt][2 * k + 1], xs & kLo, xs & kHi, ys & kLo, ys & kHi, b0[nt], b1[nt]);
+        }
+      }
+    }
+
+    // ---- end of the segment
+    if (now.c + 1 == now.s.chunks || item + 1 == items) {
+      const bool whole = now.c + 1 == now.s.chunks && now.c - (item - seg_first) == 0;
+      const float back = pow2i(min(max(vexp - 13, -126), 127));
+      float* slot = reinterpret_cast<float*>(a.ws) + (int64_t)(2 * w + (seg_first > 0)) * plan.rows_per_block * (kDim + 4);
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float lt = l[nt][j], et = esum[nt][j], dt = dsum[nt][j];
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            lt += __shfl_xor_sync(0xFFFFFFFFu, lt, o);
+            et += __shfl_xor_sync(0xFFFFFFFFu, et, o);
+            dt += __shfl_xor_sync(0xFFFFFFFFu, dt, o);
+          }
+          const int rr = nt * 8 + 2 * qd + j, r = rows0 + rr;
+          if (rr >= plan.rows_per_block || r >= plan.rows) continue;
+          const float add = et - 7.5f * dt * back, norm = whole ? (lt == 0.f ? 0.f : 1.f / lt) : 1.f;
+          float o[kDim / 8];                           // values (kDim / 8) g .. of the row
+#pragma unroll
+          for (int t = 0; t < 2 * kWords; ++t) {
+            o[2 * t] = (acc[nt][t][j] * 16777216.f * back + add) * norm;
+            o[2 * t + 1] = (acc[nt][t][2 + j] * 1048576.f * back + add) * norm;
+          }
+          if (whole) {
+            T* out = reinterpret_cast<T*>(a.o) + ((int64_t)now.b * a.n_q + r / plan.group) * a.ld_o +
+                     (int64_t)(hk * plan.group + r % plan.group) * kDim + g * (kDim / 8);
+#pragma unroll
+            for (int i = 0; i < kDim / 64; ++i)
+              *reinterpret_cast<uint4*>(out + 8 * i) =
+                  make_uint4(pair_bits<T>(o[8 * i], o[8 * i + 1]), pair_bits<T>(o[8 * i + 2], o[8 * i + 3]),
+                             pair_bits<T>(o[8 * i + 4], o[8 * i + 5]), pair_bits<T>(o[8 * i + 6], o[8 * i + 7]));
+          } else {
+            float* row = slot + rr * (kDim + 4);
+#pragma unroll
+            for (int i = 0; i < kDim / 32; ++i)
+              *reinterpret_cast<float4*>(row + g * (kDim / 8) + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            if (g == 0) *reinterpret_cast<float2*>(row + kDim) = make_float2(m[nt][j], lt);
+          }
+        }
+      fresh = true;
+    }
+    if (item + 1 < items) now.next(a, plan.heads_blocks);
+  }
+}
+
+// Joins the parts of the rows whose chunks went to more than one warp: one CTA per row, warps take the parts in turn.
+template <typename T, int kDim>
+__global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, int parts) {
+  constexpr int kVals = kDim / 32;
+  __shared__ float sums[kJoinWarps][kDim + 4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
+  const int rr = blockIdx.x % plan.rows_per_block, bh = blockIdx.x / plan.rows_per_block;
+  const int b = bh / plan.heads_blocks, hb = bh % plan.heads_blocks;
+  const int r = (hb % plan.blocks) * plan.rows_per_block + rr, hk = hb / plan.blocks;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (r >= plan.rows) return;
+  const int chunks = make_seq(a, b).chunks;
+  T* out = reinterpret_cast<T*>(a.o) + ((int64_t)b * a.n_q + r / plan.group) * a.ld_o + (int64_t)(hk * plan.group + r % plan.group) * kDim;
+  if (chunks == 0) {                                   // an empty sequence
+    for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) out[d] = out_cast<T>(0.f);
+    return;
+  }
+  const int64_t total = total_chunks(a) * plan.heads_blocks;
+  const int64_t first = chunks_before(a, b) * plan.heads_blocks + (int64_t)hb * chunks;
+  const int w0 = owner(total, parts, first), w1 = owner(total, parts, first + chunks - 1);
+  if (w0 == w1) return;                                // written already
+  float m = -INFINITY, l = 0.f, v[kVals] = {};
+  for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
+    const int64_t wb = part_begin(total, parts, w);
+    if (part_begin(total, parts, w + 1) == wb) continue;
+    const float* row = reinterpret_cast<const float*>(a.ws) + ((int64_t)(2 * w + (wb < first)) * plan.rows_per_block + rr) * (kDim + 4);
+    const float2 ml = *reinterpret_cast<const float2*>(row + kDim);
+    if (ml.x == -INFINITY) continue;                   // the part holds nothing that this row sees
+    const float top = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : ex2(m - top), p = ex2(ml.x - top);
+    m = top;
+    l = l * c + ml.y * p;
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) v[i] = v[i] * c + row[lane * kVals + i] * p;
+  }
+#pragma unroll
+  for (int i = 0; i < kVals; ++i) sums[warp][lane * kVals + i] = v[i];
+  if (lane == 0) { sums[warp][kDim] = m; sums[warp][kDim + 1] = l; }
+  __syncthreads();
+  for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, sums[i][kDim]);
+    float ls = 0.f, vs = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) {
+      const float c = sums[i][kDim] == -INFINITY ? 0.f : ex2(sums[i][kDim] - top);
+      ls += sums[i][kDim + 1] * c;
+      vs += sums[i][d] * c;
+    }
+    out[d] = out_cast<T>(ls == 0.f ? 0.f : vs / ls);
+  }
+}
+
+cudaError_t sm_count(int* n) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+  e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  if (*n > kMaxSms) *n = kMaxSms;
+  if (dev < 64) known[dev].store(*n, std::memory_order_relaxed);
+  return cudaSuccess;
+}
+
+template <typename T, int kDim, int kNT>
+cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
+  constexpr int kSmem = kWarps * kStages * kChunk * (kDim + 8);
+  static std::atomic<uint64_t> ready{0};               // devices on which the kernel's shared memory limit is set
+  int dev = 0, sms = 0;
+  cudaError_t e = sm_count(&sms);
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !((ready.load(std::memory_order_relaxed) >> dev) & 1)) {
+    e = cudaFuncSetAttribute(attention_kv4_kernel<T, kDim, kNT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
+  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attention_kv4_join_kernel<T, kDim>, (unsigned)((int64_t)a.batch * plan.heads_blocks * plan.rows_per_block),
+                    kJoinWarps * 32, 0, s, a, sms * kWarps);
 }
 
 template <typename T>
 cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
-  const unsigned grid = (unsigned)(((int64_t)a.batch * a.n_q * a.heads + 3) / 4);
-  if (a.cache.head_dim == 64) attention_kv4_kernel<T, 64><<<grid, 128, 0, s>>>(a);
-  else attention_kv4_kernel<T, 128><<<grid, 128, 0, s>>>(a);
-  return cudaGetLastError();
+  const bool few = make_plan(a.n_q, a.heads, a.cache.kv_heads).rows <= 8;
+  if (a.cache.head_dim == 64) return few ? launch_rows<T, 64, 1>(a, s) : launch_rows<T, 64, 2>(a, s);
+  return few ? launch_rows<T, 128, 1>(a, s) : launch_rows<T, 128, 2>(a, s);
 }
 
 }  // namespace
 
-size_t attention_kv4_ws_bytes(int, int, int, int, int) { return 256; }
+size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
+  const Plan p = make_plan(n_q, heads, kv_heads);
+  return (size_t)kMaxSms * kWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float) * (batch > 0);
+}
 
 cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s) {
   return a.cache.dtype == BL_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);
