@@ -14,8 +14,9 @@
 //
 // Precision.  The query operand is the query times a power of two that puts the row's largest value at 2^13 (exact
 // unless a value is 2^-24 of the largest and more below it).  p . step' is rounded to fp16 after scaling by a running power of two (2^13 / largest
-// step' so far), so its range is 2^-37 of the largest; the sum of the rounding errors is kept in fp32 and taken
-// out at the codes' mean 7.5, which leaves the error of a value of size 7.5 steps instead of 15.  Everything else
+// step' so far), so its range is 2^-37 of the largest.  The codes' mean is taken out of its rounding error: with
+// u = fp16(p step'), o = sum u (c' - 7.5) + sum p (eta' + 7.5 step'), where sum u comes from one more product
+// with a tile of ones.  Everything else
 // (scores, statistics, eta sums, accumulators) is fp32.
 //
 // Work.  The visible tokens of all sequences, in chunks of 64, times key/value heads (times blocks of query rows)
@@ -23,6 +24,8 @@
 // alike.  A warp runs on its own: its chunks stream into its part of shared memory by asynchronous copies, two
 // ahead, with no barrier between warps.  A warp that owns all chunks of a head writes the output; else its
 // unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
+#include <type_traits>
+
 #include "kv4.cuh"
 
 namespace bl {
@@ -37,17 +40,20 @@ constexpr int kStages = 3;                 // chunks of a warp in shared memory
 constexpr int kMaxSms = 160;
 constexpr int kJoinWarps = 8;
 
-struct Plan {                              // how the list is laid out; the same arithmetic in both kernels
+struct Plan {                              // how the list is laid out; made on the host, the same for both kernels
   int group, rows, rows_per_block, blocks; // query heads per key/value head; query rows; rows per block; blocks
   int heads_blocks;                        // key/value heads x blocks
+  int page_log2, parts;                    // log2 page_size; parts of the list (warps)
 };
-__host__ __device__ inline Plan make_plan(int n_q, int heads, int kv_heads) {
+inline Plan make_plan(int n_q, int heads, int kv_heads, int page_size, int parts) {
   Plan p;
   p.group = heads / kv_heads;
   p.rows = n_q * p.group;
   p.rows_per_block = p.rows <= 8 ? p.rows : 16;
   p.blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
   p.heads_blocks = kv_heads * p.blocks;
+  p.page_log2 = page_size == 16 ? 4 : page_size == 32 ? 5 : 6;
+  p.parts = parts;
   return p;
 }
 
@@ -105,9 +111,20 @@ __device__ __forceinline__ int find_seq(const Kv4AttnArgs& a, int heads_blocks, 
   return a.batch;
 }
 
-// Part w of `parts` of a list of `total` items starts at item part_begin(w); item i lies in part owner(i).
-__device__ __forceinline__ int64_t part_begin(int64_t total, int parts, int w) { return total * w / parts; }
-__device__ __forceinline__ int owner(int64_t total, int parts, int64_t i) { return (int)(((i + 1) * parts - 1) / total); }
+// a / b for a >= 0, b > 0: the 32-bit division (a fifth of the instructions) where it serves.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// The cut of a list of items into parts: part w starts at begin(w), item i lies in part owner(i).
+struct Cut {
+  int64_t each; int more;                  // items of a part; the first `more` parts have one more
+  __device__ __forceinline__ Cut(int64_t total, int parts) : each(divide(total, parts)), more((int)(total - each * parts)) {}
+  __device__ __forceinline__ int64_t begin(int w) const { return each * w + min(w, more); }
+  __device__ __forceinline__ int owner(int64_t i) const {
+    const int64_t split = (each + 1) * more;
+    return (int)(i < split ? divide(i, each + 1) : more + divide(i - split, each));
+  }
+};
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -126,6 +143,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// A warp's copy of kBytes contiguous bytes.
+template <int kBytes> __device__ __forceinline__ void copy_block(uint32_t dst, const char* src) {
+  const int at = (threadIdx.x & 31) * 16;
+#pragma unroll
+  for (int u = 0; u < kBytes; u += 512)
+    if (u + 512 <= kBytes || u + at < kBytes) copy16(dst + u + at, src + u + at);
+}
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -133,6 +157,17 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 // 2^e as a float, e in -126..127
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ int exponent(float x) { return ((__float_as_int(x) >> 23) & 255) - 127; }
+
+// Larger of two (step, eta) words, each half for itself; a NaN gives way.
+template <typename T> __device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max_pairs<__half>(uint32_t a, uint32_t b) {
+  const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <> __device__ __forceinline__ uint32_t max_pairs<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
 
 template <typename T> __device__ __forceinline__ float2 pair_floats(uint32_t w) { return scale_floats<T>(w); }
 template <typename T> __device__ __forceinline__ uint32_t pair_bits(float lo, float hi);
@@ -145,12 +180,14 @@ template <> __device__ __forceinline__ uint32_t pair_bits<__nv_bfloat16>(float l
 // Walks the items of a warp's part of the list.
 struct Walk {
   Seq s;
-  int b, hb, c;                            // sequence, key/value head x block, chunk
-  __device__ __forceinline__ void next(const Kv4AttnArgs& a, int heads_blocks) {
+  int b, hk, blk, c;                       // sequence, key/value head, block of query rows, chunk
+  __device__ __forceinline__ void next(const Kv4AttnArgs& a, const Plan& plan) {
     if (++c < s.chunks) return;
     c = 0;
-    if (++hb < heads_blocks) return;
-    hb = 0;
+    if (++blk < plan.blocks) return;
+    blk = 0;
+    if (++hk < a.cache.kv_heads) return;
+    hk = 0;
     do { ++b; } while (b < a.batch && (s = make_seq(a, b)).chunks == 0);
   }
 };
@@ -166,62 +203,76 @@ template <> __device__ __forceinline__ void load_words<2>(const char* p, uint32_
   w[0] = r.x; w[1] = r.y;
 }
 
+// What a chunk in flight is, written beside its bytes when its copies are issued.
+struct __align__(16) Item {
+  int t0, len, b, hk;                      // first token, tokens of its sequence, sequence, key/value head
+  int rows0, there, first, last;           // first query row; which runs of tokens are there (bit per page); first, last chunk of its list
+};
+
 template <typename T, int kDim, int kNT>
-__global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a, Plan plan) {
   constexpr int kWords = kDim / 32;        // words of codes per lane and 8 tokens
   constexpr int kTiles = kChunk / 16;
   constexpr int kStageBytes = kChunk * (kDim + 8);
-  constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
+  constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u, kOnes = 0x3C003C00u;
   extern __shared__ __align__(16) char smem[];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, qd = lane & 3;
-  const int w = blockIdx.x * kWarps + warp, parts = gridDim.x * kWarps;
-  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
-  const int ps = a.cache.page_size, block_bytes = Block<kDim>::bytes(ps), subs = kChunk / ps;
+  const int w = warp * gridDim.x + blockIdx.x;         // short lists spread over the SMs
+  const int ps = a.cache.page_size, pl = plan.page_log2, block_bytes = Block<kDim>::bytes(ps), subs = kChunk >> pl;
   char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
+  Item* items_of = reinterpret_cast<Item*>(smem + kWarps * kStages * kStageBytes) + warp * kStages;
 
   pdl_wait();
-  const int64_t total = total_chunks(a) * plan.heads_blocks;
-  const int64_t begin = part_begin(total, parts, w), end = part_begin(total, parts, w + 1);
-  const int items = (int)(end - begin);
+  const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
+  const int64_t begin = cut.begin(w);
+  const int items = (int)(cut.begin(w + 1) - begin);
   if (items == 0) return;
-  int64_t rest;
-  Walk now;
-  now.b = find_seq(a, plan.heads_blocks, begin, rest);
-  now.s = make_seq(a, now.b);
-  now.hb = (int)(rest / now.s.chunks);
-  now.c = (int)(rest % now.s.chunks);
 
   // ---- loads: the page numbers of a chunk are fetched one chunk before its copies are issued
-  Walk ahead = now;
+  Walk ahead;
+  {
+    int64_t rest;
+    ahead.b = find_seq(a, plan.heads_blocks, begin, rest);
+    ahead.s = make_seq(a, ahead.b);
+    const int hb = (int)divide(rest, ahead.s.chunks);
+    ahead.c = (int)(rest - (int64_t)hb * ahead.s.chunks);
+    ahead.hk = hb / plan.blocks;
+    ahead.blk = hb - ahead.hk * plan.blocks;
+  }
   auto page_of = [&](const Walk& x) -> int {           // lane i: the page of the chunk's i-th run of tokens; -1: nothing visible, or no page
     if (lane >= subs) return -1;
     const int t = x.s.start(x.c) + lane * ps;
     if (t >= x.s.len || (t + ps <= x.s.lo && t >= a.sinks)) return -1;
-    const int id = a.table[(int64_t)x.b * a.max_pages + t / ps];
+    const int id = a.table[(int64_t)x.b * a.max_pages + (t >> pl)];
     return id >= 0 && id < a.cache.num_pages ? id : -1;
   };
   int issued = 0;
-  uint32_t present = 0;                                // 4 bits per chunk in flight: which of its pages are there
   int ids = page_of(ahead);
   auto issue = [&]() {
     if (issued < items) {
-      const int hk = ahead.hb / plan.blocks;
-      const uint32_t dst = ring_addr + (issued % kStages) * kStageBytes;
-      present = (present << 4) | (__ballot_sync(0xFFFFFFFFu, ids >= 0) & 15u);
+      const int slot = issued % kStages;
+      const uint32_t dst = ring_addr + slot * kStageBytes;
+      const int there = (int)__ballot_sync(0xFFFFFFFFu, ids >= 0);
+      if (lane == 0) {
+        Item x;
+        x.t0 = ahead.s.start(ahead.c); x.len = ahead.s.len; x.b = ahead.b; x.hk = ahead.hk;
+        x.rows0 = ahead.blk * plan.rows_per_block; x.there = there; x.first = ahead.c == 0; x.last = ahead.c + 1 == ahead.s.chunks;
+        items_of[slot] = x;
+      }
       for (int i = 0; i < subs; ++i) {
         const int id = __shfl_sync(0xFFFFFFFFu, ids, i);
         if (id < 0) continue;
-        const char* src = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)id * a.cache.kv_heads + hk) * block_bytes;
-        for (int u = lane * 16; u < block_bytes; u += 512) copy16(dst + i * block_bytes + u, src + u);
+        const char* src = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)id * a.cache.kv_heads + ahead.hk) * block_bytes;
+        if (ps == 64) copy_block<64 * (kDim + 8)>(dst, src);
+        else if (ps == 32) copy_block<32 * (kDim + 8)>(dst + i * block_bytes, src);
+        else copy_block<16 * (kDim + 8)>(dst + i * block_bytes, src);
       }
       if (issued + 1 < items) {
-        ahead.next(a, plan.heads_blocks);
+        ahead.next(a, plan);
         ids = page_of(ahead);
       }
-    } else {
-      present <<= 4;
     }
     ++issued;
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -229,88 +280,87 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) issue();
 
+  // where tile i (16 tokens) of a stage has its key codes and its key (step, eta) pairs; those of the values follow
+  // v_off and 4 ps bytes later
+  int code_at[kTiles], scale_at[kTiles];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const int j0 = (i * 16) & (ps - 1), base = (i * 16 >> pl) * block_bytes;
+    code_at[i] = base + j0 * (kDim / 2) + lane * (kWords * 4);
+    scale_at[i] = base + Block<kDim>::k_scale(ps) + 4 * (j0 + g);
+  }
+  const int v_off = Block<kDim>::v_codes(ps);
+
   // ---- state of the segment (one sequence, head and block of rows) being worked on
   uint32_t qf[kNT][kWords][4];                         // query operand: per word of codes the pairs (0,4), (1,5)/16, (2,6), (3,7)/16
   float f[kNT][2], qsum[kNT][2];                       // per column: scale of the raw score, scaled sum of the query
   float acc[kNT][2 * kWords][4];
-  float m[kNT][2], l[kNT][2], esum[kNT][2], dsum[kNT][2];
-  int vexp = 0, seg_first = 0;                         // 2^vexp: running size of the value steps
-  bool fresh = true;
+  float m[kNT][2], l[kNT][2], esum[kNT][2];
+  float usum[kNT][4];                                  // sums of the rounded p . step' (every row of the tile alike)
+  int vexp = 0;                                        // 2^vexp: running size of the value steps
+  int back_first = 0, back_last = 0;                   // positions of the block's first and last query, back from the sequence's end
+  bool from_start = false, later = false;              // the segment began with its list's first chunk; it is not the warp's first
 
-  for (int item = 0; item < items; ++item) {
-    const int rows0 = (now.hb % plan.blocks) * plan.rows_per_block, hk = now.hb / plan.blocks;
-    if (fresh) {
-      fresh = false;
-      seg_first = item;
-      vexp = -1000;
-      const float sl = a.scale * 1.4426950408889634f;
+  auto begin_segment = [&](const Item& it) {
+    from_start = it.first;
+    vexp = -1000;
+    back_first = a.n_q - it.rows0 / plan.group;
+    back_last = a.n_q - (min(it.rows0 + plan.rows_per_block, plan.rows) - 1) / plan.group;
+    const float sl = a.scale * 1.4426950408889634f;
 #pragma unroll
-      for (int nt = 0; nt < kNT; ++nt) {
-        const int r = rows0 + nt * 8 + g;
-        const bool on = r < plan.rows;
-        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)now.b * a.n_q + (on ? r / plan.group : 0)) * a.ld_q +
-                     (int64_t)(hk * plan.group + (on ? r % plan.group : 0)) * kDim + qd * (kDim / 4);
-        float v[kWords][8], top = 0.f, sum = 0.f;
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int r = it.rows0 + nt * 8 + g, i_q = r / plan.group;
+      const bool on = r < plan.rows;
+      const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)it.b * a.n_q + i_q) * a.ld_q +
+                   (int64_t)(it.hk * plan.group + r - i_q * plan.group) * kDim + qd * (kDim / 4);
+      float v[kWords][8], top = 0.f, sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-          const uint4 x = on ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0, 0, 0, 0);
-          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+      for (int i = 0; i < kWords; ++i) {
+        const uint4 x = on ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0, 0, 0, 0);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 y = pair_floats<T>(xs[j]);
-            v[i][2 * j] = y.x; v[i][2 * j + 1] = y.y;
-            top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-            sum += y.x + y.y;
-          }
+        for (int j = 0; j < 4; ++j) {
+          const float2 y = pair_floats<T>(xs[j]);
+          v[i][2 * j] = y.x; v[i][2 * j + 1] = y.y;
+          top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+          sum += y.x + y.y;
         }
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1); sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-        const int e = min(13 - exponent(top), 100);    // the largest value goes to 2^13 (all zero: any scale)
-        const float up = pow2i(max(e, -114));
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-          qf[nt][i][0] = half2_bits(v[i][0] * up, v[i][4] * up);
-          qf[nt][i][1] = half2_bits(v[i][1] * up * 0.0625f, v[i][5] * up * 0.0625f);
-          qf[nt][i][2] = half2_bits(v[i][2] * up, v[i][6] * up);
-          qf[nt][i][3] = half2_bits(v[i][3] * up * 0.0625f, v[i][7] * up * 0.0625f);
-        }
-        const float fr = sl * pow2i(min(24 - max(e, -114), 127)), sr = sum * sl;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          f[nt][j] = __shfl_sync(0xFFFFFFFFu, fr, 4 * (2 * qd + j));
-          qsum[nt][j] = __shfl_sync(0xFFFFFFFFu, sr, 4 * (2 * qd + j));
-          m[nt][j] = -INFINITY;
-          l[nt][j] = esum[nt][j] = dsum[nt][j] = 0.f;
-        }
-#pragma unroll
-        for (int t = 0; t < 2 * kWords; ++t) acc[nt][t][0] = acc[nt][t][1] = acc[nt][t][2] = acc[nt][t][3] = 0.f;
       }
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1); sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+      const int e = min(13 - exponent(top), 100);      // the largest value goes to 2^13 (all zero: any scale)
+      const float up = pow2i(max(e, -114));
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        qf[nt][i][0] = half2_bits(v[i][0] * up, v[i][4] * up);
+        qf[nt][i][1] = half2_bits(v[i][1] * up * 0.0625f, v[i][5] * up * 0.0625f);
+        qf[nt][i][2] = half2_bits(v[i][2] * up, v[i][6] * up);
+        qf[nt][i][3] = half2_bits(v[i][3] * up * 0.0625f, v[i][7] * up * 0.0625f);
+      }
+      const float fr = sl * pow2i(min(24 - max(e, -114), 127)), sr = sum * sl;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f[nt][j] = __shfl_sync(0xFFFFFFFFu, fr, 4 * (2 * qd + j));
+        qsum[nt][j] = __shfl_sync(0xFFFFFFFFu, sr, 4 * (2 * qd + j));
+        m[nt][j] = -INFINITY;
+        l[nt][j] = esum[nt][j] = 0.f;
+      }
+      usum[nt][0] = usum[nt][1] = usum[nt][2] = usum[nt][3] = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2 * kWords; ++t) acc[nt][t][0] = acc[nt][t][1] = acc[nt][t][2] = acc[nt][t][3] = 0.f;
     }
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncwarp();                                      // the chunk is there, and its predecessor's stage is free
-    issue();
-    const char* stage = ring + (item % kStages) * kStageBytes;
-    const uint32_t there = (present >> (4 * (issued - 1 - item))) & 15u;
-    const int t0 = now.s.start(now.c);
-    // every query of this block sees every token of the chunk?
-    const int pos_first = now.s.len - a.n_q + rows0 / plan.group;
-    const int pos_last = now.s.len - a.n_q + (min(rows0 + plan.rows_per_block, plan.rows) - 1) / plan.group;
-    const bool clean = there == (1u << subs) - 1 && t0 + kChunk - 1 <= pos_first &&
-                       (a.window == 0 || pos_last - t0 < a.window || t0 + kChunk <= a.sinks);
-    auto tile_base = [&](int i, int& j0) -> const char* {
-      j0 = (i * 16) & (ps - 1);
-      return stage + (i * 16 / ps) * block_bytes;
-    };
+  };
 
-    // ---- scores of the chunk: tile i, row g and g + 8 (tokens), columns 2 qd and 2 qd + 1 of each 8 query rows
+  // One chunk; kMask: some query of the block does not see some token of it.
+  auto chunk = [&](const char* stage, const Item& it, auto masked) {
+    constexpr bool kMask = decltype(masked)::value;
+    // ---- scores: tile i, rows g and g + 8 (tokens), columns 2 qd and 2 qd + 1 of each 8 query rows
     float s[kTiles][kNT][4];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      int j0;
-      const char* base = tile_base(i, j0);
       uint32_t x[kWords], y[kWords];
-      load_words<kWords>(base + j0 * (kDim / 2) + lane * (kWords * 4), x);
-      load_words<kWords>(base + j0 * (kDim / 2) + 4 * kDim + lane * (kWords * 4), y);
+      load_words<kWords>(stage + code_at[i], x);
+      load_words<kWords>(stage + code_at[i] + 4 * kDim, y);
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt) s[i][nt][0] = s[i][nt][1] = s[i][nt][2] = s[i][nt][3] = 0.f;
 #pragma unroll
@@ -323,48 +373,46 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         }
       }
     }
-    float mx[kNT][2], vtop = 0.f;
+    // scaled, their largest per query row, and the largest value step
+    float mx[kNT][2];
+    uint32_t vs[kTiles][2], vmax = 0;
+    uint32_t seen = 0;                                 // 4 bits per tile and 8 query rows, as s[i][nt]
+    int pos_of[kNT][2];
+    if (kMask) {
 #pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) { mx[nt][0] = m[nt][0]; mx[nt][1] = m[nt][1]; }
-    uint32_t seen = 0xFFFFFFFFu;                       // per tile 4 bits per 8 query rows, as s[i][nt]; kNT <= 2
-    if (!clean) {
-      seen = 0;
+      for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int t = t0 + i * 16 + g + (e >> 1) * 8, r = rows0 + nt * 8 + 2 * qd + (e & 1);
-            const int pos = now.s.len - a.n_q + min(r, plan.rows - 1) / plan.group;
-            const bool v = t <= pos && ((there >> (i * 16 / ps)) & 1u) && (a.window == 0 || pos - t < a.window || t < a.sinks);
-            seen |= (uint32_t)v << ((i * kNT + nt) * 4 + e);
-          }
+        for (int j = 0; j < 2; ++j) pos_of[nt][j] = it.len - a.n_q + min(it.rows0 + nt * 8 + 2 * qd + j, plan.rows - 1) / plan.group;
     }
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      int j0;
-      const char* base = tile_base(i, j0);
-      const char* kse = base + Block<kDim>::k_scale(ps) + 4 * j0;
-      const float2 k0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(kse + 4 * g));
-      const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(kse + 4 * g + 32));
-      const char* vse = base + Block<kDim>::v_scale(ps) + 4 * j0;
-      const float v0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g)).x;
-      const float v1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g + 32)).x;
+    for (int nt = 0; nt < kNT; ++nt) { mx[nt][0] = m[nt][0]; mx[nt][1] = m[nt][1]; }
 #pragma unroll
-      for (int nt = 0; nt < kNT; ++nt) {
+    for (int i = 0; i < kTiles; ++i) {
+      const char* se = stage + scale_at[i];
+      const float2 k0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se));
+      const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se + 32));
+      vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * ps);
+      vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * ps + 32);
+      uint32_t any = 0;
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 kk = e < 2 ? k0 : k1;
-          float z = fmaf(s[i][nt][e] * f[nt][e & 1], kk.x, kk.y * qsum[nt][e & 1]);
-          if (!clean && !((seen >> ((i * kNT + nt) * 4 + e)) & 1u)) z = -INFINITY;
-          s[i][nt][e] = z;
-          mx[nt][e & 1] = fmaxf(mx[nt][e & 1], z);
+          s[i][nt][e] = fmaf(s[i][nt][e] * f[nt][e & 1], kk.x, kk.y * qsum[nt][e & 1]);
+          if (kMask) {
+            const int t = it.t0 + i * 16 + g + (e >> 1) * 8, pos = pos_of[nt][e & 1];
+            const bool v = t <= pos && ((it.there >> (i * 16 >> pl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
+            if (v) { seen |= 1u << ((i * kNT + nt) * 4 + e); any |= 1u << (e >> 1); }
+            else s[i][nt][e] = -INFINITY;
+          }
+          mx[nt][e & 1] = fmaxf(mx[nt][e & 1], s[i][nt][e]);
         }
-        const uint32_t any = clean ? 15u : (seen >> ((i * kNT + nt) * 4)) & 15u;
-        if (any & 3u) vtop = fmaxf(vtop, v0);
-        if (any & 12u) vtop = fmaxf(vtop, v1);
+      if (kMask) {                                     // a token that none of this lane's rows sees: whatever lies there counts as zero
+        if (!(any & 1u)) vs[i][0] = 0;
+        if (!(any & 2u)) vs[i][1] = 0;
       }
+      vmax = max_pairs<T>(vmax, max_pairs<T>(vs[i][0], vs[i][1]));
     }
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
@@ -373,71 +421,69 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         mx[nt][0] = fmaxf(mx[nt][0], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][0], o));
         mx[nt][1] = fmaxf(mx[nt][1], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][1], o));
       }
-      vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, o));
+      vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, o));
     }
-    if (!clean) {
-      vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, 1)); vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, 2));
+    if (kMask) {
+      vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, 1)); vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, 2));
     }
+    const float vtop = scale_floats<T>(vmax).x;
     const int ve = max(vexp, max(exponent(vtop), -100));
-    const float vshift = vexp < ve ? (vexp < ve - 100 ? 0.f : pow2i(vexp - ve)) : 1.f, vscale = pow2i(min(13 - ve, 120));
     bool moved = ve != vexp;
-    vexp = ve;
-    float mu[kNT][2];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
       for (int j = 0; j < 2; ++j) moved |= mx[nt][j] != m[nt][j];
     if (__any_sync(0xFFFFFFFFu, moved)) {
+      const float vshift = vexp < ve ? (vexp < ve - 100 ? 0.f : pow2i(vexp - ve)) : 1.f;
+      vexp = ve;
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const float c = m[nt][j] == -INFINITY ? 0.f : ex2(m[nt][j] - mx[nt][j]), cv = c * vshift;
           m[nt][j] = mx[nt][j];
-          l[nt][j] *= c; esum[nt][j] *= c; dsum[nt][j] *= cv;
+          l[nt][j] *= c; esum[nt][j] *= c; usum[nt][j] *= cv;
 #pragma unroll
           for (int t = 0; t < 2 * kWords; ++t) { acc[nt][t][j] *= cv; acc[nt][t][2 + j] *= cv; }
         }
     }
+    const float vscale = pow2i(min(13 - vexp, 120));
+    float mu[kNT][2];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) mu[nt][j] = m[nt][j] == -INFINITY ? 0.f : m[nt][j];
+      for (int j = 0; j < 2; ++j) mu[nt][j] = kMask && m[nt][j] == -INFINITY ? 0.f : m[nt][j];
 
     // ---- probabilities, and their products with the value codes
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      int j0;
-      const char* base = tile_base(i, j0);
-      const char* vse = base + Block<kDim>::v_scale(ps) + 4 * j0;
-      float2 v0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g));
-      float2 v1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(vse + 4 * g + 32));
+      float2 v0 = scale_floats<T>(vs[i][0]), v1 = scale_floats<T>(vs[i][1]);
+      v0.y = fmaf(7.5f, v0.x, v0.y); v1.y = fmaf(7.5f, v1.x, v1.y);
       v0.x *= vscale; v1.x *= vscale;
       uint32_t b0[kNT], b1[kNT];
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt) {
-        float p[4], u[4];
+        float u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = ex2(s[i][nt][e] - mu[nt][e & 1]);
-          l[nt][e & 1] += p[e];
-          const float2 vv = e < 2 ? v0 : v1;
-          u[e] = p[e] * vv.x;
-          float pe = p[e] * vv.y;
-          if (!clean && !((seen >> ((i * kNT + nt) * 4 + e)) & 1u)) u[e] = pe = 0.f;   // whatever lies there
-          esum[nt][e & 1] += pe;
+          const float p = ex2(s[i][nt][e] - mu[nt][e & 1]);
+          l[nt][e & 1] += p;
+          u[e] = p * (e < 2 ? v0.x : v1.x);
+          if (kMask) {
+            const bool v = (seen >> ((i * kNT + nt) * 4 + e)) & 1u;
+            if (!v) u[e] = 0.f;
+            esum[nt][e & 1] += v ? p * (e < 2 ? v0.y : v1.y) : 0.f;
+          } else {
+            esum[nt][e & 1] = fmaf(p, e < 2 ? v0.y : v1.y, esum[nt][e & 1]);
+          }
         }
-        b0[nt] = half2_bits(u[0], u[1]);
-        b1[nt] = half2_bits(u[2], u[3]);
-        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&b0[nt])), r1 = __half22float2(*reinterpret_cast<const __half2*>(&b1[nt]));
-        dsum[nt][0] += (r0.x - u[0]) + (r1.x - u[2]);
-        dsum[nt][1] += (r0.y - u[1]) + (r1.y - u[3]);
-        b0[nt] = transpose8x8(b0[nt]);
-        b1[nt] = transpose8x8(b1[nt]);
+        b0[nt] = transpose8x8(half2_bits(u[0], u[1]));
+        b1[nt] = transpose8x8(half2_bits(u[2], u[3]));
+        mma16816(usum[nt], kOnes, kOnes, kOnes, kOnes, b0[nt], b1[nt]);
       }
       uint32_t x[kWords], y[kWords];
-      load_words<kWords>(base + Block<kDim>::v_codes(ps) + j0 * (kDim / 2) + lane * (kWords * 4), x);
-      load_words<kWords>(base + Block<kDim>::v_codes(ps) + j0 * (kDim / 2) + 4 * kDim + lane * (kWords * 4), y);
+      load_words<kWords>(stage + code_at[i] + v_off, x);
+      load_words<kWords>(stage + code_at[i] + v_off + 4 * kDim, y);
 #pragma unroll
       for (int k = 0; k < kWords; ++k) {
         const uint32_t xs = x[k] >> 8, ys = y[k] >> 8;
@@ -448,82 +494,93 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         }
       }
     }
+  };
 
-    // ---- end of the segment
-    if (now.c + 1 == now.s.chunks || item + 1 == items) {
-      const bool whole = now.c + 1 == now.s.chunks && now.c - (item - seg_first) == 0;
-      const float back = pow2i(min(max(vexp - 13, -126), 127));
-      float* slot = reinterpret_cast<float*>(a.ws) + (int64_t)(2 * w + (seg_first > 0)) * plan.rows_per_block * (kDim + 4);
+  auto end_segment = [&](const Item& it) {
+    const bool whole = from_start && it.last;
+    const float back = pow2i(min(max(vexp - 13, -126), 127));
+    float* slot = reinterpret_cast<float*>(a.ws) + (int64_t)(2 * w + later) * plan.rows_per_block * (kDim + 4);
 #pragma unroll
-      for (int nt = 0; nt < kNT; ++nt)
+    for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float lt = l[nt][j], et = esum[nt][j], dt = dsum[nt][j];
+      for (int j = 0; j < 2; ++j) {
+        float lt = l[nt][j], et = esum[nt][j];
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            lt += __shfl_xor_sync(0xFFFFFFFFu, lt, o);
-            et += __shfl_xor_sync(0xFFFFFFFFu, et, o);
-            dt += __shfl_xor_sync(0xFFFFFFFFu, dt, o);
-          }
-          const int rr = nt * 8 + 2 * qd + j, r = rows0 + rr;
-          if (rr >= plan.rows_per_block || r >= plan.rows) continue;
-          const float add = et - 7.5f * dt * back, norm = whole ? (lt == 0.f ? 0.f : 1.f / lt) : 1.f;
-          float o[kDim / 8];                           // values (kDim / 8) g .. of the row
-#pragma unroll
-          for (int t = 0; t < 2 * kWords; ++t) {
-            o[2 * t] = (acc[nt][t][j] * 16777216.f * back + add) * norm;
-            o[2 * t + 1] = (acc[nt][t][2 + j] * 1048576.f * back + add) * norm;
-          }
-          if (whole) {
-            T* out = reinterpret_cast<T*>(a.o) + ((int64_t)now.b * a.n_q + r / plan.group) * a.ld_o +
-                     (int64_t)(hk * plan.group + r % plan.group) * kDim + g * (kDim / 8);
-#pragma unroll
-            for (int i = 0; i < kDim / 64; ++i)
-              *reinterpret_cast<uint4*>(out + 8 * i) =
-                  make_uint4(pair_bits<T>(o[8 * i], o[8 * i + 1]), pair_bits<T>(o[8 * i + 2], o[8 * i + 3]),
-                             pair_bits<T>(o[8 * i + 4], o[8 * i + 5]), pair_bits<T>(o[8 * i + 6], o[8 * i + 7]));
-          } else {
-            float* row = slot + rr * (kDim + 4);
-#pragma unroll
-            for (int i = 0; i < kDim / 32; ++i)
-              *reinterpret_cast<float4*>(row + g * (kDim / 8) + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-            if (g == 0) *reinterpret_cast<float2*>(row + kDim) = make_float2(m[nt][j], lt);
-          }
+        for (int o = 4; o < 32; o <<= 1) {
+          lt += __shfl_xor_sync(0xFFFFFFFFu, lt, o);
+          et += __shfl_xor_sync(0xFFFFFFFFu, et, o);
         }
-      fresh = true;
-    }
-    if (item + 1 < items) now.next(a, plan.heads_blocks);
+        const int rr = nt * 8 + 2 * qd + j, r = it.rows0 + rr;
+        if (rr >= plan.rows_per_block || r >= plan.rows) continue;
+        const float add = et - 7.5f * usum[nt][j] * back, norm = whole ? (lt == 0.f ? 0.f : 1.f / lt) : 1.f;
+        float o[kDim / 8];                             // values (kDim / 8) g .. of the row
+#pragma unroll
+        for (int t = 0; t < 2 * kWords; ++t) {
+          o[2 * t] = (acc[nt][t][j] * 16777216.f * back + add) * norm;
+          o[2 * t + 1] = (acc[nt][t][2 + j] * 1048576.f * back + add) * norm;
+        }
+        if (whole) {
+          const int i_q = r / plan.group;
+          T* out = reinterpret_cast<T*>(a.o) + ((int64_t)it.b * a.n_q + i_q) * a.ld_o +
+                   (int64_t)(it.hk * plan.group + r - i_q * plan.group) * kDim + g * (kDim / 8);
+#pragma unroll
+          for (int i = 0; i < kDim / 64; ++i)
+            *reinterpret_cast<uint4*>(out + 8 * i) =
+                make_uint4(pair_bits<T>(o[8 * i], o[8 * i + 1]), pair_bits<T>(o[8 * i + 2], o[8 * i + 3]),
+                           pair_bits<T>(o[8 * i + 4], o[8 * i + 5]), pair_bits<T>(o[8 * i + 6], o[8 * i + 7]));
+        } else {
+          float* row = slot + rr * (kDim + 4);
+#pragma unroll
+          for (int i = 0; i < kDim / 32; ++i)
+            *reinterpret_cast<float4*>(row + g * (kDim / 8) + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          if (g == 0) *reinterpret_cast<float2*>(row + kDim) = make_float2(m[nt][j], lt);
+        }
+      }
+    later = true;
+  };
+
+  bool fresh = true;
+  for (int item = 0; item < items; ++item) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();                                      // the chunk is there, and its predecessor's stage is free
+    const Item it = items_of[item % kStages];
+    issue();
+    if (fresh) begin_segment(it);
+    fresh = it.last;
+    const bool all_see = it.there == (1 << subs) - 1 && it.t0 + kChunk - 1 <= it.len - back_first &&
+                         (a.window == 0 || it.len - back_last - it.t0 < a.window || it.t0 + kChunk <= a.sinks);
+    const char* stage = ring + (item % kStages) * kStageBytes;
+    if (all_see) chunk(stage, it, std::false_type{});
+    else chunk(stage, it, std::true_type{});
+    if (it.last || item + 1 == items) end_segment(it);
   }
 }
 
 // Joins the parts of the rows whose chunks went to more than one warp: one CTA per row, warps take the parts in turn.
 template <typename T, int kDim>
-__global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, int parts) {
+__global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, Plan plan) {
   constexpr int kVals = kDim / 32;
   __shared__ float sums[kJoinWarps][kDim + 4];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
-  const int rr = blockIdx.x % plan.rows_per_block, bh = blockIdx.x / plan.rows_per_block;
-  const int b = bh / plan.heads_blocks, hb = bh % plan.heads_blocks;
-  const int r = (hb % plan.blocks) * plan.rows_per_block + rr, hk = hb / plan.blocks;
+  const int bh = blockIdx.x / plan.rows_per_block, rr = blockIdx.x - bh * plan.rows_per_block;
+  const int b = bh / plan.heads_blocks, hb = bh - b * plan.heads_blocks;
+  const int hk = hb / plan.blocks, r = (hb - hk * plan.blocks) * plan.rows_per_block + rr, i_q = r / plan.group;
   pdl_launch_dependents();
   pdl_wait();
   if (r >= plan.rows) return;
   const int chunks = make_seq(a, b).chunks;
-  T* out = reinterpret_cast<T*>(a.o) + ((int64_t)b * a.n_q + r / plan.group) * a.ld_o + (int64_t)(hk * plan.group + r % plan.group) * kDim;
+  T* out = reinterpret_cast<T*>(a.o) + ((int64_t)b * a.n_q + i_q) * a.ld_o + (int64_t)(hk * plan.group + r - i_q * plan.group) * kDim;
   if (chunks == 0) {                                   // an empty sequence
     for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) out[d] = out_cast<T>(0.f);
     return;
   }
-  const int64_t total = total_chunks(a) * plan.heads_blocks;
+  const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
   const int64_t first = chunks_before(a, b) * plan.heads_blocks + (int64_t)hb * chunks;
-  const int w0 = owner(total, parts, first), w1 = owner(total, parts, first + chunks - 1);
+  const int w0 = cut.owner(first), w1 = cut.owner(first + chunks - 1);
   if (w0 == w1) return;                                // written already
   float m = -INFINITY, l = 0.f, v[kVals] = {};
   for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
-    const int64_t wb = part_begin(total, parts, w);
-    if (part_begin(total, parts, w + 1) == wb) continue;
-    const float* row = reinterpret_cast<const float*>(a.ws) + ((int64_t)(2 * w + (wb < first)) * plan.rows_per_block + rr) * (kDim + 4);
+    const float* row = reinterpret_cast<const float*>(a.ws) + ((int64_t)(2 * w + (cut.begin(w) < first)) * plan.rows_per_block + rr) * (kDim + 4);
     const float2 ml = *reinterpret_cast<const float2*>(row + kDim);
     if (ml.x == -INFINITY) continue;                   // the part holds nothing that this row sees
     const float top = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : ex2(m - top), p = ex2(ml.x - top);
@@ -566,7 +623,8 @@ cudaError_t sm_count(int* n) {
 
 template <typename T, int kDim, int kNT>
 cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
-  constexpr int kSmem = kWarps * kStages * kChunk * (kDim + 8);
+  constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item));
+  static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
   static std::atomic<uint64_t> ready{0};               // devices on which the kernel's shared memory limit is set
   int dev = 0, sms = 0;
   cudaError_t e = sm_count(&sms);
@@ -577,16 +635,16 @@ cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads);
-  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a);
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
+  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan);
   if (e != cudaSuccess) return e;
   return launch_pdl(attention_kv4_join_kernel<T, kDim>, (unsigned)((int64_t)a.batch * plan.heads_blocks * plan.rows_per_block),
-                    kJoinWarps * 32, 0, s, a, sms * kWarps);
+                    kJoinWarps * 32, 0, s, a, plan);
 }
 
 template <typename T>
 cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
-  const bool few = make_plan(a.n_q, a.heads, a.cache.kv_heads).rows <= 8;
+  const bool few = (int64_t)a.n_q * (a.heads / a.cache.kv_heads) <= 8;
   if (a.cache.head_dim == 64) return few ? launch_rows<T, 64, 1>(a, s) : launch_rows<T, 64, 2>(a, s);
   return few ? launch_rows<T, 128, 1>(a, s) : launch_rows<T, 128, 2>(a, s);
 }
@@ -594,7 +652,7 @@ cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
 }  // namespace
 
 size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
-  const Plan p = make_plan(n_q, heads, kv_heads);
+  const Plan p = make_plan(n_q, heads, kv_heads, 16, 1);
   return (size_t)kMaxSms * kWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float) * (batch > 0);
 }
 
