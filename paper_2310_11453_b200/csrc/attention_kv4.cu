@@ -34,7 +34,7 @@ namespace {
 
 using namespace kv4;
 
-constexpr int kChunk = 64;                 // tokens per work item
+constexpr int kChunkLog2 = 6, kChunk = 1 << kChunkLog2;   // tokens per work item
 constexpr int kWarps = 8;                  // per CTA, one CTA per SM
 constexpr int kStages = 3;                 // chunks of a warp in shared memory
 constexpr int kMaxSms = 160;
@@ -150,6 +150,15 @@ template <int kBytes> __device__ __forceinline__ void copy_block(uint32_t dst, c
   for (int u = 0; u < kBytes; u += 512)
     if (u + 512 <= kBytes || u + at < kBytes) copy16(dst + u + at, src + u + at);
 }
+// A warp's copy of tokens j .. j + kRun - 1 out of a head's larger page of ps tokens.
+template <int kDim, int kRun> __device__ __forceinline__ void copy_part(uint32_t dst, const char* src, int ps, int j) {
+  copy_block<kRun * (kDim / 2)>(dst, src + j * (kDim / 2));
+  copy_block<kRun * (kDim / 2)>(dst + kRun * (kDim / 2), src + Block<kDim>::v_codes(ps) + j * (kDim / 2));
+  const int lane = threadIdx.x & 31, half = kRun / 4;   // 16-byte pieces of the keys' pairs, then of the values'
+  if (lane < 2 * half)
+    copy16(dst + kRun * kDim + lane * 16,
+           src + (lane < half ? Block<kDim>::k_scale(ps) + 4 * j + lane * 16 : Block<kDim>::v_scale(ps) + 4 * j + (lane - half) * 16));
+}
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -219,7 +228,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, qd = lane & 3;
   const int w = warp * gridDim.x + blockIdx.x;         // short lists spread over the SMs
-  const int ps = a.cache.page_size, pl = plan.page_log2, block_bytes = Block<kDim>::bytes(ps), subs = kChunk >> pl;
+  // a stage holds runs of rl = min(page, chunk) tokens, each laid out as a page of that size would be
+  const int ps = a.cache.page_size, pl = plan.page_log2, rs = min(ps, kChunk), rl = min(pl, kChunkLog2);
+  const int block_bytes = Block<kDim>::bytes(ps), run_bytes = Block<kDim>::bytes(rs), subs = kChunk >> rl;
   char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
   Item* items_of = reinterpret_cast<Item*>(smem + kWarps * kStages * kStageBytes) + warp * kStages;
@@ -243,8 +254,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   }
   auto page_of = [&](const Walk& x) -> int {           // lane i: the page of the chunk's i-th run of tokens; -1: nothing visible, or no page
     if (lane >= subs) return -1;
-    const int t = x.s.start(x.c) + lane * ps;
-    if (t >= x.s.len || (t + ps <= x.s.lo && t >= a.sinks)) return -1;
+    const int t = x.s.start(x.c) + lane * rs;
+    if (t >= x.s.len || (t + rs <= x.s.lo && t >= a.sinks)) return -1;
     const int id = a.table[(int64_t)x.b * a.max_pages + (t >> pl)];
     return id >= 0 && id < a.cache.num_pages ? id : -1;
   };
@@ -265,9 +276,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         const int id = __shfl_sync(0xFFFFFFFFu, ids, i);
         if (id < 0) continue;
         const char* src = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)id * a.cache.kv_heads + ahead.hk) * block_bytes;
-        if (ps == 64) copy_block<64 * (kDim + 8)>(dst, src);
-        else if (ps == 32) copy_block<32 * (kDim + 8)>(dst + i * block_bytes, src);
-        else copy_block<16 * (kDim + 8)>(dst + i * block_bytes, src);
+        if (ps > kChunk) copy_part<kDim, kChunk>(dst, src, ps, ahead.s.start(ahead.c) & (ps - 1));
+        else if (rs == kChunk) copy_block<kChunk * (kDim + 8)>(dst, src);
+        else if (rs == 32) copy_block<32 * (kDim + 8)>(dst + i * run_bytes, src);
+        else copy_block<16 * (kDim + 8)>(dst + i * run_bytes, src);
       }
       if (issued + 1 < items) {
         ahead.next(a, plan);
@@ -281,15 +293,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   for (int i = 0; i < kStages - 1; ++i) issue();
 
   // where tile i (16 tokens) of a stage has its key codes and its key (step, eta) pairs; those of the values follow
-  // v_off and 4 ps bytes later
+  // v_off and 4 rs bytes later
   int code_at[kTiles], scale_at[kTiles];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
-    const int j0 = (i * 16) & (ps - 1), base = (i * 16 >> pl) * block_bytes;
+    const int j0 = (i * 16) & (rs - 1), base = (i * 16 >> rl) * run_bytes;
     code_at[i] = base + j0 * (kDim / 2) + lane * (kWords * 4);
-    scale_at[i] = base + Block<kDim>::k_scale(ps) + 4 * (j0 + g);
+    scale_at[i] = base + Block<kDim>::k_scale(rs) + 4 * (j0 + g);
   }
-  const int v_off = Block<kDim>::v_codes(ps);
+  const int v_off = Block<kDim>::v_codes(rs);
 
   // ---- state of the segment (one sequence, head and block of rows) being worked on
   uint32_t qf[kNT][kWords][4];                         // query operand: per word of codes the pairs (0,4), (1,5)/16, (2,6), (3,7)/16
@@ -391,8 +403,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
       const char* se = stage + scale_at[i];
       const float2 k0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se));
       const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se + 32));
-      vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * ps);
-      vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * ps + 32);
+      vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * rs);
+      vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * rs + 32);
       uint32_t any = 0;
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
@@ -402,7 +414,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
           s[i][nt][e] = fmaf(s[i][nt][e] * f[nt][e & 1], kk.x, kk.y * qsum[nt][e & 1]);
           if (kMask) {
             const int t = it.t0 + i * 16 + g + (e >> 1) * 8, pos = pos_of[nt][e & 1];
-            const bool v = t <= pos && ((it.there >> (i * 16 >> pl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
+            const bool v = t <= pos && ((it.there >> (i * 16 >> rl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
             if (v) { seen |= 1u << ((i * kNT + nt) * 4 + e); any |= 1u << (e >> 1); }
             else s[i][nt][e] = -INFINITY;
           }
