@@ -402,7 +402,9 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
  *   head_dim 64 or 128; heads a multiple of kv_heads; scale 0 means 1 / sqrt(head_dim).
  * Values in invisible places have no influence, whatever they are (infinities and NaN included).
  * fp32 softmax statistics and accumulators; probabilities are rounded to the type of v for the
- * product, and one rounding on output.  batch = 0 or seq_q = 0 is valid and does nothing.  No workspace. */
+ * product, and one rounding on output.  The kernel's waits are bounded; if one ever ran out, the rows concerned are
+ * computed another way (same result up to rounding), so there is no status to collect.
+ * batch = 0 or seq_q = 0 is valid and does nothing.  No workspace. */
 bl_status bitlinear_attention_window(const void* q, const void* k, const void* v, void* o, bl_dtype dt, int batch,
                                      const int32_t* cu_q, const int32_t* cu_k, int64_t seq_q, int64_t seq_k,
                                      int64_t rows_q, int64_t rows_k, int heads, int kv_heads, int head_dim,
@@ -476,9 +478,10 @@ bl_status bitlinear_ws_status(const void* ws, void* stream);
 
 /* Test and diagnostic hook: caps the number of polls that the bounded device-side waits of
  * kernels launched afterwards by this process may make (bitlinear_gemv_decode's wait for its
- * weight copies; the meeting between the two passes of the cooperative per-tensor kernel of
+ * weight copies; the waits of bitlinear_attention_window; the meeting between the two passes of the cooperative per-tensor kernel of
  * bitlinear_quant_act).  polls < 0 restores the built-in limits; 0 means a single poll (for
- * bitlinear_gemv_decode: none at all, every warp reads its weights from global memory).
+ * bitlinear_gemv_decode and bitlinear_attention_window: none at all, weights are read from global
+ * memory, rows are computed one by one).
  * meet_skew != 0 additionally makes the cooperative kernel wait for an arrival tag that no CTA
  * publishes, so that its wait runs out by construction: the kernel then records
  * BL_ERR_TIMEOUT in the status word, writes no codes and returns (nothing hangs, traps or
@@ -492,6 +495,10 @@ bl_status bitlinear_debug_wait_limit(int64_t polls, int meet_skew);
  * instead.  The result of such a call is still correct, only slow; a healthy run returns 0.
  * -1 on a CUDA error. */
 int64_t bitlinear_debug_decode_fallbacks(void* stream);
+
+/* The same for bitlinear_attention_window: the number of CTAs whose bounded waits ran out, so that they
+ * computed their rows over the visible places one by one. */
+int64_t bitlinear_debug_window_fallbacks(void* stream);
 
 #ifdef __cplusplus
 }

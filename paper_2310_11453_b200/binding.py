@@ -35,6 +35,7 @@ EXPORTS = [
     "bitlinear_gemv_decode_batch_ws",
     "bitlinear_qk_norm_rope", "bitlinear_attention_window", "bitlinear_kv4_page_bytes", "bitlinear_kv4_append",
     "bitlinear_kv4_read", "bitlinear_attention_kv4", "bitlinear_attention_kv4_ws_bytes", "bitlinear_kv4_copy_pages",
+    "bitlinear_debug_window_fallbacks",
 ]
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -103,6 +104,8 @@ def lib():
         L.bitlinear_binarize_pack_nsplit.argtypes = [vp, ci, i64, i64, ci, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
         L.bitlinear_debug_decode_fallbacks.restype = i64
         L.bitlinear_debug_decode_fallbacks.argtypes = [vp]
+        L.bitlinear_debug_window_fallbacks.restype = i64
+        L.bitlinear_debug_window_fallbacks.argtypes = [vp]
         L.bitlinear_noalloc_status.restype = ci
         L.bitlinear_noalloc_status.argtypes = [vp]
         L.bitlinear_debug_wait_limit.restype = ci
@@ -637,6 +640,11 @@ def kv4_copy_pages(pages, pairs):
 def debug_decode_fallbacks() -> int:
     """bitlinear_debug_decode_fallbacks: synchronises; warps that read weights from global memory since the last call."""
     return int(lib().bitlinear_debug_decode_fallbacks(_stream()))
+
+
+def debug_window_fallbacks() -> int:
+    """bitlinear_debug_window_fallbacks: synchronises; CTAs of attention_window that took the slow way since the last call."""
+    return int(lib().bitlinear_debug_window_fallbacks(_stream()))
 
 
 def noalloc_status() -> int:

@@ -91,6 +91,8 @@ constexpr int kMaxHeads = 4096;
 constexpr int64_t kMaxRows = 1 << 30;  // tokens: row numbers and positions stay inside 32 bits in the kernels
 
 inline bool attention_dtype(int t) { return t == BL_F16 || t == BL_BF16; }
+// 0: no window; one that no position can leave is none.
+inline int clip_window(int window) { return window > 0 && window < kMaxRows ? window : 0; }
 inline bool aligned_to(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 // A row stride takes the row and keeps every row 16-byte aligned.
 inline bool row_stride(int64_t ld, int heads, int head_dim) { return ld >= (int64_t)heads * head_dim && ld % 8 == 0; }
@@ -556,7 +558,7 @@ bl_status bitlinear_attention_window(const void* q, const void* k, const void* v
     return BL_ERR_ALIGN;
   if ((int64_t)batch * heads * ((seq_q + 127) / 128) > 0x7FFFFFFF) return BL_ERR_SHAPE;
   WindowArgs a{q, k, v, o, dt, batch, cu_q, cu_k ? cu_k : cu_q, seq_q, seq_k, rows_q, rows_k, heads, kv_heads, head_dim, ld_q,
-               ld_k, ld_v, ld_o, window > 0 ? window : 0, sinks, scale};
+               ld_k, ld_v, ld_o, clip_window(window), sinks, scale};
   if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)head_dim);
   return launch_attention_window(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
 }
@@ -616,7 +618,7 @@ bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, 
   const size_t need = bitlinear_attention_kv4_ws_bytes(batch, n_q, heads, cache->kv_heads, cache->head_dim);
   if (!ws || ws_bytes < need) return BL_ERR_WORKSPACE;
   if (!aligned16(ws)) return BL_ERR_ALIGN;
-  Kv4AttnArgs a{q, batch, n_q, heads, ld_q, *cache, block_table, max_pages, lens, window > 0 ? window : 0, sinks, scale, o, ld_o, ws};
+  Kv4AttnArgs a{q, batch, n_q, heads, ld_q, *cache, block_table, max_pages, lens, clip_window(window), sinks, scale, o, ld_o, ws};
   if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)cache->head_dim);
   return launch_attention_kv4(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
 }
@@ -646,6 +648,13 @@ int64_t bitlinear_debug_decode_fallbacks(void* stream) {
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return -1;
   unsigned int n = 0;
   if (gemv_decode_take_fallbacks(&n) != cudaSuccess) return -1;
+  return (int64_t)n;
+}
+
+int64_t bitlinear_debug_window_fallbacks(void* stream) {
+  if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return -1;
+  unsigned int n = 0;
+  if (window_take_fallbacks(&n) != cudaSuccess) return -1;
   return (int64_t)n;
 }
 

@@ -1,11 +1,39 @@
-// Attention of prompts with a sliding window and sinks (bitlinear_attention_window).
-// One warp per (query row, head): a pass over the visible keys with the running maximum and sum of the
-// softmax, each lane holding kDim / 32 values of the query and of the output.
-#include "common.cuh"
+// Attention of prompts with a sliding window and sinks (bitlinear_attention_window):
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = e^(scale q_i . k_j - max),  j visible from i.
+//
+// A CTA owns two tiles of 128 query rows: the same rows of two heads that share their keys (even group sizes), or
+// two consecutive tiles of one head.  Keys and values pass through shared memory in tiles of 128, once for both
+// tiles; tiles that no row sees (after the rows, or between the sinks and the window) are not loaded.  Per pair of
+// tiles two products of 128 x 128 x kDim run on the tcgen05 tensor cores,
+//   S = Q K^T   both operands in shared memory (TMA, 128-byte swizzle), S in tensor memory (fp32),
+//   O += P V    P in tensor memory as 16-bit numbers, over S; V as it lies in memory (its rows are the
+//               contraction, so the descriptor says MN-major); O in tensor memory (fp32).
+// While one tile's softmax runs, the other tile's products do: issue order S0(j) S1(j) | PV0(j) S0(j+1) | PV1(j)
+// S1(j+1) | ...; the tensor core takes products in issue order, which is what keeps S(j+1) from overwriting P(j).
+//
+// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1 (a thread owns a query row: no shuffles), warp 8 issues the
+// products, warp 9 the copies.  The running maximum moves only when a row's maximum grew by more than 2^8: O is
+// then rescaled in tensor memory, which is rare; else probabilities of up to 2^8 do no harm (they are formed at 2^7
+// times their size, 2^15 at most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
+//
+// Invisible places.  A masked score is replaced, so keys there may be anything.  A value there meets a probability
+// of 0, but 0 x NaN is NaN: a row whose result is not finite is computed again by one warp from the visible
+// places alone (window_row).  Finite inputs never take that path.
+//
+// Every wait is bounded.  If one runs out, the CTA's rows are computed by window_row too and the event is
+// counted (bitlinear_debug_window_fallbacks): the result is the same up to rounding, only late.
+#include <atomic>
+#include <type_traits>
+
+#include "tc_common.cuh"
 
 namespace bl {
 
 namespace {
+
+using namespace tc;
+
+__device__ unsigned int g_window_fallbacks;      // CTAs whose waits ran out, since last asked
 
 // Rows of one sequence in q / o and in k / v.
 struct SeqRows { int q0, nq, k0, nk; };
@@ -52,28 +80,430 @@ __device__ void window_row(const WindowArgs& a, const SeqRows& r, int i, int h) 
   for (int e = 0; e < kVals; ++e) o[e] = out_cast<T>(l == 0.f ? 0.f : acc[e] / l);
 }
 
-// One CTA per (128 query rows, head, sequence), four warps.
-template <typename T, int kDim>
-__global__ void __launch_bounds__(128) attention_window_kernel(WindowArgs a) {
-  const int tiles = (int)((a.seq_q + 127) / 128);
-  const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.heads, b = blockIdx.x / tiles / a.heads;
-  const SeqRows r = seq_rows(a, b);
-  const int last = min(tile * 128 + 128, r.nq);
-  for (int i = tile * 128 + (threadIdx.x >> 5); i < last; i += 4) window_row<T, kDim>(a, r, i, h);
+constexpr int kTile = 128;                       // query rows and keys per tile
+constexpr int kSlots = 4;                        // key or value tiles in shared memory
+constexpr int kThreads = 384;
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // per thread after the split; 256 x 208 + 128 x 88 = 384 x 168
+constexpr int kLaunchRegs = 168;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "registers of the split");
+constexpr float kMoveLog2 = 8.f;                 // growth of a row's maximum that is let pass
+constexpr float kLiftLog2 = 7.f;                 // probabilities are formed 2^7 times their size
+
+struct Ctl {
+  unsigned long long q_full[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_ready[2], o_done[2], drain;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+// Bounded wait like mbar_wait, with the number of polls from the launch (tests shorten it).
+__device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
+  const uint32_t b = smem_u32(bar);
+  if (polls && mbar_try_wait(b, parity)) return true;
+  const unsigned long long t0 = global_ns();
+  for (uint32_t it = 0; it < polls; ++it) {
+    if (mbar_try_wait(b, parity)) return true;
+    if ((it & 255u) == 255u) {
+      if (*abort_flag) return false;
+      if (global_ns() - t0 > kWaitNs) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
 }
 
-template <typename T>
-cudaError_t launch_type(const WindowArgs& a, cudaStream_t s) {
-  const unsigned grid = (unsigned)((a.seq_q + 127) / 128 * a.heads * a.batch);
-  if (a.head_dim == 64) attention_window_kernel<T, 64><<<grid, 128, 0, s>>>(a);
-  else attention_window_kernel<T, 128><<<grid, 128, 0, s>>>(a);
-  return cudaGetLastError();
+// kind::f16 instruction descriptor: fp32 sums, fp16 or bf16 operands, M = 128.
+template <typename T> __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn_major) {
+  const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
+  return (1u << 4) | (type << 7) | (type << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+// K-major tile of 128-byte rows: smem_desc_sw128.  MN-major: rows of 64 values along N, groups of 8 rows (of the
+// contraction) 1024 bytes apart, the next 64 values along N one sub-tile (128 rows) further.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((kTile * 128) >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+// 32 columns of this warp's 32 lanes, without the wait.
+__device__ __forceinline__ void ld32(uint32_t taddr, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
+        "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
+        "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+template <typename R> __device__ __forceinline__ void st32(uint32_t taddr, const R* r) {
+  static_assert(sizeof(R) == 4, "32-bit columns");
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]),
+        "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
+        "r"(u[30]), "r"(u[31]) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// What a CTA works on; every role derives the same.
+struct Job {
+  SeqRows r;
+  int b, head[2], row0[2], rows[2];              // per tile: head, first query row of the sequence, rows (0: no tile)
+  int pos0[2], pos1[2];                          // positions of its first and last row
+  int sink_tiles, first, count;                  // key tiles: those of the sinks, then `first` on
+  int window, sinks;
+  __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kTile; }
+  // does a row of tile t see a key of tile j?
+  __device__ __forceinline__ bool active(int t, int j) const {
+    const int k0 = key0(j);
+    return rows[t] > 0 && k0 <= pos1[t] && (window == 0 || k0 + kTile - 1 > pos0[t] - window || k0 < sinks);
+  }
+  // does some row of tile t not see some key of tile j?
+  __device__ __forceinline__ bool edge(int t, int j) const {
+    const int k0 = key0(j);
+    return k0 + kTile - 1 > pos0[t] || (window > 0 && pos1[t] - k0 >= window && k0 + kTile > sinks);
+  }
+};
+// pair: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
+__device__ __forceinline__ Job make_job(const WindowArgs& a, bool pair) {
+  Job w;
+  const int units = pair ? a.heads / 2 : a.heads, per = pair ? kTile : 2 * kTile;
+  const int blocks = (int)((a.seq_q + per - 1) / per);
+  const int u = blockIdx.x % units, rest = blockIdx.x / units;
+  w.b = rest % a.batch;
+  const int blk = blocks - 1 - rest / a.batch;
+  w.r = seq_rows(a, w.b);
+  w.window = a.window; w.sinks = a.sinks;
+  int lo = 0x7FFFFFFF, hi = 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    w.head[t] = pair ? 2 * u + t : u;
+    w.row0[t] = blk * per + (pair ? 0 : t * kTile);
+    w.rows[t] = min(max(w.r.nq - w.row0[t], 0), kTile);
+    w.pos0[t] = w.r.nk - w.r.nq + w.row0[t];
+    w.pos1[t] = w.pos0[t] + w.rows[t] - 1;
+    if (w.rows[t] > 0 && w.pos1[t] >= 0) {
+      lo = min(lo, a.window > 0 ? max(0, w.pos0[t] - a.window + 1) : 0);
+      hi = max(hi, w.pos1[t] + 1);
+    }
+  }
+  if (hi == 0) lo = 0;
+  w.first = lo / kTile;
+  w.sink_tiles = min((min(a.sinks, lo) + kTile - 1) / kTile, w.first);
+  w.count = hi == 0 ? 0 : w.sink_tiles + (hi + kTile - 1) / kTile - w.first;
+  return w;
+}
+
+template <typename T, int kDim>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v, WindowArgs a, int pair, uint32_t polls) {
+  constexpr int kSub = kTile * 128;              // bytes of a sub-tile: 128 rows of 64 values
+  constexpr int kSubs = kDim / 64, kTileBytes = kSubs * kSub;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* sq = smem;                      // two query tiles, then the ring
+  unsigned char* ring = smem + 2 * kTileBytes;
+  Ctl* ctl = reinterpret_cast<Ctl*>(ring + kSlots * kTileBytes);
+  volatile int* abort_flag = &ctl->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&ctl->q_full[t]), 1);
+      mbar_init(smem_u32(&ctl->s_full[t]), 1);
+      mbar_init(smem_u32(&ctl->p_ready[t]), 4);
+      mbar_init(smem_u32(&ctl->o_done[t]), 1);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(smem_u32(&ctl->kv_full[s]), 1);
+      mbar_init(smem_u32(&ctl->kv_empty[s]), 1);
+    }
+    mbar_init(smem_u32(&ctl->drain), 1);
+    ctl->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;          // S0 S1 (128 columns each), O0 O1
+  pdl_wait();
+  const Job job = make_job(a, pair != 0);
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 9 && lane == 0 && job.count > 0) {             // ---- copies
+      int issued = 0;
+      for (int t = 0; t < 2; ++t) {
+        if (job.rows[t] == 0) continue;
+        mbar_arrive_expect_tx(smem_u32(&ctl->q_full[t]), kTileBytes);
+        for (int s = 0; s < kSubs; ++s)
+          tma_load_2d(smem_u32(sq + t * kTileBytes + s * kSub), &map_q, job.head[t] * kDim + 64 * s, job.r.q0 + job.row0[t],
+                      smem_u32(&ctl->q_full[t]));
+      }
+      const int hk = job.head[0] / (a.heads / a.kv_heads);
+      for (int e = 0; e < 2 * job.count; ++e) {                // entry 2 j: keys of tile j; 2 j + 1: its values
+        const int slot = e % kSlots;
+        if (e >= kSlots && !wait_for(&ctl->kv_empty[slot], ((e / kSlots) - 1) & 1, abort_flag, polls)) break;
+        mbar_arrive_expect_tx(smem_u32(&ctl->kv_full[slot]), kTileBytes);
+        for (int s = 0; s < kSubs; ++s)
+          tma_load_2d(smem_u32(ring + slot * kTileBytes + s * kSub), e & 1 ? &map_v : &map_k, hk * kDim + 64 * s,
+                      job.r.k0 + job.key0(e >> 1), smem_u32(&ctl->kv_full[slot]));
+        issued = e + 1;
+      }
+      // Copies end before the CTA does, also those of a tile that turned out to see nothing, and after a wait ran out.
+      int gave_up = 0;
+      for (int t = 0; t < 2; ++t)
+        if (job.rows[t] > 0) wait_for(&ctl->q_full[t], 0, &gave_up, kSpinLimit);
+      for (int e = max(0, issued - kSlots); e < issued; ++e) wait_for(&ctl->kv_full[e % kSlots], (e / kSlots) & 1, &gave_up, kSpinLimit);
+    } else if (warp == 8 && lane == 0 && job.count > 0) {      // ---- products
+      constexpr uint32_t kIdS = idesc<T>(kTile, false), kIdO = idesc<T>(kDim, true);
+      int pv[2] = {0, 0}, sc[2] = {0, 0};
+      bool ok = true;
+      for (int j = 0; j <= job.count && ok; ++j) {
+        const int ek = 2 * j, ev = 2 * j - 1;
+        if (j < job.count) ok = ok && wait_for(&ctl->kv_full[ek % kSlots], (ek / kSlots) & 1, abort_flag, polls);
+        if (j > 0) ok = ok && wait_for(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1, abort_flag, polls);
+        for (int t = 0; t < 2 && ok; ++t) {
+          const uint32_t ts = tmem + t * kTile, to = tmem + 2 * kTile + t * kTile;
+          if (j > 0 && job.active(t, j - 1)) {
+            ok = wait_for(&ctl->p_ready[t], pv[t] & 1, abort_flag, polls);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t dv = desc_mn(smem_u32(ring + (ev % kSlots) * kTileBytes));
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)               // 16 keys: 8 columns of P, 2048 bytes of V
+              mma_ts(to, ts + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, pv[t] > 0 || k > 0);
+            mma_commit(smem_u32(&ctl->o_done[t]));
+            ++pv[t];
+          }
+          if (j < job.count && job.active(t, j)) {
+            if (sc[t] == 0) ok = wait_for(&ctl->q_full[t], 0, abort_flag, polls);
+            if (!ok) break;
+            const uint32_t qa = smem_u32(sq + t * kTileBytes), ka = smem_u32(ring + (ek % kSlots) * kTileBytes);
+#pragma unroll
+            for (int k = 0; k < kDim / 16; ++k) {              // 16 values: 32 bytes within a sub-tile's rows
+              const uint32_t off = (k / 4) * kSub + (k % 4) * 32;
+              mma_ss(ts, smem_desc_sw128(qa + off), smem_desc_sw128(ka + off), kIdS, k > 0);
+            }
+            mma_commit(smem_u32(&ctl->s_full[t]));
+            ++sc[t];
+          }
+        }
+        if (!ok) break;
+        if (j > 0) mma_commit(smem_u32(&ctl->kv_empty[ev % kSlots]));
+        if (j < job.count) mma_commit(smem_u32(&ctl->kv_empty[ek % kSlots]));
+      }
+      int gave_up = 0;                                         // products, and the arrivals they owe, end before the CTA does
+      mma_commit(smem_u32(&ctl->drain));
+      wait_for(&ctl->drain, 0, &gave_up, kSpinLimit);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int t = warp >> 2, row = threadIdx.x & 127;          // the tile, and this thread's row of it
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * kTile + lanes, to = tmem + 2 * kTile + t * kTile + lanes;
+    const float sl = a.scale * 1.4426950408889634f;
+    const int pos = job.pos0[t] + row;
+    float m = -INFINITY, l = 0.f;
+    int n = 0;
+    bool ok = true;
+    for (int j = 0; j < job.count; ++j) {
+      if (!job.active(t, j)) continue;
+      ok = wait_for(&ctl->s_full[t], n & 1, abort_flag, polls);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      float s[kTile];
+#pragma unroll
+      for (int c = 0; c < kTile; c += 32) ld32(ts + c, s + c);
+      ld_wait();
+      if (job.edge(t, j)) {
+        const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
+        const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
+#pragma unroll
+        for (int c = 0; c < kTile; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
+      }
+      float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+#pragma unroll
+      for (int c = 4; c < kTile; c += 4) {
+        mx0 = fmaxf(mx0, s[c]); mx1 = fmaxf(mx1, s[c + 1]); mx2 = fmaxf(mx2, s[c + 2]); mx3 = fmaxf(mx3, s[c + 3]);
+      }
+      const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+      const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
+      if (__any_sync(0xFFFFFFFFu, move)) {                     // O of the tiles so far takes the new maximum
+        ok = wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const float f = move ? ex2((m - mx) * sl) : 1.f;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < kDim; c += 32) {
+          float o[32];
+          ld32(to + c, o);
+          ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] *= f;
+          st32(to + c, o);
+        }
+      }
+      if (move || m == -INFINITY) m = fmaxf(m, mx);
+      const float shift = m == -INFINITY ? 0.f : kLiftLog2 - m * sl;
+      float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < kTile; c += 64) {
+        uint32_t p[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float p0 = ex2(fmaf(s[c + 2 * i], sl, shift)), p1 = ex2(fmaf(s[c + 2 * i + 1], sl, shift));
+          l0 += p0; l1 += p1;
+          p[i] = pack2<T>(p0, p1);
+        }
+        st32(ts + c / 2, p);
+      }
+      l += l0 + l1;
+      st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t]));
+      ++n;
+    }
+    // ---- output
+    if (ok && n > 0) {
+      ok = wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      tc_fence_after();
+    }
+    if (ok) {
+      const bool mine = row < job.rows[t];
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + job.row0[t] + row) * a.ld_o + (int64_t)job.head[t] * kDim;
+      float check = 0.f;
+#pragma unroll
+      for (int c = 0; c < kDim; c += 32) {
+        float v[32];
+        if (n > 0) {
+          ld32(to + c, v);
+          ld_wait();
+        }
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = l == 0.f ? 0.f : v[2 * i] * inv, y = l == 0.f ? 0.f : v[2 * i + 1] * inv;
+          check = fmaf(x, 0.f, fmaf(y, 0.f, check));           // NaN once a value is not finite
+          w[i] = pack2<T>(x, y);
+        }
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(o + c + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+      }
+      unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f));
+      while (bad) {
+        const int i = __ffs(bad) - 1;
+        bad &= bad - 1;
+        window_row<T, kDim>(a, job.r, job.row0[t] + (warp & 3) * 32 + i, job.head[t]);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  if (*abort_flag) {
+    if (threadIdx.x == 0) atomicAdd(&g_window_fallbacks, 1u);
+    for (int t = 0; t < 2; ++t)
+      for (int i = warp; i < job.rows[t]; i += kThreads / 32) window_row<T, kDim>(a, job.r, job.row0[t] + i, job.head[t]);
+  }
+}
+
+// Tensor map of a token matrix [rows, width]: boxes of 128 rows x 64 values, rows beyond the end read as zero.
+template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t width, int64_t ld) {
+  EncodeFn enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64, kTile}, estr[2] = {1, 1};
+  return enc(map, std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+             const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int kDim>
+cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
+  constexpr size_t kSmem = (size_t)(2 + kSlots) * kTile * kDim * 2 + 1024 + sizeof(Ctl);
+  static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
+  static std::atomic<uint64_t> ready{0};         // devices on which the kernel's shared memory limit is set
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !((ready.load(std::memory_order_relaxed) >> dev) & 1)) {
+    e = cudaFuncSetAttribute(attention_window_kernel<T, kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  CUtensorMap mq, mk, mv;
+  if (!make_map<T>(&mq, a.q, a.rows_q, (int64_t)a.heads * kDim, a.ld_q)) return cudaErrorInvalidValue;
+  if (a.rows_k > 0) {
+    if (!make_map<T>(&mk, a.k, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_k) ||
+        !make_map<T>(&mv, a.v, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_v))
+      return cudaErrorInvalidValue;
+  } else {
+    mk = mv = mq;                                // no key anywhere: never used
+  }
+  const bool pair = (a.heads / a.kv_heads) % 2 == 0;
+  const int64_t per = pair ? kTile : 2 * kTile;
+  const int64_t grid = (a.seq_q + per - 1) / per * a.batch * (pair ? a.heads / 2 : a.heads);
+  const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
+  const uint32_t polls = dbg < 0 ? kSpinLimit : (uint32_t)(dbg < (long long)kSpinLimit ? dbg : kSpinLimit);
+  return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, pair ? 1 : 0, polls);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_window(const WindowArgs& a, cudaStream_t s) {
-  return a.dt == BL_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);
+  if (a.dt == BL_F16) return a.head_dim == 64 ? launch_dim<__half, 64>(a, s) : launch_dim<__half, 128>(a, s);
+  return a.head_dim == 64 ? launch_dim<__nv_bfloat16, 64>(a, s) : launch_dim<__nv_bfloat16, 128>(a, s);
+}
+
+cudaError_t window_take_fallbacks(unsigned int* out) {
+  const unsigned int zero = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(out, g_window_fallbacks, sizeof(*out));
+  return e != cudaSuccess ? e : cudaMemcpyToSymbol(g_window_fallbacks, &zero, sizeof(zero));
 }
 
 }  // namespace bl

@@ -221,6 +221,7 @@ struct WindowArgs {
   int window, sinks; float scale;
 };
 cudaError_t launch_attention_window(const WindowArgs& a, cudaStream_t s);
+cudaError_t window_take_fallbacks(unsigned int* out);       // CTAs that computed their rows the slow way after a wait ran out
 
 cudaError_t launch_kv4_append(const bl_kv4_cache& c, const void* k, const void* v, int64_t T, int64_t ld_k, int64_t ld_v,
                               const int64_t* slots, cudaStream_t s);

@@ -475,6 +475,26 @@ def test_attention_window_agrees_with_the_causal_core():
     assert torch.equal(o, B.attention_window(q, k, v, batch, seq, heads))
 
 
+def test_attention_window_when_its_waits_run_out():
+    """With no polls allowed every wait runs out: the rows are computed the slow way, and counted."""
+    heads, hk, dim, lens = 4, 2, 128, [300, 0, 140]
+    cu, at = packed(lens)
+    q, kv = randn(1, at[-1], heads * dim, dtype=F16), randn(2, at[-1], 2 * hk * dim, dtype=F16)
+    k, v = kv[:, :hk * dim], kv[:, hk * dim:]
+    B.debug_window_fallbacks()
+    want = B.attention_window(q, k, v, 3, 300, heads, hk, dim, window=100, sinks=2, cu_q=cu)
+    assert B.debug_window_fallbacks() == 0
+    B.debug_wait_limit(0)
+    try:
+        got = B.attention_window(q, k, v, 3, 300, heads, hk, dim, window=100, sinks=2, cu_q=cu)
+        assert B.debug_window_fallbacks() > 0
+    finally:
+        B.debug_wait_limit(-1)
+    check_window(q, k, v, got, [(a, n, a, n) for a, n in zip(at, lens)], heads, hk, dim, 100, 2)
+    assert (got.double() - want.double()).abs().max() <= 8 * R.half_step(F16) * float(v.abs().max())
+    assert B.debug_window_fallbacks() == 0
+
+
 # ---- together ------------------------------------------------------------------------------------
 def test_a_prompt_and_decode_steps_through_bitlinear_layers():
     """A prompt enters the cache, a sequence is forked, and both decode tokens: BitLinear projections by the decode
