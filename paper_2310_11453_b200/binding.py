@@ -448,39 +448,42 @@ def block_forward(x, weights, batch, seq, heads, ffn, ln_eps=1e-5, ws=None, fuse
 
 
 # ---- attention at inference ----------------------------------------------------------------------
-def _same(ref, **tensors):
-    """Every given tensor is a CUDA tensor on ref's device (None is allowed)."""
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device != ref.device):
-            raise ValueError(f"{name} is on {t.device}, expected a CUDA tensor on {ref.device}")
+# One decode step makes a handful of these calls per layer, a few microseconds of device time each, so the
+# wrappers are written to cost little themselves: one look at each tensor, plain integers to the C call.
+_stream_of = torch._C._cuda_getCurrentRawStream
+_device_now = torch._C._cuda_getDevice
 
 
-def _rows(name, t, dtype, width, rows=None):
-    """A token matrix [rows, width] of dtype whose rows are contiguous; returns its row stride."""
+def _bad(name, t, index, dtype, what):
+    """Why a tensor argument is refused."""
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} is on {t.device}, expected a CUDA tensor on the device of the first argument")
     if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
-    if t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({'any' if rows is None else rows}, {width})")
-    if t.stride(1) != 1:
-        raise ValueError(f"{name}: the values of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width + -width % 8)
+    raise ValueError(f"{name} has shape {tuple(t.shape)} and strides {t.stride()}, expected {what}")
 
 
-def _index(name, t, dtype, shape):
-    """A contiguous index tensor of the given dtype and shape."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected a contiguous {tuple(shape)}")
+def _rows(name, t, index, dtype, rows, width):
+    """Checks a token matrix [rows, width] whose rows are contiguous; returns its row stride."""
+    stride = t.stride()
+    if t.get_device() != index or index < 0 or t.dtype != dtype or t.shape != (rows, width) or stride[1] != 1:
+        _bad(name, t, index, dtype, f"({rows}, {width}) with the values of a row contiguous")
+    return stride[0] if rows > 1 else max(stride[0], width + -width % 8)
 
 
-def _launch(device, fn, *args):
-    """Calls a C entry point with `device` current and its current stream as the last argument."""
-    index = device.index
-    if index == torch.cuda.current_device():
-        return fn(*args, torch.cuda.current_stream(index).cuda_stream)
+def _index(name, t, index, dtype, shape):
+    """Checks a contiguous tensor of the given type and shape; returns its address."""
+    if t.get_device() != index or index < 0 or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _bad(name, t, index, dtype, f"a contiguous {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _launch(index, fn, *args):
+    """Calls a C entry point with device `index` current and its current stream as the last argument."""
+    if index == _device_now():
+        return fn(*args, _stream_of(index))
     with torch.cuda.device(index):
-        return fn(*args, torch.cuda.current_stream(index).cuda_stream)
+        return fn(*args, _stream_of(index))
 
 
 def qk_norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq=None, wk=None, eps=1e-6, interleaved=False,
@@ -488,24 +491,25 @@ def qk_norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq=None, 
     """bitlinear_qk_norm_rope.  q [T, heads*head_dim], k [T, kv_heads*head_dim] (may be column blocks of one
     buffer); positions int32 [T] (negative: padding, left as it is); inv_freq f32 [rot_dim/2]; wq, wk
     [head_dim] or None; eps < 0 skips the norm.  Returns (q_out, k_out), which may be given (q, k for in place)."""
-    T, dt = q.shape[0], q.dtype
-    _same(q, k=k, positions=positions, inv_freq=inv_freq, wq=wq, wk=wk, q_out=q_out, k_out=k_out, q=q)
-    ld_q, ld_k = _rows("q", q, dt, heads * head_dim), _rows("k", k, dt, kv_heads * head_dim, T)
-    _index("positions", positions, torch.int32, (T,))
-    _index("inv_freq", inv_freq, torch.float32, (inv_freq.numel(),))
-    for name, w in (("wq", wq), ("wk", wk)):
-        if w is not None:
-            _index(name, w, dt, (head_dim,))
+    T, dt, dev, wide, narrow = q.shape[0], q.dtype, q.get_device(), heads * head_dim, kv_heads * head_dim
+    ld_q, ld_k = _rows("q", q, dev, dt, T, wide), _rows("k", k, dev, dt, T, narrow)
+    half = inv_freq.numel()
+    pos, freq = _index("positions", positions, dev, torch.int32, (T,)), _index("inv_freq", inv_freq, dev, torch.float32, (half,))
+    w1 = None if wq is None else _index("wq", wq, dev, dt, (head_dim,))
+    w2 = None if wk is None else _index("wk", wk, dev, dt, (head_dim,))
     if q_out is None:
-        q_out = torch.empty((T, heads * head_dim), dtype=dt, device=q.device)
+        q_out, ld_qo = q.new_empty((T, wide)), wide
+    else:
+        ld_qo = _rows("q_out", q_out, dev, dt, T, wide)
     if k_out is None:
-        k_out = torch.empty((T, kv_heads * head_dim), dtype=dt, device=q.device)
-    ld_qo, ld_ko = _rows("q_out", q_out, dt, heads * head_dim, T), _rows("k_out", k_out, dt, kv_heads * head_dim, T)
-    code = _launch(q.device, lib().bitlinear_qk_norm_rope, q.data_ptr(), k.data_ptr(), _dt(q), T, heads, kv_heads, head_dim,
-                   ld_q, ld_k, None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), float(eps),
-                   2 * inv_freq.numel(), 1 if interleaved else 0, inv_freq.data_ptr(), positions.data_ptr(),
-                   q_out.data_ptr(), k_out.data_ptr(), ld_qo, ld_ko)
-    _check(code, "bitlinear_qk_norm_rope")
+        k_out, ld_ko = k.new_empty((T, narrow)), narrow
+    else:
+        ld_ko = _rows("k_out", k_out, dev, dt, T, narrow)
+    code = _launch(dev, lib().bitlinear_qk_norm_rope, q.data_ptr(), k.data_ptr(), _dt(q), T, heads, kv_heads, head_dim,
+                   ld_q, ld_k, w1, w2, eps, 2 * half, 1 if interleaved else 0, freq, pos, q_out.data_ptr(), k_out.data_ptr(),
+                   ld_qo, ld_ko)
+    if code:
+        _check(code, "bitlinear_qk_norm_rope")
     return q_out, k_out
 
 
@@ -515,21 +519,20 @@ def attention_window(q, k, v, batch, seq, heads, kv_heads=None, head_dim=128, wi
     column blocks of one buffer).  `seq` (and `seq_k`, default the same) is the common length, or with cu_q (cu_k)
     int32 [batch+1], packed sequences, an upper bound of their lengths.  Returns o [rows, heads*head_dim]."""
     kv_heads = heads if kv_heads is None else kv_heads
-    dt = q.dtype
-    _same(q, q=q, k=k, v=v, cu_q=cu_q, cu_k=cu_k, o=o)
-    ld_q, ld_k = _rows("q", q, dt, heads * head_dim), _rows("k", k, dt, kv_heads * head_dim)
-    ld_v = _rows("v", v, dt, kv_heads * head_dim, k.shape[0])
-    for name, c in (("cu_q", cu_q), ("cu_k", cu_k)):
-        if c is not None:
-            _index(name, c, torch.int32, (batch + 1,))
+    dt, dev, wide, narrow, rows, rows_k = q.dtype, q.get_device(), heads * head_dim, kv_heads * head_dim, q.shape[0], k.shape[0]
+    ld_q, ld_k = _rows("q", q, dev, dt, rows, wide), _rows("k", k, dev, dt, rows_k, narrow)
+    ld_v = _rows("v", v, dev, dt, rows_k, narrow)
+    c1 = None if cu_q is None else _index("cu_q", cu_q, dev, torch.int32, (batch + 1,))
+    c2 = None if cu_k is None else _index("cu_k", cu_k, dev, torch.int32, (batch + 1,))
     if o is None:
-        o = torch.empty((q.shape[0], heads * head_dim), dtype=dt, device=q.device)
-    ld_o = _rows("o", o, dt, heads * head_dim, q.shape[0])
-    code = _launch(q.device, lib().bitlinear_attention_window, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _dt(q),
-                   batch, None if cu_q is None else cu_q.data_ptr(), None if cu_k is None else cu_k.data_ptr(), seq,
-                   seq if seq_k is None else seq_k, q.shape[0], k.shape[0], heads, kv_heads, head_dim, ld_q, ld_k, ld_v, ld_o,
-                   window, sinks, float(scale))
-    _check(code, "bitlinear_attention_window")
+        o, ld_o = q.new_empty((rows, wide)), wide
+    else:
+        ld_o = _rows("o", o, dev, dt, rows, wide)
+    code = _launch(dev, lib().bitlinear_attention_window, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _dt(q),
+                   batch, c1, c2, seq, seq if seq_k is None else seq_k, rows, rows_k, heads, kv_heads, head_dim, ld_q, ld_k,
+                   ld_v, ld_o, window, sinks, scale)
+    if code:
+        _check(code, "bitlinear_attention_window")
     return o
 
 
@@ -547,16 +550,16 @@ class Kv4Cache:
     layer of a [layers, num_pages, page bytes] tensor.  Holds no state of its own."""
 
     def __init__(self, pages, page_size, kv_heads, head_dim, dtype):
-        nbytes = kv4_page_bytes(page_size, kv_heads, head_dim)
+        nbytes = lib().bitlinear_kv4_page_bytes(page_size, kv_heads, head_dim)
         if nbytes == 0:
             raise ValueError(f"unsupported cache: page_size {page_size}, kv_heads {kv_heads}, head_dim {head_dim}")
         if dtype not in (torch.float16, torch.bfloat16):
             raise TypeError(f"unsupported dtype {dtype}")
-        if not pages.is_cuda:
-            raise ValueError("pages must be a CUDA tensor")
-        _index("pages", pages, torch.uint8, (pages.shape[0], nbytes))
+        num = pages.shape[0]
+        self.device_index = pages.get_device()
+        address = _index("pages", pages, self.device_index, torch.uint8, (num, nbytes))
         self.pages, self.page_size, self.kv_heads, self.head_dim, self.dtype = pages, page_size, kv_heads, head_dim, dtype
-        self._struct = _Kv4CacheStruct(pages.data_ptr(), pages.shape[0], page_size, kv_heads, head_dim, _DTYPES[dtype])
+        self._struct = _Kv4CacheStruct(address, num, page_size, kv_heads, head_dim, _DTYPES[dtype])
         self._ref = C.addressof(self._struct)
 
     @staticmethod
@@ -569,27 +572,27 @@ class Kv4Cache:
 def kv4_append(cache, k, v, slots):
     """bitlinear_kv4_append.  k, v [T, kv_heads*head_dim] of the cache's dtype; slots int64 [T] (page * page_size +
     place; one outside the cache, e.g. -1, is skipped; none twice)."""
-    T, width = k.shape[0], cache.kv_heads * cache.head_dim
-    _same(cache.pages, k=k, v=v, slots=slots)
-    ld_k, ld_v = _rows("k", k, cache.dtype, width), _rows("v", v, cache.dtype, width, T)
-    _index("slots", slots, torch.int64, (T,))
-    code = _launch(k.device, lib().bitlinear_kv4_append, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, slots.data_ptr())
-    _check(code, "bitlinear_kv4_append")
+    T, width, dev, dt = k.shape[0], cache.kv_heads * cache.head_dim, cache.device_index, cache.dtype
+    ld_k, ld_v = _rows("k", k, dev, dt, T, width), _rows("v", v, dev, dt, T, width)
+    at = _index("slots", slots, dev, torch.int64, (T,))
+    code = _launch(dev, lib().bitlinear_kv4_append, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, at)
+    if code:
+        _check(code, "bitlinear_kv4_append")
 
 
 def kv4_read(cache, slots, k=None, v=None):
     """bitlinear_kv4_read.  Returns (k, v) [T, kv_heads*head_dim] at the slots int64 [T]; rows of given k, v whose slot
     is outside the cache stay as they are, rows of new ones are zero."""
-    T, width = slots.shape[0], cache.kv_heads * cache.head_dim
+    T, width, dev, dt = slots.shape[0], cache.kv_heads * cache.head_dim, cache.device_index, cache.dtype
     if k is None:
-        k = torch.zeros((T, width), dtype=cache.dtype, device=cache.pages.device)
+        k = torch.zeros((T, width), dtype=dt, device=cache.pages.device)
     if v is None:
-        v = torch.zeros((T, width), dtype=cache.dtype, device=cache.pages.device)
-    _same(cache.pages, k=k, v=v, slots=slots)
-    ld_k, ld_v = _rows("k", k, cache.dtype, width, T), _rows("v", v, cache.dtype, width, T)
-    _index("slots", slots, torch.int64, (T,))
-    code = _launch(k.device, lib().bitlinear_kv4_read, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, slots.data_ptr())
-    _check(code, "bitlinear_kv4_read")
+        v = torch.zeros((T, width), dtype=dt, device=cache.pages.device)
+    ld_k, ld_v = _rows("k", k, dev, dt, T, width), _rows("v", v, dev, dt, T, width)
+    at = _index("slots", slots, dev, torch.int64, (T,))
+    code = _launch(dev, lib().bitlinear_kv4_read, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, at)
+    if code:
+        _check(code, "bitlinear_kv4_read")
     return k, v
 
 
@@ -601,39 +604,42 @@ def attention_kv4(q, cache, block_table, lens, batch, n_q, heads, window=0, sink
     """bitlinear_attention_kv4.  q [batch*n_q, heads*head_dim] of the cache's dtype; block_table int32 [batch, max_pages];
     lens int32 [batch], the n_q new tokens included.  Returns o like q.  `ws` may carry a workspace of
     attention_kv4_ws_bytes() bytes."""
-    width = heads * cache.head_dim
-    _same(cache.pages, q=q, block_table=block_table, lens=lens, o=o, ws=ws)
-    ld_q = _rows("q", q, cache.dtype, width, batch * n_q)
+    rows, width, dev, dt, L = batch * n_q, heads * cache.head_dim, cache.device_index, cache.dtype, lib()
+    ld_q = _rows("q", q, dev, dt, rows, width)
     max_pages = block_table.shape[1]
-    _index("block_table", block_table, torch.int32, (batch, max_pages))
-    _index("lens", lens, torch.int32, (batch,))
+    table = _index("block_table", block_table, dev, torch.int32, (batch, max_pages))
+    n = _index("lens", lens, dev, torch.int32, (batch,))
     if o is None:
-        o = torch.empty((batch * n_q, width), dtype=cache.dtype, device=q.device)
-    ld_o = _rows("o", o, cache.dtype, width, batch * n_q)
-    L = lib()
+        o, ld_o = q.new_empty((rows, width)), width
+    else:
+        ld_o = _rows("o", o, dev, dt, rows, width)
     if ws is None:
-        ws = torch.empty(max(256, L.bitlinear_attention_kv4_ws_bytes(batch, n_q, heads, cache.kv_heads, cache.head_dim)),
-                         dtype=torch.uint8, device=q.device)
-    code = _launch(q.device, L.bitlinear_attention_kv4, q.data_ptr(), batch, n_q, heads, ld_q, cache._ref,
-                   block_table.data_ptr(), max_pages, lens.data_ptr(), window, sinks, float(scale), o.data_ptr(), ld_o,
-                   ws.data_ptr(), ws.numel())
-    _check(code, "bitlinear_attention_kv4")
+        nbytes = L.bitlinear_attention_kv4_ws_bytes(batch, n_q, heads, cache.kv_heads, cache.head_dim)
+        ws = cache.pages.new_empty(max(256, nbytes))
+    else:
+        nbytes = ws.numel()
+        _index("ws", ws, dev, torch.uint8, (nbytes,))
+    code = _launch(dev, L.bitlinear_attention_kv4, q.data_ptr(), batch, n_q, heads, ld_q, cache._ref, table, max_pages, n, window,
+                   sinks, scale, o.data_ptr(), ld_o, ws.data_ptr(), nbytes)
+    if code:
+        _check(code, "bitlinear_attention_kv4")
     return o
 
 
 def kv4_copy_pages(pages, pairs):
     """bitlinear_kv4_copy_pages.  pages u8 [num_pages, page bytes] or [layers, num_pages, page bytes], contiguous; pairs
     int32 [n, 2] of (source, destination).  Copies in every layer, in place; returns pages."""
-    if pages.dtype != torch.uint8 or pages.dim() not in (2, 3) or not pages.is_contiguous() or not pages.is_cuda:
-        raise ValueError("pages must be a contiguous u8 CUDA tensor [num_pages, bytes] or [layers, num_pages, bytes]")
-    _same(pages, pairs=pairs)
+    dev, shape = pages.get_device(), pages.shape
+    if len(shape) not in (2, 3):
+        _bad("pages", pages, dev, torch.uint8, "[num_pages, bytes] or [layers, num_pages, bytes]")
+    address = _index("pages", pages, dev, torch.uint8, shape)
     n = pairs.shape[0]
-    _index("pairs", pairs, torch.int32, (n, 2))
-    num_pages, nbytes = pages.shape[-2:]
-    layers = pages.shape[0] if pages.dim() == 3 else 1
-    code = _launch(pages.device, lib().bitlinear_kv4_copy_pages, pages.data_ptr(), nbytes, num_pages, layers,
-                   num_pages * nbytes, pairs.data_ptr(), n)
-    _check(code, "bitlinear_kv4_copy_pages")
+    which = _index("pairs", pairs, dev, torch.int32, (n, 2))
+    num_pages, nbytes = shape[-2], shape[-1]
+    code = _launch(dev, lib().bitlinear_kv4_copy_pages, address, nbytes, num_pages, shape[0] if len(shape) == 3 else 1,
+                   num_pages * nbytes, which, n)
+    if code:
+        _check(code, "bitlinear_kv4_copy_pages")
     return pages
 
 

@@ -573,7 +573,7 @@ bl_status bitlinear_kv4_append(const bl_kv4_cache* cache, const void* k, const v
                                int64_t ld_v, const int64_t* slots, void* stream) {
   const bl_status st = check_cache(cache);
   if (st != BL_OK) return st;
-  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 8 * kMaxRows) return BL_ERR_SHAPE;
+  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 0x7FFFFFFF - 64) return BL_ERR_SHAPE;
   if (!row_stride(ld_k, cache->kv_heads, cache->head_dim) || !row_stride(ld_v, cache->kv_heads, cache->head_dim))
     return BL_ERR_SHAPE;
   if (T == 0) return BL_OK;
@@ -586,7 +586,7 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
                              const int64_t* slots, void* stream) {
   const bl_status st = check_cache(cache);
   if (st != BL_OK) return st;
-  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 8 * kMaxRows) return BL_ERR_SHAPE;
+  if (T < 0 || T > kMaxRows || T * cache->kv_heads > 0x7FFFFFFF - 64) return BL_ERR_SHAPE;
   if (!row_stride(ld_k, cache->kv_heads, cache->head_dim) || !row_stride(ld_v, cache->kv_heads, cache->head_dim))
     return BL_ERR_SHAPE;
   if (T == 0) return BL_OK;

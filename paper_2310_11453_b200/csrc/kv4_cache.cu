@@ -2,6 +2,8 @@
 //   eta = min x, step = (max x - min x) / 15 (rounded to the cache's type), code = clip(rint((x - eta) / step)).
 // All three are bound by memory.  Append and read give each (token, head) row kDim / 8 lanes, 8 values per
 // lane: one 16-byte access to the 16-bit rows, 4 bytes of key codes and 2 x 2 bytes of value codes.
+#include <type_traits>
+
 #include "kv4.cuh"
 
 namespace bl {
@@ -17,121 +19,197 @@ template <> __device__ __forceinline__ uint32_t round_bits<__half>(double v) { r
 template <> __device__ __forceinline__ uint32_t round_bits<__nv_bfloat16>(double v) {
   return __bfloat16_as_ushort(__double2bfloat16(v));
 }
+template <typename T> __device__ __forceinline__ uint32_t bits_of(float v) {
+  const T x = out_cast<T>(v);
+  return *reinterpret_cast<const uint16_t*>(&x);
+}
 template <typename T> __device__ __forceinline__ uint32_t nan_pair();
 template <> __device__ __forceinline__ uint32_t nan_pair<__half>() { return 0x7E007E00u; }
 template <> __device__ __forceinline__ uint32_t nan_pair<__nv_bfloat16>() { return 0x7FC07FC0u; }
 
-// rint((x - eta) / step) decided as in exact arithmetic.  In fp32 the quotient is off by less than 4e-6 (its
-// size is at most 15 and a bit, three roundings), so only quotients within 1e-5 of a border go to fp64, where
-// x - eta and code * step are exact: the residual against half a step then decides, ties to the even code.
-__device__ __forceinline__ uint32_t code_of(float x, float eta, float step, float inv) {
-  const float f = (x - eta) * inv;
-  float c = rintf(f);
-  if (!(fabsf(f - c) <= 0.49999f)) {                  // near a border; and when f is not finite
-    const double d = (double)x - (double)eta, s = (double)step;
-    double e = s > 0.0 ? rint(d / s) : 0.0;
-    e = fmin(fmax(e, 0.0), 16.0);
-    const double r = fma(-e, s, d), h = 0.5 * s;
-    if (r > h || (r == h && ((int)e & 1))) e += 1.0;
-    else if (r < -h || (r == -h && ((int)e & 1))) e -= 1.0;
-    c = s > 0.0 ? (float)e : 0.f;
-  }
-  return (uint32_t)(int)fminf(fmaxf(c, 0.f), 15.f);
+// The code of a value whose quotient (x - eta) / step is within one of the code c, in exact arithmetic: in fp64 x - eta and
+// code * step are exact, so the residual against half a step decides, ties to the even code.
+__device__ __forceinline__ uint32_t border_code(float x, float eta, float step, int c) {
+  const double d = (double)x - (double)eta, s = (double)step, r = fma(-(double)c, s, d), h = 0.5 * s;
+  if (r > h || (r == h && (c & 1))) ++c;
+  else if (r < -h || (r == -h && (c & 1))) --c;
+  return (uint32_t)min(max(c, 0), 15);
+}
+// The same from any quotient (steps so small or so large that fp32 does not serve).
+__device__ __noinline__ uint32_t exact_code(float x, float eta, float step) {
+  if (!(step > 0.f)) return 0;
+  const double q = rint(((double)x - (double)eta) / (double)step);
+  return border_code(x, eta, step, (int)fmin(fmax(q, 0.0), 16.0));
+}
+// RN_T((hi - lo) / 15).  The fp32 quotient is within 2^-22 of the exact one; where rounding it 2^-21 lower and higher
+// gives two results, fp64 decides.
+template <typename T> __device__ __noinline__ uint32_t step_bits64(float lo, float hi) { return round_bits<T>(((double)hi - (double)lo) / 15.0); }
+template <typename T> __device__ __forceinline__ uint32_t step_bits(float lo, float hi) {
+  const float q = (hi - lo) * (1.0f / 15.0f);
+  const uint32_t down = bits_of<T>(q * (1.f - 0x1p-21f)), up = bits_of<T>(q * (1.f + 0x1p-21f));
+  return down == up && q < 1e38f ? down : step_bits64<T>(lo, hi);
+}
+// Smaller of two pairs, each half for itself; a NaN wins.
+template <typename T> __device__ __forceinline__ uint32_t min_pairs(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t min_pairs<__half>(uint32_t a, uint32_t b) {
+  const __half2 m = __hmin2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <> __device__ __forceinline__ uint32_t min_pairs<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
 }
 
 // A row's 8 codes of this lane as nibbles (value i in bits 4 i), and the row's (step, eta) word.
+// In fp32 the quotient (x - eta) / step is off by less than 4e-6 (it is at most 15 and a bit, and three roundings enter),
+// so a value whose quotient lies further than 1e-5 from a border between codes has its code from the fp32 sum with
+// 1.5 * 2^23, whose low bits are the rounded quotient.  Others go to fp64: with bf16 rows about one value in 300 lies on a
+// border exactly, so that path is short.  Steps below the type's normal range (quotients may pass 15.5) or at the end of
+// fp32's take exact_code.
 template <typename T, int kLanes>
-__device__ __forceinline__ void quantise_row(const float (&v)[8], uint32_t& nib, uint32_t& scale) {
-  float lo = v[0], hi = v[0], sum = 0.f;
+__device__ __forceinline__ void quantise_row(const uint4& raw, uint32_t& nib, uint32_t& scale) {
+  constexpr float kMagic = 12582912.f;
+  constexpr float kLeast = std::is_same<T, __half>::value ? 6.2e-5f : 1e-30f;
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  // smallest value and smallest negated value, side by side in one word through the shuffles
+  const uint32_t mn = min_pairs<T>(min_pairs<T>(w[0], w[1]), min_pairs<T>(w[2], w[3]));
+  const uint32_t mx = min_pairs<T>(min_pairs<T>(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u), min_pairs<T>(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
+  uint32_t both = min_pairs<T>(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); sum += v[i] * 0.f; }   // sum: NaN unless all finite
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  }
-  const uint32_t sb = round_bits<T>(((double)hi - (double)lo) / 15.0);
+  for (int o = kLanes / 2; o > 0; o >>= 1) both = min_pairs<T>(both, __shfl_xor_sync(0xFFFFFFFFu, both, o));
+  const float2 ends = scale_floats<T>(both);
+  const float lo = ends.x, hi = -ends.y;
+  const uint32_t sb = step_bits<T>(lo, hi);
   const float step = scale_floats<T>(sb).x;
-  // steps at the ends of the fp32 range go to the fp64 path: their reciprocal is not accurate, or not finite
-  const float inv = step > 1e-30f && step < 1e30f ? 1.0f / step : __int_as_float(0x7FC00000);
-  nib = 0;
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
+  float v[8], c[8], far = 0.f;                        // values, codes; largest distance from a code
 #pragma unroll
-  for (int i = 0; i < 8; ++i) nib |= code_of(v[i], lo, step, inv) << (4 * i);
-  scale = sb | (round_bits<T>((double)lo) << 16);     // lo is a value of T: nothing is rounded
-  if (!(sum == 0.f)) { nib = 0; scale = nan_pair<T>(); }
+  for (int i = 0; i < 4; ++i) { const float2 f = scale_floats<T>(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float d = v[i] - lo;
+    c[i] = fmaf(d, inv, kMagic) - kMagic;
+    far = fmaxf(far, fabsf(fmaf(d, inv, -c[i])));
+  }
+  const float n0 = fmaf(c[1], 16.f, c[0]) + fmaf(c[3], 4096.f, c[2] * 256.f);
+  const float n1 = fmaf(c[5], 16.f, c[4]) + fmaf(c[7], 4096.f, c[6] * 256.f);
+  nib = __byte_perm(__float_as_uint(n0 + 8388608.f), __float_as_uint(n1 + 8388608.f), 0x5410);
+  if (!(step > kLeast && step < 1e30f)) {
+    nib = 0;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      float x = v[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) x = i == j ? v[j] : x;
+      nib |= exact_code(x, lo, step) << (4 * i);
+    }
+  } else if (far > 0.49999f) {
+    uint32_t doubt = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) doubt |= fabsf(fmaf(v[i] - lo, inv, -c[i])) > 0.49999f ? 1u << i : 0u;
+#pragma unroll 1
+    while (doubt) {
+      const int i = __ffs(doubt) - 1;
+      doubt &= doubt - 1;
+      const uint32_t word = i < 4 ? (i < 2 ? w[0] : w[1]) : (i < 6 ? w[2] : w[3]);
+      const float2 f = scale_floats<T>(word);
+      nib = (nib & ~(15u << (4 * i))) | (border_code(i & 1 ? f.y : f.x, lo, step, (int)((nib >> (4 * i)) & 15u)) << (4 * i));
+    }
+  }
+  scale = __byte_perm(sb, both, 0x5410);
+  if (!(lo >= -3.4e38f && hi <= 3.4e38f)) { nib = 0; scale = nan_pair<T>(); }
 }
 
-template <typename T, int kDim>
+// Where a lane's part of a (token, head) row lies; kUnroll rows per lane, a block's rows interleaved.
+struct Place { char* block; int j; bool on; };
+template <int kDim> __device__ __forceinline__ Place place_of(const bl_kv4_cache& c, int64_t slot, int h) {
+  const int pl = 31 - __clz(c.page_size);             // page sizes are powers of two
+  Place p;
+  p.on = slot >= 0 && (slot >> pl) < c.num_pages;
+  p.j = (int)slot & (c.page_size - 1);
+  p.block = reinterpret_cast<char*>(c.pages) + ((slot >> pl) * c.kv_heads + h) * (int64_t)Block<kDim>::bytes(c.page_size);
+  return p;
+}
+template <typename T, int kDim, int kUnroll>
 __global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, const T* __restrict__ k, const T* __restrict__ v,
                                                                int64_t T_, int64_t ld_k, int64_t ld_v,
                                                                const int64_t* __restrict__ slots) {
   constexpr int kLanes = kDim / 8, kRows = kKvThreads / kLanes;
   const int sub = threadIdx.x % kLanes, d = sub * 8;
-  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
-  const int64_t t = row / c.kv_heads;
-  const int h = (int)(row % c.kv_heads);
-  const int64_t slot = t < T_ ? slots[t] : -1;
-  const bool on = slot >= 0 && slot < c.num_pages * (int64_t)c.page_size;
-  float kx[8] = {}, vx[8] = {};
-  if (on) {
-    Elem<T>::load8(k + t * ld_k + (int64_t)h * kDim + d, kx);
-    Elem<T>::load8(v + t * ld_v + (int64_t)h * kDim + d, vx);
+  const uint32_t row0 = blockIdx.x * (kRows * kUnroll) + threadIdx.x / kLanes;         // fewer than 2^31 rows
+  uint4 kr[kUnroll], vr[kUnroll];
+  Place at[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
+    const int h = (int)(row - t * (uint32_t)c.kv_heads);
+    at[u] = place_of<kDim>(c, t < T_ ? slots[t] : -1, h);
+    kr[u] = vr[u] = make_uint4(0, 0, 0, 0);
+    if (at[u].on) {
+      kr[u] = __ldg(reinterpret_cast<const uint4*>(k + t * ld_k + (int64_t)h * kDim + d));
+      vr[u] = __ldg(reinterpret_cast<const uint4*>(v + t * ld_v + (int64_t)h * kDim + d));
+    }
   }
-  uint32_t kn, ks, vn, vs;
-  quantise_row<T, kLanes>(kx, kn, ks);
-  quantise_row<T, kLanes>(vx, vn, vs);
-  if (!on) return;
-  const int j = (int)(slot % c.page_size);
-  char* block = reinterpret_cast<char*>(c.pages) + ((slot / c.page_size) * c.kv_heads + h) * (int64_t)Block<kDim>::bytes(c.page_size);
-  *reinterpret_cast<uint32_t*>(block + j * (kDim / 2) + d / 2) = kn;
-  char* vc = block + Block<kDim>::v_codes(c.page_size);
-  *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d)) = (uint16_t)vn;
-  *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d + 4)) = (uint16_t)(vn >> 16);
-  if (sub == 0) *reinterpret_cast<uint32_t*>(block + Block<kDim>::k_scale(c.page_size) + 4 * j) = ks;
-  if (sub == 1) *reinterpret_cast<uint32_t*>(block + Block<kDim>::v_scale(c.page_size) + 4 * j) = vs;
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    uint32_t kn, ks, vn, vs;
+    quantise_row<T, kLanes>(kr[u], kn, ks);
+    quantise_row<T, kLanes>(vr[u], vn, vs);
+    if (!at[u].on) continue;
+    char* block = at[u].block;
+    const int j = at[u].j;
+    *reinterpret_cast<uint32_t*>(block + j * (kDim / 2) + d / 2) = kn;
+    char* vc = block + Block<kDim>::v_codes(c.page_size);
+    *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d)) = (uint16_t)vn;
+    *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d + 4)) = (uint16_t)(vn >> 16);
+    if (sub == 0) *reinterpret_cast<uint32_t*>(block + Block<kDim>::k_scale(c.page_size) + 4 * j) = ks;
+    if (sub == 1) *reinterpret_cast<uint32_t*>(block + Block<kDim>::v_scale(c.page_size) + 4 * j) = vs;
+  }
 }
 
-template <typename T> __device__ __forceinline__ void store_values(T* p, uint32_t nib, float2 se);
-template <> __device__ __forceinline__ void store_values<__half>(__half* p, uint32_t nib, float2 se) {
-  uint4 r;
-  __half2* o = reinterpret_cast<__half2*>(&r);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    o[i] = __floats2half2_rn(fmaf((float)((nib >> (8 * i)) & 15u), se.x, se.y), fmaf((float)((nib >> (8 * i + 4)) & 15u), se.x, se.y));
-  *reinterpret_cast<uint4*>(p) = r;
+// eta + step * code of two neighbouring codes, as stored; 2^23 + code is the float with the code in its low bits.
+template <typename T> __device__ __forceinline__ uint32_t two_values(uint32_t nib, int at, float2 se) {
+  const float c0 = __uint_as_float(0x4B000000u | ((nib >> at) & 15u)) - 8388608.f;
+  const float c1 = __uint_as_float(0x4B000000u | ((nib >> (at + 4)) & 15u)) - 8388608.f;
+  const T a = out_cast<T>(fmaf(c0, se.x, se.y)), b = out_cast<T>(fmaf(c1, se.x, se.y));
+  return (uint32_t)*reinterpret_cast<const uint16_t*>(&a) | ((uint32_t)*reinterpret_cast<const uint16_t*>(&b) << 16);
 }
-template <> __device__ __forceinline__ void store_values<__nv_bfloat16>(__nv_bfloat16* p, uint32_t nib, float2 se) {
-  uint4 r;
-  __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(&r);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    o[i] = __floats2bfloat162_rn(fmaf((float)((nib >> (8 * i)) & 15u), se.x, se.y), fmaf((float)((nib >> (8 * i + 4)) & 15u), se.x, se.y));
-  *reinterpret_cast<uint4*>(p) = r;
+template <typename T> __device__ __forceinline__ void store_values(T* p, uint32_t nib, float2 se) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(two_values<T>(nib, 0, se), two_values<T>(nib, 8, se), two_values<T>(nib, 16, se), two_values<T>(nib, 24, se));
 }
 
-template <typename T, int kDim>
+template <typename T, int kDim, int kUnroll>
 __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T* __restrict__ k, T* __restrict__ v, int64_t T_,
                                                              int64_t ld_k, int64_t ld_v, const int64_t* __restrict__ slots) {
   constexpr int kLanes = kDim / 8, kRows = kKvThreads / kLanes;
   const int d = (threadIdx.x % kLanes) * 8;
-  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
-  const int64_t t = row / c.kv_heads;
-  const int h = (int)(row % c.kv_heads);
-  if (t >= T_) return;
-  const int64_t slot = slots[t];
-  if (slot < 0 || slot >= c.num_pages * (int64_t)c.page_size) return;
-  const int j = (int)(slot % c.page_size);
-  const char* block = reinterpret_cast<const char*>(c.pages) +
-                      ((slot / c.page_size) * c.kv_heads + h) * (int64_t)Block<kDim>::bytes(c.page_size);
-  const char* vc = block + Block<kDim>::v_codes(c.page_size);
-  const uint32_t kn = *reinterpret_cast<const uint32_t*>(block + j * (kDim / 2) + d / 2);
-  const uint32_t vn = *reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(j, d)) |
-                      ((uint32_t)*reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(j, d + 4)) << 16);
-  const uint32_t ks = *reinterpret_cast<const uint32_t*>(block + Block<kDim>::k_scale(c.page_size) + 4 * j);
-  const uint32_t vs = *reinterpret_cast<const uint32_t*>(block + Block<kDim>::v_scale(c.page_size) + 4 * j);
-  store_values<T>(k + t * ld_k + (int64_t)h * kDim + d, kn, scale_floats<T>(ks));
-  store_values<T>(v + t * ld_v + (int64_t)h * kDim + d, vn, scale_floats<T>(vs));
+  const uint32_t row0 = blockIdx.x * (kRows * kUnroll) + threadIdx.x / kLanes;
+  uint32_t kn[kUnroll], vn[kUnroll], ks[kUnroll], vs[kUnroll];
+  bool on[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
+    const Place p = place_of<kDim>(c, t < T_ ? __ldg(slots + t) : -1, (int)(row - t * (uint32_t)c.kv_heads));
+    on[u] = p.on;
+    kn[u] = vn[u] = ks[u] = vs[u] = 0;
+    if (p.on) {
+      const char* vc = p.block + Block<kDim>::v_codes(c.page_size);
+      kn[u] = *reinterpret_cast<const uint32_t*>(p.block + p.j * (kDim / 2) + d / 2);
+      vn[u] = *reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(p.j, d)) |
+              ((uint32_t)*reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(p.j, d + 4)) << 16);
+      ks[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::k_scale(c.page_size) + 4 * p.j);
+      vs[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::v_scale(c.page_size) + 4 * p.j);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    if (!on[u]) continue;
+    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
+    const int h = (int)(row - t * (uint32_t)c.kv_heads);
+    store_values<T>(k + t * ld_k + (int64_t)h * kDim + d, kn[u], scale_floats<T>(ks[u]));
+    store_values<T>(v + t * ld_v + (int64_t)h * kDim + d, vn[u], scale_floats<T>(vs[u]));
+  }
 }
 
 // One CTA copies kCopyBytes of one page of one layer; 16 bytes per access, all loads of a thread in flight at once.
@@ -155,29 +233,43 @@ __global__ void __launch_bounds__(kKvThreads) kv4_copy_kernel(char* pages, int64
     if (off + i * (kKvThreads * 16) < page_bytes) *reinterpret_cast<uint4*>(dst + i * (kKvThreads * 16)) = r[i];
 }
 
-unsigned row_blocks(const bl_kv4_cache& c, int64_t T) {
-  const int rows = kKvThreads / (c.head_dim / 8);
+// Rows per lane: kMany where that still fills the GPU eight times over, so that a lane has that many loads in flight; else one.
+constexpr int kMany = 2;
+unsigned row_blocks(const bl_kv4_cache& c, int64_t T, int unroll) {
+  const int64_t rows = (int64_t)kKvThreads / (c.head_dim / 8) * unroll;
   return (unsigned)((T * c.kv_heads + rows - 1) / rows);
 }
 
+template <typename T, int kDim>
+cudaError_t append_dim(const bl_kv4_cache& c, const void* k, const void* v, int64_t n, int64_t ld_k, int64_t ld_v,
+                       const int64_t* slots, cudaStream_t s) {
+  const T* kp = reinterpret_cast<const T*>(k);
+  const T* vp = reinterpret_cast<const T*>(v);
+  const unsigned many = row_blocks(c, n, kMany);
+  if (many >= 8 * 148) kv4_append_kernel<T, kDim, kMany><<<many, kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
+  else kv4_append_kernel<T, kDim, 1><<<row_blocks(c, n, 1), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
+  return cudaGetLastError();
+}
 template <typename T>
 cudaError_t append_type(const bl_kv4_cache& c, const void* k, const void* v, int64_t n, int64_t ld_k, int64_t ld_v,
                         const int64_t* slots, cudaStream_t s) {
-  const T* kp = reinterpret_cast<const T*>(k);
-  const T* vp = reinterpret_cast<const T*>(v);
-  if (c.head_dim == 64) kv4_append_kernel<T, 64><<<row_blocks(c, n), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  else kv4_append_kernel<T, 128><<<row_blocks(c, n), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  return cudaGetLastError();
+  return c.head_dim == 64 ? append_dim<T, 64>(c, k, v, n, ld_k, ld_v, slots, s) : append_dim<T, 128>(c, k, v, n, ld_k, ld_v, slots, s);
 }
 
+template <typename T, int kDim>
+cudaError_t read_dim(const bl_kv4_cache& c, void* k, void* v, int64_t n, int64_t ld_k, int64_t ld_v, const int64_t* slots,
+                     cudaStream_t s) {
+  T* kp = reinterpret_cast<T*>(k);
+  T* vp = reinterpret_cast<T*>(v);
+  const unsigned many = row_blocks(c, n, kMany);
+  if (many >= 8 * 148) kv4_read_kernel<T, kDim, kMany><<<many, kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
+  else kv4_read_kernel<T, kDim, 1><<<row_blocks(c, n, 1), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
+  return cudaGetLastError();
+}
 template <typename T>
 cudaError_t read_type(const bl_kv4_cache& c, void* k, void* v, int64_t n, int64_t ld_k, int64_t ld_v, const int64_t* slots,
                       cudaStream_t s) {
-  T* kp = reinterpret_cast<T*>(k);
-  T* vp = reinterpret_cast<T*>(v);
-  if (c.head_dim == 64) kv4_read_kernel<T, 64><<<row_blocks(c, n), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  else kv4_read_kernel<T, 128><<<row_blocks(c, n), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  return cudaGetLastError();
+  return c.head_dim == 64 ? read_dim<T, 64>(c, k, v, n, ld_k, ld_v, slots, s) : read_dim<T, 128>(c, k, v, n, ld_k, ld_v, slots, s);
 }
 
 }  // namespace
