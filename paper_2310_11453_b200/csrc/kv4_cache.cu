@@ -1,7 +1,7 @@
 // The 4-bit key/value cache: quantising token rows into it, reading them back, copying its pages.
 //   eta = min x, step = (max x - min x) / 15 (rounded to the cache's type), code = clip(rint((x - eta) / step)).
-// All three are bound by memory.  Append and read give each (token, head) row kDim / 8 lanes, 8 values per
-// lane: one 16-byte access to the 16-bit rows, 4 bytes of key codes and 2 x 2 bytes of value codes.
+// All three are bound by memory.  Append and read give each (token, head) row kDim / 16 lanes, 16 values per
+// lane: two 16-byte accesses to the 16-bit rows, 8 bytes of key codes and 4 x 2 bytes of value codes.
 #include <type_traits>
 
 #include "kv4.cuh"
@@ -60,20 +60,21 @@ template <> __device__ __forceinline__ uint32_t min_pairs<__nv_bfloat16>(uint32_
   return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-// A row's 8 codes of this lane as nibbles (value i in bits 4 i), and the row's (step, eta) word.
+// A row's 16 codes of this lane as nibbles (value i in bits 4 i % 32 of word i / 8), and the row's (step, eta) word.
 // In fp32 the quotient (x - eta) / step is off by less than 4e-6 (it is at most 15 and a bit, and three roundings enter),
 // so a value whose quotient lies further than 1e-5 from a border between codes has its code from the fp32 sum with
 // 1.5 * 2^23, whose low bits are the rounded quotient.  Others go to fp64: with bf16 rows about one value in 300 lies on a
 // border exactly, so that path is short.  Steps below the type's normal range (quotients may pass 15.5) or at the end of
 // fp32's take exact_code.
 template <typename T, int kLanes>
-__device__ __forceinline__ void quantise_row(const uint4& raw, uint32_t& nib, uint32_t& scale) {
+__device__ __forceinline__ void quantise_row(const uint4 (&raw)[2], uint32_t (&nib)[2], uint32_t& scale) {
   constexpr float kMagic = 12582912.f;
   constexpr float kLeast = std::is_same<T, __half>::value ? 6.2e-5f : 1e-30f;
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
   // smallest value and smallest negated value, side by side in one word through the shuffles
-  const uint32_t mn = min_pairs<T>(min_pairs<T>(w[0], w[1]), min_pairs<T>(w[2], w[3]));
-  const uint32_t mx = min_pairs<T>(min_pairs<T>(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u), min_pairs<T>(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
+  uint32_t mn = w[0], mx = w[0] ^ 0x80008000u;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) { mn = min_pairs<T>(mn, w[i]); mx = min_pairs<T>(mx, w[i] ^ 0x80008000u); }
   uint32_t both = min_pairs<T>(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
 #pragma unroll
   for (int o = kLanes / 2; o > 0; o >>= 1) both = min_pairs<T>(both, __shfl_xor_sync(0xFFFFFFFFu, both, o));
@@ -83,42 +84,47 @@ __device__ __forceinline__ void quantise_row(const uint4& raw, uint32_t& nib, ui
   const float step = scale_floats<T>(sb).x;
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
-  float v[8], c[8], far = 0.f;                        // values, codes; largest distance from a code
+  float far = 0.f;                                    // largest distance of a quotient from its code
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 f = scale_floats<T>(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+  for (int k = 0; k < 2; ++k) {
+    float c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float d = v[i] - lo;
-    c[i] = fmaf(d, inv, kMagic) - kMagic;
-    far = fmaxf(far, fabsf(fmaf(d, inv, -c[i])));
-  }
-  const float n0 = fmaf(c[1], 16.f, c[0]) + fmaf(c[3], 4096.f, c[2] * 256.f);
-  const float n1 = fmaf(c[5], 16.f, c[4]) + fmaf(c[7], 4096.f, c[6] * 256.f);
-  nib = __byte_perm(__float_as_uint(n0 + 8388608.f), __float_as_uint(n1 + 8388608.f), 0x5410);
-  if (!(step > kLeast && step < 1e30f)) {
-    nib = 0;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      float x = v[0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) x = i == j ? v[j] : x;
-      nib |= exact_code(x, lo, step) << (4 * i);
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = scale_floats<T>(w[4 * k + i]);
+      const float d0 = f.x - lo, d1 = f.y - lo;
+      c[2 * i] = fmaf(d0, inv, kMagic) - kMagic;
+      c[2 * i + 1] = fmaf(d1, inv, kMagic) - kMagic;
+      far = fmaxf(far, fmaxf(fabsf(fmaf(d0, inv, -c[2 * i])), fabsf(fmaf(d1, inv, -c[2 * i + 1]))));
     }
-  } else if (far > 0.49999f) {
-    uint32_t doubt = 0;
+    const float n0 = fmaf(c[1], 16.f, c[0]) + fmaf(c[3], 4096.f, c[2] * 256.f);
+    const float n1 = fmaf(c[5], 16.f, c[4]) + fmaf(c[7], 4096.f, c[6] * 256.f);
+    nib[k] = __byte_perm(__float_as_uint(n0 + 8388608.f), __float_as_uint(n1 + 8388608.f), 0x5410);
+  }
+  const bool odd_step = !(step > kLeast && step < 1e30f);
+  if (odd_step || far > 0.49999f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) doubt |= fabsf(fmaf(v[i] - lo, inv, -c[i])) > 0.49999f ? 1u << i : 0u;
+    for (int k = 0; k < 2; ++k) {
+      uint32_t doubt = odd_step ? 0xFFu : 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 f = scale_floats<T>(w[4 * k + i / 2]);
+        const float q = ((i & 1 ? f.y : f.x) - lo) * inv;
+        doubt |= fabsf(q - rintf(q)) > 0.49998f ? 1u << i : 0u;
+      }
 #pragma unroll 1
-    while (doubt) {
-      const int i = __ffs(doubt) - 1;
-      doubt &= doubt - 1;
-      const uint32_t word = i < 4 ? (i < 2 ? w[0] : w[1]) : (i < 6 ? w[2] : w[3]);
-      const float2 f = scale_floats<T>(word);
-      nib = (nib & ~(15u << (4 * i))) | (border_code(i & 1 ? f.y : f.x, lo, step, (int)((nib >> (4 * i)) & 15u)) << (4 * i));
+      while (doubt) {
+        const int i = __ffs(doubt) - 1;
+        doubt &= doubt - 1;
+        const uint32_t word = i < 4 ? (i < 2 ? w[4 * k] : w[4 * k + 1]) : (i < 6 ? w[4 * k + 2] : w[4 * k + 3]);
+        const float2 f = scale_floats<T>(word);
+        const float x = i & 1 ? f.y : f.x;
+        const uint32_t code = odd_step ? exact_code(x, lo, step) : border_code(x, lo, step, (int)((nib[k] >> (4 * i)) & 15u));
+        nib[k] = (nib[k] & ~(15u << (4 * i))) | (code << (4 * i));
+      }
     }
   }
   scale = __byte_perm(sb, both, 0x5410);
-  if (!(lo >= -3.4e38f && hi <= 3.4e38f)) { nib = 0; scale = nan_pair<T>(); }
+  if (!(lo >= -3.4e38f && hi <= 3.4e38f)) { nib[0] = nib[1] = 0; scale = nan_pair<T>(); }
 }
 
 // Where a lane's part of a (token, head) row lies; kUnroll rows per lane, a block's rows interleaved.
@@ -131,40 +137,61 @@ template <int kDim> __device__ __forceinline__ Place place_of(const bl_kv4_cache
   p.block = reinterpret_cast<char*>(c.pages) + ((slot >> pl) * c.kv_heads + h) * (int64_t)Block<kDim>::bytes(c.page_size);
   return p;
 }
+// The rows of a warp: 32 / kLanes consecutive tokens of one head (so that two tokens whose value codes interleave are
+// neighbours), kUnroll times over.  job counts (run of tokens, head).
+template <int kLanes, int kUnroll> struct Rows {
+  uint32_t t0; int h;
+  __device__ __forceinline__ Rows(int kv_heads) {
+    const uint32_t job = blockIdx.x * (kKvThreads / 32) + (threadIdx.x >> 5), run = job / (uint32_t)kv_heads;
+    h = (int)(job - run * (uint32_t)kv_heads);
+    t0 = run * (32 / kLanes * kUnroll) + (threadIdx.x & 31) / kLanes;
+  }
+  __device__ __forceinline__ int64_t token(int u) const { return (int64_t)t0 + u * (32 / kLanes); }
+};
+
 template <typename T, int kDim, int kUnroll>
 __global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, const T* __restrict__ k, const T* __restrict__ v,
                                                                int64_t T_, int64_t ld_k, int64_t ld_v,
                                                                const int64_t* __restrict__ slots) {
-  constexpr int kLanes = kDim / 8, kRows = kKvThreads / kLanes;
-  const int sub = threadIdx.x % kLanes, d = sub * 8;
-  const uint32_t row0 = blockIdx.x * (kRows * kUnroll) + threadIdx.x / kLanes;         // fewer than 2^31 rows
-  uint4 kr[kUnroll], vr[kUnroll];
-  Place at[kUnroll];
+  constexpr int kLanes = kDim / 16;
+  const int lane = threadIdx.x & 31, sub = lane % kLanes, d = sub * 16, odd = (lane / kLanes) & 1;
+  const Rows<kLanes, kUnroll> rows(c.kv_heads);
+  uint4 kr[kUnroll][2], vr[kUnroll][2];
+  int64_t slot[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
-    const int h = (int)(row - t * (uint32_t)c.kv_heads);
-    at[u] = place_of<kDim>(c, t < T_ ? slots[t] : -1, h);
-    kr[u] = vr[u] = make_uint4(0, 0, 0, 0);
-    if (at[u].on) {
-      kr[u] = __ldg(reinterpret_cast<const uint4*>(k + t * ld_k + (int64_t)h * kDim + d));
-      vr[u] = __ldg(reinterpret_cast<const uint4*>(v + t * ld_v + (int64_t)h * kDim + d));
+    const int64_t t = rows.token(u);
+    slot[u] = t < T_ ? slots[t] : -1;
+    kr[u][0] = kr[u][1] = vr[u][0] = vr[u][1] = make_uint4(0, 0, 0, 0);
+    if (t < T_) {
+      const uint4* kp = reinterpret_cast<const uint4*>(k + t * ld_k + (int64_t)rows.h * kDim + d);
+      const uint4* vp = reinterpret_cast<const uint4*>(v + t * ld_v + (int64_t)rows.h * kDim + d);
+      kr[u][0] = __ldg(kp); kr[u][1] = __ldg(kp + 1);
+      vr[u][0] = __ldg(vp); vr[u][1] = __ldg(vp + 1);
     }
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    uint32_t kn, ks, vn, vs;
+    uint32_t kn[2], ks, vn[2], vs;
     quantise_row<T, kLanes>(kr[u], kn, ks);
     quantise_row<T, kLanes>(vr[u], vn, vs);
-    if (!at[u].on) continue;
-    char* block = at[u].block;
-    const int j = at[u].j;
-    *reinterpret_cast<uint32_t*>(block + j * (kDim / 2) + d / 2) = kn;
-    char* vc = block + Block<kDim>::v_codes(c.page_size);
-    *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d)) = (uint16_t)vn;
-    *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(j, d + 4)) = (uint16_t)(vn >> 16);
-    if (sub == 0) *reinterpret_cast<uint32_t*>(block + Block<kDim>::k_scale(c.page_size) + 4 * j) = ks;
-    if (sub == 1) *reinterpret_cast<uint32_t*>(block + Block<kDim>::v_scale(c.page_size) + 4 * j) = vs;
+    const Place p = place_of<kDim>(c, slot[u], rows.h);
+    // two tokens in neighbouring slots share words of value codes: each lane of the pair writes two whole words
+    const int64_t other = __shfl_xor_sync(0xFFFFFFFFu, slot[u], kLanes);
+    const uint32_t theirs = __shfl_xor_sync(0xFFFFFFFFu, odd ? vn[0] : vn[1], kLanes);
+    if (!p.on) continue;
+    *reinterpret_cast<uint2*>(p.block + p.j * (kDim / 2) + d / 2) = make_uint2(kn[0], kn[1]);
+    char* vc = p.block + Block<kDim>::v_codes(c.page_size);
+    if ((slot[u] ^ other) == 1 && (p.j & 1) == odd) {
+      const uint32_t lo = odd ? theirs : vn[0], hi = odd ? vn[1] : theirs;
+      *reinterpret_cast<uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d + 8 * odd)) = make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(p.j, d + 4 * i)) = (uint16_t)(vn[i >> 1] >> (16 * (i & 1)));
+    }
+    if (sub == 0) *reinterpret_cast<uint32_t*>(p.block + Block<kDim>::k_scale(c.page_size) + 4 * p.j) = ks;
+    if (sub == 1) *reinterpret_cast<uint32_t*>(p.block + Block<kDim>::v_scale(c.page_size) + 4 * p.j) = vs;
   }
 }
 
@@ -182,22 +209,25 @@ template <typename T> __device__ __forceinline__ void store_values(T* p, uint32_
 template <typename T, int kDim, int kUnroll>
 __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T* __restrict__ k, T* __restrict__ v, int64_t T_,
                                                              int64_t ld_k, int64_t ld_v, const int64_t* __restrict__ slots) {
-  constexpr int kLanes = kDim / 8, kRows = kKvThreads / kLanes;
-  const int d = (threadIdx.x % kLanes) * 8;
-  const uint32_t row0 = blockIdx.x * (kRows * kUnroll) + threadIdx.x / kLanes;
-  uint32_t kn[kUnroll], vn[kUnroll], ks[kUnroll], vs[kUnroll];
-  bool on[kUnroll];
+  constexpr int kLanes = kDim / 16;
+  const int d = ((threadIdx.x & 31) % kLanes) * 16;
+  const Rows<kLanes, kUnroll> rows(c.kv_heads);
+  uint2 kn[kUnroll], v0[kUnroll], v1[kUnroll];         // key codes; words of value codes, of this token and its pair's other
+  uint32_t ks[kUnroll], vs[kUnroll];
+  bool on[kUnroll], high[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
-    const Place p = place_of<kDim>(c, t < T_ ? __ldg(slots + t) : -1, (int)(row - t * (uint32_t)c.kv_heads));
+    const int64_t t = rows.token(u);
+    const Place p = place_of<kDim>(c, t < T_ ? __ldg(slots + t) : -1, rows.h);
     on[u] = p.on;
-    kn[u] = vn[u] = ks[u] = vs[u] = 0;
+    high[u] = p.j & 1;
+    kn[u] = v0[u] = v1[u] = make_uint2(0, 0);
+    ks[u] = vs[u] = 0;
     if (p.on) {
       const char* vc = p.block + Block<kDim>::v_codes(c.page_size);
-      kn[u] = *reinterpret_cast<const uint32_t*>(p.block + p.j * (kDim / 2) + d / 2);
-      vn[u] = *reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(p.j, d)) |
-              ((uint32_t)*reinterpret_cast<const uint16_t*>(vc + Block<kDim>::v_at(p.j, d + 4)) << 16);
+      kn[u] = *reinterpret_cast<const uint2*>(p.block + p.j * (kDim / 2) + d / 2);
+      v0[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d));
+      v1[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d + 8));
       ks[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::k_scale(c.page_size) + 4 * p.j);
       vs[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::v_scale(c.page_size) + 4 * p.j);
     }
@@ -205,10 +235,13 @@ __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T*
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     if (!on[u]) continue;
-    const uint32_t row = row0 + u * kRows, t = row / (uint32_t)c.kv_heads;
-    const int h = (int)(row - t * (uint32_t)c.kv_heads);
-    store_values<T>(k + t * ld_k + (int64_t)h * kDim + d, kn[u], scale_floats<T>(ks[u]));
-    store_values<T>(v + t * ld_v + (int64_t)h * kDim + d, vn[u], scale_floats<T>(vs[u]));
+    const int64_t t = rows.token(u);
+    T* kp = k + t * ld_k + (int64_t)rows.h * kDim + d;
+    T* vp = v + t * ld_v + (int64_t)rows.h * kDim + d;
+    const float2 kse = scale_floats<T>(ks[u]), vse = scale_floats<T>(vs[u]);
+    const uint32_t pick = high[u] ? 0x7632u : 0x5410u;
+    store_values<T>(kp, kn[u].x, kse); store_values<T>(kp + 8, kn[u].y, kse);
+    store_values<T>(vp, __byte_perm(v0[u].x, v0[u].y, pick), vse); store_values<T>(vp + 8, __byte_perm(v1[u].x, v1[u].y, pick), vse);
   }
 }
 
@@ -236,8 +269,8 @@ __global__ void __launch_bounds__(kKvThreads) kv4_copy_kernel(char* pages, int64
 // Rows per lane: kMany where that still fills the GPU eight times over, so that a lane has that many loads in flight; else one.
 constexpr int kMany = 2;
 unsigned row_blocks(const bl_kv4_cache& c, int64_t T, int unroll) {
-  const int64_t rows = (int64_t)kKvThreads / (c.head_dim / 8) * unroll;
-  return (unsigned)((T * c.kv_heads + rows - 1) / rows);
+  const int64_t run = 32 / (c.head_dim / 16) * unroll, jobs = (T + run - 1) / run * c.kv_heads;
+  return (unsigned)((jobs + kKvThreads / 32 - 1) / (kKvThreads / 32));
 }
 
 template <typename T, int kDim>
