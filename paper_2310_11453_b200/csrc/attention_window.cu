@@ -86,6 +86,8 @@ constexpr int kThreads = 384;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // per thread after the split; 256 x 208 + 128 x 88 = 384 x 168
 constexpr int kLaunchRegs = 168;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "registers of the split");
+constexpr int kNarrow = 32;                      // keys of a product with a tile that holds only sinks
+constexpr int kPolyOf4 = 1;                      // of four pairs of exponentials, those formed by ex2_poly
 constexpr float kMoveLog2 = 8.f;                 // growth of a row's maximum that is let pass
 constexpr float kLiftLog2 = 7.f;                 // probabilities are formed 2^7 times their size
 
@@ -98,13 +100,14 @@ struct Ctl {
 // Bounded wait like mbar_wait, with the number of polls from the launch (tests shorten it).
 __device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
   const uint32_t b = smem_u32(bar);
-  if (polls && mbar_try_wait(b, parity)) return true;
-  const unsigned long long t0 = global_ns();
+  unsigned long long t0 = 0;                     // the clock is read only once a wait has become long
   for (uint32_t it = 0; it < polls; ++it) {
     if (mbar_try_wait(b, parity)) return true;
     if ((it & 255u) == 255u) {
       if (*abort_flag) return false;
-      if (global_ns() - t0 > kWaitNs) break;
+      const unsigned long long now = global_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > kWaitNs) break;
     }
   }
   *abort_flag = 1;
@@ -127,13 +130,27 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
   d |= (uint64_t)2 << 61;
   return d;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-               ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+// The instructions of the tensor core, issued by the lane whose `on` is set.  The whole warp executes them: in code that one
+// lane runs alone the operands cannot stay in the uniform registers that the instruction reads, and moving them there cost
+// more than the product itself (85 clocks per product of 64; the pair of tiles took 4520 clocks instead of 3300).
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t on;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(on));
+  return on;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t on, uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile("{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 e, %5, 0;\n"
+               "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(on) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t on, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile("{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 e, %5, 0;\n"
+               "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(on) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t on, unsigned long long* bar) {
+  asm volatile("{\n.reg .pred e;\nsetp.ne.b32 e, %1, 0;\n"
+               "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_u32(bar)), "r"(on) : "memory");
 }
 // 32 columns of this warp's 32 lanes, without the wait.
 __device__ __forceinline__ void ld32(uint32_t taddr, float* r) {
@@ -161,6 +178,39 @@ template <typename R> __device__ __forceinline__ void st32(uint32_t taddr, const
         "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
         "r"(u[30]), "r"(u[31]) : "memory");
 }
+template <typename R> __device__ __forceinline__ void st16(uint32_t taddr, const R* r) {
+  static_assert(sizeof(R) == 4, "32-bit columns");
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]) : "memory");
+}
+// Two fp32 numbers in one 64-bit register, and the instructions that work on both.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 halves(f32x2 r) { float2 v; asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r)); return v; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+// 2^x of two numbers without the special-function unit, which the softmax would otherwise wait for: x = n + f with n whole and
+// |f| <= 1/2, 2^f by its minimax polynomial of degree 4 (relative error 2.6e-6, found by exchange on [-1/2, 1/2]), n added
+// to the exponent.  x below -126 counts as -126; a NaN comes out as a huge number or NaN.
+__device__ __forceinline__ float2 ex2_poly(f32x2 x2) {
+  const float2 x = halves(x2);
+  const f32x2 xc = pair(max_nan(x.x, -126.f), max_nan(x.y, -126.f));
+  const f32x2 t = add2(xc, pair(12582912.f, 12582912.f)), n = add2(t, pair(-12582912.f, -12582912.f));
+  const f32x2 f = fma2(n, pair(-1.f, -1.f), xc);
+  f32x2 p = pair(0.009570102207362652f, 0.009570102207362652f);
+  p = fma2(p, f, pair(0.05591785907745361f, 0.05591785907745361f));
+  p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
+  p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
+  p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
+  const float2 pv = halves(p), tv = halves(t);
+  return make_float2(__int_as_float(__float_as_int(pv.x) + (__float_as_int(tv.x) << 23)),
+                     __int_as_float(__float_as_int(pv.y) + (__float_as_int(tv.y) << 23)));
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -177,45 +227,46 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, f
 }
 
 // What a CTA works on; every role derives the same.
+struct Span { int head, row0, rows, pos0, pos1; };   // a tile: head, first query row of the sequence, rows (0: none), their positions
 struct Job {
   SeqRows r;
-  int b, head[2], row0[2], rows[2];              // per tile: head, first query row of the sequence, rows (0: no tile)
-  int pos0[2], pos1[2];                          // positions of its first and last row
+  Span tile[2];
   int sink_tiles, first, count;                  // key tiles: those of the sinks, then `first` on
   int window, sinks;
   __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kTile; }
-  // does a row of tile t see a key of tile j?
-  __device__ __forceinline__ bool active(int t, int j) const {
+  // does a row of the tile see a key of key tile j?
+  __device__ __forceinline__ bool active(const Span& s, int j) const {
     const int k0 = key0(j);
-    return rows[t] > 0 && k0 <= pos1[t] && (window == 0 || k0 + kTile - 1 > pos0[t] - window || k0 < sinks);
+    return s.rows > 0 && k0 <= s.pos1 && (window == 0 || k0 + kTile - 1 > s.pos0 - window || k0 < sinks);
   }
-  // does some row of tile t not see some key of tile j?
-  __device__ __forceinline__ bool edge(int t, int j) const {
+  // does some row of the tile not see some key of key tile j?
+  __device__ __forceinline__ bool edge(const Span& s, int j) const {
     const int k0 = key0(j);
-    return k0 + kTile - 1 > pos0[t] || (window > 0 && pos1[t] - k0 >= window && k0 + kTile > sinks);
+    return k0 + kTile - 1 > s.pos0 || (window > 0 && s.pos1 - k0 >= window && k0 + kTile > sinks);
   }
+  // a tile of which only the sinks are visible, and few: its products take kNarrow keys
+  __device__ __forceinline__ bool narrow(int j) const { return j < sink_tiles && sinks - j * kTile <= kNarrow; }
 };
-// pair: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
-__device__ __forceinline__ Job make_job(const WindowArgs& a, bool pair) {
+// two_heads: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
+__device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
   Job w;
-  const int units = pair ? a.heads / 2 : a.heads, per = pair ? kTile : 2 * kTile;
+  const int units = two_heads ? a.heads / 2 : a.heads, per = two_heads ? kTile : 2 * kTile;
   const int blocks = (int)((a.seq_q + per - 1) / per);
-  const int u = blockIdx.x % units, rest = blockIdx.x / units;
-  w.b = rest % a.batch;
-  const int blk = blocks - 1 - rest / a.batch;
-  w.r = seq_rows(a, w.b);
+  const int u = blockIdx.x % units, rest = blockIdx.x / units, b = rest % a.batch, blk = blocks - 1 - rest / a.batch;
+  w.r = seq_rows(a, b);
   w.window = a.window; w.sinks = a.sinks;
   int lo = 0x7FFFFFFF, hi = 0;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    w.head[t] = pair ? 2 * u + t : u;
-    w.row0[t] = blk * per + (pair ? 0 : t * kTile);
-    w.rows[t] = min(max(w.r.nq - w.row0[t], 0), kTile);
-    w.pos0[t] = w.r.nk - w.r.nq + w.row0[t];
-    w.pos1[t] = w.pos0[t] + w.rows[t] - 1;
-    if (w.rows[t] > 0 && w.pos1[t] >= 0) {
-      lo = min(lo, a.window > 0 ? max(0, w.pos0[t] - a.window + 1) : 0);
-      hi = max(hi, w.pos1[t] + 1);
+    Span& s = w.tile[t];
+    s.head = two_heads ? 2 * u + t : u;
+    s.row0 = blk * per + (two_heads ? 0 : t * kTile);
+    s.rows = min(max(w.r.nq - s.row0, 0), kTile);
+    s.pos0 = w.r.nk - w.r.nq + s.row0;
+    s.pos1 = s.pos0 + s.rows - 1;
+    if (s.rows > 0 && s.pos1 >= 0) {
+      lo = min(lo, a.window > 0 ? max(0, s.pos0 - a.window + 1) : 0);
+      hi = max(hi, s.pos1 + 1);
     }
   }
   if (hi == 0) lo = 0;
@@ -225,10 +276,74 @@ __device__ __forceinline__ Job make_job(const WindowArgs& a, bool pair) {
   return w;
 }
 
+// The softmax of one tile's scores, by the four warps that own its rows: a thread holds a row.
+template <typename T, int kDim> struct Softmax {
+  uint32_t ts, to;                               // tensor memory of S (then P) and of O, at this warp's lanes
+  float sl;                                      // scale in units of log2
+  float m, l;                                    // running maximum (raw score) and sum
+
+  // kCols columns; kMask: places from `last` on, and before `from` unless before `sink`, are not seen.  False: a wait ran out.
+  template <int kCols, bool kMask, typename Wait>
+  __device__ __forceinline__ bool step(int last, int from, int sink, Wait o_ready) {
+    float s[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; c += 32) ld32(ts + c, s + c);
+    ld_wait();
+    if (kMask) {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
+    }
+    float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]), mx2 = s[6], mx3 = s[7];
+#pragma unroll
+    for (int c = 8; c < kCols; c += 8) {
+      mx0 = max3(mx0, s[c], s[c + 1]); mx1 = max3(mx1, s[c + 2], s[c + 3]);
+      mx2 = max3(mx2, s[c + 4], s[c + 5]); mx3 = max3(mx3, s[c + 6], s[c + 7]);
+    }
+    const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
+    const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
+    if (__any_sync(0xFFFFFFFFu, move)) {         // O of the tiles so far takes the new maximum
+      if (!o_ready()) return false;
+      const float f = move ? ex2((m - mx) * sl) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < kDim; c += 32) {
+        float o[32];
+        ld32(to + c, o);
+        ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] *= f;
+        st32(to + c, o);
+      }
+    }
+    if (move || m == -INFINITY) m = fmaxf(m, mx);
+    const float shift = m == -INFINITY ? 0.f : kLiftLog2 - m * sl;
+    const f32x2 sl2 = pair(sl, sl), shift2 = pair(shift, shift);
+    f32x2 l0 = pair(0.f, 0.f), l1 = l0;
+#pragma unroll
+    for (int c = 0; c < kCols; c += 32) {
+      uint32_t p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const f32x2 x = fma2(pair(s[c + 2 * i], s[c + 2 * i + 1]), sl2, shift2);
+        float2 v;
+        if (!kMask && i % 4 >= 4 - kPolyOf4) v = ex2_poly(x);
+        else { v = halves(x); v.x = ex2(v.x); v.y = ex2(v.y); }
+        if (i & 1) l1 = add2(l1, pair(v.x, v.y)); else l0 = add2(l0, pair(v.x, v.y));
+        p[i] = pack2<T>(v.x, v.y);
+      }
+      st16(ts + c / 2, p);
+    }
+    const float2 sum = halves(add2(l0, l1));
+    l += sum.x + sum.y;
+    st_wait();
+    return true;
+  }
+};
+
 template <typename T, int kDim>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                        const __grid_constant__ CUtensorMap map_v, WindowArgs a, int pair, uint32_t polls) {
+                        const __grid_constant__ CUtensorMap map_v, WindowArgs a, int two_heads, uint32_t polls) {
   constexpr int kSub = kTile * 128;              // bytes of a sub-tile: 128 rows of 64 values
   constexpr int kSubs = kDim / 64, kTileBytes = kSubs * kSub;
   extern __shared__ unsigned char smem_raw[];
@@ -264,20 +379,21 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;          // S0 S1 (128 columns each), O0 O1
   pdl_wait();
-  const Job job = make_job(a, pair != 0);
+  const Job job = make_job(a, two_heads != 0);
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 9 && lane == 0 && job.count > 0) {             // ---- copies
       int issued = 0;
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (job.rows[t] == 0) continue;
+        if (job.tile[t].rows == 0) continue;
         mbar_arrive_expect_tx(smem_u32(&ctl->q_full[t]), kTileBytes);
         for (int s = 0; s < kSubs; ++s)
-          tma_load_2d(smem_u32(sq + t * kTileBytes + s * kSub), &map_q, job.head[t] * kDim + 64 * s, job.r.q0 + job.row0[t],
+          tma_load_2d(smem_u32(sq + t * kTileBytes + s * kSub), &map_q, job.tile[t].head * kDim + 64 * s, job.r.q0 + job.tile[t].row0,
                       smem_u32(&ctl->q_full[t]));
       }
-      const int hk = job.head[0] / (a.heads / a.kv_heads);
+      const int hk = job.tile[0].head / (a.heads / a.kv_heads);
       for (int e = 0; e < 2 * job.count; ++e) {                // entry 2 j: keys of tile j; 2 j + 1: its values
         const int slot = e % kSlots;
         if (e >= kSlots && !wait_for(&ctl->kv_empty[slot], ((e / kSlots) - 1) & 1, abort_flag, polls)) break;
@@ -289,131 +405,97 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       }
       // Copies end before the CTA does, also those of a tile that turned out to see nothing, and after a wait ran out.
       int gave_up = 0;
+#pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (job.rows[t] > 0) wait_for(&ctl->q_full[t], 0, &gave_up, kSpinLimit);
+        if (job.tile[t].rows > 0) wait_for(&ctl->q_full[t], 0, &gave_up, kSpinLimit);
       for (int e = max(0, issued - kSlots); e < issued; ++e) wait_for(&ctl->kv_full[e % kSlots], (e / kSlots) & 1, &gave_up, kSpinLimit);
-    } else if (warp == 8 && lane == 0 && job.count > 0) {      // ---- products
-      constexpr uint32_t kIdS = idesc<T>(kTile, false), kIdO = idesc<T>(kDim, true);
+    } else if (warp == 8 && job.count > 0) {                   // ---- products (the whole warp; one lane issues)
+      constexpr uint32_t kIdS = idesc<T>(kTile, false), kIdSn = idesc<T>(kNarrow, false), kIdO = idesc<T>(kDim, true);
+      const uint32_t on = elect(), q_at = smem_u32(sq), ring_at = smem_u32(ring);
       int pv[2] = {0, 0}, sc[2] = {0, 0};
-      bool ok = true;
-      for (int j = 0; j <= job.count && ok; ++j) {
-        const int ek = 2 * j, ev = 2 * j - 1;
-        if (j < job.count) ok = ok && wait_for(&ctl->kv_full[ek % kSlots], (ek / kSlots) & 1, abort_flag, polls);
-        if (j > 0) ok = ok && wait_for(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1, abort_flag, polls);
-        for (int t = 0; t < 2 && ok; ++t) {
-          const uint32_t ts = tmem + t * kTile, to = tmem + 2 * kTile + t * kTile;
-          if (j > 0 && job.active(t, j - 1)) {
-            ok = wait_for(&ctl->p_ready[t], pv[t] & 1, abort_flag, polls);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t dv = desc_mn(smem_u32(ring + (ev % kSlots) * kTileBytes));
+      auto half = [&](auto which, int j, uint32_t k_at, uint32_t v_at) -> bool {   // tile `which`: PV of key tile j - 1, S of key tile j
+        constexpr int t = decltype(which)::value;
+        const Span& span = job.tile[t];
+        const uint32_t ts = tmem + t * kTile, to = tmem + 2 * kTile + t * kTile;
+        if (j > 0 && job.active(span, j - 1)) {
+          if (!__all_sync(0xFFFFFFFFu, wait_for(&ctl->p_ready[t], pv[t] & 1, abort_flag, polls))) return false;
+          tc_fence_after();
+          const uint64_t dv = desc_mn(v_at);
+          const int steps = job.narrow(j - 1) ? kNarrow / 16 : kTile / 16;
+          const uint32_t more = pv[t] > 0;
 #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)               // 16 keys: 8 columns of P, 2048 bytes of V
-              mma_ts(to, ts + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, pv[t] > 0 || k > 0);
-            mma_commit(smem_u32(&ctl->o_done[t]));
-            ++pv[t];
-          }
-          if (j < job.count && job.active(t, j)) {
-            if (sc[t] == 0) ok = wait_for(&ctl->q_full[t], 0, abort_flag, polls);
-            if (!ok) break;
-            const uint32_t qa = smem_u32(sq + t * kTileBytes), ka = smem_u32(ring + (ek % kSlots) * kTileBytes);
-#pragma unroll
-            for (int k = 0; k < kDim / 16; ++k) {              // 16 values: 32 bytes within a sub-tile's rows
-              const uint32_t off = (k / 4) * kSub + (k % 4) * 32;
-              mma_ss(ts, smem_desc_sw128(qa + off), smem_desc_sw128(ka + off), kIdS, k > 0);
-            }
-            mma_commit(smem_u32(&ctl->s_full[t]));
-            ++sc[t];
-          }
+          for (int k = 0; k < kTile / 16; ++k)                 // 16 keys: 8 columns of P, 2048 bytes of V
+            if (k < steps) mma_ts(on, to, ts + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, k > 0 ? 1u : more);
+          commit(on, &ctl->o_done[t]);
+          ++pv[t];
         }
-        if (!ok) break;
-        if (j > 0) mma_commit(smem_u32(&ctl->kv_empty[ev % kSlots]));
-        if (j < job.count) mma_commit(smem_u32(&ctl->kv_empty[ek % kSlots]));
+        if (j < job.count && job.active(span, j)) {
+          if (sc[t] == 0 && !__all_sync(0xFFFFFFFFu, wait_for(&ctl->q_full[t], 0, abort_flag, polls))) return false;
+          const uint64_t dq = smem_desc_sw128(q_at + t * kTileBytes), dk = smem_desc_sw128(k_at);
+          const uint32_t id = job.narrow(j) ? kIdSn : kIdS;
+#pragma unroll
+          for (int k = 0; k < kDim / 16; ++k) {                // 16 values: 32 bytes within a sub-tile's rows
+            const uint64_t off = (uint64_t)(((k / 4) * kSub + (k % 4) * 32) >> 4);
+            mma_ss(on, ts, dq + off, dk + off, id, k > 0);
+          }
+          commit(on, &ctl->s_full[t]);
+          ++sc[t];
+        }
+        return true;
+      };
+      for (int j = 0; j <= job.count; ++j) {
+        const int ek = 2 * j, ev = 2 * j - 1;
+        bool ok = true;
+        if (j < job.count) ok = wait_for(&ctl->kv_full[ek % kSlots], (ek / kSlots) & 1, abort_flag, polls);
+        if (j > 0) ok = ok && wait_for(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1, abort_flag, polls);
+        if (!__all_sync(0xFFFFFFFFu, ok)) break;
+        const uint32_t k_at = ring_at + (ek % kSlots) * kTileBytes, v_at = ring_at + ((ev + kSlots) % kSlots) * kTileBytes;
+        if (!half(std::integral_constant<int, 0>{}, j, k_at, v_at)) break;
+        if (!half(std::integral_constant<int, 1>{}, j, k_at, v_at)) break;
+        if (j > 0) commit(on, &ctl->kv_empty[ev % kSlots]);
+        if (j < job.count) commit(on, &ctl->kv_empty[ek % kSlots]);
       }
       int gave_up = 0;                                         // products, and the arrivals they owe, end before the CTA does
-      mma_commit(smem_u32(&ctl->drain));
+      commit(on, &ctl->drain);
       wait_for(&ctl->drain, 0, &gave_up, kSpinLimit);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int t = warp >> 2, row = threadIdx.x & 127;          // the tile, and this thread's row of it
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * kTile + lanes, to = tmem + 2 * kTile + t * kTile + lanes;
-    const float sl = a.scale * 1.4426950408889634f;
-    const int pos = job.pos0[t] + row;
-    float m = -INFINITY, l = 0.f;
+    const Span span = t ? job.tile[1] : job.tile[0];
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + 2 * kTile + t * kTile + lanes;
+    Softmax<T, kDim> sm{tmem + t * kTile + lanes, to, a.scale * 1.4426950408889634f, -INFINITY, 0.f};
+    const int pos = span.pos0 + row;
     int n = 0;
     bool ok = true;
+    auto o_ready = [&]() -> bool {
+      const bool r = __all_sync(0xFFFFFFFFu, wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls));
+      tc_fence_after();
+      return r;
+    };
     for (int j = 0; j < job.count; ++j) {
-      if (!job.active(t, j)) continue;
-      ok = wait_for(&ctl->s_full[t], n & 1, abort_flag, polls);
-      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!job.active(span, j)) continue;
+      ok = __all_sync(0xFFFFFFFFu, wait_for(&ctl->s_full[t], n & 1, abort_flag, polls));
       if (!ok) break;
       tc_fence_after();
-      float s[kTile];
-#pragma unroll
-      for (int c = 0; c < kTile; c += 32) ld32(ts + c, s + c);
-      ld_wait();
-      if (job.edge(t, j)) {
-        const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
-        const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
-#pragma unroll
-        for (int c = 0; c < kTile; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
-      }
-      float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
-#pragma unroll
-      for (int c = 4; c < kTile; c += 4) {
-        mx0 = fmaxf(mx0, s[c]); mx1 = fmaxf(mx1, s[c + 1]); mx2 = fmaxf(mx2, s[c + 2]); mx3 = fmaxf(mx3, s[c + 3]);
-      }
-      const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-      const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
-      if (__any_sync(0xFFFFFFFFu, move)) {                     // O of the tiles so far takes the new maximum
-        ok = wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) break;
-        tc_fence_after();
-        const float f = move ? ex2((m - mx) * sl) : 1.f;
-        l *= f;
-#pragma unroll
-        for (int c = 0; c < kDim; c += 32) {
-          float o[32];
-          ld32(to + c, o);
-          ld_wait();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] *= f;
-          st32(to + c, o);
-        }
-      }
-      if (move || m == -INFINITY) m = fmaxf(m, mx);
-      const float shift = m == -INFINITY ? 0.f : kLiftLog2 - m * sl;
-      float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-      for (int c = 0; c < kTile; c += 64) {
-        uint32_t p[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float p0 = ex2(fmaf(s[c + 2 * i], sl, shift)), p1 = ex2(fmaf(s[c + 2 * i + 1], sl, shift));
-          l0 += p0; l1 += p1;
-          p[i] = pack2<T>(p0, p1);
-        }
-        st32(ts + c / 2, p);
-      }
-      l += l0 + l1;
-      st_wait();
+      const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
+      const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
+      if (job.narrow(j)) ok = sm.template step<kNarrow, true>(last, from, sink, o_ready);
+      else if (job.edge(span, j)) ok = sm.template step<kTile, true>(last, from, sink, o_ready);
+      else ok = sm.template step<kTile, false>(last, from, sink, o_ready);
+      if (!ok) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t]));
       ++n;
     }
+    const float l = sm.l;
     // ---- output
-    if (ok && n > 0) {
-      ok = wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls);
-      ok = __all_sync(0xFFFFFFFFu, ok);
-      tc_fence_after();
-    }
+    if (ok && n > 0) ok = o_ready();
     if (ok) {
-      const bool mine = row < job.rows[t];
+      const bool mine = row < span.rows;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + job.row0[t] + row) * a.ld_o + (int64_t)job.head[t] * kDim;
+      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + span.row0 + row) * a.ld_o + (int64_t)span.head * kDim;
       float check = 0.f;
 #pragma unroll
       for (int c = 0; c < kDim; c += 32) {
@@ -438,7 +520,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       while (bad) {
         const int i = __ffs(bad) - 1;
         bad &= bad - 1;
-        window_row<T, kDim>(a, job.r, job.row0[t] + (warp & 3) * 32 + i, job.head[t]);
+        window_row<T, kDim>(a, job.r, span.row0 + (warp & 3) * 32 + i, span.head);
       }
     }
   }
@@ -447,8 +529,11 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   if (*abort_flag) {
     if (threadIdx.x == 0) atomicAdd(&g_window_fallbacks, 1u);
-    for (int t = 0; t < 2; ++t)
-      for (int i = warp; i < job.rows[t]; i += kThreads / 32) window_row<T, kDim>(a, job.r, job.row0[t] + i, job.head[t]);
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+      const Span span = t ? job.tile[1] : job.tile[0];
+      for (int i = warp; i < span.rows; i += kThreads / 32) window_row<T, kDim>(a, job.r, span.row0 + i, span.head);
+    }
   }
 }
 
@@ -485,12 +570,12 @@ cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
   } else {
     mk = mv = mq;                                // no key anywhere: never used
   }
-  const bool pair = (a.heads / a.kv_heads) % 2 == 0;
-  const int64_t per = pair ? kTile : 2 * kTile;
-  const int64_t grid = (a.seq_q + per - 1) / per * a.batch * (pair ? a.heads / 2 : a.heads);
+  const bool two_heads = (a.heads / a.kv_heads) % 2 == 0;
+  const int64_t per = two_heads ? kTile : 2 * kTile;
+  const int64_t grid = (a.seq_q + per - 1) / per * a.batch * (two_heads ? a.heads / 2 : a.heads);
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
   const uint32_t polls = dbg < 0 ? kSpinLimit : (uint32_t)(dbg < (long long)kSpinLimit ? dbg : kSpinLimit);
-  return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, pair ? 1 : 0, polls);
+  return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, two_heads ? 1 : 0, polls);
 }
 
 }  // namespace
