@@ -2,19 +2,21 @@
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = e^(scale q_i . k_j - max),  j visible from i.
 //
 // A CTA owns two tiles of 128 query rows: the same rows of two heads that share their keys (even group sizes), or
-// two consecutive tiles of one head.  Keys and values pass through shared memory in tiles of 128, once for both
-// tiles; tiles that no row sees (after the rows, or between the sinks and the window) are not loaded.  Per pair of
-// tiles two products of 128 x 128 x kDim run on the tcgen05 tensor cores,
+// two consecutive tiles of one head.  Keys and values pass through shared memory in tiles of 64, once for both
+// tiles; tiles that no row sees (after the rows, or between the sinks and the window) are not loaded.  Per query and
+// key tile two products of 128 x 64 x kDim run on the tcgen05 tensor cores,
 //   S = Q K^T   both operands in shared memory (TMA, 128-byte swizzle), S in tensor memory (fp32),
 //   O += P V    P in tensor memory as 16-bit numbers, over S; V as it lies in memory (its rows are the
 //               contraction, so the descriptor says MN-major); O in tensor memory (fp32).
-// While one tile's softmax runs, the other tile's products do: issue order S0(j) S1(j) | PV0(j) S0(j+1) | PV1(j)
-// S1(j+1) | ...; the tensor core takes products in issue order, which is what keeps S(j+1) from overwriting P(j).
+// Each query tile has two places for S: while the softmax works on S(i), S(i+1) is being formed or is there already,
+// so that it never waits for a product.  A thread's products run in issue order S(i+1), PV(i), S(i+2), .., which is what
+// keeps S(i+2) from overwriting P(i).  With one place of 128 keys the same kernel took 1.6 times as long: a tile's
+// softmax (1900 clocks) and products (1700 with their latencies) then take turns.
 //
-// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1 (a thread owns a query row: no shuffles), warp 8 issues the
-// products, warp 9 the copies.  The running maximum moves only when a row's maximum grew by more than 2^8: O is
-// then rescaled in tensor memory, which is rare; else probabilities of up to 2^8 do no harm (they are formed at 2^7
-// times their size, 2^15 at most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
+// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1 (a thread owns a query row: no shuffles), warps 8 and 10 issue
+// the products of tile 0 and 1, warp 9 the copies.  The running maximum moves only when a row's maximum grew by more
+// than 2^8: O is then rescaled in tensor memory, which is rare; else probabilities of up to 2^8 do no harm (they are
+// formed at 2^7 times their size, 2^15 at most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
 //
 // Invisible places.  A masked score is replaced, so keys there may be anything.  A value there meets a probability
 // of 0, but 0 x NaN is NaN: a row whose result is not finite is computed again by one warp from the visible
@@ -80,19 +82,16 @@ __device__ void window_row(const WindowArgs& a, const SeqRows& r, int i, int h) 
   for (int e = 0; e < kVals; ++e) o[e] = out_cast<T>(l == 0.f ? 0.f : acc[e] / l);
 }
 
-constexpr int kTile = 128;                       // query rows and keys per tile
-constexpr int kSlots = 4;                        // key or value tiles in shared memory
+constexpr int kRows = 128;                       // query rows per tile
+constexpr int kKeys = 64;                        // keys per tile
+constexpr int kSlots = 8;                        // key or value tiles in shared memory
 constexpr int kThreads = 384;
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;   // per thread after the split; 256 x 208 + 128 x 88 = 384 x 168
-constexpr int kLaunchRegs = 168;
-static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "registers of the split");
-constexpr int kNarrow = 32;                      // keys of a product with a tile that holds only sinks
-constexpr int kPolyOf4 = 1;                      // of four pairs of exponentials, those formed by ex2_poly
+constexpr int kPolyOf4 = 0;                      // of four pairs of exponentials, those formed by ex2_poly
 constexpr float kMoveLog2 = 8.f;                 // growth of a row's maximum that is let pass
 constexpr float kLiftLog2 = 7.f;                 // probabilities are formed 2^7 times their size
 
 struct Ctl {
-  unsigned long long q_full[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_ready[2], o_done[2], drain;
+  unsigned long long q_full[2], kv_full[kSlots], kv_empty[kSlots], s_full[2][2], p_ready[2][2], o_done[2][2], drain[2];   // [tile][place]
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -120,11 +119,11 @@ template <typename T> __host__ __device__ constexpr uint32_t idesc(int n, bool b
   return (1u << 4) | (type << 7) | (type << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 // K-major tile of 128-byte rows: smem_desc_sw128.  MN-major: rows of 64 values along N, groups of 8 rows (of the
-// contraction) 1024 bytes apart, the next 64 values along N one sub-tile (128 rows) further.
+// contraction) 1024 bytes apart, the next 64 values along N one sub-tile (kKeys rows) further.
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
   uint64_t d = 0;
   d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)((kTile * 128) >> 4) << 16;
+  d |= (uint64_t)((kKeys * 128) >> 4) << 16;
   d |= (uint64_t)(1024 >> 4) << 32;
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
@@ -178,14 +177,6 @@ template <typename R> __device__ __forceinline__ void st32(uint32_t taddr, const
         "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
         "r"(u[30]), "r"(u[31]) : "memory");
 }
-template <typename R> __device__ __forceinline__ void st16(uint32_t taddr, const R* r) {
-  static_assert(sizeof(R) == 4, "32-bit columns");
-  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
-        "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]) : "memory");
-}
 // Two fp32 numbers in one 64-bit register, and the instructions that work on both.
 using f32x2 = unsigned long long;
 __device__ __forceinline__ f32x2 pair(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
@@ -227,30 +218,29 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, f
 }
 
 // What a CTA works on; every role derives the same.
-struct Span { int head, row0, rows, pos0, pos1; };   // a tile: head, first query row of the sequence, rows (0: none), their positions
+struct Span {                                    // a tile
+  int head, row0, rows, pos0, pos1;              // head, first query row of the sequence, rows (0: none), their positions
+  int from, to;                                  // key tiles of its window: from .. to (and those that hold sinks)
+};
 struct Job {
   SeqRows r;
   Span tile[2];
   int sink_tiles, first, count;                  // key tiles: those of the sinks, then `first` on
+  int sink_end;                                  // key tiles before this one hold sinks
   int window, sinks;
-  __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kTile; }
+  __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kKeys; }
   // does a row of the tile see a key of key tile j?
-  __device__ __forceinline__ bool active(const Span& s, int j) const {
-    const int k0 = key0(j);
-    return s.rows > 0 && k0 <= s.pos1 && (window == 0 || k0 + kTile - 1 > s.pos0 - window || k0 < sinks);
-  }
+  __device__ __forceinline__ bool active(const Span& s, int j) const { return j <= s.to && (j >= s.from || j < sink_end); }
   // does some row of the tile not see some key of key tile j?
   __device__ __forceinline__ bool edge(const Span& s, int j) const {
     const int k0 = key0(j);
-    return k0 + kTile - 1 > s.pos0 || (window > 0 && s.pos1 - k0 >= window && k0 + kTile > sinks);
+    return k0 + kKeys - 1 > s.pos0 || (window > 0 && s.pos1 - k0 >= window && k0 + kKeys > sinks);
   }
-  // a tile of which only the sinks are visible, and few: its products take kNarrow keys
-  __device__ __forceinline__ bool narrow(int j) const { return j < sink_tiles && sinks - j * kTile <= kNarrow; }
 };
 // two_heads: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
 __device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
   Job w;
-  const int units = two_heads ? a.heads / 2 : a.heads, per = two_heads ? kTile : 2 * kTile;
+  const int units = two_heads ? a.heads / 2 : a.heads, per = two_heads ? kRows : 2 * kRows;
   const int blocks = (int)((a.seq_q + per - 1) / per);
   const int u = blockIdx.x % units, rest = blockIdx.x / units, b = rest % a.batch, blk = blocks - 1 - rest / a.batch;
   w.r = seq_rows(a, b);
@@ -260,8 +250,8 @@ __device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
   for (int t = 0; t < 2; ++t) {
     Span& s = w.tile[t];
     s.head = two_heads ? 2 * u + t : u;
-    s.row0 = blk * per + (two_heads ? 0 : t * kTile);
-    s.rows = min(max(w.r.nq - s.row0, 0), kTile);
+    s.row0 = blk * per + (two_heads ? 0 : t * kRows);
+    s.rows = min(max(w.r.nq - s.row0, 0), kRows);
     s.pos0 = w.r.nk - w.r.nq + s.row0;
     s.pos1 = s.pos0 + s.rows - 1;
     if (s.rows > 0 && s.pos1 >= 0) {
@@ -270,32 +260,41 @@ __device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
     }
   }
   if (hi == 0) lo = 0;
-  w.first = lo / kTile;
-  w.sink_tiles = min((min(a.sinks, lo) + kTile - 1) / kTile, w.first);
-  w.count = hi == 0 ? 0 : w.sink_tiles + (hi + kTile - 1) / kTile - w.first;
+  w.first = lo / kKeys;
+  w.sink_tiles = min((min(a.sinks, lo) + kKeys - 1) / kKeys, w.first);
+  w.count = hi == 0 ? 0 : w.sink_tiles + (hi + kKeys - 1) / kKeys - w.first;
+  w.sink_end = w.sink_tiles + max(0, (min(a.sinks, hi) + kKeys - 1) / kKeys - w.first);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    Span& s = w.tile[t];
+    const bool sees = s.rows > 0 && s.pos1 >= 0;
+    s.from = sees ? w.sink_tiles + (a.window > 0 ? max(0, s.pos0 - a.window + 1) : 0) / kKeys - w.first : 0;
+    s.to = sees ? w.sink_tiles + s.pos1 / kKeys - w.first : -1;
+  }
   return w;
 }
 
-// The softmax of one tile's scores, by the four warps that own its rows: a thread holds a row.
+// The softmax of one query tile, by the four warps that own its rows: a thread holds a row.
 template <typename T, int kDim> struct Softmax {
-  uint32_t ts, to;                               // tensor memory of S (then P) and of O, at this warp's lanes
+  uint32_t to;                                   // tensor memory of O at this warp's lanes
   float sl;                                      // scale in units of log2
   float m, l;                                    // running maximum (raw score) and sum
 
-  // kCols columns; kMask: places from `last` on, and before `from` unless before `sink`, are not seen.  False: a wait ran out.
-  template <int kCols, bool kMask, typename Wait>
-  __device__ __forceinline__ bool step(int last, int from, int sink, Wait o_ready) {
-    float s[kCols];
+  // The scores at ts, one key tile; P replaces them.  kMask: places from `last` on, and before `from` unless before `sink`,
+  // are not seen.  False: a wait ran out.
+  template <bool kMask, typename Wait>
+  __device__ __forceinline__ bool step(uint32_t ts, int last, int from, int sink, Wait o_ready) {
+    float s[kKeys];
 #pragma unroll
-    for (int c = 0; c < kCols; c += 32) ld32(ts + c, s + c);
+    for (int c = 0; c < kKeys; c += 32) ld32(ts + c, s + c);
     ld_wait();
     if (kMask) {
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
+      for (int c = 0; c < kKeys; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
     }
     float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]), mx2 = s[6], mx3 = s[7];
 #pragma unroll
-    for (int c = 8; c < kCols; c += 8) {
+    for (int c = 8; c < kKeys; c += 8) {
       mx0 = max3(mx0, s[c], s[c + 1]); mx1 = max3(mx1, s[c + 2], s[c + 3]);
       mx2 = max3(mx2, s[c + 4], s[c + 5]); mx3 = max3(mx3, s[c + 6], s[c + 7]);
     }
@@ -319,20 +318,17 @@ template <typename T, int kDim> struct Softmax {
     const float shift = m == -INFINITY ? 0.f : kLiftLog2 - m * sl;
     const f32x2 sl2 = pair(sl, sl), shift2 = pair(shift, shift);
     f32x2 l0 = pair(0.f, 0.f), l1 = l0;
+    uint32_t p[kKeys / 2];
 #pragma unroll
-    for (int c = 0; c < kCols; c += 32) {
-      uint32_t p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const f32x2 x = fma2(pair(s[c + 2 * i], s[c + 2 * i + 1]), sl2, shift2);
-        float2 v;
-        if (!kMask && i % 4 >= 4 - kPolyOf4) v = ex2_poly(x);
-        else { v = halves(x); v.x = ex2(v.x); v.y = ex2(v.y); }
-        if (i & 1) l1 = add2(l1, pair(v.x, v.y)); else l0 = add2(l0, pair(v.x, v.y));
-        p[i] = pack2<T>(v.x, v.y);
-      }
-      st16(ts + c / 2, p);
+    for (int i = 0; i < kKeys / 2; ++i) {
+      const f32x2 x = fma2(pair(s[2 * i], s[2 * i + 1]), sl2, shift2);
+      float2 v;
+      if (!kMask && i % 4 >= 4 - kPolyOf4) v = ex2_poly(x);
+      else { v = halves(x); v.x = ex2(v.x); v.y = ex2(v.y); }
+      if (i & 1) l1 = add2(l1, pair(v.x, v.y)); else l0 = add2(l0, pair(v.x, v.y));
+      p[i] = pack2<T>(v.x, v.y);
     }
+    st32(ts, p);
     const float2 sum = halves(add2(l0, l1));
     l += sum.x + sum.y;
     st_wait();
@@ -344,12 +340,12 @@ template <typename T, int kDim>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v, WindowArgs a, int two_heads, uint32_t polls) {
-  constexpr int kSub = kTile * 128;              // bytes of a sub-tile: 128 rows of 64 values
-  constexpr int kSubs = kDim / 64, kTileBytes = kSubs * kSub;
+  constexpr int kSubs = kDim / 64;               // a tile is kSubs sub-tiles of 64 values per row (128 bytes)
+  constexpr int kQSub = kRows * 128, kQBytes = kSubs * kQSub, kSub = kKeys * 128, kTileBytes = kSubs * kSub;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* sq = smem;                      // two query tiles, then the ring
-  unsigned char* ring = smem + 2 * kTileBytes;
+  unsigned char* ring = smem + 2 * kQBytes;
   Ctl* ctl = reinterpret_cast<Ctl*>(ring + kSlots * kTileBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -357,15 +353,17 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&ctl->q_full[t]), 1);
-      mbar_init(smem_u32(&ctl->s_full[t]), 1);
-      mbar_init(smem_u32(&ctl->p_ready[t]), 4);
-      mbar_init(smem_u32(&ctl->o_done[t]), 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&ctl->s_full[t][i]), 1);
+        mbar_init(smem_u32(&ctl->p_ready[t][i]), 4);
+        mbar_init(smem_u32(&ctl->o_done[t][i]), 1);
+      }
+      mbar_init(smem_u32(&ctl->drain[t]), 1);
     }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&ctl->kv_full[s]), 1);
-      mbar_init(smem_u32(&ctl->kv_empty[s]), 1);
+      mbar_init(smem_u32(&ctl->kv_empty[s]), 2);       // both tiles
     }
-    mbar_init(smem_u32(&ctl->drain), 1);
     ctl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -377,20 +375,19 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;          // S0 S1 (128 columns each), O0 O1
+  const uint32_t tmem = ctl->tmem_base;          // two places for S of tile 0, of tile 1 (64 columns each), O of tile 0, of tile 1
   pdl_wait();
   const Job job = make_job(a, two_heads != 0);
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 9 && lane == 0 && job.count > 0) {             // ---- copies
       int issued = 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (job.tile[t].rows == 0) continue;
-        mbar_arrive_expect_tx(smem_u32(&ctl->q_full[t]), kTileBytes);
+        mbar_arrive_expect_tx(smem_u32(&ctl->q_full[t]), kQBytes);
         for (int s = 0; s < kSubs; ++s)
-          tma_load_2d(smem_u32(sq + t * kTileBytes + s * kSub), &map_q, job.tile[t].head * kDim + 64 * s, job.r.q0 + job.tile[t].row0,
+          tma_load_2d(smem_u32(sq + t * kQBytes + s * kQSub), &map_q, job.tile[t].head * kDim + 64 * s, job.r.q0 + job.tile[t].row0,
                       smem_u32(&ctl->q_full[t]));
       }
       const int hk = job.tile[0].head / (a.heads / a.kv_heads);
@@ -409,84 +406,85 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       for (int t = 0; t < 2; ++t)
         if (job.tile[t].rows > 0) wait_for(&ctl->q_full[t], 0, &gave_up, kSpinLimit);
       for (int e = max(0, issued - kSlots); e < issued; ++e) wait_for(&ctl->kv_full[e % kSlots], (e / kSlots) & 1, &gave_up, kSpinLimit);
-    } else if (warp == 8 && job.count > 0) {                   // ---- products (the whole warp; one lane issues)
-      constexpr uint32_t kIdS = idesc<T>(kTile, false), kIdSn = idesc<T>(kNarrow, false), kIdO = idesc<T>(kDim, true);
-      const uint32_t on = elect(), q_at = smem_u32(sq), ring_at = smem_u32(ring);
-      int pv[2] = {0, 0}, sc[2] = {0, 0};
-      auto half = [&](auto which, int j, uint32_t k_at, uint32_t v_at) -> bool {   // tile `which`: PV of key tile j - 1, S of key tile j
-        constexpr int t = decltype(which)::value;
-        const Span& span = job.tile[t];
-        const uint32_t ts = tmem + t * kTile, to = tmem + 2 * kTile + t * kTile;
-        if (j > 0 && job.active(span, j - 1)) {
-          if (!__all_sync(0xFFFFFFFFu, wait_for(&ctl->p_ready[t], pv[t] & 1, abort_flag, polls))) return false;
-          tc_fence_after();
-          const uint64_t dv = desc_mn(v_at);
-          const int steps = job.narrow(j - 1) ? kNarrow / 16 : kTile / 16;
-          const uint32_t more = pv[t] > 0;
+    } else if ((warp == 8 || warp == 10) && job.count > 0) {   // ---- products of tile 0, of tile 1 (the whole warp; one lane issues)
+      constexpr uint32_t kIdS = idesc<T>(kKeys, false), kIdO = idesc<T>(kDim, true);
+      const int t = (warp - 8) >> 1;
+      const Span span = t ? job.tile[1] : job.tile[0];
+      const uint32_t on = elect(), ring_at = smem_u32(ring), ts = tmem + t * 2 * kKeys, to = tmem + 4 * kKeys + t * 128;
+      const uint64_t dq = smem_desc_sw128(smem_u32(sq + t * kQBytes));
+      auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_for(bar, parity, abort_flag, polls)); };
+      int n = 0, v_before = 0;                                 // key tiles taken; ring entry of the last one's values
+      auto pv = [&](int i, int ev) -> bool {                   // O += P(i) V of ring entry ev
+        const int slot = ev % kSlots;
+        if (!wait(&ctl->kv_full[slot], (ev / kSlots) & 1)) return false;
+        if (!wait(&ctl->p_ready[t][i & 1], (i >> 1) & 1)) return false;
+        tc_fence_after();
+        const uint64_t dv = desc_mn(ring_at + slot * kTileBytes);
+        const uint32_t tp = ts + (i & 1) * kKeys, more = i > 0;
 #pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)                 // 16 keys: 8 columns of P, 2048 bytes of V
-            if (k < steps) mma_ts(on, to, ts + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, k > 0 ? 1u : more);
-          commit(on, &ctl->o_done[t]);
-          ++pv[t];
-        }
-        if (j < job.count && job.active(span, j)) {
-          if (sc[t] == 0 && !__all_sync(0xFFFFFFFFu, wait_for(&ctl->q_full[t], 0, abort_flag, polls))) return false;
-          const uint64_t dq = smem_desc_sw128(q_at + t * kTileBytes), dk = smem_desc_sw128(k_at);
-          const uint32_t id = job.narrow(j) ? kIdSn : kIdS;
-#pragma unroll
-          for (int k = 0; k < kDim / 16; ++k) {                // 16 values: 32 bytes within a sub-tile's rows
-            const uint64_t off = (uint64_t)(((k / 4) * kSub + (k % 4) * 32) >> 4);
-            mma_ss(on, ts, dq + off, dk + off, id, k > 0);
-          }
-          commit(on, &ctl->s_full[t]);
-          ++sc[t];
-        }
+        for (int k = 0; k < kKeys / 16; ++k)                   // 16 keys: 8 columns of P, 2048 bytes of V
+          mma_ts(on, to, tp + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, k > 0 ? 1u : more);
+        commit(on, &ctl->o_done[t][i & 1]);
+        commit(on, &ctl->kv_empty[slot]);
         return true;
       };
-      for (int j = 0; j <= job.count; ++j) {
-        const int ek = 2 * j, ev = 2 * j - 1;
-        bool ok = true;
-        if (j < job.count) ok = wait_for(&ctl->kv_full[ek % kSlots], (ek / kSlots) & 1, abort_flag, polls);
-        if (j > 0) ok = ok && wait_for(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1, abort_flag, polls);
-        if (!__all_sync(0xFFFFFFFFu, ok)) break;
-        const uint32_t k_at = ring_at + (ek % kSlots) * kTileBytes, v_at = ring_at + ((ev + kSlots) % kSlots) * kTileBytes;
-        if (!half(std::integral_constant<int, 0>{}, j, k_at, v_at)) break;
-        if (!half(std::integral_constant<int, 1>{}, j, k_at, v_at)) break;
-        if (j > 0) commit(on, &ctl->kv_empty[ev % kSlots]);
-        if (j < job.count) commit(on, &ctl->kv_empty[ek % kSlots]);
+      bool ok = span.to < 0 || wait(&ctl->q_full[t], 0);
+      for (int j = 0; j < job.count && ok; ++j) {
+        const int ek = 2 * j, ev = ek + 1, slot = ek % kSlots;
+        if (!job.active(span, j)) {                            // only the other tile takes it
+          ok = wait(&ctl->kv_full[slot], (ek / kSlots) & 1) && wait(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1);
+          if (ok && lane == 0) { mbar_arrive(smem_u32(&ctl->kv_empty[slot])); mbar_arrive(smem_u32(&ctl->kv_empty[ev % kSlots])); }
+          continue;
+        }
+        if (!(ok = wait(&ctl->kv_full[slot], (ek / kSlots) & 1))) break;
+        const uint64_t dk = smem_desc_sw128(ring_at + slot * kTileBytes);
+#pragma unroll
+        for (int k = 0; k < kDim / 16; ++k)                    // 16 values: 32 bytes within a sub-tile's rows
+          mma_ss(on, ts + (n & 1) * kKeys, dq + (uint64_t)(((k / 4) * kQSub + (k % 4) * 32) >> 4),
+                 dk + (uint64_t)(((k / 4) * kSub + (k % 4) * 32) >> 4), kIdS, k > 0);
+        commit(on, &ctl->s_full[t][n & 1]);
+        commit(on, &ctl->kv_empty[slot]);
+        if (n > 0) ok = pv(n - 1, v_before);
+        v_before = ev;
+        ++n;
       }
+      if (ok && n > 0) pv(n - 1, v_before);
       int gave_up = 0;                                         // products, and the arrivals they owe, end before the CTA does
-      commit(on, &ctl->drain);
-      wait_for(&ctl->drain, 0, &gave_up, kSpinLimit);
+      commit(on, &ctl->drain[t]);
+      wait_for(&ctl->drain[t], 0, &gave_up, kSpinLimit);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int t = warp >> 2, row = threadIdx.x & 127;          // the tile, and this thread's row of it
     const Span span = t ? job.tile[1] : job.tile[0];
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + 2 * kTile + t * kTile + lanes;
-    Softmax<T, kDim> sm{tmem + t * kTile + lanes, to, a.scale * 1.4426950408889634f, -INFINITY, 0.f};
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * 2 * kKeys + lanes, to = tmem + 4 * kKeys + t * 128 + lanes;
+    Softmax<T, kDim> sm{to, a.scale * 1.4426950408889634f, -INFINITY, 0.f};
     const int pos = span.pos0 + row;
     int n = 0;
     bool ok = true;
+    // PV(n - 1) is complete.  Two barriers in turn: PV(n - 3), the one before on the same barrier, is complete for certain
+    // (S(n - 1) was issued behind it), PV(n - 2) is not.
     auto o_ready = [&]() -> bool {
-      const bool r = __all_sync(0xFFFFFFFFu, wait_for(&ctl->o_done[t], (n - 1) & 1, abort_flag, polls));
+      const bool r = __all_sync(0xFFFFFFFFu, wait_for(&ctl->o_done[t][(n - 1) & 1], ((n - 1) >> 1) & 1, abort_flag, polls));
       tc_fence_after();
       return r;
     };
     for (int j = 0; j < job.count; ++j) {
       if (!job.active(span, j)) continue;
-      ok = __all_sync(0xFFFFFFFFu, wait_for(&ctl->s_full[t], n & 1, abort_flag, polls));
+      ok = __all_sync(0xFFFFFFFFu, wait_for(&ctl->s_full[t][n & 1], (n >> 1) & 1, abort_flag, polls));
       if (!ok) break;
       tc_fence_after();
-      const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
-      const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
-      if (job.narrow(j)) ok = sm.template step<kNarrow, true>(last, from, sink, o_ready);
-      else if (job.edge(span, j)) ok = sm.template step<kTile, true>(last, from, sink, o_ready);
-      else ok = sm.template step<kTile, false>(last, from, sink, o_ready);
+      const uint32_t at = ts + (n & 1) * kKeys;
+      if (job.edge(span, j)) {
+        const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
+        const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
+        ok = sm.template step<true>(at, last, from, sink, o_ready);
+      } else {
+        ok = sm.template step<false>(at, 0, 0, 0, o_ready);
+      }
       if (!ok) break;
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t]));
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t][n & 1]));
       ++n;
     }
     const float l = sm.l;
@@ -537,12 +535,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   }
 }
 
-// Tensor map of a token matrix [rows, width]: boxes of 128 rows x 64 values, rows beyond the end read as zero.
-template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t width, int64_t ld) {
+// Tensor map of a token matrix [rows, width]: boxes of box_rows x 64 values, rows beyond the end read as zero.
+template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t width, int64_t ld, int box_rows) {
   EncodeFn enc = encode_fn();
   if (!enc) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t box[2] = {64, kTile}, estr[2] = {1, 1};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   return enc(map, std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
              const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -550,7 +548,7 @@ template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t row
 
 template <typename T, int kDim>
 cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
-  constexpr size_t kSmem = (size_t)(2 + kSlots) * kTile * kDim * 2 + 1024 + sizeof(Ctl);
+  constexpr size_t kSmem = (size_t)(2 * kRows + kSlots * kKeys) * kDim * 2 + 1024 + sizeof(Ctl);
   static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
   static std::atomic<uint64_t> ready{0};         // devices on which the kernel's shared memory limit is set
   int dev = 0;
@@ -562,16 +560,16 @@ cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   CUtensorMap mq, mk, mv;
-  if (!make_map<T>(&mq, a.q, a.rows_q, (int64_t)a.heads * kDim, a.ld_q)) return cudaErrorInvalidValue;
+  if (!make_map<T>(&mq, a.q, a.rows_q, (int64_t)a.heads * kDim, a.ld_q, kRows)) return cudaErrorInvalidValue;
   if (a.rows_k > 0) {
-    if (!make_map<T>(&mk, a.k, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_k) ||
-        !make_map<T>(&mv, a.v, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_v))
+    if (!make_map<T>(&mk, a.k, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_k, kKeys) ||
+        !make_map<T>(&mv, a.v, a.rows_k, (int64_t)a.kv_heads * kDim, a.ld_v, kKeys))
       return cudaErrorInvalidValue;
   } else {
     mk = mv = mq;                                // no key anywhere: never used
   }
   const bool two_heads = (a.heads / a.kv_heads) % 2 == 0;
-  const int64_t per = two_heads ? kTile : 2 * kTile;
+  const int64_t per = two_heads ? kRows : 2 * kRows;
   const int64_t grid = (a.seq_q + per - 1) / per * a.batch * (two_heads ? a.heads / 2 : a.heads);
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
   const uint32_t polls = dbg < 0 ? kSpinLimit : (uint32_t)(dbg < (long long)kSpinLimit ? dbg : kSpinLimit);
