@@ -86,7 +86,6 @@ constexpr int kRows = 128;                       // query rows per tile
 constexpr int kKeys = 64;                        // keys per tile
 constexpr int kSlots = 8;                        // key or value tiles in shared memory
 constexpr int kThreads = 384;
-constexpr int kPolyOf4 = 0;                      // of four pairs of exponentials, those formed by ex2_poly
 constexpr float kMoveLog2 = 8.f;                 // growth of a row's maximum that is let pass
 constexpr float kLiftLog2 = 7.f;                 // probabilities are formed 2^7 times their size
 
@@ -111,6 +110,12 @@ __device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parit
   }
   *abort_flag = 1;
   return false;
+}
+
+// The same by a whole warp, with one answer for all of it.
+__device__ __forceinline__ bool wait_warp(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
+  if (polls && __all_sync(0xFFFFFFFFu, mbar_try_wait(smem_u32(bar), parity))) return true;
+  return __all_sync(0xFFFFFFFFu, wait_for(bar, parity, abort_flag, polls));
 }
 
 // kind::f16 instruction descriptor: fp32 sums, fp16 or bf16 operands, M = 128.
@@ -163,7 +168,15 @@ __device__ __forceinline__ void ld32(uint32_t taddr, float* r) {
         "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(taddr));
 }
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads above; r, what one of them loaded, is an operand so that no use of it moves ahead of the wait.
+__device__ __forceinline__ void ld_wait(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]),
+                 "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]), "+f"(r[17]), "+f"(r[18]),
+                 "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]),
+                 "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
+               :: "memory");
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <typename R> __device__ __forceinline__ void st32(uint32_t taddr, const R* r) {
   static_assert(sizeof(R) == 4, "32-bit columns");
@@ -184,24 +197,6 @@ __device__ __forceinline__ float2 halves(f32x2 r) { float2 v; asm("mov.b64 {%0, 
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-// 2^x of two numbers without the special-function unit, which the softmax would otherwise wait for: x = n + f with n whole and
-// |f| <= 1/2, 2^f by its minimax polynomial of degree 4 (relative error 2.6e-6, found by exchange on [-1/2, 1/2]), n added
-// to the exponent.  x below -126 counts as -126; a NaN comes out as a huge number or NaN.
-__device__ __forceinline__ float2 ex2_poly(f32x2 x2) {
-  const float2 x = halves(x2);
-  const f32x2 xc = pair(max_nan(x.x, -126.f), max_nan(x.y, -126.f));
-  const f32x2 t = add2(xc, pair(12582912.f, 12582912.f)), n = add2(t, pair(-12582912.f, -12582912.f));
-  const f32x2 f = fma2(n, pair(-1.f, -1.f), xc);
-  f32x2 p = pair(0.009570102207362652f, 0.009570102207362652f);
-  p = fma2(p, f, pair(0.05591785907745361f, 0.05591785907745361f));
-  p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
-  p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
-  p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
-  const float2 pv = halves(p), tv = halves(t);
-  return make_float2(__int_as_float(__float_as_int(pv.x) + (__float_as_int(tv.x) << 23)),
-                     __int_as_float(__float_as_int(pv.y) + (__float_as_int(tv.y) << 23)));
-}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -221,6 +216,7 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, f
 struct Span {                                    // a tile
   int head, row0, rows, pos0, pos1;              // head, first query row of the sequence, rows (0: none), their positions
   int from, to;                                  // key tiles of its window: from .. to (and those that hold sinks)
+  int clean_from, clean_to;                      // those that every row sees as a whole: clean_from .. clean_to - 1
 };
 struct Job {
   SeqRows r;
@@ -231,11 +227,8 @@ struct Job {
   __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kKeys; }
   // does a row of the tile see a key of key tile j?
   __device__ __forceinline__ bool active(const Span& s, int j) const { return j <= s.to && (j >= s.from || j < sink_end); }
-  // does some row of the tile not see some key of key tile j?
-  __device__ __forceinline__ bool edge(const Span& s, int j) const {
-    const int k0 = key0(j);
-    return k0 + kKeys - 1 > s.pos0 || (window > 0 && s.pos1 - k0 >= window && k0 + kKeys > sinks);
-  }
+  // does every row of the tile see every key of key tile j?  (Tiles of nothing but sinks are not counted in.)
+  __device__ __forceinline__ bool clean(const Span& s, int j) const { return j >= s.clean_from && j < s.clean_to; }
 };
 // two_heads: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
 __device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
@@ -270,71 +263,40 @@ __device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
     const bool sees = s.rows > 0 && s.pos1 >= 0;
     s.from = sees ? w.sink_tiles + (a.window > 0 ? max(0, s.pos0 - a.window + 1) : 0) / kKeys - w.first : 0;
     s.to = sees ? w.sink_tiles + s.pos1 / kKeys - w.first : -1;
+    s.clean_from = w.sink_tiles + max((a.window > 0 ? max(0, s.pos1 - a.window + kKeys) : 0) / kKeys - w.first, 0);
+    s.clean_to = w.sink_tiles + (s.pos0 >= 0 ? (s.pos0 + 1) / kKeys - w.first : 0);
   }
   return w;
 }
 
-// The softmax of one query tile, by the four warps that own its rows: a thread holds a row.
-template <typename T, int kDim> struct Softmax {
-  uint32_t to;                                   // tensor memory of O at this warp's lanes
-  float sl;                                      // scale in units of log2
-  float m, l;                                    // running maximum (raw score) and sum
-
-  // The scores at ts, one key tile; P replaces them.  kMask: places from `last` on, and before `from` unless before `sink`,
-  // are not seen.  False: a wait ran out.
-  template <bool kMask, typename Wait>
-  __device__ __forceinline__ bool step(uint32_t ts, int last, int from, int sink, Wait o_ready) {
-    float s[kKeys];
+// Largest of kKeys scores; those that are not seen (column > last, or before `from` and not before `sink`) become -infinity.
+__device__ __forceinline__ void mask_scores(float (&s)[kKeys], int last, int from, int sink) {
 #pragma unroll
-    for (int c = 0; c < kKeys; c += 32) ld32(ts + c, s + c);
-    ld_wait();
-    if (kMask) {
+  for (int c = 0; c < kKeys; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
+}
+__device__ __forceinline__ float largest(const float (&s)[kKeys]) {
+  float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]), mx2 = s[6], mx3 = s[7];
 #pragma unroll
-      for (int c = 0; c < kKeys; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
-    }
-    float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]), mx2 = s[6], mx3 = s[7];
-#pragma unroll
-    for (int c = 8; c < kKeys; c += 8) {
-      mx0 = max3(mx0, s[c], s[c + 1]); mx1 = max3(mx1, s[c + 2], s[c + 3]);
-      mx2 = max3(mx2, s[c + 4], s[c + 5]); mx3 = max3(mx3, s[c + 6], s[c + 7]);
-    }
-    const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
-    const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
-    if (__any_sync(0xFFFFFFFFu, move)) {         // O of the tiles so far takes the new maximum
-      if (!o_ready()) return false;
-      const float f = move ? ex2((m - mx) * sl) : 1.f;
-      l *= f;
-#pragma unroll
-      for (int c = 0; c < kDim; c += 32) {
-        float o[32];
-        ld32(to + c, o);
-        ld_wait();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] *= f;
-        st32(to + c, o);
-      }
-    }
-    if (move || m == -INFINITY) m = fmaxf(m, mx);
-    const float shift = m == -INFINITY ? 0.f : kLiftLog2 - m * sl;
-    const f32x2 sl2 = pair(sl, sl), shift2 = pair(shift, shift);
-    f32x2 l0 = pair(0.f, 0.f), l1 = l0;
-    uint32_t p[kKeys / 2];
-#pragma unroll
-    for (int i = 0; i < kKeys / 2; ++i) {
-      const f32x2 x = fma2(pair(s[2 * i], s[2 * i + 1]), sl2, shift2);
-      float2 v;
-      if (!kMask && i % 4 >= 4 - kPolyOf4) v = ex2_poly(x);
-      else { v = halves(x); v.x = ex2(v.x); v.y = ex2(v.y); }
-      if (i & 1) l1 = add2(l1, pair(v.x, v.y)); else l0 = add2(l0, pair(v.x, v.y));
-      p[i] = pack2<T>(v.x, v.y);
-    }
-    st32(ts, p);
-    const float2 sum = halves(add2(l0, l1));
-    l += sum.x + sum.y;
-    st_wait();
-    return true;
+  for (int c = 8; c < kKeys; c += 8) {
+    mx0 = max3(mx0, s[c], s[c + 1]); mx1 = max3(mx1, s[c + 2], s[c + 3]);
+    mx2 = max3(mx2, s[c + 4], s[c + 5]); mx3 = max3(mx3, s[c + 6], s[c + 7]);
   }
-};
+  return fmaxf(max3(mx0, mx1, mx2), mx3);
+}
+// Exponentials of the scores, rounded into p, and summed.
+template <typename T>
+__device__ __forceinline__ f32x2 exponentials(const float (&s)[kKeys], float sl, float shift, uint32_t (&p)[kKeys / 2]) {
+  const f32x2 sl2 = pair(sl, sl), shift2 = pair(shift, shift);
+  f32x2 l0 = pair(0.f, 0.f), l1 = l0;
+#pragma unroll
+  for (int i = 0; i < kKeys / 2; ++i) {
+    float2 v = halves(fma2(pair(s[2 * i], s[2 * i + 1]), sl2, shift2));
+    v.x = ex2(v.x); v.y = ex2(v.y);
+    if (i & 1) l1 = add2(l1, pair(v.x, v.y)); else l0 = add2(l0, pair(v.x, v.y));
+    p[i] = pack2<T>(v.x, v.y);
+  }
+  return add2(l0, l1);
+}
 
 template <typename T, int kDim>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -412,7 +374,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       const Span span = t ? job.tile[1] : job.tile[0];
       const uint32_t on = elect(), ring_at = smem_u32(ring), ts = tmem + t * 2 * kKeys, to = tmem + 4 * kKeys + t * 128;
       const uint64_t dq = smem_desc_sw128(smem_u32(sq + t * kQBytes));
-      auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_for(bar, parity, abort_flag, polls)); };
+      auto wait = [&](unsigned long long* bar, uint32_t parity) { return wait_warp(bar, parity, abort_flag, polls); };
       int n = 0, v_before = 0;                                 // key tiles taken; ring entry of the last one's values
       auto pv = [&](int i, int ev) -> bool {                   // O += P(i) V of ring entry ev
         const int slot = ev % kSlots;
@@ -457,37 +419,58 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     const int t = warp >> 2, row = threadIdx.x & 127;          // the tile, and this thread's row of it
     const Span span = t ? job.tile[1] : job.tile[0];
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * 2 * kKeys + lanes, to = tmem + 4 * kKeys + t * 128 + lanes;
-    Softmax<T, kDim> sm{to, a.scale * 1.4426950408889634f, -INFINITY, 0.f};
-    const int pos = span.pos0 + row;
-    int n = 0;
+    const float sl = a.scale * 1.4426950408889634f;
+    const int pos = span.pos0 + row, key_end = min(pos, job.r.nk - 1);
+    float m = -INFINITY, l = 0.f;                              // running maximum (raw score) and sum of the row
+    int n = 0;                                                 // key tiles taken
     bool ok = true;
     // PV(n - 1) is complete.  Two barriers in turn: PV(n - 3), the one before on the same barrier, is complete for certain
     // (S(n - 1) was issued behind it), PV(n - 2) is not.
     auto o_ready = [&]() -> bool {
-      const bool r = __all_sync(0xFFFFFFFFu, wait_for(&ctl->o_done[t][(n - 1) & 1], ((n - 1) >> 1) & 1, abort_flag, polls));
+      const bool r = wait_warp(&ctl->o_done[t][(n - 1) & 1], ((n - 1) >> 1) & 1, abort_flag, polls);
       tc_fence_after();
       return r;
     };
     for (int j = 0; j < job.count; ++j) {
       if (!job.active(span, j)) continue;
-      ok = __all_sync(0xFFFFFFFFu, wait_for(&ctl->s_full[t][n & 1], (n >> 1) & 1, abort_flag, polls));
-      if (!ok) break;
-      tc_fence_after();
+      const bool clean = job.clean(span, j);
+      const int k0 = job.key0(j);
       const uint32_t at = ts + (n & 1) * kKeys;
-      if (job.edge(span, j)) {
-        const int k0 = job.key0(j), last = min(pos, job.r.nk - 1) - k0;
-        const int from = a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, sink = a.sinks - k0;
-        ok = sm.template step<true>(at, last, from, sink, o_ready);
-      } else {
-        ok = sm.template step<false>(at, 0, 0, 0, o_ready);
+      if (!(ok = wait_warp(&ctl->s_full[t][n & 1], (n >> 1) & 1, abort_flag, polls))) break;
+      tc_fence_after();
+      float s[kKeys];
+      ld32(at, s);
+      ld32(at + 32, s + 32);
+      ld_wait(s);
+      ld_wait(s + 32);
+      if (!clean) mask_scores(s, key_end - k0, a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, a.sinks - k0);
+      const float mx = largest(s);
+      const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
+      if (__any_sync(0xFFFFFFFFu, move)) {                     // O of the tiles so far takes the new maximum
+        if (!(ok = o_ready())) break;
+        const float f = move ? ex2((m - mx) * sl) : 1.f;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < kDim; c += 32) {
+          float o[32];
+          ld32(to + c, o);
+          ld_wait(o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] *= f;
+          st32(to + c, o);
+        }
       }
-      if (!ok) break;
+      if (move || m == -INFINITY) m = fmaxf(m, mx);
+      uint32_t p[kKeys / 2];
+      const float2 sum = halves(exponentials<T>(s, sl, m == -INFINITY ? 0.f : kLiftLog2 - m * sl, p));
+      st32(at, p);
+      l += sum.x + sum.y;
+      st_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t][n & 1]));
       ++n;
     }
-    const float l = sm.l;
     // ---- output
     if (ok && n > 0) ok = o_ready();
     if (ok) {
@@ -500,7 +483,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         float v[32];
         if (n > 0) {
           ld32(to + c, v);
-          ld_wait();
+          ld_wait(v);
         }
         uint32_t w[16];
 #pragma unroll
