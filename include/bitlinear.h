@@ -456,7 +456,9 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
  * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined by a
  * second kernel in a fixed order (same inputs and sizes, same bits).  batch = 0 does nothing.
- * Workspace: bitlinear_attention_kv4_ws_bytes(); calls that may overlap need workspaces of their own. */
+ * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; its first word is the status word of
+ * bitlinear_ws_status: the kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means o of
+ * this call is not valid); calls that may overlap need workspaces of their own. */
 bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, int64_t ld_q, const bl_kv4_cache* cache,
                                   const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
                                   int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,
@@ -478,10 +480,10 @@ bl_status bitlinear_ws_status(const void* ws, void* stream);
 
 /* Test and diagnostic hook: caps the number of polls that the bounded device-side waits of
  * kernels launched afterwards by this process may make (bitlinear_gemv_decode's wait for its
- * weight copies; the waits of bitlinear_attention_window; the meeting between the two passes of the cooperative per-tensor kernel of
+ * weight copies; the waits of bitlinear_attention_window and bitlinear_attention_kv4; the meeting between the two passes of the cooperative per-tensor kernel of
  * bitlinear_quant_act).  polls < 0 restores the built-in limits; 0 means a single poll (for
  * bitlinear_gemv_decode and bitlinear_attention_window: none at all, weights are read from global
- * memory, rows are computed one by one).
+ * memory, rows are computed one by one; for bitlinear_attention_kv4: none, it reports the timeout).
  * meet_skew != 0 additionally makes the cooperative kernel wait for an arrival tag that no CTA
  * publishes, so that its wait runs out by construction: the kernel then records
  * BL_ERR_TIMEOUT in the status word, writes no codes and returns (nothing hangs, traps or

@@ -21,12 +21,14 @@
 //
 // Work.  The visible tokens of all sequences, in chunks of 64, times key/value heads (times blocks of query rows)
 // form one list that is cut into equal parts, one per warp: ragged batches and single long sequences balance
-// alike.  A warp runs on its own: its chunks stream into its part of shared memory by asynchronous copies, two
-// ahead, with no barrier between warps.  A warp that owns all chunks of a head writes the output; else its
+// alike.  A warp runs on its own: its chunks stream into its part of shared memory by bulk copies, two ahead (139 KB
+// in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is reported in
+// the workspace's status word.  A warp that owns all chunks of a head writes the output; else its
 // unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
 #include <type_traits>
 
 #include "kv4.cuh"
+#include "tc_common.cuh"
 
 namespace bl {
 
@@ -34,10 +36,11 @@ namespace {
 
 using namespace kv4;
 
-constexpr int kChunkLog2 = 6, kChunk = 1 << kChunkLog2;   // tokens per work item
+constexpr int kChunk = 64;                 // tokens per work item
 constexpr int kWarps = 8;                  // per CTA, one CTA per SM
 constexpr int kStages = 3;                 // chunks of a warp in shared memory
 constexpr int kMaxSms = 160;
+constexpr size_t kStatusBytes = 256;       // the status word lies at the start of the workspace
 constexpr int kJoinWarps = 8;
 
 struct Plan {                              // how the list is laid out; made on the host, the same for both kernels
@@ -140,24 +143,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-// A warp's copy of kBytes contiguous bytes.
-template <int kBytes> __device__ __forceinline__ void copy_block(uint32_t dst, const char* src) {
-  const int at = (threadIdx.x & 31) * 16;
-#pragma unroll
-  for (int u = 0; u < kBytes; u += 512)
-    if (u + 512 <= kBytes || u + at < kBytes) copy16(dst + u + at, src + u + at);
-}
-// A warp's copy of tokens j .. j + kRun - 1 out of a head's larger page of ps tokens.
-template <int kDim, int kRun> __device__ __forceinline__ void copy_part(uint32_t dst, const char* src, int ps, int j) {
-  copy_block<kRun * (kDim / 2)>(dst, src + j * (kDim / 2));
-  copy_block<kRun * (kDim / 2)>(dst + kRun * (kDim / 2), src + Block<kDim>::v_codes(ps) + j * (kDim / 2));
-  const int lane = threadIdx.x & 31, half = kRun / 4;   // 16-byte pieces of the keys' pairs, then of the values'
-  if (lane < 2 * half)
-    copy16(dst + kRun * kDim + lane * 16,
-           src + (lane < half ? Block<kDim>::k_scale(ps) + 4 * j + lane * 16 : Block<kDim>::v_scale(ps) + 4 * j + (lane - half) * 16));
+// kBytes contiguous bytes by the copy engine, counted on a barrier (both addresses and the size are multiples of 16).
+__device__ __forceinline__ void copy_bulk(uint32_t dst, const void* src, int bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -219,7 +208,7 @@ struct __align__(16) Item {
 };
 
 template <typename T, int kDim, int kNT>
-__global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a, Plan plan) {
+__global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a, Plan plan, uint32_t polls) {
   constexpr int kWords = kDim / 32;        // words of codes per lane and 8 tokens
   constexpr int kTiles = kChunk / 16;
   constexpr int kStageBytes = kChunk * (kDim + 8);
@@ -228,14 +217,19 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, qd = lane & 3;
   const int w = warp * gridDim.x + blockIdx.x;         // short lists spread over the SMs
-  // a stage holds runs of rl = min(page, chunk) tokens, each laid out as a page of that size would be
-  const int ps = a.cache.page_size, pl = plan.page_log2, rs = min(ps, kChunk), rl = min(pl, kChunkLog2);
-  const int block_bytes = Block<kDim>::bytes(ps), run_bytes = Block<kDim>::bytes(rs), subs = kChunk >> rl;
+  const int ps = a.cache.page_size, pl = plan.page_log2, block_bytes = Block<kDim>::bytes(ps), subs = kChunk >> pl;
   char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
   Item* items_of = reinterpret_cast<Item*>(smem + kWarps * kStages * kStageBytes) + warp * kStages;
+  const uint32_t bar_addr = (uint32_t)__cvta_generic_to_shared(smem + kWarps * kStages * (kStageBytes + sizeof(Item))) + warp * kStages * 8;
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) tc::mbar_init(bar_addr + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
 
   pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.ws) = 0;   // the status word
   const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
   const int64_t begin = cut.begin(w);
   const int items = (int)(cut.begin(w + 1) - begin);
@@ -254,8 +248,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   }
   auto page_of = [&](const Walk& x) -> int {           // lane i: the page of the chunk's i-th run of tokens; -1: nothing visible, or no page
     if (lane >= subs) return -1;
-    const int t = x.s.start(x.c) + lane * rs;
-    if (t >= x.s.len || (t + rs <= x.s.lo && t >= a.sinks)) return -1;
+    const int t = x.s.start(x.c) + lane * ps;
+    if (t >= x.s.len || (t + ps <= x.s.lo && t >= a.sinks)) return -1;
     const int id = a.table[(int64_t)x.b * a.max_pages + (t >> pl)];
     return id >= 0 && id < a.cache.num_pages ? id : -1;
   };
@@ -272,36 +266,31 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         x.rows0 = ahead.blk * plan.rows_per_block; x.there = there; x.first = ahead.c == 0; x.last = ahead.c + 1 == ahead.s.chunks;
         items_of[slot] = x;
       }
-      for (int i = 0; i < subs; ++i) {
-        const int id = __shfl_sync(0xFFFFFFFFu, ids, i);
-        if (id < 0) continue;
-        const char* src = reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)id * a.cache.kv_heads + ahead.hk) * block_bytes;
-        if (ps > kChunk) copy_part<kDim, kChunk>(dst, src, ps, ahead.s.start(ahead.c) & (ps - 1));
-        else if (rs == kChunk) copy_block<kChunk * (kDim + 8)>(dst, src);
-        else if (rs == 32) copy_block<32 * (kDim + 8)>(dst + i * run_bytes, src);
-        else copy_block<16 * (kDim + 8)>(dst + i * run_bytes, src);
-      }
+      if (lane == 0) tc::mbar_arrive_expect_tx(bar_addr + 8 * slot, __popc(there) * block_bytes);
+      __syncwarp();
+      if (ids >= 0)                                    // lane i copies the i-th page's block
+        copy_bulk(dst + lane * block_bytes, reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)ids * a.cache.kv_heads + ahead.hk) * block_bytes,
+                  block_bytes, bar_addr + 8 * slot);
       if (issued + 1 < items) {
         ahead.next(a, plan);
         ids = page_of(ahead);
       }
     }
     ++issued;
-    asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) issue();
 
   // where tile i (16 tokens) of a stage has its key codes and its key (step, eta) pairs; those of the values follow
-  // v_off and 4 rs bytes later
+  // v_off and 4 ps bytes later
   int code_at[kTiles], scale_at[kTiles];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
-    const int j0 = (i * 16) & (rs - 1), base = (i * 16 >> rl) * run_bytes;
+    const int j0 = (i * 16) & (ps - 1), base = (i * 16 >> pl) * block_bytes;
     code_at[i] = base + j0 * (kDim / 2) + lane * (kWords * 4);
-    scale_at[i] = base + Block<kDim>::k_scale(rs) + 4 * (j0 + g);
+    scale_at[i] = base + Block<kDim>::k_scale(ps) + 4 * (j0 + g);
   }
-  const int v_off = Block<kDim>::v_codes(rs);
+  const int v_off = Block<kDim>::v_codes(ps);
 
   // ---- state of the segment (one sequence, head and block of rows) being worked on
   uint32_t qf[kNT][kWords][4];                         // query operand: per word of codes the pairs (0,4), (1,5)/16, (2,6), (3,7)/16
@@ -403,8 +392,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
       const char* se = stage + scale_at[i];
       const float2 k0 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se));
       const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se + 32));
-      vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * rs);
-      vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * rs + 32);
+      vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * ps);
+      vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * ps + 32);
       uint32_t any = 0;
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
@@ -414,7 +403,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
           s[i][nt][e] = fmaf(s[i][nt][e] * f[nt][e & 1], kk.x, kk.y * qsum[nt][e & 1]);
           if (kMask) {
             const int t = it.t0 + i * 16 + g + (e >> 1) * 8, pos = pos_of[nt][e & 1];
-            const bool v = t <= pos && ((it.there >> (i * 16 >> rl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
+            const bool v = t <= pos && ((it.there >> (i * 16 >> pl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
             if (v) { seen |= 1u << ((i * kNT + nt) * 4 + e); any |= 1u << (e >> 1); }
             else s[i][nt][e] = -INFINITY;
           }
@@ -511,7 +500,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   auto end_segment = [&](const Item& it) {
     const bool whole = from_start && it.last;
     const float back = pow2i(min(max(vexp - 13, -126), 127));
-    float* slot = reinterpret_cast<float*>(a.ws) + (int64_t)(2 * w + later) * plan.rows_per_block * (kDim + 4);
+    float* slot = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kStatusBytes) + (int64_t)(2 * w + later) * plan.rows_per_block * (kDim + 4);
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -551,10 +540,29 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     later = true;
   };
 
+  // The copies of an item have come (and, all lanes being here, its predecessor's stage is free).  False: the wait ran out.
+  auto arrived = [&](int item, uint32_t limit) -> bool {
+    const uint32_t bar = bar_addr + 8 * (item % kStages), parity = (uint32_t)(item / kStages) & 1u;
+    if (limit && __all_sync(0xFFFFFFFFu, tc::mbar_try_wait(bar, parity))) return true;
+    bool ok = false;
+    unsigned long long t0 = 0;
+    for (uint32_t i = 0; i < limit && !ok; ++i) {
+      ok = tc::mbar_try_wait(bar, parity);
+      if ((i & 255u) == 255u) {
+        const unsigned long long now = tc::global_ns();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > tc::kWaitNs) break;
+      }
+    }
+    return __all_sync(0xFFFFFFFFu, ok);
+  };
   bool fresh = true;
   for (int item = 0; item < items; ++item) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncwarp();                                      // the chunk is there, and its predecessor's stage is free
+    if (!arrived(item, polls)) {                       // the copies did not come: reported, nothing more is done
+      if (lane == 0) *reinterpret_cast<volatile uint32_t*>(a.ws) = BL_ERR_TIMEOUT;
+      for (int i = item; i < min(issued, items); ++i) arrived(i, tc::kSpinLimit);   // those in flight end before the CTA does (bounded)
+      return;
+    }
     const Item it = items_of[item % kStages];
     issue();
     if (fresh) begin_segment(it);
@@ -592,7 +600,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4
   if (w0 == w1) return;                                // written already
   float m = -INFINITY, l = 0.f, v[kVals] = {};
   for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
-    const float* row = reinterpret_cast<const float*>(a.ws) + ((int64_t)(2 * w + (cut.begin(w) < first)) * plan.rows_per_block + rr) * (kDim + 4);
+    const float* row = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.ws) + kStatusBytes) + ((int64_t)(2 * w + (cut.begin(w) < first)) * plan.rows_per_block + rr) * (kDim + 4);
     const float2 ml = *reinterpret_cast<const float2*>(row + kDim);
     if (ml.x == -INFINITY) continue;                   // the part holds nothing that this row sees
     const float top = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : ex2(m - top), p = ex2(ml.x - top);
@@ -635,7 +643,7 @@ cudaError_t sm_count(int* n) {
 
 template <typename T, int kDim, int kNT>
 cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
-  constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item));
+  constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item) + 8);
   static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
   static std::atomic<uint64_t> ready{0};               // devices on which the kernel's shared memory limit is set
   int dev = 0, sms = 0;
@@ -648,7 +656,9 @@ cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
-  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan);
+  const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
+  const uint32_t polls = dbg < 0 ? tc::kSpinLimit : (uint32_t)(dbg < (long long)tc::kSpinLimit ? dbg : tc::kSpinLimit);
+  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
   if (e != cudaSuccess) return e;
   return launch_pdl(attention_kv4_join_kernel<T, kDim>, (unsigned)((int64_t)a.batch * plan.heads_blocks * plan.rows_per_block),
                     kJoinWarps * 32, 0, s, a, plan);
@@ -665,7 +675,7 @@ cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
 
 size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
   const Plan p = make_plan(n_q, heads, kv_heads, 16, 1);
-  return (size_t)kMaxSms * kWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float) * (batch > 0);
+  return batch == 0 ? 0 : kStatusBytes + (size_t)kMaxSms * kWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float);
 }
 
 cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s) {

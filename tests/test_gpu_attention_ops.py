@@ -309,6 +309,23 @@ def test_attention_kv4_in_a_graph_and_on_two_streams():
         assert all(torch.equal(a, b) for a, b in zip(outs, wants))
 
 
+def test_attention_kv4_reports_waits_that_run_out():
+    hk, dim, page, dt = 2, 128, 32, F16
+    cache, table = fill(2, [700, 300], page, hk, dim, dt, seed=3)
+    q, lens = randn(1, 2, 2 * hk * dim, dtype=dt), torch.tensor([700, 300], device=DEV).int()
+    ws = torch.empty(B.attention_kv4_ws_bytes(2, 1, 2 * hk, hk, dim), dtype=torch.uint8, device=DEV)
+    want = B.attention_kv4(q, cache, table, lens, 2, 1, 2 * hk, ws=ws)
+    assert B.ws_status(ws) == B.OK
+    B.debug_wait_limit(0)
+    try:
+        B.attention_kv4(q, cache, table, lens, 2, 1, 2 * hk, ws=ws)
+        assert B.ws_status(ws) == B.ERR_TIMEOUT
+    finally:
+        B.debug_wait_limit(-1)
+    assert torch.equal(B.attention_kv4(q, cache, table, lens, 2, 1, 2 * hk, ws=ws), want)
+    assert B.ws_status(ws) == B.OK
+
+
 def test_cache_beyond_32_bit_offsets():
     """A cache of 5 GB: the last pages lie beyond 2^32 bytes."""
     page, hk, dim, dt = 64, 8, 128, F16
