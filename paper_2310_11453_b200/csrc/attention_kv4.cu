@@ -21,10 +21,11 @@
 //
 // Work.  The visible tokens of all sequences, in chunks of 64, times key/value heads (times blocks of query rows)
 // form one list that is cut into equal parts, one per warp: ragged batches and single long sequences balance
-// alike.  A warp runs on its own: its chunks stream into its part of shared memory by bulk copies, two ahead (139 KB
-// in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is reported in
+// alike.  A warp runs on its own: its chunks stream into its part of shared memory by bulk copies, one or two ahead
+// (104 or 139 KB in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is reported in
 // the workspace's status word.  A warp that owns all chunks of a head writes the output; else its
 // unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
+#include <algorithm>
 #include <type_traits>
 
 #include "kv4.cuh"
@@ -37,8 +38,7 @@ namespace {
 using namespace kv4;
 
 constexpr int kChunk = 64;                 // tokens per work item
-constexpr int kWarps = 8;                  // per CTA, one CTA per SM
-constexpr int kStages = 3;                 // chunks of a warp in shared memory
+constexpr int kMostWarps = 12;             // per CTA, one CTA per SM
 constexpr int kMaxSms = 160;
 constexpr size_t kStatusBytes = 256;       // the status word lies at the start of the workspace
 constexpr int kJoinWarps = 8;
@@ -207,7 +207,8 @@ struct __align__(16) Item {
   int rows0, there, first, last;           // first query row; which runs of tokens are there (bit per page); first, last chunk of its list
 };
 
-template <typename T, int kDim, int kNT>
+// kNT: tiles of 8 query rows; kWarps per CTA, each with kStages chunks in shared memory.
+template <typename T, int kDim, int kNT, int kWarps, int kStages>
 __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a, Plan plan, uint32_t polls) {
   constexpr int kWords = kDim / 32;        // words of codes per lane and 8 tokens
   constexpr int kTiles = kChunk / 16;
@@ -641,7 +642,7 @@ cudaError_t sm_count(int* n) {
   return cudaSuccess;
 }
 
-template <typename T, int kDim, int kNT>
+template <typename T, int kDim, int kNT, int kWarps, int kStages>
 cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
   constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item) + 8);
   static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
@@ -651,31 +652,43 @@ cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((ready.load(std::memory_order_relaxed) >> dev) & 1)) {
-    e = cudaFuncSetAttribute(attention_kv4_kernel<T, kDim, kNT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    e = cudaFuncSetAttribute(attention_kv4_kernel<T, kDim, kNT, kWarps, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
   const uint32_t polls = dbg < 0 ? tc::kSpinLimit : (uint32_t)(dbg < (long long)tc::kSpinLimit ? dbg : tc::kSpinLimit);
-  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
+  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT, kWarps, kStages>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
   if (e != cudaSuccess) return e;
   return launch_pdl(attention_kv4_join_kernel<T, kDim>, (unsigned)((int64_t)a.batch * plan.heads_blocks * plan.rows_per_block),
                     kJoinWarps * 32, 0, s, a, plan);
 }
 
+// Up to 8 query rows: 12 warps with two chunks each keep the SM busier (32 x 8192 tokens, 8 heads, 4 rows: 45.4 us against
+// 49.3 with 8 warps and three chunks), but the next kernel finds no room beside them before they end, which costs a short
+// list 2 us (1000 tokens, 16 heads: 11.1 against 9.2), so lists of at most two chunks per warp take 8.  More rows: 8 warps, whose
+// 255 registers hold the second tile of rows (12: spills, 116 us against 83 for 2 x 150001 tokens).
+template <typename T, int kDim>
+cudaError_t launch_dim(const Kv4AttnArgs& a, cudaStream_t s) {
+  const int64_t rows = (int64_t)a.n_q * (a.heads / a.cache.kv_heads);
+  if (rows > 8) return launch_rows<T, kDim, 2, 8, 3>(a, s);
+  int64_t tokens = a.max_pages * a.cache.page_size;
+  if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + a.sinks + a.n_q + 2 * kChunk);
+  const bool few = (tokens + kChunk - 1) / kChunk * a.cache.kv_heads * a.batch <= 2 * 8 * 148;
+  return few ? launch_rows<T, kDim, 1, 8, 3>(a, s) : launch_rows<T, kDim, 1, 12, 2>(a, s);
+}
+
 template <typename T>
 cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
-  const bool few = (int64_t)a.n_q * (a.heads / a.cache.kv_heads) <= 8;
-  if (a.cache.head_dim == 64) return few ? launch_rows<T, 64, 1>(a, s) : launch_rows<T, 64, 2>(a, s);
-  return few ? launch_rows<T, 128, 1>(a, s) : launch_rows<T, 128, 2>(a, s);
+  return a.cache.head_dim == 64 ? launch_dim<T, 64>(a, s) : launch_dim<T, 128>(a, s);
 }
 
 }  // namespace
 
 size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
   const Plan p = make_plan(n_q, heads, kv_heads, 16, 1);
-  return batch == 0 ? 0 : kStatusBytes + (size_t)kMaxSms * kWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float);
+  return batch == 0 ? 0 : kStatusBytes + (size_t)kMaxSms * kMostWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float);
 }
 
 cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s) {
