@@ -318,6 +318,11 @@ def forward_latent(x, W, G=1, mode=ABSMAX, gran=PER_TOKEN, ln_eps=1e-5, eta_corr
     return dict(y=y, alpha=alpha, beta=beta, ws=ws)
 
 
+class _Kv4CacheStruct(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("num_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("dtype", C.c_int)]
+
+
 class _Epilogue(C.Structure):
     _fields_ = [("beta_rows", C.c_int64), ("relu", C.c_int), ("residual", C.c_void_p), ("ld_res", C.c_int64),
                 ("ld_y", C.c_int64)]
@@ -448,42 +453,26 @@ def block_forward(x, weights, batch, seq, heads, ffn, ln_eps=1e-5, ws=None, fuse
 
 
 # ---- attention at inference ----------------------------------------------------------------------
-# One decode step makes a handful of these calls per layer, a few microseconds of device time each, so the
-# wrappers are written to cost little themselves: one look at each tensor, plain integers to the C call.
-_stream_of = torch._C._cuda_getCurrentRawStream
-_device_now = torch._C._cuda_getDevice
+# One decode step makes a handful of these calls per layer, a few microseconds of device time each.  Looking at their
+# tensors, allocating what is not given and converting their arguments is compiled (csrc/marshal.cpp): 3 microseconds
+# instead of 10.  Tensors on another device or of another type or shape than stated are refused (ValueError, TypeError);
+# the kernels run on the tensors' device, on its current stream.
+_fast = None
 
 
-def _bad(name, t, index, dtype, what):
-    """Why a tensor argument is refused."""
-    if t.get_device() != index or index < 0:
-        raise ValueError(f"{name} is on {t.device}, expected a CUDA tensor on the device of the first argument")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
-    raise ValueError(f"{name} has shape {tuple(t.shape)} and strides {t.stride()}, expected {what}")
-
-
-def _rows(name, t, index, dtype, rows, width):
-    """Checks a token matrix [rows, width] whose rows are contiguous; returns its row stride."""
-    stride = t.stride()
-    if t.get_device() != index or index < 0 or t.dtype != dtype or t.shape != (rows, width) or stride[1] != 1:
-        _bad(name, t, index, dtype, f"({rows}, {width}) with the values of a row contiguous")
-    return stride[0] if rows > 1 else max(stride[0], width + -width % 8)
-
-
-def _index(name, t, index, dtype, shape):
-    """Checks a contiguous tensor of the given type and shape; returns its address."""
-    if t.get_device() != index or index < 0 or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        _bad(name, t, index, dtype, f"a contiguous {tuple(shape)}")
-    return t.data_ptr()
-
-
-def _launch(index, fn, *args):
-    """Calls a C entry point with device `index` current and its current stream as the last argument."""
-    if index == _device_now():
-        return fn(*args, _stream_of(index))
-    with torch.cuda.device(index):
-        return fn(*args, _stream_of(index))
+def _marshal():
+    global _fast
+    if _fast is None:
+        L = lib()
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise ImportError(f"_marshal.so is missing or does not load: run `python -m paper_2310_11453_b200.build` ({e})")
+        m.bind(*(C.cast(getattr(L, "bitlinear_" + n), C.c_void_p).value for n in
+                 ("qk_norm_rope", "attention_window", "kv4_page_bytes", "kv4_append", "kv4_read", "attention_kv4",
+                  "attention_kv4_ws_bytes", "kv4_copy_pages")))
+        _fast = m
+    return _fast
 
 
 def qk_norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq=None, wk=None, eps=1e-6, interleaved=False,
@@ -491,26 +480,10 @@ def qk_norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq=None, 
     """bitlinear_qk_norm_rope.  q [T, heads*head_dim], k [T, kv_heads*head_dim] (may be column blocks of one
     buffer); positions int32 [T] (negative: padding, left as it is); inv_freq f32 [rot_dim/2]; wq, wk
     [head_dim] or None; eps < 0 skips the norm.  Returns (q_out, k_out), which may be given (q, k for in place)."""
-    T, dt, dev, wide, narrow = q.shape[0], q.dtype, q.get_device(), heads * head_dim, kv_heads * head_dim
-    ld_q, ld_k = _rows("q", q, dev, dt, T, wide), _rows("k", k, dev, dt, T, narrow)
-    half = inv_freq.numel()
-    pos, freq = _index("positions", positions, dev, torch.int32, (T,)), _index("inv_freq", inv_freq, dev, torch.float32, (half,))
-    w1 = None if wq is None else _index("wq", wq, dev, dt, (head_dim,))
-    w2 = None if wk is None else _index("wk", wk, dev, dt, (head_dim,))
-    if q_out is None:
-        q_out, ld_qo = q.new_empty((T, wide)), wide
-    else:
-        ld_qo = _rows("q_out", q_out, dev, dt, T, wide)
-    if k_out is None:
-        k_out, ld_ko = k.new_empty((T, narrow)), narrow
-    else:
-        ld_ko = _rows("k_out", k_out, dev, dt, T, narrow)
-    code = _launch(dev, lib().bitlinear_qk_norm_rope, q.data_ptr(), k.data_ptr(), _dt(q), T, heads, kv_heads, head_dim,
-                   ld_q, ld_k, w1, w2, eps, 2 * half, 1 if interleaved else 0, freq, pos, q_out.data_ptr(), k_out.data_ptr(),
-                   ld_qo, ld_ko)
-    if code:
-        _check(code, "bitlinear_qk_norm_rope")
-    return q_out, k_out
+    r = (_fast or _marshal()).norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq, wk, eps, interleaved, q_out, k_out)
+    if type(r) is int:
+        _check(r, "bitlinear_qk_norm_rope")
+    return r
 
 
 def attention_window(q, k, v, batch, seq, heads, kv_heads=None, head_dim=128, window=0, sinks=0, cu_q=None, cu_k=None,
@@ -518,27 +491,11 @@ def attention_window(q, k, v, batch, seq, heads, kv_heads=None, head_dim=128, wi
     """bitlinear_attention_window.  q [rows, heads*head_dim], k, v [rows_k, kv_heads*head_dim] fp16 or bf16 (may be
     column blocks of one buffer).  `seq` (and `seq_k`, default the same) is the common length, or with cu_q (cu_k)
     int32 [batch+1], packed sequences, an upper bound of their lengths.  Returns o [rows, heads*head_dim]."""
-    kv_heads = heads if kv_heads is None else kv_heads
-    dt, dev, wide, narrow, rows, rows_k = q.dtype, q.get_device(), heads * head_dim, kv_heads * head_dim, q.shape[0], k.shape[0]
-    ld_q, ld_k = _rows("q", q, dev, dt, rows, wide), _rows("k", k, dev, dt, rows_k, narrow)
-    ld_v = _rows("v", v, dev, dt, rows_k, narrow)
-    c1 = None if cu_q is None else _index("cu_q", cu_q, dev, torch.int32, (batch + 1,))
-    c2 = None if cu_k is None else _index("cu_k", cu_k, dev, torch.int32, (batch + 1,))
-    if o is None:
-        o, ld_o = q.new_empty((rows, wide)), wide
-    else:
-        ld_o = _rows("o", o, dev, dt, rows, wide)
-    code = _launch(dev, lib().bitlinear_attention_window, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _dt(q),
-                   batch, c1, c2, seq, seq if seq_k is None else seq_k, rows, rows_k, heads, kv_heads, head_dim, ld_q, ld_k,
-                   ld_v, ld_o, window, sinks, scale)
-    if code:
-        _check(code, "bitlinear_attention_window")
-    return o
-
-
-class _Kv4CacheStruct(C.Structure):
-    _fields_ = [("pages", C.c_void_p), ("num_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int),
-                ("head_dim", C.c_int), ("dtype", C.c_int)]
+    r = (_fast or _marshal()).window(q, k, v, batch, seq, heads, heads if kv_heads is None else kv_heads, head_dim, window, sinks,
+                                     cu_q, cu_k, seq if seq_k is None else seq_k, scale, o)
+    if type(r) is int:
+        _check(r, "bitlinear_attention_window")
+    return r
 
 
 def kv4_page_bytes(page_size, kv_heads, head_dim) -> int:
@@ -550,17 +507,11 @@ class Kv4Cache:
     layer of a [layers, num_pages, page bytes] tensor.  Holds no state of its own."""
 
     def __init__(self, pages, page_size, kv_heads, head_dim, dtype):
-        nbytes = lib().bitlinear_kv4_page_bytes(page_size, kv_heads, head_dim)
-        if nbytes == 0:
-            raise ValueError(f"unsupported cache: page_size {page_size}, kv_heads {kv_heads}, head_dim {head_dim}")
         if dtype not in (torch.float16, torch.bfloat16):
             raise TypeError(f"unsupported dtype {dtype}")
-        num = pages.shape[0]
-        self.device_index = pages.get_device()
-        address = _index("pages", pages, self.device_index, torch.uint8, (num, nbytes))
         self.pages, self.page_size, self.kv_heads, self.head_dim, self.dtype = pages, page_size, kv_heads, head_dim, dtype
-        self._struct = _Kv4CacheStruct(address, num, page_size, kv_heads, head_dim, _DTYPES[dtype])
-        self._ref = C.addressof(self._struct)
+        self._args = (pages, page_size, kv_heads, head_dim, _DTYPES[dtype])
+        (_fast or _marshal()).cache(*self._args)
 
     @staticmethod
     def empty(num_pages, page_size, kv_heads, head_dim, dtype, device):
@@ -572,28 +523,18 @@ class Kv4Cache:
 def kv4_append(cache, k, v, slots):
     """bitlinear_kv4_append.  k, v [T, kv_heads*head_dim] of the cache's dtype; slots int64 [T] (page * page_size +
     place; one outside the cache, e.g. -1, is skipped; none twice)."""
-    T, width, dev, dt = k.shape[0], cache.kv_heads * cache.head_dim, cache.device_index, cache.dtype
-    ld_k, ld_v = _rows("k", k, dev, dt, T, width), _rows("v", v, dev, dt, T, width)
-    at = _index("slots", slots, dev, torch.int64, (T,))
-    code = _launch(dev, lib().bitlinear_kv4_append, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, at)
-    if code:
-        _check(code, "bitlinear_kv4_append")
+    r = (_fast or _marshal()).append(*cache._args, k, v, slots)
+    if r is not None:
+        _check(r, "bitlinear_kv4_append")
 
 
 def kv4_read(cache, slots, k=None, v=None):
     """bitlinear_kv4_read.  Returns (k, v) [T, kv_heads*head_dim] at the slots int64 [T]; rows of given k, v whose slot
     is outside the cache stay as they are, rows of new ones are zero."""
-    T, width, dev, dt = slots.shape[0], cache.kv_heads * cache.head_dim, cache.device_index, cache.dtype
-    if k is None:
-        k = torch.zeros((T, width), dtype=dt, device=cache.pages.device)
-    if v is None:
-        v = torch.zeros((T, width), dtype=dt, device=cache.pages.device)
-    ld_k, ld_v = _rows("k", k, dev, dt, T, width), _rows("v", v, dev, dt, T, width)
-    at = _index("slots", slots, dev, torch.int64, (T,))
-    code = _launch(dev, lib().bitlinear_kv4_read, cache._ref, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, at)
-    if code:
-        _check(code, "bitlinear_kv4_read")
-    return k, v
+    r = (_fast or _marshal()).read(*cache._args, slots, k, v)
+    if type(r) is int:
+        _check(r, "bitlinear_kv4_read")
+    return r
 
 
 def attention_kv4_ws_bytes(batch, n_q, heads, kv_heads, head_dim) -> int:
@@ -603,44 +544,20 @@ def attention_kv4_ws_bytes(batch, n_q, heads, kv_heads, head_dim) -> int:
 def attention_kv4(q, cache, block_table, lens, batch, n_q, heads, window=0, sinks=0, scale=0.0, o=None, ws=None):
     """bitlinear_attention_kv4.  q [batch*n_q, heads*head_dim] of the cache's dtype; block_table int32 [batch, max_pages];
     lens int32 [batch], the n_q new tokens included.  Returns o like q.  `ws` may carry a workspace of
-    attention_kv4_ws_bytes() bytes."""
-    rows, width, dev, dt, L = batch * n_q, heads * cache.head_dim, cache.device_index, cache.dtype, lib()
-    ld_q = _rows("q", q, dev, dt, rows, width)
-    max_pages = block_table.shape[1]
-    table = _index("block_table", block_table, dev, torch.int32, (batch, max_pages))
-    n = _index("lens", lens, dev, torch.int32, (batch,))
-    if o is None:
-        o, ld_o = q.new_empty((rows, width)), width
-    else:
-        ld_o = _rows("o", o, dev, dt, rows, width)
-    if ws is None:
-        nbytes = L.bitlinear_attention_kv4_ws_bytes(batch, n_q, heads, cache.kv_heads, cache.head_dim)
-        ws = cache.pages.new_empty(max(256, nbytes))
-    else:
-        nbytes = ws.numel()
-        _index("ws", ws, dev, torch.uint8, (nbytes,))
-    code = _launch(dev, L.bitlinear_attention_kv4, q.data_ptr(), batch, n_q, heads, ld_q, cache._ref, table, max_pages, n, window,
-                   sinks, scale, o.data_ptr(), ld_o, ws.data_ptr(), nbytes)
-    if code:
-        _check(code, "bitlinear_attention_kv4")
-    return o
+    attention_kv4_ws_bytes() bytes (its first word is the status word)."""
+    r = (_fast or _marshal()).kv4(*cache._args, q, block_table, lens, batch, n_q, heads, window, sinks, scale, o, ws)
+    if type(r) is int:
+        _check(r, "bitlinear_attention_kv4")
+    return r
 
 
 def kv4_copy_pages(pages, pairs):
     """bitlinear_kv4_copy_pages.  pages u8 [num_pages, page bytes] or [layers, num_pages, page bytes], contiguous; pairs
     int32 [n, 2] of (source, destination).  Copies in every layer, in place; returns pages."""
-    dev, shape = pages.get_device(), pages.shape
-    if len(shape) not in (2, 3):
-        _bad("pages", pages, dev, torch.uint8, "[num_pages, bytes] or [layers, num_pages, bytes]")
-    address = _index("pages", pages, dev, torch.uint8, shape)
-    n = pairs.shape[0]
-    which = _index("pairs", pairs, dev, torch.int32, (n, 2))
-    num_pages, nbytes = shape[-2], shape[-1]
-    code = _launch(dev, lib().bitlinear_kv4_copy_pages, address, nbytes, num_pages, shape[0] if len(shape) == 3 else 1,
-                   num_pages * nbytes, which, n)
-    if code:
-        _check(code, "bitlinear_kv4_copy_pages")
-    return pages
+    r = (_fast or _marshal()).copy_pages(pages, pairs)
+    if type(r) is int:
+        _check(r, "bitlinear_kv4_copy_pages")
+    return r
 
 
 def debug_decode_fallbacks() -> int:

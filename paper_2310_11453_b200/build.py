@@ -1,12 +1,15 @@
-"""Compile the CUDA sources into paper_2310_11453_b200/libbitlinear_b200.so for sm_100a.
+"""Compile the CUDA sources into paper_2310_11453_b200/libbitlinear_b200.so for sm_100a, and the argument
+marshalling of the attention operators into paper_2310_11453_b200/_marshal.so.
 
 nvcc cross-compiles without a GPU.  The library links the static CUDA runtime and nothing else,
-so it loads in any process (with or without torch) on a box that has the driver.
+so it loads in any process (with or without torch) on a box that has the driver; _marshal is a Python
+module against torch's C++ interface.
 """
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -16,24 +19,40 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std
          "-Xcompiler", "-fPIC", "-fmad=true"]
 
 
+MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")
+MARSHAL = os.path.join(HERE, "_marshal.so")
+
+
 def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(MARSHAL):
         return True
-    t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + \
+    t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
+    deps = sources() + [MARSHAL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + \
         [os.path.join(HERE, "..", "include", "bitlinear.h")]
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _marshal_command():
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc, libs = os.path.join(root, "include"), os.path.join(root, "lib")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + inc,
+            "-I" + os.path.join(inc, "torch", "csrc", "api", "include"), "-I" + sysconfig.get_paths()["include"], "-I" + cuda,
+            MARSHAL_SRC, "-o", MARSHAL, "-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+            "-Wl,-rpath," + libs]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     objs = []
-    procs = []
+    procs = [(MARSHAL_SRC, subprocess.Popen(_marshal_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT))]
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     for src in sources():
         obj = os.path.join(HERE, "_build", os.path.basename(src)[:-3] + ".o")
@@ -45,7 +64,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         out = p.communicate()[0].decode()
         if p.returncode != 0:
             failed = True
-            sys.stderr.write(f"nvcc failed on {src}:\n{out}\n")
+            sys.stderr.write(f"compiling {src} failed:\n{out}\n")
         elif verbose or out.strip():
             sys.stderr.write(out)
     if failed:
