@@ -100,8 +100,10 @@ __device__ __forceinline__ void quantise_row(const uint4 (&raw)[2], uint32_t (&n
     const float n1 = fmaf(c[5], 16.f, c[4]) + fmaf(c[7], 4096.f, c[6] * 256.f);
     nib[k] = __byte_perm(__float_as_uint(n0 + 8388608.f), __float_as_uint(n1 + 8388608.f), 0x5410);
   }
-  const bool odd_step = !(step > kLeast && step < 1e30f);
-  if (odd_step || far > 0.49999f) {
+  const bool odd_step = !(step > kLeast && step < 1e30f) && step != 0.f;
+  if (step == 0.f) {                                  // a constant row (or no row at all)
+    nib[0] = nib[1] = 0;
+  } else if (odd_step || far > 0.49999f) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       uint32_t doubt = odd_step ? 0xFFu : 0u;
@@ -156,6 +158,8 @@ __global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, 
   constexpr int kLanes = kDim / 16;
   const int lane = threadIdx.x & 31, sub = lane % kLanes, d = sub * 16, odd = (lane / kLanes) & 1;
   const Rows<kLanes, kUnroll> rows(c.kv_heads);
+  pdl_launch_dependents();
+  pdl_wait();
   uint4 kr[kUnroll][2], vr[kUnroll][2];
   int64_t slot[kUnroll];
 #pragma unroll
@@ -212,6 +216,8 @@ __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T*
   constexpr int kLanes = kDim / 16;
   const int d = ((threadIdx.x & 31) % kLanes) * 16;
   const Rows<kLanes, kUnroll> rows(c.kv_heads);
+  pdl_launch_dependents();
+  pdl_wait();
   uint2 kn[kUnroll], v0[kUnroll], v1[kUnroll];         // key codes; words of value codes, of this token and its pair's other
   uint32_t ks[kUnroll], vs[kUnroll];
   bool on[kUnroll], high[kUnroll];
@@ -251,6 +257,8 @@ constexpr int kCopyBytes = kKvThreads * 16 * kCopyUnroll;
 
 __global__ void __launch_bounds__(kKvThreads) kv4_copy_kernel(char* pages, int64_t page_bytes, int64_t num_pages, int64_t layer_stride,
                                                              const int2* __restrict__ pairs, unsigned chunks) {
+  pdl_launch_dependents();
+  pdl_wait();
   const int2 pr = pairs[blockIdx.x / chunks];
   if (pr.x < 0 || pr.y < 0 || pr.x >= num_pages || pr.y >= num_pages || pr.x == pr.y) return;
   char* layer = pages + (int64_t)blockIdx.y * layer_stride;
@@ -279,9 +287,8 @@ cudaError_t append_dim(const bl_kv4_cache& c, const void* k, const void* v, int6
   const T* kp = reinterpret_cast<const T*>(k);
   const T* vp = reinterpret_cast<const T*>(v);
   const unsigned many = row_blocks(c, n, kMany);
-  if (many >= 8 * 148) kv4_append_kernel<T, kDim, kMany><<<many, kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  else kv4_append_kernel<T, kDim, 1><<<row_blocks(c, n, 1), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  return cudaGetLastError();
+  if (many >= 8 * 148) return launch_pdl(kv4_append_kernel<T, kDim, kMany>, many, kKvThreads, 0, s, c, kp, vp, n, ld_k, ld_v, slots);
+  return launch_pdl(kv4_append_kernel<T, kDim, 1>, row_blocks(c, n, 1), kKvThreads, 0, s, c, kp, vp, n, ld_k, ld_v, slots);
 }
 template <typename T>
 cudaError_t append_type(const bl_kv4_cache& c, const void* k, const void* v, int64_t n, int64_t ld_k, int64_t ld_v,
@@ -295,9 +302,8 @@ cudaError_t read_dim(const bl_kv4_cache& c, void* k, void* v, int64_t n, int64_t
   T* kp = reinterpret_cast<T*>(k);
   T* vp = reinterpret_cast<T*>(v);
   const unsigned many = row_blocks(c, n, kMany);
-  if (many >= 8 * 148) kv4_read_kernel<T, kDim, kMany><<<many, kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  else kv4_read_kernel<T, kDim, 1><<<row_blocks(c, n, 1), kKvThreads, 0, s>>>(c, kp, vp, n, ld_k, ld_v, slots);
-  return cudaGetLastError();
+  if (many >= 8 * 148) return launch_pdl(kv4_read_kernel<T, kDim, kMany>, many, kKvThreads, 0, s, c, kp, vp, n, ld_k, ld_v, slots);
+  return launch_pdl(kv4_read_kernel<T, kDim, 1>, row_blocks(c, n, 1), kKvThreads, 0, s, c, kp, vp, n, ld_k, ld_v, slots);
 }
 template <typename T>
 cudaError_t read_type(const bl_kv4_cache& c, void* k, void* v, int64_t n, int64_t ld_k, int64_t ld_v, const int64_t* slots,
@@ -322,10 +328,8 @@ cudaError_t launch_kv4_read(const bl_kv4_cache& c, void* k, void* v, int64_t T, 
 cudaError_t launch_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
                                   const int32_t* pairs, int64_t n, cudaStream_t s) {
   const unsigned chunks = (unsigned)((page_bytes + kCopyBytes - 1) / kCopyBytes);
-  kv4_copy_kernel<<<dim3((unsigned)n * chunks, (unsigned)layers), kKvThreads, 0, s>>>(
-      reinterpret_cast<char*>(pages), (int64_t)page_bytes, num_pages, (int64_t)layer_stride, reinterpret_cast<const int2*>(pairs),
-      chunks);
-  return cudaGetLastError();
+  return launch_pdl(kv4_copy_kernel, dim3((unsigned)n * chunks, (unsigned)layers), kKvThreads, 0, s, reinterpret_cast<char*>(pages),
+                    (int64_t)page_bytes, num_pages, (int64_t)layer_stride, reinterpret_cast<const int2*>(pairs), chunks);
 }
 
 }  // namespace bl

@@ -119,11 +119,13 @@ __device__ __forceinline__ void turn_heads(const Heads<T>& x, const NormRopeArgs
 // key heads in one row of numbers.
 template <typename T, int kLanes, bool kInter>
 __global__ void __launch_bounds__(kNrWarps * 32) qk_norm_rope_kernel(NormRopeArgs a, int parts, int per) {
+  pdl_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % kLanes;
   const int64_t job = (int64_t)blockIdx.x * kNrWarps + (threadIdx.x >> 5);
   const int64_t t = parts == 1 ? job : job / parts;
   if (t >= a.T) return;
   const int h0 = (int)(job - t * parts) * per, h1 = min(h0 + per, a.heads + a.kv_heads);
+  pdl_wait();
   const int pos = a.positions[t];
   if (pos < 0) return;                             // padding: rows stay as they are
   const int half = a.rot_dim / 2;
@@ -168,9 +170,8 @@ cudaError_t launch_lanes(const NormRopeArgs& a, cudaStream_t s) {
   const int parts = (heads + per - 1) / per;
   const int64_t blocks = (a.T * parts + kNrWarps - 1) / kNrWarps;
   if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  if (a.interleaved) qk_norm_rope_kernel<T, kLanes, true><<<(unsigned)blocks, kNrWarps * 32, 0, s>>>(a, parts, per);
-  else qk_norm_rope_kernel<T, kLanes, false><<<(unsigned)blocks, kNrWarps * 32, 0, s>>>(a, parts, per);
-  return cudaGetLastError();
+  return launch_pdl(a.interleaved ? qk_norm_rope_kernel<T, kLanes, true> : qk_norm_rope_kernel<T, kLanes, false>, (unsigned)blocks,
+                    kNrWarps * 32, 0, s, a, parts, per);
 }
 
 template <typename T>
