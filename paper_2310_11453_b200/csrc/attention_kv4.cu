@@ -577,11 +577,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   }
 }
 
-// Joins the parts of the rows whose chunks went to more than one warp: one CTA per row, warps take the parts in turn.
+// Joins the parts of the rows whose chunks went to more than one warp: one CTA per row.  All maxima and sums are loaded at
+// once and turned into weights; then the parts' values are summed, four loads of a warp in flight.
 template <typename T, int kDim>
 __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, Plan plan) {
-  constexpr int kVals = kDim / 32;
-  __shared__ float sums[kJoinWarps][kDim + 4];
+  constexpr int kVals = kDim / 32, kMostParts = kMaxSms * kMostWarps;
+  __shared__ float weight[kMostParts], sums[kJoinWarps][kDim], tops[kJoinWarps], totals[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int bh = blockIdx.x / plan.rows_per_block, rr = blockIdx.x - bh * plan.rows_per_block;
   const int b = bh / plan.heads_blocks, hb = bh - b * plan.heads_blocks;
@@ -597,34 +598,58 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4
   }
   const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
   const int64_t first = chunks_before(a, b) * plan.heads_blocks + (int64_t)hb * chunks;
-  const int w0 = cut.owner(first), w1 = cut.owner(first + chunks - 1);
-  if (w0 == w1) return;                                // written already
-  float m = -INFINITY, l = 0.f, v[kVals] = {};
-  for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
-    const float* row = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.ws) + kStatusBytes) + ((int64_t)(2 * w + (cut.begin(w) < first)) * plan.rows_per_block + rr) * (kDim + 4);
-    const float2 ml = *reinterpret_cast<const float2*>(row + kDim);
-    if (ml.x == -INFINITY) continue;                   // the part holds nothing that this row sees
-    const float top = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : ex2(m - top), p = ex2(ml.x - top);
-    m = top;
-    l = l * c + ml.y * p;
+  const int w0 = cut.owner(first), parts = cut.owner(first + chunks - 1) - w0 + 1;
+  if (parts == 1) return;                              // written already
+  // part 0 of the row is in its warp's second slot if that warp began with another row; the others are in first slots
+  const int64_t stride = (int64_t)plan.rows_per_block * (kDim + 4);
+  const float* rows = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.ws) + kStatusBytes) + (int64_t)rr * (kDim + 4) +
+                      2 * (int64_t)w0 * stride;
+  const int64_t shift = cut.begin(w0) < first ? stride : 0;
+  auto row = [&](int i) { return rows + 2 * (int64_t)i * stride + (i == 0 ? shift : 0); };
+  float top = -INFINITY;
+  for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
+    const float m = row(i)[kDim];
+    weight[i] = m;
+    top = fmaxf(top, m);
+  }
+  top = warp_max(top);
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kVals; ++i) v[i] = v[i] * c + row[lane * kVals + i] * p;
+  for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
+  float l = 0.f;
+  for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
+    const float m = weight[i], c = m == -INFINITY ? 0.f : ex2(m - top);   // -infinity: the part holds nothing that this row sees
+    weight[i] = c;
+    if (m != -INFINITY) l = fmaf(row(i)[kDim + 1], c, l);
+  }
+  l = warp_sum(l);
+  if (lane == 0) totals[warp] = l;
+  __syncthreads();
+  float v[kVals] = {};
+  for (int base = warp; base < parts; base += 4 * kJoinWarps) {
+    float x[4][kVals];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = base + u * kJoinWarps;
+#pragma unroll
+      for (int e = 0; e < kVals; ++e) x[u][e] = i < parts ? row(i)[lane * kVals + e] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = base + u * kJoinWarps;
+      const float c = i < parts ? weight[i] : 0.f;
+#pragma unroll
+      for (int e = 0; e < kVals; ++e) v[e] = c == 0.f ? v[e] : fmaf(x[u][e], c, v[e]);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < kVals; ++i) sums[warp][lane * kVals + i] = v[i];
-  if (lane == 0) { sums[warp][kDim] = m; sums[warp][kDim + 1] = l; }
+  for (int e = 0; e < kVals; ++e) sums[warp][lane * kVals + e] = v[e];
   __syncthreads();
   for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, sums[i][kDim]);
     float ls = 0.f, vs = 0.f;
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) {
-      const float c = sums[i][kDim] == -INFINITY ? 0.f : ex2(sums[i][kDim] - top);
-      ls += sums[i][kDim + 1] * c;
-      vs += sums[i][d] * c;
-    }
+    for (int i = 0; i < kJoinWarps; ++i) { ls += totals[i]; vs += sums[i][d]; }
     out[d] = out_cast<T>(ls == 0.f ? 0.f : vs / ls);
   }
 }
