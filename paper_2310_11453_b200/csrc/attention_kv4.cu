@@ -47,6 +47,7 @@ struct Plan {                              // how the list is laid out; made on 
   int group, rows, rows_per_block, blocks; // query heads per key/value head; query rows; rows per block; blocks
   int heads_blocks;                        // key/value heads x blocks
   int page_log2, parts;                    // log2 page_size; parts of the list (warps)
+  uint32_t parts_magic;                    // floor(2^32 / parts) + 1
 };
 inline Plan make_plan(int n_q, int heads, int kv_heads, int page_size, int parts) {
   Plan p;
@@ -57,6 +58,7 @@ inline Plan make_plan(int n_q, int heads, int kv_heads, int page_size, int parts
   p.heads_blocks = kv_heads * p.blocks;
   p.page_log2 = page_size == 16 ? 4 : page_size == 32 ? 5 : 6;
   p.parts = parts;
+  p.parts_magic = (uint32_t)((1ull << 32) / (unsigned)parts) + 1;
   return p;
 }
 
@@ -76,57 +78,71 @@ __device__ __forceinline__ Seq make_seq(const Kv4AttnArgs& a, int b) {
   return s;
 }
 
-// Chunks of all sequences (by a whole warp).
-__device__ __forceinline__ int64_t total_chunks(const Kv4AttnArgs& a) {
-  const int lane = threadIdx.x & 31;
-  int64_t sum = 0;
-  for (int base = 0; base < a.batch; base += 32) sum += warp_sum(base + lane < a.batch ? make_seq(a, base + lane).chunks : 0);
-  return sum;
-}
-// Chunks of the sequences before b (by a whole warp).
-__device__ __forceinline__ int64_t chunks_before(const Kv4AttnArgs& a, int b) {
-  const int lane = threadIdx.x & 31;
-  int64_t sum = 0;
-  for (int base = 0; base < b; base += 32) sum += warp_sum(base + lane < b ? make_seq(a, base + lane).chunks : 0);
-  return sum;
-}
-// The sequence that item `at` of the list falls into, and the item's place among that sequence's (by a whole warp).
-__device__ __forceinline__ int find_seq(const Kv4AttnArgs& a, int heads_blocks, int64_t at, int64_t& rest) {
-  const int lane = threadIdx.x & 31;
-  int64_t before = 0;
-  for (int base = 0; base < a.batch; base += 32) {
-    const int n = base + lane < a.batch ? make_seq(a, base + lane).chunks : 0;
-    int incl = n;
+// Where the sequences' chunks lie in one row of numbers (by a whole warp).  Up to 32 sequences: found out once, each lane
+// keeping one; more: added up again when asked.
+struct Spread {
+  int mine, upto;                          // chunks of sequence `lane`, and of those up to it
+  int64_t all;                             // chunks of all sequences
+  __device__ __forceinline__ explicit Spread(const Kv4AttnArgs& a) {
+    const int lane = threadIdx.x & 31;
+    all = 0;
+    for (int base = 0; base < a.batch; base += 32) {
+      scan(base + lane < a.batch ? make_seq(a, base + lane).chunks : 0);
+      all += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+  }
+  __device__ __forceinline__ void scan(int n) {
+    const int lane = threadIdx.x & 31;
+    mine = upto = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += up;
+      const int up = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += up;
     }
-    const unsigned past = __ballot_sync(0xFFFFFFFFu, (before + incl) * heads_blocks > at);
-    if (past) {
-      const int f = __ffs(past) - 1;
-      rest = at - (before + __shfl_sync(0xFFFFFFFFu, incl - n, f)) * heads_blocks;
-      return base + f;
-    }
-    before += __shfl_sync(0xFFFFFFFFu, incl, 31);
   }
-  rest = 0;
-  return a.batch;
+  // The sequence that item `at` of the list falls into, and the item's place among that sequence's.
+  __device__ __forceinline__ int find(const Kv4AttnArgs& a, int heads_blocks, int64_t at, int64_t& rest) {
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int base = 0; base < a.batch; base += 32) {
+      if (a.batch > 32) scan(base + lane < a.batch ? make_seq(a, base + lane).chunks : 0);
+      const unsigned past = __ballot_sync(0xFFFFFFFFu, (before + upto) * heads_blocks > at);
+      if (past) {
+        const int f = __ffs(past) - 1;
+        rest = at - (before + __shfl_sync(0xFFFFFFFFu, upto - mine, f)) * heads_blocks;
+        return base + f;
+      }
+      before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    rest = 0;
+    return a.batch;
+  }
+};
+
+// Workspace: the status word, the parts (two slots per warp), then two numbers per sequence, head and block of rows.
+__host__ __device__ inline int64_t slot_floats(const Plan& plan, int head_dim) { return (int64_t)plan.rows_per_block * (head_dim + 4); }
+__device__ __forceinline__ float* slots_of(const Kv4AttnArgs& a) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kStatusBytes); }
+__device__ __forceinline__ int* ends_of(const Kv4AttnArgs& a, const Plan& plan) {
+  return reinterpret_cast<int*>(slots_of(a) + 2 * plan.parts * slot_floats(plan, a.cache.head_dim));
 }
 
 // a / b for a >= 0, b > 0: the 32-bit division (a fifth of the instructions) where it serves.
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// The cut of a list of items into parts: part w starts at begin(w), item i lies in part owner(i).
+// The cut of a list of items into parts: part w starts at begin(w).
 struct Cut {
   int64_t each; int more;                  // items of a part; the first `more` parts have one more
-  __device__ __forceinline__ Cut(int64_t total, int parts) : each(divide(total, parts)), more((int)(total - each * parts)) {}
-  __device__ __forceinline__ int64_t begin(int w) const { return each * w + min(w, more); }
-  __device__ __forceinline__ int owner(int64_t i) const {
-    const int64_t split = (each + 1) * more;
-    return (int)(i < split ? divide(i, each + 1) : more + divide(i - split, each));
+  __device__ __forceinline__ Cut(int64_t total, const Plan& plan) {
+    if (total >> 31) {
+      each = total / plan.parts;
+    } else {                               // n / parts is at most half a unit below n magic / 2^32 for n < 2^31
+      const uint32_t n = (uint32_t)total, q = __umulhi(n, plan.parts_magic);
+      each = q * (uint32_t)plan.parts > n ? q - 1 : q;
+    }
+    more = (int)(total - each * plan.parts);
   }
+  __device__ __forceinline__ int64_t begin(int w) const { return each * w + min(w, more); }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -231,7 +247,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
 
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.ws) = 0;   // the status word
-  const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
+  Spread spread(a);
+  const Cut cut(spread.all * plan.heads_blocks, plan);
   const int64_t begin = cut.begin(w);
   const int items = (int)(cut.begin(w + 1) - begin);
   if (items == 0) return;
@@ -240,11 +257,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   Walk ahead;
   {
     int64_t rest;
-    ahead.b = find_seq(a, plan.heads_blocks, begin, rest);
+    ahead.b = spread.find(a, plan.heads_blocks, begin, rest);
     ahead.s = make_seq(a, ahead.b);
     const int hb = (int)divide(rest, ahead.s.chunks);
     ahead.c = (int)(rest - (int64_t)hb * ahead.s.chunks);
-    ahead.hk = hb / plan.blocks;
+    ahead.hk = plan.blocks == 1 ? hb : hb / plan.blocks;
     ahead.blk = hb - ahead.hk * plan.blocks;
   }
   auto page_of = [&](const Walk& x) -> int {           // lane i: the page of the chunk's i-th run of tokens; -1: nothing visible, or no page
@@ -500,8 +517,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
 
   auto end_segment = [&](const Item& it) {
     const bool whole = from_start && it.last;
+    // where the join finds the row block's parts: that of the first chunk (slot), that of the last (warp)
+    if (lane == 0) {
+      int* where = ends_of(a, plan) + 2 * (((int64_t)it.b * a.cache.kv_heads + it.hk) * plan.blocks + it.rows0 / plan.rows_per_block);
+      if (from_start) where[0] = 2 * w + later;
+      if (it.last) where[1] = w;
+    }
     const float back = pow2i(min(max(vexp - 13, -126), 127));
-    float* slot = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kStatusBytes) + (int64_t)(2 * w + later) * plan.rows_per_block * (kDim + 4);
+    float* slot = slots_of(a) + (2 * w + later) * slot_floats(plan, kDim);
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -557,7 +580,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     }
     return __all_sync(0xFFFFFFFFu, ok);
   };
-  bool fresh = true;
+  __syncwarp();
+  begin_segment(items_of[0]);                          // while the first chunk is on its way
+  bool fresh = false;
   for (int item = 0; item < items; ++item) {
     if (!arrived(item, polls)) {                       // the copies did not come: reported, nothing more is done
       if (lane == 0) *reinterpret_cast<volatile uint32_t*>(a.ws) = BL_ERR_TIMEOUT;
@@ -596,16 +621,15 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4
     for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) out[d] = out_cast<T>(0.f);
     return;
   }
-  const Cut cut(total_chunks(a) * plan.heads_blocks, plan.parts);
-  const int64_t first = chunks_before(a, b) * plan.heads_blocks + (int64_t)hb * chunks;
-  const int w0 = cut.owner(first), parts = cut.owner(first + chunks - 1) - w0 + 1;
+  const int2 ends = *reinterpret_cast<const int2*>(ends_of(a, plan) + 2 * bh);
+  const int w0 = ends.x >> 1, parts = ends.y - w0 + 1;
   if (parts == 1) return;                              // written already
-  // part 0 of the row is in its warp's second slot if that warp began with another row; the others are in first slots
-  const int64_t stride = (int64_t)plan.rows_per_block * (kDim + 4);
-  const float* rows = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.ws) + kStatusBytes) + (int64_t)rr * (kDim + 4) +
-                      2 * (int64_t)w0 * stride;
-  const int64_t shift = cut.begin(w0) < first ? stride : 0;
-  auto row = [&](int i) { return rows + 2 * (int64_t)i * stride + (i == 0 ? shift : 0); };
+  if (w0 < 0 || parts < 1 || ends.y >= plan.parts) return;   // never written: the first kernel gave up (status word)
+  // the first part may be in its warp's second slot; the others are in first slots
+  const int64_t stride = slot_floats(plan, kDim);
+  const float* rows = slots_of(a) + 2 * w0 * stride + rr * (kDim + 4);
+  const int64_t shift = (ends.x & 1) * stride;
+  auto row = [&](int i) { return rows + 2 * i * stride + (i == 0 ? shift : 0); };
   float top = -INFINITY;
   for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
     const float m = row(i)[kDim];
@@ -713,7 +737,8 @@ cudaError_t launch_type(const Kv4AttnArgs& a, cudaStream_t s) {
 
 size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
   const Plan p = make_plan(n_q, heads, kv_heads, 16, 1);
-  return batch == 0 ? 0 : kStatusBytes + (size_t)kMaxSms * kMostWarps * 2 * p.rows_per_block * (head_dim + 4) * sizeof(float);
+  return batch == 0 ? 0 : kStatusBytes + (size_t)kMaxSms * kMostWarps * 2 * (size_t)slot_floats(p, head_dim) * sizeof(float) +
+                              (size_t)batch * (size_t)p.heads_blocks * 2 * sizeof(int);
 }
 
 cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s) {

@@ -209,7 +209,7 @@ def check_kv4(q, cache, table, lens, batch, n_q, heads, window, sinks, scale, o,
     ([700, 5, 0, 2], 4, 2, 4, 64, 32, 0, 0), ([300, 17, 129], 3, 3, 3, 128, 16, 50, 4), ([515, 64], 2, 1, 8, 64, 64, 64, 0),
     ([200, 90], 1, 4, 2, 128, 32, 1, 0), ([200, 90], 1, 4, 2, 128, 32, 1, 3), ([130], 9, 2, 5, 64, 16, 16, 1), ([333, 40], 21, 1, 1, 128, 16, 0, 0),
     ([5000, 777], 1, 2, 16, 128, 64, 0, 0), ([4097], 5, 5, 2, 64, 64, 100, 200), ([2500] * 9 + [1] * 8, 1, 8, 4, 128, 16, 1000, 17),
-    ([40000], 2, 1, 4, 128, 64, 30000, 5)])
+    ([40000], 2, 1, 4, 128, 64, 30000, 5), ([i * 37 % 301 for i in range(70)], 1, 2, 2, 64, 16, 0, 0), ([0] * 33 + [900, 0, 65], 2, 1, 1, 64, 64, 0, 0)])
 def test_attention_kv4(dt, lens, n_q, hk, g, dim, page, window, sinks):
     batch, heads = len(lens), hk * g
     cache, table = fill(batch, lens, page, hk, dim, dt, seed=len(lens) + n_q)
