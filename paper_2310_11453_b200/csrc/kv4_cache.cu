@@ -1,7 +1,8 @@
 // The 4-bit key/value cache: quantising token rows into it, reading them back, copying its pages.
 //   eta = min x, step = (max x - min x) / 15 (rounded to the cache's type), code = clip(rint((x - eta) / step)).
 // All three are bound by memory.  Append and read give each (token, head) row kDim / 16 lanes, 16 values per
-// lane: two 16-byte accesses to the 16-bit rows, 8 bytes of key codes and 4 x 2 bytes of value codes.
+// lane in two runs of 8, half a row apart (a warp's access then covers whole sectors): two 16-byte accesses to the 16-bit
+// rows, 2 x 4 bytes of key codes and two words of value codes.
 #include <type_traits>
 
 #include "kv4.cuh"
@@ -152,11 +153,11 @@ template <int kLanes, int kUnroll> struct Rows {
 };
 
 template <typename T, int kDim, int kUnroll>
-__global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, const T* __restrict__ k, const T* __restrict__ v,
+__global__ void __launch_bounds__(kKvThreads, 4) kv4_append_kernel(bl_kv4_cache c, const T* __restrict__ k, const T* __restrict__ v,
                                                                int64_t T_, int64_t ld_k, int64_t ld_v,
                                                                const int64_t* __restrict__ slots) {
   constexpr int kLanes = kDim / 16;
-  const int lane = threadIdx.x & 31, sub = lane % kLanes, d = sub * 16, odd = (lane / kLanes) & 1;
+  const int lane = threadIdx.x & 31, sub = lane % kLanes, d0 = sub * 8, d1 = kDim / 2 + d0, odd = (lane / kLanes) & 1;
   const Rows<kLanes, kUnroll> rows(c.kv_heads);
   pdl_launch_dependents();
   pdl_wait();
@@ -168,10 +169,10 @@ __global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, 
     slot[u] = t < T_ ? slots[t] : -1;
     kr[u][0] = kr[u][1] = vr[u][0] = vr[u][1] = make_uint4(0, 0, 0, 0);
     if (t < T_) {
-      const uint4* kp = reinterpret_cast<const uint4*>(k + t * ld_k + (int64_t)rows.h * kDim + d);
-      const uint4* vp = reinterpret_cast<const uint4*>(v + t * ld_v + (int64_t)rows.h * kDim + d);
-      kr[u][0] = __ldg(kp); kr[u][1] = __ldg(kp + 1);
-      vr[u][0] = __ldg(vp); vr[u][1] = __ldg(vp + 1);
+      const T* kp = k + t * ld_k + (int64_t)rows.h * kDim;
+      const T* vp = v + t * ld_v + (int64_t)rows.h * kDim;
+      kr[u][0] = __ldg(reinterpret_cast<const uint4*>(kp + d0)); kr[u][1] = __ldg(reinterpret_cast<const uint4*>(kp + d1));
+      vr[u][0] = __ldg(reinterpret_cast<const uint4*>(vp + d0)); vr[u][1] = __ldg(reinterpret_cast<const uint4*>(vp + d1));
     }
   }
 #pragma unroll
@@ -184,15 +185,16 @@ __global__ void __launch_bounds__(kKvThreads) kv4_append_kernel(bl_kv4_cache c, 
     const int64_t other = __shfl_xor_sync(0xFFFFFFFFu, slot[u], kLanes);
     const uint32_t theirs = __shfl_xor_sync(0xFFFFFFFFu, odd ? vn[0] : vn[1], kLanes);
     if (!p.on) continue;
-    *reinterpret_cast<uint2*>(p.block + p.j * (kDim / 2) + d / 2) = make_uint2(kn[0], kn[1]);
+    *reinterpret_cast<uint32_t*>(p.block + p.j * (kDim / 2) + d0 / 2) = kn[0];
+    *reinterpret_cast<uint32_t*>(p.block + p.j * (kDim / 2) + d1 / 2) = kn[1];
     char* vc = p.block + Block<kDim>::v_codes(c.page_size);
     if ((slot[u] ^ other) == 1 && (p.j & 1) == odd) {
       const uint32_t lo = odd ? theirs : vn[0], hi = odd ? vn[1] : theirs;
-      *reinterpret_cast<uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d + 8 * odd)) = make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+      *reinterpret_cast<uint2*>(vc + Block<kDim>::v_at(p.j & ~1, odd ? d1 : d0)) = make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(p.j, d + 4 * i)) = (uint16_t)(vn[i >> 1] >> (16 * (i & 1)));
+        *reinterpret_cast<uint16_t*>(vc + Block<kDim>::v_at(p.j, (i < 2 ? d0 : d1) + 4 * (i & 1))) = (uint16_t)(vn[i >> 1] >> (16 * (i & 1)));
     }
     if (sub == 0) *reinterpret_cast<uint32_t*>(p.block + Block<kDim>::k_scale(c.page_size) + 4 * p.j) = ks;
     if (sub == 1) *reinterpret_cast<uint32_t*>(p.block + Block<kDim>::v_scale(c.page_size) + 4 * p.j) = vs;
@@ -214,7 +216,7 @@ template <typename T, int kDim, int kUnroll>
 __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T* __restrict__ k, T* __restrict__ v, int64_t T_,
                                                              int64_t ld_k, int64_t ld_v, const int64_t* __restrict__ slots) {
   constexpr int kLanes = kDim / 16;
-  const int d = ((threadIdx.x & 31) % kLanes) * 16;
+  const int d0 = ((threadIdx.x & 31) % kLanes) * 8, d1 = kDim / 2 + d0;
   const Rows<kLanes, kUnroll> rows(c.kv_heads);
   pdl_launch_dependents();
   pdl_wait();
@@ -231,9 +233,10 @@ __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T*
     ks[u] = vs[u] = 0;
     if (p.on) {
       const char* vc = p.block + Block<kDim>::v_codes(c.page_size);
-      kn[u] = *reinterpret_cast<const uint2*>(p.block + p.j * (kDim / 2) + d / 2);
-      v0[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d));
-      v1[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d + 8));
+      kn[u].x = *reinterpret_cast<const uint32_t*>(p.block + p.j * (kDim / 2) + d0 / 2);
+      kn[u].y = *reinterpret_cast<const uint32_t*>(p.block + p.j * (kDim / 2) + d1 / 2);
+      v0[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d0));
+      v1[u] = *reinterpret_cast<const uint2*>(vc + Block<kDim>::v_at(p.j & ~1, d1));
       ks[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::k_scale(c.page_size) + 4 * p.j);
       vs[u] = *reinterpret_cast<const uint32_t*>(p.block + Block<kDim>::v_scale(c.page_size) + 4 * p.j);
     }
@@ -242,12 +245,12 @@ __global__ void __launch_bounds__(kKvThreads) kv4_read_kernel(bl_kv4_cache c, T*
   for (int u = 0; u < kUnroll; ++u) {
     if (!on[u]) continue;
     const int64_t t = rows.token(u);
-    T* kp = k + t * ld_k + (int64_t)rows.h * kDim + d;
-    T* vp = v + t * ld_v + (int64_t)rows.h * kDim + d;
+    T* kp = k + t * ld_k + (int64_t)rows.h * kDim;
+    T* vp = v + t * ld_v + (int64_t)rows.h * kDim;
     const float2 kse = scale_floats<T>(ks[u]), vse = scale_floats<T>(vs[u]);
     const uint32_t pick = high[u] ? 0x7632u : 0x5410u;
-    store_values<T>(kp, kn[u].x, kse); store_values<T>(kp + 8, kn[u].y, kse);
-    store_values<T>(vp, __byte_perm(v0[u].x, v0[u].y, pick), vse); store_values<T>(vp + 8, __byte_perm(v1[u].x, v1[u].y, pick), vse);
+    store_values<T>(kp + d0, kn[u].x, kse); store_values<T>(kp + d1, kn[u].y, kse);
+    store_values<T>(vp + d0, __byte_perm(v0[u].x, v0[u].y, pick), vse); store_values<T>(vp + d1, __byte_perm(v1[u].x, v1[u].y, pick), vse);
   }
 }
 
