@@ -85,46 +85,35 @@ __device__ __forceinline__ void quantise_row(const uint4 (&raw)[2], uint32_t (&n
   const float step = scale_floats<T>(sb).x;
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
-  float far = 0.f;                                    // largest distance of a quotient from its code
+  uint32_t doubt = 0;                                 // values whose quotient is too near a border, one bit each
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     float c[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = scale_floats<T>(w[4 * k + i]);
-      const float d0 = f.x - lo, d1 = f.y - lo;
-      c[2 * i] = fmaf(d0, inv, kMagic) - kMagic;
-      c[2 * i + 1] = fmaf(d1, inv, kMagic) - kMagic;
-      far = fmaxf(far, fmaxf(fabsf(fmaf(d0, inv, -c[2 * i])), fabsf(fmaf(d1, inv, -c[2 * i + 1]))));
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = scale_floats<T>(w[4 * k + i / 2]);
+      const float d = (i & 1 ? f.y : f.x) - lo;
+      c[i] = fmaf(d, inv, kMagic) - kMagic;
+      if (fabsf(fmaf(d, inv, -c[i])) > 0.49999f) doubt |= 1u << (8 * k + i);
     }
     const float n0 = fmaf(c[1], 16.f, c[0]) + fmaf(c[3], 4096.f, c[2] * 256.f);
     const float n1 = fmaf(c[5], 16.f, c[4]) + fmaf(c[7], 4096.f, c[6] * 256.f);
     nib[k] = __byte_perm(__float_as_uint(n0 + 8388608.f), __float_as_uint(n1 + 8388608.f), 0x5410);
   }
-  const bool odd_step = !(step > kLeast && step < 1e30f) && step != 0.f;
-  if (step == 0.f) {                                  // a constant row (or no row at all)
-    nib[0] = nib[1] = 0;
-  } else if (odd_step || far > 0.49999f) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      uint32_t doubt = odd_step ? 0xFFu : 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 f = scale_floats<T>(w[4 * k + i / 2]);
-        const float q = ((i & 1 ? f.y : f.x) - lo) * inv;
-        doubt |= fabsf(q - rintf(q)) > 0.49998f ? 1u << i : 0u;
-      }
+  const bool odd_step = !(step > kLeast && step < 1e30f);
+  if (odd_step) doubt = 0xFFFFu;
+  if (step == 0.f) { nib[0] = nib[1] = 0; doubt = 0; }   // a constant row (or no row at all)
 #pragma unroll 1
-      while (doubt) {
-        const int i = __ffs(doubt) - 1;
-        doubt &= doubt - 1;
-        const uint32_t word = i < 4 ? (i < 2 ? w[4 * k] : w[4 * k + 1]) : (i < 6 ? w[4 * k + 2] : w[4 * k + 3]);
-        const float2 f = scale_floats<T>(word);
-        const float x = i & 1 ? f.y : f.x;
-        const uint32_t code = odd_step ? exact_code(x, lo, step) : border_code(x, lo, step, (int)((nib[k] >> (4 * i)) & 15u));
-        nib[k] = (nib[k] & ~(15u << (4 * i))) | (code << (4 * i));
-      }
-    }
+  while (doubt) {
+    const int i = __ffs(doubt) - 1, shift = 4 * (i & 7);
+    doubt &= doubt - 1;
+    const uint32_t a0 = i & 2 ? w[1] : w[0], a1 = i & 2 ? w[3] : w[2], a2 = i & 2 ? w[5] : w[4], a3 = i & 2 ? w[7] : w[6];
+    const uint32_t b0 = i & 4 ? a1 : a0, b1 = i & 4 ? a3 : a2, have = i & 8 ? nib[1] : nib[0];
+    const float2 f = scale_floats<T>(i & 8 ? b1 : b0);
+    const float x = i & 1 ? f.y : f.x;
+    const uint32_t code = odd_step ? exact_code(x, lo, step) : border_code(x, lo, step, (int)((have >> shift) & 15u));
+    const uint32_t made = (have & ~(15u << shift)) | (code << shift);
+    if (i & 8) nib[1] = made; else nib[0] = made;
   }
   scale = __byte_perm(sb, both, 0x5410);
   if (!(lo >= -3.4e38f && hi <= 3.4e38f)) { nib[0] = nib[1] = 0; scale = nan_pair<T>(); }
