@@ -118,7 +118,7 @@ __device__ __forceinline__ void turn_heads(const Heads<T>& x, const NormRopeArgs
 // kLanes lanes per head (head_dim <= 16 kLanes).  Warp (token, part) takes heads part * per .. of the token's query and
 // key heads in one row of numbers.
 template <typename T, int kLanes, bool kInter>
-__global__ void __launch_bounds__(kNrWarps * 32) qk_norm_rope_kernel(NormRopeArgs a, int parts, int per) {
+__global__ void __launch_bounds__(kNrWarps * 32, sizeof(T) == 2 ? 5 : 4) qk_norm_rope_kernel(NormRopeArgs a, int parts, int per) {
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % kLanes;
   const int64_t job = (int64_t)blockIdx.x * kNrWarps + (threadIdx.x >> 5);
