@@ -316,13 +316,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   float acc[kNT][2 * kWords][4];
   float m[kNT][2], l[kNT][2], esum[kNT][2];
   float usum[kNT][4];                                  // sums of the rounded p . step' (every row of the tile alike)
-  int vexp = 0;                                        // 2^vexp: running size of the value steps
+  int vexp[kNT][2];                                    // 2^vexp: running size of the value steps that the row has seen
   int back_first = 0, back_last = 0;                   // positions of the block's first and last query, back from the sequence's end
   bool from_start = false, later = false;              // the segment began with its list's first chunk; it is not the warp's first
 
   auto begin_segment = [&](const Item& it) {
     from_start = it.first;
-    vexp = -1000;
     back_first = a.n_q - it.rows0 / plan.group;
     back_last = a.n_q - (min(it.rows0 + plan.rows_per_block, plan.rows) - 1) / plan.group;
     const float sl = a.scale * 1.4426950408889634f;
@@ -363,6 +362,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         qsum[nt][j] = __shfl_sync(0xFFFFFFFFu, sr, 4 * (2 * qd + j));
         m[nt][j] = -INFINITY;
         l[nt][j] = esum[nt][j] = 0.f;
+        vexp[nt][j] = -1000;
       }
       usum[nt][0] = usum[nt][1] = usum[nt][2] = usum[nt][3] = 0.f;
 #pragma unroll
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     }
     // scaled, their largest per query row, and the largest value step
     float mx[kNT][2];
-    uint32_t vs[kTiles][2], vmax = 0;
+    uint32_t vs[kTiles][2], vmax[kMask ? kNT : 1][kMask ? 2 : 1] = {};   // largest value step: of all, or of those that a query sees
     uint32_t seen = 0;                                 // 4 bits per tile and 8 query rows, as s[i][nt]
     int pos_of[kNT][2];
     if (kMask) {
@@ -412,7 +412,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
       const float2 k1 = scale_floats<T>(*reinterpret_cast<const uint32_t*>(se + 32));
       vs[i][0] = *reinterpret_cast<const uint32_t*>(se + 4 * ps);
       vs[i][1] = *reinterpret_cast<const uint32_t*>(se + 4 * ps + 32);
-      uint32_t any = 0;
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -422,16 +421,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
           if (kMask) {
             const int t = it.t0 + i * 16 + g + (e >> 1) * 8, pos = pos_of[nt][e & 1];
             const bool v = t <= pos && ((it.there >> (i * 16 >> pl)) & 1) && (a.window == 0 || pos - t < a.window || t < a.sinks);
-            if (v) { seen |= 1u << ((i * kNT + nt) * 4 + e); any |= 1u << (e >> 1); }
-            else s[i][nt][e] = -INFINITY;
+            if (v) {
+              seen |= 1u << ((i * kNT + nt) * 4 + e);
+              vmax[kMask ? nt : 0][kMask ? e & 1 : 0] = max_pairs<T>(vmax[kMask ? nt : 0][kMask ? e & 1 : 0], vs[i][e >> 1]);
+            } else {
+              s[i][nt][e] = -INFINITY;
+            }
           }
           mx[nt][e & 1] = fmaxf(mx[nt][e & 1], s[i][nt][e]);
         }
-      if (kMask) {                                     // a token that none of this lane's rows sees: whatever lies there counts as zero
-        if (!(any & 1u)) vs[i][0] = 0;
-        if (!(any & 2u)) vs[i][1] = 0;
-      }
-      vmax = max_pairs<T>(vmax, max_pairs<T>(vs[i][0], vs[i][1]));
+      if (!kMask) vmax[0][0] = max_pairs<T>(vmax[0][0], max_pairs<T>(vs[i][0], vs[i][1]));
     }
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
@@ -440,25 +439,28 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         mx[nt][0] = fmaxf(mx[nt][0], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][0], o));
         mx[nt][1] = fmaxf(mx[nt][1], __shfl_xor_sync(0xFFFFFFFFu, mx[nt][1], o));
       }
-      vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, o));
+#pragma unroll
+      for (int nt = 0; nt < (kMask ? kNT : 1); ++nt)
+#pragma unroll
+        for (int j = 0; j < (kMask ? 2 : 1); ++j) vmax[nt][j] = max_pairs<T>(vmax[nt][j], __shfl_xor_sync(0xFFFFFFFFu, vmax[nt][j], o));
     }
-    if (kMask) {
-      vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, 1)); vmax = max_pairs<T>(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, 2));
-    }
-    const float vtop = scale_floats<T>(vmax).x;
-    const int ve = max(vexp, max(exponent(vtop), -100));
-    bool moved = ve != vexp;
+    int ve[kNT][2];
+    bool moved = false;
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) moved |= mx[nt][j] != m[nt][j];
+      for (int j = 0; j < 2; ++j) {
+        ve[nt][j] = max(vexp[nt][j], max(exponent(scale_floats<T>(vmax[kMask ? nt : 0][kMask ? j : 0]).x), -100));
+        moved |= mx[nt][j] != m[nt][j] || ve[nt][j] != vexp[nt][j];
+      }
     if (__any_sync(0xFFFFFFFFu, moved)) {
-      const float vshift = vexp < ve ? (vexp < ve - 100 ? 0.f : pow2i(vexp - ve)) : 1.f;
-      vexp = ve;
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          const int up = ve[nt][j] - vexp[nt][j];
+          const float vshift = up > 100 ? 0.f : pow2i(-up);
+          vexp[nt][j] = ve[nt][j];
           const float c = m[nt][j] == -INFINITY ? 0.f : ex2(m[nt][j] - mx[nt][j]), cv = c * vshift;
           m[nt][j] = mx[nt][j];
           l[nt][j] *= c; esum[nt][j] *= c; usum[nt][j] *= cv;
@@ -466,8 +468,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
           for (int t = 0; t < 2 * kWords; ++t) { acc[nt][t][j] *= cv; acc[nt][t][2 + j] *= cv; }
         }
     }
-    const float vscale = pow2i(min(13 - vexp, 120));
-    float mu[kNT][2];
+    float mu[kNT][2], vscale[kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) vscale[nt][j] = pow2i(min(13 - vexp[nt][j], 120));
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -478,7 +483,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     for (int i = 0; i < kTiles; ++i) {
       float2 v0 = scale_floats<T>(vs[i][0]), v1 = scale_floats<T>(vs[i][1]);
       v0.y = fmaf(7.5f, v0.x, v0.y); v1.y = fmaf(7.5f, v1.x, v1.y);
-      v0.x *= vscale; v1.x *= vscale;
       uint32_t b0[kNT], b1[kNT];
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt) {
@@ -487,7 +491,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         for (int e = 0; e < 4; ++e) {
           const float p = ex2(s[i][nt][e] - mu[nt][e & 1]);
           l[nt][e & 1] += p;
-          u[e] = p * (e < 2 ? v0.x : v1.x);
+          u[e] = p * ((e < 2 ? v0.x : v1.x) * vscale[nt][e & 1]);
           if (kMask) {
             const bool v = (seen >> ((i * kNT + nt) * 4 + e)) & 1u;
             if (!v) u[e] = 0.f;
@@ -523,7 +527,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
       if (from_start) where[0] = 2 * w + later;
       if (it.last) where[1] = w;
     }
-    const float back = pow2i(min(max(vexp - 13, -126), 127));
     float* slot = slots_of(a) + (2 * w + later) * slot_floats(plan, kDim);
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
@@ -537,6 +540,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         }
         const int rr = nt * 8 + 2 * qd + j, r = it.rows0 + rr;
         if (rr >= plan.rows_per_block || r >= plan.rows) continue;
+        const float back = pow2i(min(max(vexp[nt][j] - 13, -126), 127));
         const float add = et - 7.5f * usum[nt][j] * back, norm = whole ? (lt == 0.f ? 0.f : 1.f / lt) : 1.f;
         float o[kDim / 8];                             // values (kDim / 8) g .. of the row
 #pragma unroll

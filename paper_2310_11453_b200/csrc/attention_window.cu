@@ -19,8 +19,9 @@
 // formed at 2^7 times their size, 2^15 at most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
 //
 // Invisible places.  A masked score is replaced, so keys there may be anything.  A value there meets a probability
-// of 0, but 0 x NaN is NaN: a row whose result is not finite is computed again by one warp from the visible
-// places alone (window_row).  Finite inputs never take that path.
+// of 0, but 0 x NaN is NaN: values behind a sequence's end are cleared in shared memory, and a row whose result is not
+// finite although its sum is, is computed again by one warp from the visible places alone (window_row).  Finite values
+// never take that path.
 //
 // Every wait is bounded.  If one runs out, the CTA's rows are computed by window_row too and the event is
 // counted (bitlinear_debug_window_fallbacks): the result is the same up to rounding, only late.
@@ -379,6 +380,16 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       auto pv = [&](int i, int ev) -> bool {                   // O += P(i) V of ring entry ev
         const int slot = ev % kSlots;
         if (!wait(&ctl->kv_full[slot], (ev / kSlots) & 1)) return false;
+        // Rows behind the sequence's last key (padding, or another sequence) meet probabilities of 0: they become zeros, so that
+        // whatever they hold stays out of O.  Both warps do so, each before its own products.
+        const int there = job.r.nk - job.key0(ev >> 1);
+        if (there < kKeys) {
+          for (int s = 0; s < kSubs; ++s)
+            for (int c = there * 8 + lane; c < kKeys * 8; c += 32)
+              *reinterpret_cast<uint4*>(ring + slot * kTileBytes + s * kSub + c * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
         if (!wait(&ctl->p_ready[t][i & 1], (i >> 1) & 1)) return false;
         tc_fence_after();
         const uint64_t dv = desc_mn(ring_at + slot * kTileBytes);
@@ -497,7 +508,8 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(o + c + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         }
       }
-      unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f));
+      // (a sum l that is not finite comes from scores that are seen: the row's result is NaN by definition)
+      unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f) && l - l == 0.f);
       while (bad) {
         const int i = __ffs(bad) - 1;
         bad &= bad - 1;

@@ -227,9 +227,9 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor &k = tensor(a[5], "k"), &v = tensor(a[6], "v"), &slots = tensor(a[7], "slots");
     const int64_t T = k.dim() > 0 ? k.size(0) : 0;
     const int64_t ld_k = rows_of(k, "k", c.dev, c.type, T, c.width), ld_v = rows_of(v, "v", c.dev, c.type, T, c.width);
-    void* at = flat(slots, "slots", c.dev, at::kLong, T);
+    void* sp = flat(slots, "slots", c.dev, at::kLong, T);
     const c10::cuda::CUDAGuard guard(c.dev);
-    const bl_status st = entry.append(&c.c, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, (const int64_t*)at, stream_of(c.dev));
+    const bl_status st = entry.append(&c.c, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, (const int64_t*)sp, stream_of(c.dev));
     if (st != BL_OK) return status(st);
     Py_RETURN_NONE;
   });
@@ -247,8 +247,8 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor k = a[6] == Py_None ? at::zeros({T, c.width}, options) : tensor(a[6], "k");
     const Tensor v = a[7] == Py_None ? at::zeros({T, c.width}, options) : tensor(a[7], "v");
     const int64_t ld_k = rows_of(k, "k", c.dev, c.type, T, c.width), ld_v = rows_of(v, "v", c.dev, c.type, T, c.width);
-    void* at = flat(slots, "slots", c.dev, at::kLong, T);
-    const bl_status st = entry.read(&c.c, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, (const int64_t*)at, stream_of(c.dev));
+    void* sp = flat(slots, "slots", c.dev, at::kLong, T);
+    const bl_status st = entry.read(&c.c, k.data_ptr(), v.data_ptr(), T, ld_k, ld_v, (const int64_t*)sp, stream_of(c.dev));
     if (st != BL_OK) return status(st);
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();

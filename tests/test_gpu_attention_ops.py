@@ -276,6 +276,22 @@ def test_attention_kv4_of_what_it_must_not_see():
     assert torch.isfinite(B.attention_kv4(q, cache2, table2, torch.tensor([18], device=DEV).int(), 1, 2, heads)).all()
 
 
+@pytest.mark.parametrize("dt,big", [(F16, 60000.0), (BF16, 1e30)])
+def test_attention_kv4_huge_values_of_a_later_token(dt, big):
+    """The last drafted token's values are huge: the queries before it are as if it were not there."""
+    hk, g, dim, page, n, n_q = 1, 2, 128, 32, 200, 3
+    cache, table = fill(1, [n], page, hk, dim, dt, seed=11)
+    q = randn(2, n_q, g * hk * dim, dtype=dt)
+    at = table[0, (n - 1) // page].long().view(1) * page + (n - 1) % page
+    B.kv4_append(cache, randn(3, 1, hk * dim, dtype=dt), randn(4, 1, hk * dim, dtype=F32).mul(big / 4).clamp(-big, big).to(dt), at)
+    lens = torch.tensor([n], device=DEV).int()
+    o = B.attention_kv4(q, cache, table, lens, 1, n_q, g * hk)
+    check_kv4(q, cache, table, [n], 1, n_q, g * hk, 0, 0, 0.0, o)
+    short = B.attention_kv4(q[:2], cache, table, lens - 1, 1, 2, g * hk)
+    check_kv4(q[:2], cache, table, [n - 1], 1, 2, g * hk, 0, 0, 0.0, short)
+    assert (o[:2].double() - short.double()).abs().max() <= 4 * R.half_step(dt) * float(short.abs().max())
+
+
 def test_attention_kv4_in_a_graph_and_on_two_streams():
     hk, g, dim, page, dt, batch = 4, 4, 128, 32, F16, 3
     heads = hk * g
@@ -473,6 +489,27 @@ def test_attention_window_of_what_it_must_not_see(dt, dim):
             assert (err <= 4 * R.half_step(dt) * v.abs().max().double()).all()
             if math.isnan(bad):
                 assert torch.isnan(got[seen]).all()
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_attention_window_rows_of_padding_hold_anything(dt):
+    """Rows between and behind the sequences are never initialised: NaN and infinities there change nothing."""
+    heads, hk, dim = 4, 2, 128
+    q0, lens = [0, 150, 400], [130, 193, 57]
+    rows = 600
+    q, k, v = (randn(i, rows, w * dim, dtype=dt) for i, w in ((1, heads), (2, hk), (3, hk)))
+    inside = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    for a, n in zip(q0, lens):
+        inside[a:a + n] = True
+    for x, bad in ((q, math.nan), (k, math.inf), (v, math.nan)):
+        x[~inside] = bad
+    for a, n in zip(q0, lens):                                        # one sequence at a time: cu need not be contiguous
+        cu = torch.tensor([a, a + n], device=DEV, dtype=torch.int32)
+        o = B.attention_window(q, k, v, 1, n, heads, hk, dim, window=70, sinks=2, cu_q=cu, o=torch.full_like(q, 3.0))
+        check_window(q, k, v, o, [(a, n, a, n)], heads, hk, dim, 70, 2)
+        keep = torch.ones(rows, dtype=torch.bool, device=DEV)
+        keep[a:a + n] = False
+        assert (o[keep] == 3.0).all()
 
 
 def test_attention_window_agrees_with_the_causal_core():
