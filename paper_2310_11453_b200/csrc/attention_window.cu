@@ -1,22 +1,23 @@
 // Attention of prompts with a sliding window and sinks (bitlinear_attention_window):
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = e^(scale q_i . k_j - max),  j visible from i.
 //
-// A CTA owns two tiles of 128 query rows: the same rows of two heads that share their keys (even group sizes), or
-// two consecutive tiles of one head.  Keys and values pass through shared memory in tiles of 64, once for both
-// tiles; tiles that no row sees (after the rows, or between the sinks and the window) are not loaded.  Per query and
-// key tile two products of 128 x 64 x kDim run on the tcgen05 tensor cores,
+// A CTA owns a tile of 128 query rows of one head; two CTAs share an SM, so that one's softmax, copies, start and end
+// run beside the other's products.  Keys and values pass through shared memory in tiles of 64; tiles that no row sees
+// (after the rows, or between the sinks and the window) are not loaded.  Per key tile two products of 128 x 64 x kDim
+// run on the tcgen05 tensor cores,
 //   S = Q K^T   both operands in shared memory (TMA, 128-byte swizzle), S in tensor memory (fp32),
 //   O += P V    P in tensor memory as 16-bit numbers, over S; V as it lies in memory (its rows are the
 //               contraction, so the descriptor says MN-major); O in tensor memory (fp32).
-// Each query tile has two places for S: while the softmax works on S(i), S(i+1) is being formed or is there already,
-// so that it never waits for a product.  A thread's products run in issue order S(i+1), PV(i), S(i+2), .., which is what
-// keeps S(i+2) from overwriting P(i).  With one place of 128 keys the same kernel took 1.6 times as long: a tile's
-// softmax (1900 clocks) and products (1700 with their latencies) then take turns.
+// There are two places for S: while the softmax works on S(i), S(i+1) is being formed or is there already.  The products
+// run in issue order S(i+1), PV(i), S(i+2), .., which is what keeps S(i+2) from overwriting P(i).  With one place of 128
+// keys the softmax (1900 clocks) and the products (1700 with their latencies) took turns: 1.6 times as long.  Two query
+// tiles in one CTA per SM share the loads of a group's keys, but run in step: 3 % faster on one prompt of 8192 with a
+// window of 4096 (372 against 380 us), 5 to 20 % slower on shorter prompts and windows and with heads of 64.
 //
-// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1 (a thread owns a query row: no shuffles), warps 8 and 10 issue
-// the products of tile 0 and 1, warp 9 the copies.  The running maximum moves only when a row's maximum grew by more
-// than 2^8: O is then rescaled in tensor memory, which is rare; else probabilities of up to 2^8 do no harm (they are
-// formed at 2^7 times their size, 2^15 at most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
+// Roles: warps 0-3 the softmax (a thread owns a query row: no shuffles), warp 4 issues the products, warp 5 the
+// copies.  The running maximum moves only when a row's maximum grew by more than 2^8: O is then rescaled in tensor
+// memory, which is rare; else probabilities of up to 2^8 do no harm (they are formed at 2^7 times their size, 2^15 at
+// most, so that the smallest fp16 probability is 2^-31 of a row's largest or less).
 //
 // Invisible places.  A masked score is replaced, so keys there may be anything.  A value there meets a probability
 // of 0, but 0 x NaN is NaN: values behind a sequence's end are cleared in shared memory, and a row whose result is not
@@ -83,15 +84,16 @@ __device__ void window_row(const WindowArgs& a, const SeqRows& r, int i, int h) 
   for (int e = 0; e < kVals; ++e) o[e] = out_cast<T>(l == 0.f ? 0.f : acc[e] / l);
 }
 
-constexpr int kRows = 128;                       // query rows per tile
+constexpr int kRows = 128;                       // query rows per CTA
 constexpr int kKeys = 64;                        // keys per tile
-constexpr int kSlots = 8;                        // key or value tiles in shared memory
-constexpr int kThreads = 384;
+constexpr int kMostSlots = 8;                    // key or value tiles in shared memory
+constexpr int kThreads = 192, kIssuer = 4, kCopier = 5;
+constexpr int kTmemCols = 256;                   // two places for S (64 columns each), O (128)
 constexpr float kMoveLog2 = 8.f;                 // growth of a row's maximum that is let pass
 constexpr float kLiftLog2 = 7.f;                 // probabilities are formed 2^7 times their size
 
 struct Ctl {
-  unsigned long long q_full[2], kv_full[kSlots], kv_empty[kSlots], s_full[2][2], p_ready[2][2], o_done[2][2], drain[2];   // [tile][place]
+  unsigned long long q_full, kv_full[kMostSlots], kv_empty[kMostSlots], s_full[2], p_ready[2], o_done[2], drain;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -214,58 +216,33 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, f
 }
 
 // What a CTA works on; every role derives the same.
-struct Span {                                    // a tile
-  int head, row0, rows, pos0, pos1;              // head, first query row of the sequence, rows (0: none), their positions
-  int from, to;                                  // key tiles of its window: from .. to (and those that hold sinks)
-  int clean_from, clean_to;                      // those that every row sees as a whole: clean_from .. clean_to - 1
-};
 struct Job {
   SeqRows r;
-  Span tile[2];
+  int head, row0, rows, pos0, pos1;              // head, first query row of the sequence, rows (0: none), their positions
   int sink_tiles, first, count;                  // key tiles: those of the sinks, then `first` on
-  int sink_end;                                  // key tiles before this one hold sinks
-  int window, sinks;
+  int clean_from, clean_to;                      // those that every row sees as a whole (tiles of nothing but sinks are not counted in)
   __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kKeys; }
-  // does a row of the tile see a key of key tile j?
-  __device__ __forceinline__ bool active(const Span& s, int j) const { return j <= s.to && (j >= s.from || j < sink_end); }
-  // does every row of the tile see every key of key tile j?  (Tiles of nothing but sinks are not counted in.)
-  __device__ __forceinline__ bool clean(const Span& s, int j) const { return j >= s.clean_from && j < s.clean_to; }
 };
-// two_heads: the two tiles are two heads' (same rows), else consecutive rows of one head.  Blocks with the most keys first.
-__device__ __forceinline__ Job make_job(const WindowArgs& a, bool two_heads) {
+// Blocks with the most keys first; the heads of a group side by side, so that they find their keys in L2.
+__device__ __forceinline__ Job make_job(const WindowArgs& a) {
   Job w;
-  const int units = two_heads ? a.heads / 2 : a.heads, per = two_heads ? kRows : 2 * kRows;
-  const int blocks = (int)((a.seq_q + per - 1) / per);
-  const int u = blockIdx.x % units, rest = blockIdx.x / units, b = rest % a.batch, blk = blocks - 1 - rest / a.batch;
+  const int blocks = (int)((a.seq_q + kRows - 1) / kRows);
+  const int rest = blockIdx.x / a.heads, b = rest % a.batch;
+  w.head = blockIdx.x - rest * a.heads;
   w.r = seq_rows(a, b);
-  w.window = a.window; w.sinks = a.sinks;
-  int lo = 0x7FFFFFFF, hi = 0;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    Span& s = w.tile[t];
-    s.head = two_heads ? 2 * u + t : u;
-    s.row0 = blk * per + (two_heads ? 0 : t * kRows);
-    s.rows = min(max(w.r.nq - s.row0, 0), kRows);
-    s.pos0 = w.r.nk - w.r.nq + s.row0;
-    s.pos1 = s.pos0 + s.rows - 1;
-    if (s.rows > 0 && s.pos1 >= 0) {
-      lo = min(lo, a.window > 0 ? max(0, s.pos0 - a.window + 1) : 0);
-      hi = max(hi, s.pos1 + 1);
-    }
-  }
-  if (hi == 0) lo = 0;
-  w.first = lo / kKeys;
-  w.sink_tiles = min((min(a.sinks, lo) + kKeys - 1) / kKeys, w.first);
-  w.count = hi == 0 ? 0 : w.sink_tiles + (hi + kKeys - 1) / kKeys - w.first;
-  w.sink_end = w.sink_tiles + max(0, (min(a.sinks, hi) + kKeys - 1) / kKeys - w.first);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    Span& s = w.tile[t];
-    const bool sees = s.rows > 0 && s.pos1 >= 0;
-    s.from = sees ? w.sink_tiles + (a.window > 0 ? max(0, s.pos0 - a.window + 1) : 0) / kKeys - w.first : 0;
-    s.to = sees ? w.sink_tiles + s.pos1 / kKeys - w.first : -1;
-    s.clean_from = w.sink_tiles + max((a.window > 0 ? max(0, s.pos1 - a.window + kKeys) : 0) / kKeys - w.first, 0);
-    s.clean_to = w.sink_tiles + (s.pos0 >= 0 ? (s.pos0 + 1) / kKeys - w.first : 0);
+  w.row0 = (blocks - 1 - rest / a.batch) * kRows;
+  w.rows = min(max(w.r.nq - w.row0, 0), kRows);
+  w.pos0 = w.r.nk - w.r.nq + w.row0;
+  w.pos1 = w.pos0 + w.rows - 1;
+  w.sink_tiles = w.first = w.count = w.clean_from = w.clean_to = 0;
+  if (w.rows > 0 && w.pos1 >= 0) {
+    const int lo = a.window > 0 ? max(0, w.pos0 - a.window + 1) : 0;      // first key of the first row's window
+    w.first = lo / kKeys;
+    w.sink_tiles = min((min(a.sinks, lo) + kKeys - 1) / kKeys, w.first);
+    w.count = w.sink_tiles + w.pos1 / kKeys + 1 - w.first;
+    const int all_from = a.window > 0 ? max(0, w.pos1 - a.window + 1) : 0;   // first key of the last row's window
+    w.clean_from = w.sink_tiles + (all_from + kKeys - 1) / kKeys - w.first;
+    w.clean_to = w.sink_tiles + (w.pos0 >= 0 ? (w.pos0 + 1) / kKeys - w.first : 0);
   }
   return w;
 }
@@ -299,61 +276,57 @@ __device__ __forceinline__ f32x2 exponentials(const float (&s)[kKeys], float sl,
   return add2(l0, l1);
 }
 
+template <int kDim> constexpr int kSlotsOf = kDim == 64 ? 8 : 4;   // two CTAs fit an SM
+
 template <typename T, int kDim>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                        const __grid_constant__ CUtensorMap map_v, WindowArgs a, int two_heads, uint32_t polls) {
+                        const __grid_constant__ CUtensorMap map_v, WindowArgs a, uint32_t polls) {
+  constexpr int kSlots = kSlotsOf<kDim>;
   constexpr int kSubs = kDim / 64;               // a tile is kSubs sub-tiles of 64 values per row (128 bytes)
   constexpr int kQSub = kRows * 128, kQBytes = kSubs * kQSub, kSub = kKeys * 128, kTileBytes = kSubs * kSub;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  unsigned char* sq = smem;                      // two query tiles, then the ring
-  unsigned char* ring = smem + 2 * kQBytes;
+  unsigned char* sq = smem;                      // the query tile, then the ring
+  unsigned char* ring = smem + kQBytes;
   Ctl* ctl = reinterpret_cast<Ctl*>(ring + kSlots * kTileBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&ctl->q_full[t]), 1);
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(smem_u32(&ctl->s_full[t][i]), 1);
-        mbar_init(smem_u32(&ctl->p_ready[t][i]), 4);
-        mbar_init(smem_u32(&ctl->o_done[t][i]), 1);
-      }
-      mbar_init(smem_u32(&ctl->drain[t]), 1);
+    mbar_init(smem_u32(&ctl->q_full), 1);
+    mbar_init(smem_u32(&ctl->drain), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&ctl->s_full[i]), 1);
+      mbar_init(smem_u32(&ctl->p_ready[i]), 4);
+      mbar_init(smem_u32(&ctl->o_done[i]), 1);
     }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&ctl->kv_full[s]), 1);
-      mbar_init(smem_u32(&ctl->kv_empty[s]), 2);       // both tiles
+      mbar_init(smem_u32(&ctl->kv_empty[s]), 1);
     }
     ctl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512) : "memory");
+  if (warp == kIssuer) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;          // two places for S of tile 0, of tile 1 (64 columns each), O of tile 0, of tile 1
+  const uint32_t tmem = ctl->tmem_base, t_s = tmem, t_o = tmem + 2 * kKeys;
   pdl_wait();
-  const Job job = make_job(a, two_heads != 0);
+  const Job job = make_job(a);
 
-  if (warp >= 8) {
-    if (warp == 9 && lane == 0 && job.count > 0) {             // ---- copies
+  if (warp == kCopier) {                                       // ---- copies
+    if (lane == 0 && job.count > 0) {
       int issued = 0;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (job.tile[t].rows == 0) continue;
-        mbar_arrive_expect_tx(smem_u32(&ctl->q_full[t]), kQBytes);
-        for (int s = 0; s < kSubs; ++s)
-          tma_load_2d(smem_u32(sq + t * kQBytes + s * kQSub), &map_q, job.tile[t].head * kDim + 64 * s, job.r.q0 + job.tile[t].row0,
-                      smem_u32(&ctl->q_full[t]));
-      }
-      const int hk = job.tile[0].head / (a.heads / a.kv_heads);
+      mbar_arrive_expect_tx(smem_u32(&ctl->q_full), kQBytes);
+      for (int s = 0; s < kSubs; ++s)
+        tma_load_2d(smem_u32(sq + s * kQSub), &map_q, job.head * kDim + 64 * s, job.r.q0 + job.row0, smem_u32(&ctl->q_full));
+      const int hk = job.head / (a.heads / a.kv_heads);
       for (int e = 0; e < 2 * job.count; ++e) {                // entry 2 j: keys of tile j; 2 j + 1: its values
         const int slot = e % kSlots;
         if (e >= kSlots && !wait_for(&ctl->kv_empty[slot], ((e / kSlots) - 1) & 1, abort_flag, polls)) break;
@@ -363,26 +336,22 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                       job.r.k0 + job.key0(e >> 1), smem_u32(&ctl->kv_full[slot]));
         issued = e + 1;
       }
-      // Copies end before the CTA does, also those of a tile that turned out to see nothing, and after a wait ran out.
-      int gave_up = 0;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (job.tile[t].rows > 0) wait_for(&ctl->q_full[t], 0, &gave_up, kSpinLimit);
+      int gave_up = 0;                                         // copies end before the CTA does, also after a wait ran out
+      wait_for(&ctl->q_full, 0, &gave_up, kSpinLimit);
       for (int e = max(0, issued - kSlots); e < issued; ++e) wait_for(&ctl->kv_full[e % kSlots], (e / kSlots) & 1, &gave_up, kSpinLimit);
-    } else if ((warp == 8 || warp == 10) && job.count > 0) {   // ---- products of tile 0, of tile 1 (the whole warp; one lane issues)
+    }
+  } else if (warp == kIssuer) {                                // ---- products (the whole warp; one lane issues)
+    if (job.count > 0) {
       constexpr uint32_t kIdS = idesc<T>(kKeys, false), kIdO = idesc<T>(kDim, true);
-      const int t = (warp - 8) >> 1;
-      const Span span = t ? job.tile[1] : job.tile[0];
-      const uint32_t on = elect(), ring_at = smem_u32(ring), ts = tmem + t * 2 * kKeys, to = tmem + 4 * kKeys + t * 128;
-      const uint64_t dq = smem_desc_sw128(smem_u32(sq + t * kQBytes));
+      const uint32_t on = elect(), ring_at = smem_u32(ring);
+      const uint64_t dq = smem_desc_sw128(smem_u32(sq));
       auto wait = [&](unsigned long long* bar, uint32_t parity) { return wait_warp(bar, parity, abort_flag, polls); };
-      int n = 0, v_before = 0;                                 // key tiles taken; ring entry of the last one's values
-      auto pv = [&](int i, int ev) -> bool {                   // O += P(i) V of ring entry ev
-        const int slot = ev % kSlots;
+      auto pv = [&](int j) -> bool {                           // O += P(j) V(j)
+        const int ev = 2 * j + 1, slot = ev % kSlots;
         if (!wait(&ctl->kv_full[slot], (ev / kSlots) & 1)) return false;
         // Rows behind the sequence's last key (padding, or another sequence) meet probabilities of 0: they become zeros, so that
-        // whatever they hold stays out of O.  Both warps do so, each before its own products.
-        const int there = job.r.nk - job.key0(ev >> 1);
+        // whatever they hold stays out of O.
+        const int there = job.r.nk - job.key0(j);
         if (there < kKeys) {
           for (int s = 0; s < kSubs; ++s)
             for (int c = there * 8 + lane; c < kKeys * 8; c += 32)
@@ -390,75 +359,65 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           fence_proxy_async_smem();
           __syncwarp();
         }
-        if (!wait(&ctl->p_ready[t][i & 1], (i >> 1) & 1)) return false;
+        if (!wait(&ctl->p_ready[j & 1], (j >> 1) & 1)) return false;
         tc_fence_after();
         const uint64_t dv = desc_mn(ring_at + slot * kTileBytes);
-        const uint32_t tp = ts + (i & 1) * kKeys, more = i > 0;
+        const uint32_t tp = t_s + (j & 1) * kKeys, more = j > 0;
 #pragma unroll
         for (int k = 0; k < kKeys / 16; ++k)                   // 16 keys: 8 columns of P, 2048 bytes of V
-          mma_ts(on, to, tp + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, k > 0 ? 1u : more);
-        commit(on, &ctl->o_done[t][i & 1]);
+          mma_ts(on, t_o, tp + 8 * k, dv + (uint64_t)(k * (2048 >> 4)), kIdO, k > 0 ? 1u : more);
+        commit(on, &ctl->o_done[j & 1]);
         commit(on, &ctl->kv_empty[slot]);
         return true;
       };
-      bool ok = span.to < 0 || wait(&ctl->q_full[t], 0);
+      bool ok = wait(&ctl->q_full, 0);
       for (int j = 0; j < job.count && ok; ++j) {
-        const int ek = 2 * j, ev = ek + 1, slot = ek % kSlots;
-        if (!job.active(span, j)) {                            // only the other tile takes it
-          ok = wait(&ctl->kv_full[slot], (ek / kSlots) & 1) && wait(&ctl->kv_full[ev % kSlots], (ev / kSlots) & 1);
-          if (ok && lane == 0) { mbar_arrive(smem_u32(&ctl->kv_empty[slot])); mbar_arrive(smem_u32(&ctl->kv_empty[ev % kSlots])); }
-          continue;
-        }
+        const int ek = 2 * j, slot = ek % kSlots;
         if (!(ok = wait(&ctl->kv_full[slot], (ek / kSlots) & 1))) break;
         const uint64_t dk = smem_desc_sw128(ring_at + slot * kTileBytes);
 #pragma unroll
         for (int k = 0; k < kDim / 16; ++k)                    // 16 values: 32 bytes within a sub-tile's rows
-          mma_ss(on, ts + (n & 1) * kKeys, dq + (uint64_t)(((k / 4) * kQSub + (k % 4) * 32) >> 4),
+          mma_ss(on, t_s + (j & 1) * kKeys, dq + (uint64_t)(((k / 4) * kQSub + (k % 4) * 32) >> 4),
                  dk + (uint64_t)(((k / 4) * kSub + (k % 4) * 32) >> 4), kIdS, k > 0);
-        commit(on, &ctl->s_full[t][n & 1]);
+        commit(on, &ctl->s_full[j & 1]);
         commit(on, &ctl->kv_empty[slot]);
-        if (n > 0) ok = pv(n - 1, v_before);
-        v_before = ev;
-        ++n;
+        if (j > 0) ok = pv(j - 1);
       }
-      if (ok && n > 0) pv(n - 1, v_before);
+      if (ok) pv(job.count - 1);
       int gave_up = 0;                                         // products, and the arrivals they owe, end before the CTA does
-      commit(on, &ctl->drain[t]);
-      wait_for(&ctl->drain[t], 0, &gave_up, kSpinLimit);
+      commit(on, &ctl->drain);
+      wait_for(&ctl->drain, 0, &gave_up, kSpinLimit);
     }
-  } else {
-    const int t = warp >> 2, row = threadIdx.x & 127;          // the tile, and this thread's row of it
-    const Span span = t ? job.tile[1] : job.tile[0];
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * 2 * kKeys + lanes, to = tmem + 4 * kKeys + t * 128 + lanes;
+  } else {                                                     // ---- softmax and output
+    const int row = threadIdx.x;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16, ts = t_s + lanes, to = t_o + lanes;
     const float sl = a.scale * 1.4426950408889634f;
-    const int pos = span.pos0 + row, key_end = min(pos, job.r.nk - 1);
+    const int pos = job.pos0 + row, key_end = min(pos, job.r.nk - 1);
     float m = -INFINITY, l = 0.f;                              // running maximum (raw score) and sum of the row
-    int n = 0;                                                 // key tiles taken
     bool ok = true;
-    // PV(n - 1) is complete.  Two barriers in turn: PV(n - 3), the one before on the same barrier, is complete for certain
-    // (S(n - 1) was issued behind it), PV(n - 2) is not.
-    auto o_ready = [&]() -> bool {
-      const bool r = wait_warp(&ctl->o_done[t][(n - 1) & 1], ((n - 1) >> 1) & 1, abort_flag, polls);
+    // PV(j) is complete.  Two barriers in turn: PV(j - 2), the one before on the same barrier, is complete for certain
+    // (S(j), which the caller has seen, was issued behind it), PV(j - 1) is not.
+    auto o_ready = [&](int j) -> bool {
+      const bool r = wait_warp(&ctl->o_done[j & 1], (j >> 1) & 1, abort_flag, polls);
       tc_fence_after();
       return r;
     };
     for (int j = 0; j < job.count; ++j) {
-      if (!job.active(span, j)) continue;
-      const bool clean = job.clean(span, j);
       const int k0 = job.key0(j);
-      const uint32_t at = ts + (n & 1) * kKeys;
-      if (!(ok = wait_warp(&ctl->s_full[t][n & 1], (n >> 1) & 1, abort_flag, polls))) break;
+      const uint32_t at = ts + (j & 1) * kKeys;
+      if (!(ok = wait_warp(&ctl->s_full[j & 1], (j >> 1) & 1, abort_flag, polls))) break;
       tc_fence_after();
       float s[kKeys];
       ld32(at, s);
       ld32(at + 32, s + 32);
       ld_wait(s);
       ld_wait(s + 32);
-      if (!clean) mask_scores(s, key_end - k0, a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, a.sinks - k0);
+      if (j < job.clean_from || j >= job.clean_to)
+        mask_scores(s, key_end - k0, a.window > 0 ? pos - a.window + 1 - k0 : -0x40000000, a.sinks - k0);
       const float mx = largest(s);
       const bool move = m > -INFINITY && (mx - m) * sl > kMoveLog2;
       if (__any_sync(0xFFFFFFFFu, move)) {                     // O of the tiles so far takes the new maximum
-        if (!(ok = o_ready())) break;
+        if (!(ok = o_ready(j - 1))) break;
         const float f = move ? ex2((m - mx) * sl) : 1.f;
         l *= f;
 #pragma unroll
@@ -479,20 +438,18 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[t][n & 1]));
-      ++n;
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[j & 1]));
     }
-    // ---- output
-    if (ok && n > 0) ok = o_ready();
+    if (ok && job.count > 0) ok = o_ready(job.count - 1);
     if (ok) {
-      const bool mine = row < span.rows;
+      const bool mine = row < job.rows;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + span.row0 + row) * a.ld_o + (int64_t)span.head * kDim;
+      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + job.row0 + row) * a.ld_o + (int64_t)job.head * kDim;
       float check = 0.f;
 #pragma unroll
       for (int c = 0; c < kDim; c += 32) {
         float v[32];
-        if (n > 0) {
+        if (job.count > 0) {
           ld32(to + c, v);
           ld_wait(v);
         }
@@ -513,20 +470,16 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       while (bad) {
         const int i = __ffs(bad) - 1;
         bad &= bad - 1;
-        window_row<T, kDim>(a, job.r, span.row0 + (warp & 3) * 32 + i, span.head);
+        window_row<T, kDim>(a, job.r, job.row0 + warp * 32 + i, job.head);
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   if (*abort_flag) {
     if (threadIdx.x == 0) atomicAdd(&g_window_fallbacks, 1u);
-#pragma unroll 1
-    for (int t = 0; t < 2; ++t) {
-      const Span span = t ? job.tile[1] : job.tile[0];
-      for (int i = warp; i < span.rows; i += kThreads / 32) window_row<T, kDim>(a, job.r, span.row0 + i, span.head);
-    }
+    for (int i = warp; i < job.rows; i += kThreads / 32) window_row<T, kDim>(a, job.r, job.row0 + i, job.head);
   }
 }
 
@@ -543,8 +496,8 @@ template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t row
 
 template <typename T, int kDim>
 cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
-  constexpr size_t kSmem = (size_t)(2 * kRows + kSlots * kKeys) * kDim * 2 + 1024 + sizeof(Ctl);
-  static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
+  constexpr size_t kSmem = (size_t)(kRows + kSlotsOf<kDim> * kKeys) * kDim * 2 + 1024 + sizeof(Ctl);
+  static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs exceed the shared memory of an SM");
   static std::atomic<uint64_t> ready{0};         // devices on which the kernel's shared memory limit is set
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -563,12 +516,10 @@ cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
   } else {
     mk = mv = mq;                                // no key anywhere: never used
   }
-  const bool two_heads = (a.heads / a.kv_heads) % 2 == 0;
-  const int64_t per = two_heads ? kRows : 2 * kRows;
-  const int64_t grid = (a.seq_q + per - 1) / per * a.batch * (two_heads ? a.heads / 2 : a.heads);
+  const int64_t grid = (a.seq_q + kRows - 1) / kRows * a.batch * a.heads;
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
   const uint32_t polls = dbg < 0 ? kSpinLimit : (uint32_t)(dbg < (long long)kSpinLimit ? dbg : kSpinLimit);
-  return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, two_heads ? 1 : 0, polls);
+  return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, polls);
 }
 
 }  // namespace
