@@ -549,6 +549,96 @@ def test_attention_window_when_its_waits_run_out():
     assert B.debug_window_fallbacks() == 0
 
 
+def test_calls_with_nothing_to_do():
+    dt, hk, dim, page = F16, 2, 64, 16
+    cache = B.Kv4Cache.empty(2, page, hk, dim, dt, DEV)
+    none = torch.empty((0, hk * dim), device=DEV, dtype=dt)
+    at = torch.empty(0, device=DEV, dtype=torch.int64)
+    B.kv4_append(cache, none, none, at)
+    assert B.kv4_read(cache, at)[0].shape == (0, hk * dim)
+    lens = torch.zeros(3, device=DEV, dtype=torch.int32)
+    q = randn(1, 3, 2 * hk * dim, dtype=dt)
+    assert not B.attention_kv4(q, cache, torch.empty((3, 0), device=DEV, dtype=torch.int32), lens + 5, 3, 1, 2 * hk).any()
+    assert not B.attention_kv4(q, cache, torch.zeros((3, 2), device=DEV, dtype=torch.int32), lens, 3, 1, 2 * hk).any()
+    assert B.attention_kv4(q[:0], cache, torch.empty((0, 2), device=DEV, dtype=torch.int32), lens[:0], 0, 1, 2 * hk).shape == (0, 2 * hk * dim)
+    assert B.attention_window(q[:0], none, none, 0, 0, 2 * hk, hk, dim).shape == (0, 2 * hk * dim)
+    assert not B.attention_window(q, none, none, 3, 1, 2 * hk, hk, dim, seq_k=0).any()          # queries, and not a key
+    empty = B.Kv4Cache.empty(0, page, hk, dim, dt, DEV)
+    B.kv4_append(empty, q[:, :hk * dim], q[:, :hk * dim], torch.zeros(3, device=DEV, dtype=torch.int64))
+    assert not B.attention_kv4(q, empty, torch.zeros((3, 1), device=DEV, dtype=torch.int32), lens + 1, 3, 1, 2 * hk).any()
+    B.kv4_copy_pages(empty.pages, torch.zeros((1, 2), device=DEV, dtype=torch.int32))
+
+
+def test_arguments_that_do_not_fit_each_other_are_refused():
+    dt, hk, dim, page = F16, 2, 64, 16
+    cache = B.Kv4Cache.empty(4, page, hk, dim, dt, DEV)
+    k, at = randn(1, 3, hk * dim, dtype=dt), torch.arange(3, device=DEV)
+    table, lens, q = torch.zeros((3, 2), device=DEV, dtype=torch.int32), torch.ones(3, device=DEV, dtype=torch.int32), randn(2, 3, 2 * hk * dim, dtype=dt)
+    pos, freq = torch.zeros(3, device=DEV, dtype=torch.int32), torch.ones(32, device=DEV)
+    for bad in (lambda: B.kv4_append(cache, k, k[:2], at), lambda: B.kv4_append(cache, k, k, at[:2]), lambda: B.kv4_append(cache, k, k, at.cpu()),
+                lambda: B.kv4_append(cache, k.t().contiguous().t(), k, at), lambda: B.kv4_read(cache, at, k=k[:, :64]),
+                lambda: B.attention_kv4(q[:2], cache, table, lens, 3, 1, 2 * hk), lambda: B.attention_kv4(q, cache, table[:2], lens, 3, 1, 2 * hk),
+                lambda: B.attention_kv4(q, cache, table.t(), lens, 3, 1, 2 * hk), lambda: B.attention_kv4(q, cache, table, lens[:2], 3, 1, 2 * hk),
+                lambda: B.attention_window(q, k, k[:2], 1, 3, 2 * hk, hk, dim), lambda: B.attention_window(q, k, k, 1, 3, 2 * hk, hk, dim, cu_q=pos),
+                lambda: B.qk_norm_rope(q, k, pos[:2], freq, 2 * hk, hk, dim), lambda: B.qk_norm_rope(q, k, pos, freq, 2 * hk, hk, 2 * dim),
+                lambda: B.kv4_copy_pages(cache.pages, table[:, :1]), lambda: B.kv4_copy_pages(cache.pages[:, :16], table)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: B.kv4_append(cache, k.float(), k, at), lambda: B.kv4_append(cache, k, k, at.int()), lambda: B.kv4_append(cache, None, k, at),
+                lambda: B.attention_kv4(q.bfloat16(), cache, table, lens, 3, 1, 2 * hk), lambda: B.attention_kv4(q, cache, table.long(), lens, 3, 1, 2 * hk),
+                lambda: B.attention_window(q, k.float(), k, 1, 3, 2 * hk, hk, dim), lambda: B.qk_norm_rope(q, k, pos.long(), freq, 2 * hk, hk, dim),
+                lambda: B.qk_norm_rope(q, k, pos, freq, 2 * hk, hk, dim, wq=torch.ones(dim, device=DEV)), lambda: B.attention_window(q, k, k, "1", 3, 4, 2, dim)):
+        with pytest.raises(TypeError):
+            bad()
+    small = torch.empty(256, device=DEV, dtype=torch.uint8)
+    for bad, code in ((lambda: B.attention_kv4(q, cache, table, lens, 3, 1, 2 * hk, ws=small), B.ERR_WORKSPACE),
+                      (lambda: B.attention_window(q.float(), k.float(), k.float(), 1, 3, 2 * hk, hk, dim), B.ERR_UNSUPPORTED),
+                      (lambda: B.attention_kv4(q, cache, table, lens, 3, 1, 2 * hk, scale=-1.0), B.ERR_SHAPE)):
+        with pytest.raises(B.BitLinearError) as err:
+            bad()
+        assert err.value.code == code
+
+
+def test_a_captured_decode_step_replayed():
+    """Norm and rotation in place, append, attention and a copy of pages in one graph; positions and lengths advance inside it."""
+    heads, hk, dim, page, dt, batch = 8, 2, 128, 16, BF16, 3
+    freq = (10000.0 ** (-torch.arange(0, dim, 2, device=DEV).double() / dim)).float()
+    pages = torch.zeros((2, 40, B.kv4_page_bytes(page, hk, dim)), dtype=torch.uint8, device=DEV)
+    cache = B.Kv4Cache(pages[0], page, hk, dim, dt)
+    table = torch.randperm(36, device=DEV)[:batch * 10].view(batch, 10).int()
+    start = torch.tensor([0, 15, 70], device=DEV).int()
+    lens = start.clone()
+    x = randn(1, 12, batch, (heads + 2 * hk) * dim, dtype=dt)
+    step = torch.zeros(1, device=DEV, dtype=torch.int64)
+    o = torch.empty((batch, heads * dim), device=DEV, dtype=dt)
+    pairs = torch.tensor([[0, 38], [1, 39]], device=DEV).int()
+
+    def decode(out):
+        y = x[step][0].clone()
+        q, k, v = y[:, :heads * dim], y[:, heads * dim:(heads + hk) * dim], y[:, (heads + hk) * dim:]
+        B.qk_norm_rope(q, k, lens, freq, heads, hk, dim, q_out=q, k_out=k)
+        at = lens.long()
+        B.kv4_append(cache, k, v, table.long().gather(1, (at // page)[:, None])[:, 0] * page + at % page)
+        lens.add_(1)
+        B.attention_kv4(q, cache, table, lens, batch, 1, heads, window=40, sinks=3, o=out)
+        B.kv4_copy_pages(pages, pairs)
+        step.add_(1)
+    wants = []
+    for _ in range(12):
+        decode(o)
+        wants.append(o.clone())
+    final = pages.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        decode(o)
+    for _ in range(2):
+        pages.zero_(); lens.copy_(start); step.zero_()
+        for want in wants:
+            graph.replay()
+            assert torch.equal(o, want)
+        assert torch.equal(pages, final) and torch.equal(pages[:, 38], pages[:, 0])
+
+
 # ---- together ------------------------------------------------------------------------------------
 def test_a_prompt_and_decode_steps_through_bitlinear_layers():
     """A prompt enters the cache, a sequence is forked, and both decode tokens: BitLinear projections by the decode
