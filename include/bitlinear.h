@@ -395,7 +395,8 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
  *   (packed prompts of different lengths), or NULL: sequence b owns rows b * seq_q .. (seq_k for keys).
  *   cu_k may be NULL with cu_q given: the key rows are then those of cu_q.  seq_q, seq_k: the common
  *   length, or with cu_* an upper bound of the lengths (rows of a sequence beyond it are not
- *   processed).  rows_q, rows_k: rows present in q / o and k / v; entries of cu_* are clamped to them.
+ *   processed).  rows_q, rows_k: rows present in q / o and k / v; entries of cu_* are clamped to them, and
+ *   must not decrease (else which rows are processed is not defined).
  *   A sequence with fewer query rows than key rows has its queries at the last positions (a chunk
  *   behind tokens that are already known); with more, the first ones see nothing.  A query that sees
  *   nothing gets zeros.  Rows of o outside every sequence are left as they were.

@@ -556,7 +556,9 @@ bl_status bitlinear_attention_window(const void* q, const void* k, const void* v
   if (!q || !o || (rows_k > 0 && (!k || !v))) return BL_ERR_NULL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned_to(cu_q, 4) || !aligned_to(cu_k, 4))
     return BL_ERR_ALIGN;
-  if ((int64_t)batch * heads * ((seq_q + 127) / 128) > 0x7FFFFFFF) return BL_ERR_SHAPE;
+  int64_t blocks = (seq_q + 127) / 128 * batch;                  // blocks of query rows, at most
+  if (cu_q && blocks > rows_q / 128 + batch) blocks = rows_q / 128 + batch;
+  if (blocks * heads > 0x7FFFFFFF) return BL_ERR_SHAPE;
   WindowArgs a{q, k, v, o, dt, batch, cu_q, cu_k ? cu_k : cu_q, seq_q, seq_k, rows_q, rows_k, heads, kv_heads, head_dim, ld_q,
                ld_k, ld_v, ld_o, clip_window(window), sinks, scale};
   if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)head_dim);

@@ -26,6 +26,7 @@
 //
 // Every wait is bounded.  If one runs out, the CTA's rows are computed by window_row too and the event is
 // counted (bitlinear_debug_window_fallbacks): the result is the same up to rounding, only late.
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -223,18 +224,45 @@ struct Job {
   int clean_from, clean_to;                      // those that every row sees as a whole (tiles of nothing but sinks are not counted in)
   __device__ __forceinline__ int key0(int j) const { return (j < sink_tiles ? j : first + j - sink_tiles) * kKeys; }
 };
-// Blocks with the most keys first; the heads of a group side by side, so that they find their keys in L2.
+// The heads of a group lie side by side, so that they find their keys in L2; within a sequence (with equal lengths: in the
+// whole batch) the blocks with the most keys come first.  Packed sequences have as many blocks as their rows need, found by
+// a sum over the batch: a bound of the lengths far above most of them costs nothing.  By whole warps, each for itself.
 __device__ __forceinline__ Job make_job(const WindowArgs& a) {
   Job w;
-  const int blocks = (int)((a.seq_q + kRows - 1) / kRows);
-  const int rest = blockIdx.x / a.heads, b = rest % a.batch;
-  w.head = blockIdx.x - rest * a.heads;
+  const int unit = blockIdx.x / a.heads, lane = threadIdx.x & 31;
+  int b = a.batch, blk = 0;
+  w.head = blockIdx.x - unit * a.heads;
+  if (!a.cu_q) {
+    b = unit % a.batch;
+    blk = (int)((a.seq_q + kRows - 1) / kRows) - 1 - unit / a.batch;
+  } else {
+    int before = 0;
+    for (int base = 0; base < a.batch; base += 32) {
+      const int n = base + lane < a.batch ? (seq_rows(a, base + lane).nq + kRows - 1) / kRows : 0;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += up;
+      }
+      const unsigned past = __ballot_sync(0xFFFFFFFFu, before + upto > unit);
+      if (past) {
+        const int f = __ffs(past) - 1;
+        b = base + f;
+        blk = before + __shfl_sync(0xFFFFFFFFu, upto, f) - 1 - unit;
+        break;
+      }
+      before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+  }
+  w.rows = 0;
+  w.sink_tiles = w.first = w.count = w.clean_from = w.clean_to = 0;
+  if (b == a.batch) return w;
   w.r = seq_rows(a, b);
-  w.row0 = (blocks - 1 - rest / a.batch) * kRows;
+  w.row0 = blk * kRows;
   w.rows = min(max(w.r.nq - w.row0, 0), kRows);
   w.pos0 = w.r.nk - w.r.nq + w.row0;
   w.pos1 = w.pos0 + w.rows - 1;
-  w.sink_tiles = w.first = w.count = w.clean_from = w.clean_to = 0;
   if (w.rows > 0 && w.pos1 >= 0) {
     const int lo = a.window > 0 ? max(0, w.pos0 - a.window + 1) : 0;      // first key of the first row's window
     w.first = lo / kKeys;
@@ -293,6 +321,9 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
+  pdl_wait();
+  const Job job = make_job(a);
+  if (job.rows == 0) return;                     // no block of rows for this CTA
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&ctl->q_full), 1);
     mbar_init(smem_u32(&ctl->drain), 1);
@@ -317,8 +348,6 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base, t_s = tmem, t_o = tmem + 2 * kKeys;
-  pdl_wait();
-  const Job job = make_job(a);
 
   if (warp == kCopier) {                                       // ---- copies
     if (lane == 0 && job.count > 0) {
@@ -516,7 +545,9 @@ cudaError_t launch_dim(const WindowArgs& a, cudaStream_t s) {
   } else {
     mk = mv = mq;                                // no key anywhere: never used
   }
-  const int64_t grid = (a.seq_q + kRows - 1) / kRows * a.batch * a.heads;
+  int64_t units = (a.seq_q + kRows - 1) / kRows * a.batch;      // blocks of rows, at most
+  if (a.cu_q) units = std::min(units, a.rows_q / kRows + a.batch);
+  const int64_t grid = units * a.heads;
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
   const uint32_t polls = dbg < 0 ? kSpinLimit : (uint32_t)(dbg < (long long)kSpinLimit ? dbg : kSpinLimit);
   return launch_pdl(attention_window_kernel<T, kDim>, (unsigned)grid, kThreads, kSmem, s, mq, mk, mv, a, polls);

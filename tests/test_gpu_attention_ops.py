@@ -443,6 +443,20 @@ def test_attention_window_unpacked_and_behind_known_tokens(dt, batch, seq_q, seq
     check_window(q, k, v, o, [(b * seq_q, seq_q, b * seq_k, seq_k) for b in range(batch)], heads, hk, dim, window, sinks)
 
 
+@pytest.mark.parametrize("batch", [70, 33])
+def test_attention_window_many_ragged_prompts(batch):
+    """One long prompt among many short and empty ones: each block of rows is found in a batch of more than a warp's lanes."""
+    heads, hk, dim, dt = 2, 1, 64, F16
+    lens = [(i * 53) % 200 if i % 5 else 0 for i in range(batch)]
+    lens[batch - 2] = 1500
+    cu, at = packed(lens)
+    q, k, v = (randn(i, at[-1], w * dim, dtype=dt) for i, w in ((1, heads), (2, hk), (3, hk)))
+    o = B.attention_window(q, k, v, batch, 1500, heads, hk, dim, window=100, sinks=1, cu_q=cu)
+    check_window(q, k, v, o, [(a, n, a, n) for a, n in zip(at, lens)], heads, hk, dim, 100, 1)
+    big = B.attention_window(q, k, v, batch, 1 << 20, heads, hk, dim, window=100, sinks=1, cu_q=cu)
+    assert torch.equal(big, o)
+
+
 def test_attention_window_lengths_apart_and_rows_outside():
     """Queries and keys packed apart, bounds below the lengths, offsets that are no offsets."""
     heads, hk, dim, dt = 2, 1, 64, F16
