@@ -275,10 +275,16 @@ __device__ __forceinline__ Job make_job(const WindowArgs& a) {
   return w;
 }
 
-// Largest of kKeys scores; those that are not seen (column > last, or before `from` and not before `sink`) become -infinity.
+// Scores that are not seen (column > last, or before `from` and not before `sink`) become -infinity.  One bit per column:
+// short prompts, whose tiles are all masked, take 9.6 us where three comparisons per score took 11.8.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
 __device__ __forceinline__ void mask_scores(float (&s)[kKeys], int last, int from, int sink) {
 #pragma unroll
-  for (int c = 0; c < kKeys; ++c) s[c] = c <= last && (c >= from || c < sink) ? s[c] : -INFINITY;
+  for (int w = 0; w < kKeys; w += 32) {
+    const uint32_t seen = first_bits(last + 1 - w) & (~first_bits(from - w) | first_bits(sink - w));
+#pragma unroll
+    for (int c = 0; c < 32; ++c) s[w + c] = seen & (1u << c) ? s[w + c] : -INFINITY;
+  }
 }
 __device__ __forceinline__ float largest(const float (&s)[kKeys]) {
   float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]), mx2 = s[6], mx3 = s[7];
@@ -471,9 +477,11 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     }
     if (ok && job.count > 0) ok = o_ready(job.count - 1);
     if (ok) {
+      // Through shared memory (the query tile's, which no product reads any more), each warp its own rows: whole rows leave
+      // together.  Written from the registers, 16 bytes of each of 32 rows at a time, the whole kernel took 2 % longer.
       const bool mine = row < job.rows;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + job.row0 + row) * a.ld_o + (int64_t)job.head * kDim;
+      unsigned char* stage = sq + warp * 32 * kDim * 2;
       float check = 0.f;
 #pragma unroll
       for (int c = 0; c < kDim; c += 32) {
@@ -489,11 +497,21 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           check = fmaf(x, 0.f, fmaf(y, 0.f, check));           // NaN once a value is not finite
           w[i] = pack2<T>(x, y);
         }
-        if (mine) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(o + c + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        }
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<uint4*>(stage + lane * kDim * 2 + (((c >> 3) + i) ^ (lane & 7)) * 16) =
+              make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
       }
+      __syncwarp();
+      constexpr int kParts = kDim / 8, kAtOnce = 32 / kParts;  // 16-byte parts of a row, rows per instruction
+      T* o = reinterpret_cast<T*>(a.o) + (int64_t)(job.r.q0 + job.row0 + warp * 32) * a.ld_o + (int64_t)job.head * kDim;
+#pragma unroll
+      for (int i = lane / kParts; i < 32; i += kAtOnce) {
+        const int part = lane % kParts;
+        if (warp * 32 + i < job.rows)
+          *reinterpret_cast<uint4*>(o + (int64_t)i * a.ld_o + part * 8) = *reinterpret_cast<const uint4*>(stage + i * kDim * 2 + (part ^ (i & 7)) * 16);
+      }
+      __syncwarp();
       // (a sum l that is not finite comes from scores that are seen: the row's result is NaN by definition)
       unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f) && l - l == 0.f);
       while (bad) {
