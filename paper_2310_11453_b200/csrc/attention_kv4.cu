@@ -25,6 +25,8 @@
 // (104 or 139 KB in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is reported in
 // the workspace's status word.  A warp that owns all chunks of a head writes the output; else its
 // unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
+// Few and short lists go to clusters of CTAs instead, one per list (a sequence, key/value head and block of rows), which
+// join their parts through each other's shared memory: one kernel (launch_dim gives the rule).
 #include <algorithm>
 #include <type_traits>
 
@@ -40,17 +42,20 @@ using namespace kv4;
 constexpr int kChunk = 64;                 // tokens per work item
 constexpr int kMostWarps = 12;             // per CTA, one CTA per SM
 constexpr int kMaxSms = 160;
+constexpr int kMostClusterLog2 = 3, kMostCluster = 1 << kMostClusterLog2;   // CTAs of a cluster
+constexpr int kClusterChunks = 4;          // chunks per warp up to which a cluster takes a list
 constexpr size_t kStatusBytes = 256;       // the status word lies at the start of the workspace
-constexpr int kJoinWarps = 8;
 
 struct Plan {                              // how the list is laid out; made on the host, the same for both kernels
   int group, rows, rows_per_block, blocks; // query heads per key/value head; query rows; rows per block; blocks
   int heads_blocks;                        // key/value heads x blocks
   int page_log2, parts;                    // log2 page_size; parts of the list (warps)
+  int cluster_log2;                        // log2 CTAs of a cluster, where each works on a list of its own
   uint32_t parts_magic;                    // floor(2^32 / parts) + 1
 };
-inline Plan make_plan(int n_q, int heads, int kv_heads, int page_size, int parts) {
+inline Plan make_plan(int n_q, int heads, int kv_heads, int page_size, int parts, int cluster_log2 = 0) {
   Plan p;
+  p.cluster_log2 = cluster_log2;
   p.group = heads / kv_heads;
   p.rows = n_q * p.group;
   p.rows_per_block = p.rows <= 8 ? p.rows : 16;
@@ -164,6 +169,17 @@ __device__ __forceinline__ void copy_bulk(uint32_t dst, const void* src, int byt
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+// Barrier of a cluster's threads; a number in the shared memory of its CTA `rank`, at p in one's own.
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float2 peer_float2(const float* p, int rank) {
+  uint32_t addr;
+  float2 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -223,8 +239,8 @@ struct __align__(16) Item {
   int rows0, there, first, last;           // first query row; which runs of tokens are there (bit per page); first, last chunk of its list
 };
 
-// kNT: tiles of 8 query rows; kWarps per CTA, each with kStages chunks in shared memory.
-template <typename T, int kDim, int kNT, int kWarps, int kStages>
+// kNT: tiles of 8 query rows; kWarps per CTA, each with kStages chunks in shared memory; kCluster: a cluster per list.
+template <typename T, int kDim, int kNT, int kWarps, int kStages, bool kCluster>
 __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnArgs a, Plan plan, uint32_t polls) {
   constexpr int kWords = kDim / 32;        // words of codes per lane and 8 tokens
   constexpr int kTiles = kChunk / 16;
@@ -247,15 +263,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
 
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.ws) = 0;   // the status word
-  Spread spread(a);
-  const Cut cut(spread.all * plan.heads_blocks, plan);
-  const int64_t begin = cut.begin(w);
-  const int items = (int)(cut.begin(w + 1) - begin);
-  if (items == 0) return;
-
   // ---- loads: the page numbers of a chunk are fetched one chunk before its copies are issued
   Walk ahead;
-  {
+  int items;
+  const int rank = blockIdx.x & ((1 << plan.cluster_log2) - 1);
+  if (kCluster) {                                      // the chunks of the cluster's list, cut for its warps
+    const int unit = blockIdx.x >> plan.cluster_log2, part = (warp << plan.cluster_log2) + rank;
+    ahead.b = unit / plan.heads_blocks;
+    const int hb = unit - ahead.b * plan.heads_blocks;
+    ahead.s = make_seq(a, ahead.b);
+    ahead.hk = hb / plan.blocks;
+    ahead.blk = hb - ahead.hk * plan.blocks;
+    ahead.c = (int)((uint32_t)(ahead.s.chunks * part) / (uint32_t)plan.parts);
+    items = (int)((uint32_t)(ahead.s.chunks * (part + 1)) / (uint32_t)plan.parts) - ahead.c;
+  } else {
+    Spread spread(a);
+    const Cut cut(spread.all * plan.heads_blocks, plan);
+    const int64_t begin = cut.begin(w);
+    items = (int)(cut.begin(w + 1) - begin);
+    if (items == 0) return;
     int64_t rest;
     ahead.b = spread.find(a, plan.heads_blocks, begin, rest);
     ahead.s = make_seq(a, ahead.b);
@@ -272,7 +298,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     return id >= 0 && id < a.cache.num_pages ? id : -1;
   };
   int issued = 0;
-  int ids = page_of(ahead);
+  int ids = items > 0 ? page_of(ahead) : -1;
   auto issue = [&]() {
     if (issued < items) {
       const int slot = issued % kStages;
@@ -290,7 +316,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         copy_bulk(dst + lane * block_bytes, reinterpret_cast<const char*>(a.cache.pages) + ((int64_t)ids * a.cache.kv_heads + ahead.hk) * block_bytes,
                   block_bytes, bar_addr + 8 * slot);
       if (issued + 1 < items) {
-        ahead.next(a, plan);
+        if (kCluster) ++ahead.c; else ahead.next(a, plan);
         ids = page_of(ahead);
       }
     }
@@ -520,14 +546,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   };
 
   auto end_segment = [&](const Item& it) {
-    const bool whole = from_start && it.last;
+    const bool whole = !kCluster && from_start && it.last;
     // where the join finds the row block's parts: that of the first chunk (slot), that of the last (warp)
-    if (lane == 0) {
+    if (!kCluster && lane == 0) {
       int* where = ends_of(a, plan) + 2 * (((int64_t)it.b * a.cache.kv_heads + it.hk) * plan.blocks + it.rows0 / plan.rows_per_block);
       if (from_start) where[0] = 2 * w + later;
       if (it.last) where[1] = w;
     }
-    float* slot = slots_of(a) + (2 * w + later) * slot_floats(plan, kDim);
+    if (kCluster) __syncwarp();                        // the part's sums take the place of its chunks
+    float* slot = kCluster ? reinterpret_cast<float*>(ring) : slots_of(a) + (2 * w + later) * slot_floats(plan, kDim);
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -585,13 +612,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     return __all_sync(0xFFFFFFFFu, ok);
   };
   __syncwarp();
-  begin_segment(items_of[0]);                          // while the first chunk is on its way
+  if (!kCluster || items > 0) begin_segment(items_of[0]);   // while the first chunk is on its way
   bool fresh = false;
   for (int item = 0; item < items; ++item) {
     if (!arrived(item, polls)) {                       // the copies did not come: reported, nothing more is done
       if (lane == 0) *reinterpret_cast<volatile uint32_t*>(a.ws) = BL_ERR_TIMEOUT;
       for (int i = item; i < min(issued, items); ++i) arrived(i, tc::kSpinLimit);   // those in flight end before the CTA does (bounded)
-      return;
+      if (!kCluster) return;
+      items = 0;
+      break;
     }
     const Item it = items_of[item % kStages];
     issue();
@@ -604,14 +633,80 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     else chunk(stage, it, std::true_type{});
     if (it.last || item + 1 == items) end_segment(it);
   }
+  if (!kCluster) return;
+
+  // ---- the parts of the CTA's warps become one, then those of the cluster's CTAs
+  constexpr int kRow = kDim + 4;                       // a row's sums, its maximum, the sum of its probabilities
+  float* joined = reinterpret_cast<float*>(smem + kWarps * kStages * (kStageBytes + (int)sizeof(Item) + 8));
+  if (items == 0 && lane < plan.rows_per_block)        // nothing, or not all of it came
+    *reinterpret_cast<float2*>(reinterpret_cast<float*>(ring) + lane * kRow + kDim) = make_float2(-INFINITY, 0.f);
+  __syncthreads();
+  const int rows0 = ahead.blk * plan.rows_per_block, rows = min(plan.rows_per_block, plan.rows - rows0);
+  for (int e = 2 * threadIdx.x; e < rows * kDim; e += kWarps * 64) {
+    const int rr = e / kDim, d = e & (kDim - 1);
+    const float* part = reinterpret_cast<const float*>(smem) + rr * kRow;
+    float top = -INFINITY, l = 0.f;
+    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, part[i * (kStages * kStageBytes / 4) + kDim]);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float* x = part + i * (kStages * kStageBytes / 4);
+      if (x[kDim] == -INFINITY) continue;
+      const float c = ex2(x[kDim] - top);
+      l = fmaf(x[kDim + 1], c, l);
+      v.x = fmaf(x[d], c, v.x); v.y = fmaf(x[d + 1], c, v.y);
+    }
+    *reinterpret_cast<float2*>(joined + rr * kRow + d) = v;
+    if (d == 0) *reinterpret_cast<float2*>(joined + rr * kRow + kDim) = make_float2(top, l);
+  }
+  __syncwarp();
+  cluster_meet();
+  const int ctas = 1 << plan.cluster_log2;
+  for (int e = 2 * (rank * kWarps * 32 + threadIdx.x); e < rows * kDim; e += ctas * kWarps * 64) {
+    const int rr = e / kDim, d = e & (kDim - 1), r = rows0 + rr, i_q = r / plan.group;
+    float2 stat[kMostCluster], x[kMostCluster];
+#pragma unroll
+    for (int i = 0; i < kMostCluster; ++i) {
+      stat[i] = i < ctas ? peer_float2(joined + rr * kRow + kDim, i) : make_float2(-INFINITY, 0.f);
+      x[i] = i < ctas ? peer_float2(joined + rr * kRow + d, i) : make_float2(0.f, 0.f);
+    }
+    float top = -INFINITY, l = 0.f;
+    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kMostCluster; ++i) top = fmaxf(top, stat[i].x);
+#pragma unroll
+    for (int i = 0; i < kMostCluster; ++i) {
+      if (stat[i].x == -INFINITY) continue;
+      const float c = ex2(stat[i].x - top);
+      l = fmaf(stat[i].y, c, l);
+      v.x = fmaf(x[i].x, c, v.x); v.y = fmaf(x[i].y, c, v.y);
+    }
+    const float norm = l == 0.f ? 0.f : 1.f / l;
+    T* out = reinterpret_cast<T*>(a.o) + ((int64_t)ahead.b * a.n_q + i_q) * a.ld_o + (int64_t)(ahead.hk * plan.group + r - i_q * plan.group) * kDim + d;
+    *reinterpret_cast<uint32_t*>(out) = pair_bits<T>(v.x * norm, v.y * norm);
+  }
+  __syncwarp();
+  cluster_meet();                                      // the others have read this CTA's sums
+}
+
+template <int kVals> __device__ __forceinline__ void load_values(const float* p, float (&x)[kVals]);
+template <> __device__ __forceinline__ void load_values<4>(const float* p, float (&x)[4]) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+template <> __device__ __forceinline__ void load_values<2>(const float* p, float (&x)[2]) {
+  const float2 v = *reinterpret_cast<const float2*>(p);
+  x[0] = v.x; x[1] = v.y;
 }
 
 // Joins the parts of the rows whose chunks went to more than one warp: one CTA per row.  All maxima and sums are loaded at
-// once and turned into weights; then the parts' values are summed, four loads of a warp in flight.
-template <typename T, int kDim>
+// once; then the parts' values are summed, kJoinLoads parts of a warp in flight.
+template <typename T, int kDim, int kJoinWarps>
 __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, Plan plan) {
-  constexpr int kVals = kDim / 32, kMostParts = kMaxSms * kMostWarps;
-  __shared__ float weight[kMostParts], sums[kJoinWarps][kDim], tops[kJoinWarps], totals[kJoinWarps];
+  constexpr int kVals = kDim / 32, kMostParts = kMaxSms * kMostWarps, kJoinLoads = kJoinWarps > 8 ? 4 : 8;
+  __shared__ float2 stats[kMostParts];
+  __shared__ float sums[kJoinWarps][kDim], tops[kJoinWarps], totals[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int bh = blockIdx.x / plan.rows_per_block, rr = blockIdx.x - bh * plan.rows_per_block;
   const int b = bh / plan.heads_blocks, hb = bh - b * plan.heads_blocks;
@@ -636,41 +731,36 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4
   auto row = [&](int i) { return rows + 2 * i * stride + (i == 0 ? shift : 0); };
   float top = -INFINITY;
   for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
-    const float m = row(i)[kDim];
-    weight[i] = m;
-    top = fmaxf(top, m);
+    const float2 x = *reinterpret_cast<const float2*>(row(i) + kDim);
+    stats[i] = x;
+    top = fmaxf(top, x.x);
   }
   top = warp_max(top);
   if (lane == 0) tops[warp] = top;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
-  float l = 0.f;
-  for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
-    const float m = weight[i], c = m == -INFINITY ? 0.f : ex2(m - top);   // -infinity: the part holds nothing that this row sees
-    weight[i] = c;
-    if (m != -INFINITY) l = fmaf(row(i)[kDim + 1], c, l);
+  float l = 0.f, v[kVals] = {};
+  for (int base = warp; base < parts; base += kJoinLoads * kJoinWarps) {
+    float x[kJoinLoads][kVals];
+#pragma unroll
+    for (int u = 0; u < kJoinLoads; ++u) {
+      const int i = base + u * kJoinWarps;
+      if (i < parts) load_values<kVals>(row(i) + lane * kVals, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kJoinLoads; ++u) {
+      const int i = base + u * kJoinWarps;
+      if (i >= parts) break;
+      const float2 st = stats[i];
+      if (st.x == -INFINITY) continue;                 // the part holds nothing that this row sees
+      const float c = ex2(st.x - top);
+      l = fmaf(st.y, c, l);
+#pragma unroll
+      for (int e = 0; e < kVals; ++e) v[e] = fmaf(x[u][e], c, v[e]);
+    }
   }
-  l = warp_sum(l);
   if (lane == 0) totals[warp] = l;
-  __syncthreads();
-  float v[kVals] = {};
-  for (int base = warp; base < parts; base += 4 * kJoinWarps) {
-    float x[4][kVals];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = base + u * kJoinWarps;
-#pragma unroll
-      for (int e = 0; e < kVals; ++e) x[u][e] = i < parts ? row(i)[lane * kVals + e] : 0.f;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = base + u * kJoinWarps;
-      const float c = i < parts ? weight[i] : 0.f;
-#pragma unroll
-      for (int e = 0; e < kVals; ++e) v[e] = c == 0.f ? v[e] : fmaf(x[u][e], c, v[e]);
-    }
-  }
 #pragma unroll
   for (int e = 0; e < kVals; ++e) sums[warp][lane * kVals + e] = v[e];
   __syncthreads();
@@ -682,54 +772,99 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4
   }
 }
 
-cudaError_t sm_count(int* n) {
+cudaError_t sm_count(int dev, int* n) {
   static std::atomic<int> known[64];
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
   if (dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
-  e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+  const cudaError_t e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   if (*n > kMaxSms) *n = kMaxSms;
   if (dev < 64) known[dev].store(*n, std::memory_order_relaxed);
   return cudaSuccess;
 }
 
-template <typename T, int kDim, int kNT, int kWarps, int kStages>
-cudaError_t launch_rows(const Kv4AttnArgs& a, cudaStream_t s) {
-  constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item) + 8);
+template <int kDim, int kNT, int kWarps, int kStages, bool kCluster> constexpr int smem_bytes() {
+  constexpr int kSmem = kWarps * kStages * (kChunk * (kDim + 8) + (int)sizeof(Item) + 8) + (kCluster ? kNT * 8 * (kDim + 4) * 4 : 0);
   static_assert(kSmem <= 232448, "exceeds the shared memory of one CTA");
-  static std::atomic<uint64_t> ready{0};               // devices on which the kernel's shared memory limit is set
-  int dev = 0, sms = 0;
-  cudaError_t e = sm_count(&sms);
-  if (e == cudaSuccess) e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !((ready.load(std::memory_order_relaxed) >> dev) & 1)) {
-    e = cudaFuncSetAttribute(attention_kv4_kernel<T, kDim, kNT, kWarps, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
-  }
-  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
+  static_assert(!kCluster || kNT * 8 * (kDim + 4) * 4 <= kStages * kChunk * (kDim + 8), "a part's sums exceed the place of its chunks");
+  return kSmem;
+}
+// Lets the kernel have its shared memory, once per device.
+template <typename T, int kDim, int kNT, int kWarps, int kStages, bool kCluster> cudaError_t allow_smem(int dev) {
+  static std::atomic<uint64_t> ready{0};
+  if (dev < 64 && ((ready.load(std::memory_order_relaxed) >> dev) & 1)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(attention_kv4_kernel<T, kDim, kNT, kWarps, kStages, kCluster>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<kDim, kNT, kWarps, kStages, kCluster>());
+  if (e == cudaSuccess && dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
+inline uint32_t wait_polls() {
   const long long dbg = g_debug_wait_polls.load(std::memory_order_relaxed);
-  const uint32_t polls = dbg < 0 ? tc::kSpinLimit : (uint32_t)(dbg < (long long)tc::kSpinLimit ? dbg : tc::kSpinLimit);
-  e = launch_pdl(attention_kv4_kernel<T, kDim, kNT, kWarps, kStages>, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(attention_kv4_join_kernel<T, kDim>, (unsigned)((int64_t)a.batch * plan.heads_blocks * plan.rows_per_block),
-                    kJoinWarps * 32, 0, s, a, plan);
+  return dbg < 0 ? tc::kSpinLimit : (uint32_t)(dbg < (long long)tc::kSpinLimit ? dbg : tc::kSpinLimit);
 }
 
-// Up to 8 query rows: 12 warps with two chunks each keep the SM busier (32 x 8192 tokens, 8 heads, 4 rows: 45.4 us against
-// 49.3 with 8 warps and three chunks), but the next kernel finds no room beside them before they end, which costs a short
-// list 2 us (1000 tokens, 16 heads: 11.1 against 9.2), so lists of at most two chunks per warp take 8.  More rows: 8 warps, whose
-// 255 registers hold the second tile of rows (12: spills, 116 us against 83 for 2 x 150001 tokens).
+// A cluster per list, if all of them fit the GPU at once and have at most four chunks per warp; *done says whether.  Of the
+// sizes that fit, the smallest that leaves a warp no more than one chunk, else the largest.  Against the cut list and the join
+// (us, 128-wide heads): 1 x 1000 tokens, 16 heads 6.3 / 8.3; 4 x 4000, 8 heads of 4 rows 8.9 / 13.0; 1 x 8000, 8 heads of 16 rows
+// 13.0 / 14.7; 1 x 16000, 16 heads (8 chunks per warp) 18.7 / 16.1; clusters that do not fit at once 11.9 / 9.5 (1 x 4000, 16 heads).
+template <typename T, int kDim, int kNT>
+cudaError_t launch_clusters(const Kv4AttnArgs& a, int dev, int64_t lists, int64_t chunks, cudaStream_t s, bool* done) {
+  static std::atomic<int> known[64][kMostClusterLog2 + 1];     // clusters of 2^i CTAs that fit, and 1
+  const auto kernel = attention_kv4_kernel<T, kDim, kNT, 8, 2, true>;
+  constexpr int kSmem = smem_bytes<kDim, kNT, 8, 2, true>();
+  *done = false;
+  int size = -1;
+  for (int i = 0; i <= kMostClusterLog2 && (size < 0 || chunks > 8 << size); ++i) {
+    int fit = dev < 64 ? known[dev][i].load(std::memory_order_relaxed) - 1 : -1;
+    if (fit < 0) {
+      cudaError_t e = allow_smem<T, kDim, kNT, 8, 2, true>(dev);
+      if (e == cudaSuccess) e = max_clusters(kernel, 1u << i, 256, kSmem, &fit);
+      if (e != cudaSuccess) return e;
+      if (dev < 64) known[dev][i].store(fit + 1, std::memory_order_relaxed);
+    }
+    if (lists <= fit) size = i;
+  }
+  if (size < 0 || chunks > kClusterChunks * 8 << size) return cudaSuccess;
+  *done = true;
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, 8 << size, size);
+  return launch_pdl_clusters(kernel, (unsigned)lists << size, 1u << size, 256, kSmem, s, a, plan, wait_polls());
+}
+
+template <typename T, int kDim, int kNT, int kWarps, int kStages>
+cudaError_t launch_rows(const Kv4AttnArgs& a, int dev, int sms, cudaStream_t s) {
+  constexpr int kSmem = smem_bytes<kDim, kNT, kWarps, kStages, false>();
+  const auto kernel = attention_kv4_kernel<T, kDim, kNT, kWarps, kStages, false>;
+  cudaError_t e = allow_smem<T, kDim, kNT, kWarps, kStages, false>(dev);
+  if (e != cudaSuccess) return e;
+  const uint32_t polls = wait_polls();
+  const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
+  e = launch_pdl(kernel, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
+  if (e != cudaSuccess) return e;
+  // One CTA per row: 32 warps while each has an SM to itself (32000 tokens, 8 heads, 4 rows: 17.3 us against 23.8), 8 where there
+  // are more rows (16 x 1000 tokens: 12.0 us against 14.5).
+  const int64_t rows = (int64_t)a.batch * plan.heads_blocks * plan.rows_per_block;
+  return rows <= sms ? launch_pdl(attention_kv4_join_kernel<T, kDim, 32>, (unsigned)rows, 1024, 0, s, a, plan)
+                     : launch_pdl(attention_kv4_join_kernel<T, kDim, 8>, (unsigned)rows, 256, 0, s, a, plan);
+}
+
+// Longer or more lists.  Up to 8 query rows: 12 warps with two chunks each keep the SM busier (32 x 8192 tokens, 8 heads, 4 rows:
+// 45.4 us against 49.3 with 8 warps and three chunks), but the next kernel finds no room beside them before they end, which costs
+// a short list 1 to 2 us (64 x 120 tokens, 16 heads: 18.5 against 16.2), so lists of at most two chunks per warp take 8.  More
+// rows: 8 warps, whose 255 registers hold the second tile of rows (12: spills, 116 us against 83 for 2 x 150001 tokens).
 template <typename T, int kDim>
 cudaError_t launch_dim(const Kv4AttnArgs& a, cudaStream_t s) {
   const int64_t rows = (int64_t)a.n_q * (a.heads / a.cache.kv_heads);
-  if (rows > 8) return launch_rows<T, kDim, 2, 8, 3>(a, s);
   int64_t tokens = a.max_pages * a.cache.page_size;
   if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + a.sinks + a.n_q + 2 * kChunk);
-  const bool few = (tokens + kChunk - 1) / kChunk * a.cache.kv_heads * a.batch <= 2 * 8 * 148;
-  return few ? launch_rows<T, kDim, 1, 8, 3>(a, s) : launch_rows<T, kDim, 1, 12, 2>(a, s);
+  const int64_t chunks = (tokens + kChunk - 1) / kChunk, lists = (int64_t)a.batch * a.cache.kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16);
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = sm_count(dev, &sms);
+  if (e != cudaSuccess) return e;
+  bool done = false;
+  e = rows > 8 ? launch_clusters<T, kDim, 2>(a, dev, lists, chunks, s, &done) : launch_clusters<T, kDim, 1>(a, dev, lists, chunks, s, &done);
+  if (done || e != cudaSuccess) return e;
+  if (rows > 8) return launch_rows<T, kDim, 2, 8, 3>(a, dev, sms, s);
+  return chunks * lists <= 2 * 8 * 148 ? launch_rows<T, kDim, 1, 8, 3>(a, dev, sms, s) : launch_rows<T, kDim, 1, 12, 2>(a, dev, sms, s);
 }
 
 template <typename T>
