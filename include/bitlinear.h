@@ -405,7 +405,7 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
  * fp32 softmax statistics and accumulators; probabilities are rounded to the type of v for the
  * product, and one rounding on output.  The kernel's waits are bounded; if one ever ran out, the rows concerned are
  * computed another way (same result up to rounding), so there is no status to collect.
- * batch = 0 or seq_q = 0 is valid and does nothing.  No workspace. */
+ * o must not overlap q, k or v.  batch = 0 or seq_q = 0 is valid and does nothing.  No workspace. */
 bl_status bitlinear_attention_window(const void* q, const void* k, const void* v, void* o, bl_dtype dt, int batch,
                                      const int32_t* cu_q, const int32_t* cu_k, int64_t seq_q, int64_t seq_k,
                                      int64_t rows_q, int64_t rows_k, int heads, int kv_heads, int head_dim,
@@ -455,8 +455,8 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   0..max_pages * page_size).  Query i of n_q stands at position lens - n_q + i; one that sees nothing
  *   (negative position, empty sequence) gets zeros.
  *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
- * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined by a
- * second kernel in a fixed order (same inputs and sizes, same bits).  batch = 0 does nothing.
+ * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
+ * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.
  * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; its first word is the status word of
  * bitlinear_ws_status: the kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means o of
  * this call is not valid); calls that may overlap need workspaces of their own. */

@@ -326,7 +326,6 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   Ctl* ctl = reinterpret_cast<Ctl*>(ring + kSlots * kTileBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_launch_dependents();
   pdl_wait();
   const Job job = make_job(a);
   if (job.rows == 0) return;                     // no block of rows for this CTA
@@ -353,6 +352,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_launch_dependents();                       // not before the tensor memory is ours: a kernel behind this one may take some, then wait for this one
   const uint32_t tmem = ctl->tmem_base, t_s = tmem, t_o = tmem + 2 * kKeys;
 
   if (warp == kCopier) {                                       // ---- copies
