@@ -43,6 +43,7 @@ constexpr int kChunk = 64;                 // tokens per work item
 constexpr int kMostWarps = 12;             // per CTA, one CTA per SM
 constexpr int kMaxSms = 160;
 constexpr int kMostClusterLog2 = 3, kMostCluster = 1 << kMostClusterLog2;   // CTAs of a cluster
+constexpr int kCtaRows = 4;                // rows of the result per SM up to which the join has a CTA for each
 constexpr int kClusterChunks = 4;          // chunks per warp up to which a cluster takes a list
 constexpr size_t kStatusBytes = 256;       // the status word lies at the start of the workspace
 
@@ -700,76 +701,134 @@ template <> __device__ __forceinline__ void load_values<2>(const float* p, float
   x[0] = v.x; x[1] = v.y;
 }
 
-// Joins the parts of the rows whose chunks went to more than one warp: one CTA per row.  All maxima and sums are loaded at
-// once; then the parts' values are summed, kJoinLoads parts of a warp in flight.
-template <typename T, int kDim, int kJoinWarps>
-__global__ void __launch_bounds__(kJoinWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, Plan plan) {
-  constexpr int kVals = kDim / 32, kMostParts = kMaxSms * kMostWarps, kJoinLoads = kJoinWarps > 8 ? 4 : 8;
-  __shared__ float2 stats[kMostParts];
-  __shared__ float sums[kJoinWarps][kDim], tops[kJoinWarps], totals[kJoinWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int bh = blockIdx.x / plan.rows_per_block, rr = blockIdx.x - bh * plan.rows_per_block;
+// The parts of one row of the result.
+template <typename T> struct JoinRow {
+  const float* first;                                  // the first part's sums; the others lie `stride` apart behind
+  const float* others;                                 // that of part i > 0 at others + i * stride
+  int64_t stride;
+  int parts;                                           // 0: an empty sequence; 1: written already, or nothing to write
+  T* out;
+  __device__ __forceinline__ const float* part(int i) const { return i == 0 ? first : others + i * stride; }
+};
+template <typename T, int kDim> __device__ __forceinline__ JoinRow<T> join_row(const Kv4AttnArgs& a, const Plan& plan, int64_t index) {
+  JoinRow<T> x;
+  x.parts = 1;
+  x.first = x.others = nullptr; x.stride = 0; x.out = nullptr;
+  const int bh = (int)((uint32_t)index / (uint32_t)plan.rows_per_block), rr = (int)(index - (int64_t)bh * plan.rows_per_block);
   const int b = bh / plan.heads_blocks, hb = bh - b * plan.heads_blocks;
+  if (b >= a.batch) return x;
   const int hk = hb / plan.blocks, r = (hb - hk * plan.blocks) * plan.rows_per_block + rr, i_q = r / plan.group;
-  pdl_launch_dependents();
-  pdl_wait();
-  if (r >= plan.rows) return;
-  const int chunks = make_seq(a, b).chunks;
-  T* out = reinterpret_cast<T*>(a.o) + ((int64_t)b * a.n_q + i_q) * a.ld_o + (int64_t)(hk * plan.group + r - i_q * plan.group) * kDim;
-  if (chunks == 0) {                                   // an empty sequence
-    for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) out[d] = out_cast<T>(0.f);
-    return;
+  if (r >= plan.rows) return x;
+  x.out = reinterpret_cast<T*>(a.o) + ((int64_t)b * a.n_q + i_q) * a.ld_o + (int64_t)(hk * plan.group + r - i_q * plan.group) * kDim;
+  const int2 ends = *reinterpret_cast<const int2*>(ends_of(a, plan) + 2 * (int64_t)bh);
+  if (make_seq(a, b).chunks == 0) {
+    x.parts = 0;
+    return x;
   }
-  const int2 ends = *reinterpret_cast<const int2*>(ends_of(a, plan) + 2 * bh);
   const int w0 = ends.x >> 1, parts = ends.y - w0 + 1;
-  if (parts == 1) return;                              // written already
-  if (w0 < 0 || parts < 1 || ends.y >= plan.parts) return;   // never written: the first kernel gave up (status word)
+  if (w0 < 0 || parts < 1 || ends.y >= plan.parts) return x;   // never written: the first kernel gave up (status word)
   // the first part may be in its warp's second slot; the others are in first slots
-  const int64_t stride = slot_floats(plan, kDim);
-  const float* rows = slots_of(a) + 2 * w0 * stride + rr * (kDim + 4);
-  const int64_t shift = (ends.x & 1) * stride;
-  auto row = [&](int i) { return rows + 2 * i * stride + (i == 0 ? shift : 0); };
+  x.parts = parts;
+  x.stride = 2 * slot_floats(plan, kDim);
+  x.others = slots_of(a) + w0 * x.stride + rr * (kDim + 4);
+  x.first = x.others + (ends.x & 1) * (x.stride / 2);
+  return x;
+}
+
+// Joins a row by a CTA.  All maxima and sums are loaded at once; then the parts' values are summed, kLoads parts of a warp in flight.
+template <int kDim, int kWarps> struct JoinSpace { float2 stats[kMaxSms * kMostWarps]; float sums[kWarps][kDim], tops[kWarps], totals[kWarps]; };
+template <typename T, int kDim, int kWarps> __device__ __forceinline__ void join_by_cta(const JoinRow<T>& x, JoinSpace<kDim, kWarps>& sh) {
+  constexpr int kVals = kDim / 32, kLoads = kWarps > 8 ? 4 : 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float top = -INFINITY;
-  for (int i = threadIdx.x; i < parts; i += kJoinWarps * 32) {
-    const float2 x = *reinterpret_cast<const float2*>(row(i) + kDim);
-    stats[i] = x;
-    top = fmaxf(top, x.x);
+  for (int i = threadIdx.x; i < x.parts; i += kWarps * 32) {
+    const float2 st = *reinterpret_cast<const float2*>(x.part(i) + kDim);
+    sh.stats[i] = st;
+    top = fmaxf(top, st.x);
   }
   top = warp_max(top);
-  if (lane == 0) tops[warp] = top;
+  if (lane == 0) sh.tops[warp] = top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
+  for (int i = 0; i < kWarps; ++i) top = fmaxf(top, sh.tops[i]);
   float l = 0.f, v[kVals] = {};
-  for (int base = warp; base < parts; base += kJoinLoads * kJoinWarps) {
-    float x[kJoinLoads][kVals];
+  for (int base = warp; base < x.parts; base += kLoads * kWarps) {
+    float y[kLoads][kVals];
 #pragma unroll
-    for (int u = 0; u < kJoinLoads; ++u) {
-      const int i = base + u * kJoinWarps;
-      if (i < parts) load_values<kVals>(row(i) + lane * kVals, x[u]);
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = base + u * kWarps;
+      if (i < x.parts) load_values<kVals>(x.part(i) + lane * kVals, y[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kJoinLoads; ++u) {
-      const int i = base + u * kJoinWarps;
-      if (i >= parts) break;
-      const float2 st = stats[i];
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = base + u * kWarps;
+      if (i >= x.parts) break;
+      const float2 st = sh.stats[i];
       if (st.x == -INFINITY) continue;                 // the part holds nothing that this row sees
       const float c = ex2(st.x - top);
       l = fmaf(st.y, c, l);
 #pragma unroll
-      for (int e = 0; e < kVals; ++e) v[e] = fmaf(x[u][e], c, v[e]);
+      for (int e = 0; e < kVals; ++e) v[e] = fmaf(y[u][e], c, v[e]);
     }
   }
-  if (lane == 0) totals[warp] = l;
+  if (lane == 0) sh.totals[warp] = l;
 #pragma unroll
-  for (int e = 0; e < kVals; ++e) sums[warp][lane * kVals + e] = v[e];
+  for (int e = 0; e < kVals; ++e) sh.sums[warp][lane * kVals + e] = v[e];
   __syncthreads();
-  for (int d = threadIdx.x; d < kDim; d += kJoinWarps * 32) {
+  for (int d = threadIdx.x; d < kDim; d += kWarps * 32) {
     float ls = 0.f, vs = 0.f;
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) { ls += totals[i]; vs += sums[i][d]; }
-    out[d] = out_cast<T>(ls == 0.f ? 0.f : vs / ls);
+    for (int i = 0; i < kWarps; ++i) { ls += sh.totals[i]; vs += sh.sums[i][d]; }
+    x.out[d] = out_cast<T>(ls == 0.f ? 0.f : vs / ls);
   }
+}
+
+// Joins the parts of the rows whose chunks went to more than one warp.  kPerWarp: a warp per row (one of more than 32 parts is
+// left to the whole CTA), for many rows of mostly few parts; else a CTA per row.
+template <typename T, int kDim, int kWarps, bool kPerWarp>
+__global__ void __launch_bounds__(kWarps * 32) attention_kv4_join_kernel(Kv4AttnArgs a, Plan plan) {
+  __shared__ JoinSpace<kDim, kWarps> space;
+  __shared__ JoinRow<T> rows[kPerWarp ? kWarps : 1];
+  constexpr int kVals = kDim / 32, kLoads = 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_launch_dependents();
+  pdl_wait();
+  const JoinRow<T> x = join_row<T, kDim>(a, plan, kPerWarp ? (int64_t)blockIdx.x * kWarps + warp : (int64_t)blockIdx.x);
+  if (x.parts == 0 && (kPerWarp || warp == 0)) {
+    for (int d = lane; d < kDim; d += 32) x.out[d] = out_cast<T>(0.f);
+  }
+  if (!kPerWarp) {
+    if (x.parts > 1) join_by_cta<T, kDim, kWarps>(x, space);
+    return;
+  }
+  if (x.parts > 1 && x.parts <= 32) {
+    const float2 st = lane < x.parts ? *reinterpret_cast<const float2*>(x.part(lane) + kDim) : make_float2(-INFINITY, 0.f);
+    const float top = warp_max(st.x), c = st.x == -INFINITY ? 0.f : ex2(st.x - top);
+    const float l = warp_sum(st.x == -INFINITY ? 0.f : st.y * c);
+    float v[kVals] = {};
+    for (int base = 0; base < x.parts; base += kLoads) {
+      float y[kLoads][kVals];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+        if (base + u < x.parts) load_values<kVals>(x.part(base + u) + lane * kVals, y[u]);
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const float cu = __shfl_sync(0xFFFFFFFFu, c, (base + u) & 31), m = __shfl_sync(0xFFFFFFFFu, st.x, (base + u) & 31);
+        if (base + u >= x.parts || m == -INFINITY) continue;
+#pragma unroll
+        for (int e = 0; e < kVals; ++e) v[e] = fmaf(y[u][e], cu, v[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kVals; ++e) x.out[lane * kVals + e] = out_cast<T>(l == 0.f ? 0.f : v[e] / l);
+  }
+  if (lane == 0) rows[warp] = x;
+  if (!__syncthreads_or(x.parts > 32)) return;
+  for (int i = 0; i < kWarps; ++i)
+    if (rows[i].parts > 32) {
+      join_by_cta<T, kDim, kWarps>(rows[i], space);
+      __syncthreads();
+    }
 }
 
 cudaError_t sm_count(int dev, int* n) {
@@ -839,11 +898,13 @@ cudaError_t launch_rows(const Kv4AttnArgs& a, int dev, int sms, cudaStream_t s) 
   const Plan plan = make_plan(a.n_q, a.heads, a.cache.kv_heads, a.cache.page_size, sms * kWarps);
   e = launch_pdl(kernel, (unsigned)sms, kWarps * 32, kSmem, s, a, plan, polls);
   if (e != cudaSuccess) return e;
-  // One CTA per row: 32 warps while each has an SM to itself (32000 tokens, 8 heads, 4 rows: 17.3 us against 23.8), 8 where there
-  // are more rows (16 x 1000 tokens: 12.0 us against 14.5).
+  // A CTA per row, of 32 warps while each has an SM to itself (32000 tokens, 8 heads, 4 rows: 17.3 us against 23.8 with 8; with
+  // more rows 16 warps already lose, 14.5 against 12.0 at 16 x 1000 tokens).  Many rows have few parts each, and get a warp (256 x
+  // 1000 tokens, 8 heads, 4 rows: 70 us against 93; 256 x 60: 18 against 30; but 8 x 16000, 256 rows: 40 against 34).
   const int64_t rows = (int64_t)a.batch * plan.heads_blocks * plan.rows_per_block;
-  return rows <= sms ? launch_pdl(attention_kv4_join_kernel<T, kDim, 32>, (unsigned)rows, 1024, 0, s, a, plan)
-                     : launch_pdl(attention_kv4_join_kernel<T, kDim, 8>, (unsigned)rows, 256, 0, s, a, plan);
+  if (rows <= sms) return launch_pdl(attention_kv4_join_kernel<T, kDim, 32, false>, (unsigned)rows, 1024, 0, s, a, plan);
+  if (rows <= kCtaRows * sms) return launch_pdl(attention_kv4_join_kernel<T, kDim, 8, false>, (unsigned)rows, 256, 0, s, a, plan);
+  return launch_pdl(attention_kv4_join_kernel<T, kDim, 8, true>, (unsigned)((rows + 7) / 8), 256, 0, s, a, plan);
 }
 
 // Longer or more lists.  Up to 8 query rows: 12 warps with two chunks each keep the SM busier (32 x 8192 tokens, 8 heads, 4 rows:

@@ -231,6 +231,7 @@ def test_attention_kv4(dt, lens, n_q, hk, g, dim, page, window, sinks):
     ([i * 37 % 301 for i in range(110)], 1, 2, 3, 64, 16, 0, 0),                   # more lists than the GPU holds CTAs, short
     ([3, 700] + [i * 29 % 90 for i in range(38)], 1, 8, 1, 128, 64, 0, 0),         # the same with a long bound of the lengths
     ([i * 31 % 200 for i in range(80)], 3, 2, 4, 64, 32, 60, 2),                   # with more than 8 query rows
+    ([4500] + [0] * 50 + [1, 130] * 75, 1, 1, 4, 64, 64, 0, 0),                    # one long list among many
     ([20000], 4, 1, 4, 128, 64, 0, 0), ([20000, 9], 1, 2, 4, 64, 32, 0, 0),        # lists too long for a cluster
     ([16384], 1, 1, 2, 64, 64, 0, 0), ([8191, 70, 0, 1], 1, 4, 2, 128, 64, 0, 0),  # clusters with four chunks per warp, and ragged
     ([64 * 8, 64 * 8 + 1], 6, 2, 2, 128, 16, 0, 0)])                               # one chunk per warp of a CTA, and one more
