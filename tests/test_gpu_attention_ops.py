@@ -361,6 +361,43 @@ def test_attention_kv4_reports_waits_that_run_out():
     assert B.ws_status(ws) == B.OK
 
 
+@pytest.mark.parametrize("batch,longest", [(2, 16500), (80, 200)])       # lists cut over the GPU: too long for clusters, too many
+def test_attention_kv4_cut_lists_in_a_graph_on_two_streams_and_when_waits_run_out(batch, longest):
+    hk, heads, dim, page, dt = 2, 8, 64, 64, BF16
+    first = [longest] + [(i * 53 + 1) % longest for i in range(1, batch)]
+    cache, table = fill(batch, first, page, hk, dim, dt, seed=9)
+    lens = torch.tensor(first, device=DEV).int() - 3
+    qs = [randn(20 + i, batch, heads * dim, dtype=dt) for i in range(2)]
+    ws = [torch.empty(B.attention_kv4_ws_bytes(batch, 1, heads, hk, dim), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    wants = [[B.attention_kv4(x, cache, table, lens + i, batch, 1, heads) for i in range(3)] for x in qs]
+    check_kv4(qs[0], cache, table, [max(n - 3, 0) for n in first], batch, 1, heads, 0, 0, 0.0, wants[0][0], some=[1])
+    o, graph = torch.empty_like(qs[0]), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.attention_kv4(qs[0], cache, table, lens, batch, 1, heads, o=o, ws=ws[0])
+        lens.add_(1)
+    for i in range(3):
+        graph.replay()
+        assert torch.equal(o, wants[0][i])
+    lens.sub_(3)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        outs = []
+        for s, x, w in zip(streams, qs, ws):
+            with torch.cuda.stream(s):
+                outs.append(B.attention_kv4(x, cache, table, lens, batch, 1, heads, ws=w))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b[0]) for a, b in zip(outs, wants))
+    B.debug_wait_limit(0)
+    try:
+        B.attention_kv4(qs[0], cache, table, lens, batch, 1, heads, ws=ws[0])
+        assert B.ws_status(ws[0]) == B.ERR_TIMEOUT
+    finally:
+        B.debug_wait_limit(-1)
+    assert torch.equal(B.attention_kv4(qs[0], cache, table, lens, batch, 1, heads, ws=ws[0]), wants[0][0])
+    assert B.ws_status(ws[0]) == B.OK
+
+
 def test_cache_beyond_32_bit_offsets():
     """A cache of 5 GB: the last pages lie beyond 2^32 bytes."""
     page, hk, dim, dt = 64, 8, 128, F16
