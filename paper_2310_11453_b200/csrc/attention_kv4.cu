@@ -725,8 +725,8 @@ template <typename T, int kDim> __device__ __forceinline__ JoinRow<T> join_row(c
     x.parts = 0;
     return x;
   }
-  const int w0 = ends.x >> 1, parts = ends.y - w0 + 1;
-  if (w0 < 0 || parts < 1 || ends.y >= plan.parts) return x;   // never written: the first kernel gave up (status word)
+  const int w0 = ends.x >> 1, parts = part_count(ends.x, ends.y, plan.parts);
+  if (parts == 0) return x;                            // never written: the first kernel gave up (status word)
   // the first part may be in its warp's second slot; the others are in first slots
   x.parts = parts;
   x.stride = 2 * slot_floats(plan, kDim);

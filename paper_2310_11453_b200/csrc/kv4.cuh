@@ -21,6 +21,13 @@ template <int kDim> struct Block {
   }
 };
 
+// How many parts a list of attention_kv4 has, of the slot (two per warp) of its first part and the warp of its last; 0 where
+// the two do not name parts of `warps` warps (a workspace that nobody wrote may hold any bits).
+__host__ __device__ inline int part_count(int first_slot, int last_warp, int warps) {
+  const int w0 = first_slot >> 1;
+  return w0 < 0 || last_warp < w0 || last_warp >= warps ? 0 : last_warp - w0 + 1;
+}
+
 // (step, eta) as stored: two 16-bit numbers of the cache's type.
 template <typename T> __device__ __forceinline__ float2 scale_floats(uint32_t w);
 template <> __device__ __forceinline__ float2 scale_floats<__half>(uint32_t w) {

@@ -1,5 +1,6 @@
 """What the attention operators refuse, on the host and before any launch, and their sizes."""
 import ctypes as C
+import subprocess
 
 import pytest
 import torch
@@ -143,3 +144,18 @@ def test_layout_reference_is_a_bijection():
     for dim in (64, 128):
         seen = {value_place(t, d, dim) for t in range(32) for d in range(dim)}
         assert len(seen) == 32 * dim and max(b for b, _ in seen) == 32 * dim // 2 - 1
+
+
+def test_parts_named_by_any_bits_stay_within_the_workspace(tmp_path):
+    """part_count of csrc/kv4.cuh, compiled for the host: what it lets pass lies within the warps' parts, whatever it is given."""
+    from paper_2310_11453_b200.build import CSRC, NVCC
+    src, exe = tmp_path / "parts.cu", tmp_path / "parts"
+    src.write_text('#include <stdio.h>\n#include <stdlib.h>\n#include "kv4.cuh"\nint main(int n, char** v) {\n'
+                   '  for (int i = 1; i + 2 < n; i += 3) printf("%d\\n", bl::kv4::part_count(atoi(v[i]), atoi(v[i + 1]), atoi(v[i + 2])));\n}\n')
+    subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", CSRC, str(src), "-o", str(exe)], check=True)
+    ends = (-2 ** 31, -2 ** 31 + 1, -10 ** 9, -1, 0, 1, 2, 3, 50, 1775, 1776, 3551, 3552, 10 ** 9, 2 ** 31 - 2, 2 ** 31 - 1)
+    args = [(a, b, w) for a in ends for b in ends for w in (1, 64, 1776)]
+    out = subprocess.run([str(exe)] + [str(x) for t in args for x in t], check=True, capture_output=True, text=True).stdout.split()
+    for (first, last, warps), n in zip(args, map(int, out), strict=True):
+        w0 = first // 2
+        assert n == (last - w0 + 1 if 0 <= w0 <= last < warps else 0), (first, last, warps)
