@@ -454,6 +454,7 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   lens int32 [batch]: tokens of the sequence in the cache, the n_q new ones included (clamped to
  *   0..max_pages * page_size).  Query i of n_q stands at position lens - n_q + i; one that sees nothing
  *   (negative position, empty sequence) gets zeros.
+ *   A query whose visible scores have no softmax (a NaN or +infinity among them, or nothing but -infinity) gets NaN.
  *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
  * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
  * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.

@@ -181,6 +181,9 @@ __device__ __forceinline__ float2 peer_float2(const float* p, int rank) {
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
+// Whether a part with this maximum and sum of a row holds nothing that the row sees.  The maximum alone does not say: fmaxf passes
+// NaN over, so a row of scores that are NaN, or all -infinity, has a maximum of -infinity too, and a sum that is NaN.
+__device__ __forceinline__ bool sees_nothing(float top, float sum) { return top == -INFINITY && sum == 0.f; }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -495,15 +498,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
           for (int t = 0; t < 2 * kWords; ++t) { acc[nt][t][j] *= cv; acc[nt][t][2 + j] *= cv; }
         }
     }
-    float mu[kNT][2], vscale[kNT][2];
+    float vscale[kNT][2];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
       for (int j = 0; j < 2; ++j) vscale[nt][j] = pow2i(min(13 - vexp[nt][j], 120));
-#pragma unroll
-    for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) mu[nt][j] = kMask && m[nt][j] == -INFINITY ? 0.f : m[nt][j];
 
     // ---- probabilities, and their products with the value codes
 #pragma unroll
@@ -516,11 +515,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         float u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = ex2(s[i][nt][e] - mu[nt][e & 1]);
+          const bool v = !kMask || ((seen >> ((i * kNT + nt) * 4 + e)) & 1u);
+          const float p = v ? ex2(s[i][nt][e] - m[nt][e & 1]) : 0.f;
           l[nt][e & 1] += p;
           u[e] = p * ((e < 2 ? v0.x : v1.x) * vscale[nt][e & 1]);
           if (kMask) {
-            const bool v = (seen >> ((i * kNT + nt) * 4 + e)) & 1u;
             if (!v) u[e] = 0.f;
             esum[nt][e & 1] += v ? p * (e < 2 ? v0.y : v1.y) : 0.f;
           } else {
@@ -653,7 +652,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
       const float* x = part + i * (kStages * kStageBytes / 4);
-      if (x[kDim] == -INFINITY) continue;
+      if (sees_nothing(x[kDim], x[kDim + 1])) continue;
       const float c = ex2(x[kDim] - top);
       l = fmaf(x[kDim + 1], c, l);
       v.x = fmaf(x[d], c, v.x); v.y = fmaf(x[d + 1], c, v.y);
@@ -678,7 +677,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     for (int i = 0; i < kMostCluster; ++i) top = fmaxf(top, stat[i].x);
 #pragma unroll
     for (int i = 0; i < kMostCluster; ++i) {
-      if (stat[i].x == -INFINITY) continue;
+      if (sees_nothing(stat[i].x, stat[i].y)) continue;
       const float c = ex2(stat[i].x - top);
       l = fmaf(stat[i].y, c, l);
       v.x = fmaf(x[i].x, c, v.x); v.y = fmaf(x[i].y, c, v.y);
@@ -764,7 +763,7 @@ template <typename T, int kDim, int kWarps> __device__ __forceinline__ void join
       const int i = base + u * kWarps;
       if (i >= x.parts) break;
       const float2 st = sh.stats[i];
-      if (st.x == -INFINITY) continue;                 // the part holds nothing that this row sees
+      if (sees_nothing(st.x, st.y)) continue;
       const float c = ex2(st.x - top);
       l = fmaf(st.y, c, l);
 #pragma unroll
@@ -803,8 +802,10 @@ __global__ void __launch_bounds__(kWarps * 32) attention_kv4_join_kernel(Kv4Attn
   }
   if (x.parts > 1 && x.parts <= 32) {
     const float2 st = lane < x.parts ? *reinterpret_cast<const float2*>(x.part(lane) + kDim) : make_float2(-INFINITY, 0.f);
-    const float top = warp_max(st.x), c = st.x == -INFINITY ? 0.f : ex2(st.x - top);
-    const float l = warp_sum(st.x == -INFINITY ? 0.f : st.y * c);
+    const bool none = sees_nothing(st.x, st.y);
+    const float top = warp_max(st.x), c = none ? 0.f : ex2(st.x - top);
+    const float l = warp_sum(none ? 0.f : st.y * c);
+    const unsigned takes = __ballot_sync(0xFFFFFFFFu, !none);
     float v[kVals] = {};
     for (int base = 0; base < x.parts; base += kLoads) {
       float y[kLoads][kVals];
@@ -813,8 +814,8 @@ __global__ void __launch_bounds__(kWarps * 32) attention_kv4_join_kernel(Kv4Attn
         if (base + u < x.parts) load_values<kVals>(x.part(base + u) + lane * kVals, y[u]);
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        const float cu = __shfl_sync(0xFFFFFFFFu, c, (base + u) & 31), m = __shfl_sync(0xFFFFFFFFu, st.x, (base + u) & 31);
-        if (base + u >= x.parts || m == -INFINITY) continue;
+        const float cu = __shfl_sync(0xFFFFFFFFu, c, (base + u) & 31);
+        if (base + u >= x.parts || !((takes >> ((base + u) & 31)) & 1u)) continue;
 #pragma unroll
         for (int e = 0; e < kVals; ++e) v[e] = fmaf(y[u][e], cu, v[e]);
       }

@@ -1,0 +1,81 @@
+"""The attention operators at inputs where a wrong answer hides."""
+import math
+
+import pytest
+import torch
+
+from paper_2310_11453_b200 import binding as B
+from tests.test_gpu_attention_ops import BF16, DEV, F16, fill, randn
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention over the cache: what is not finite shows, however the work was cut ------------------
+# lengths, n_q, key/value heads, group, head_dim, page: each way of cutting the lists
+CUTS = [
+    ([129], 1, 2, 2, 64, 16), ([65, 641, 1], 1, 2, 4, 128, 32), ([321, 64 * 6 + 1], 3, 2, 4, 64, 64),          # clusters
+    ([64 * 320 + 1], 1, 1, 4, 128, 64), ([64 * 313 + 1, 9], 2, 2, 8, 64, 32),                                  # a CTA of 32 warps joins a row
+    ([64 * 266 + 1, 9, 321, 65], 1, 8, 8, 64, 64),                                                             # a CTA of 8 warps
+    ([64 * (i % 5) + 1 for i in range(110)], 1, 2, 3, 64, 16), ([65 + 64 * (i % 3) for i in range(80)], 3, 2, 4, 64, 32),   # a warp, and lists
+    ([64 * 70 + 1] + [0] * 50 + [1, 129] * 75, 1, 1, 4, 64, 64),                                               # that one warp holds as a whole
+]
+
+
+def laid_out(dt, cut, positive=False):
+    lens, n_q, hk, g, dim, page = cut
+    cache, table = fill(len(lens), lens, page, hk, dim, dt, seed=len(lens) + n_q)
+    if positive:                                                       # every key value lies between 1 and 2
+        T = cache.pages.shape[0] * page
+        rows = torch.rand((T, hk * dim), device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)) + 1
+        B.kv4_append(cache, rows.to(dt), randn(4, T, hk * dim, dtype=dt), torch.arange(T, device=DEV))
+    q = randn(5, len(lens) * n_q, hk * g * dim, dtype=dt)
+    return cache, table, torch.tensor(lens, device=DEV, dtype=torch.int32), q
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("dt,bad,positive", [(F16, math.nan, False), (BF16, math.inf, False), (F16, -math.inf, False), (BF16, -math.inf, True)])
+def test_attention_kv4_query_that_is_not_finite(dt, bad, positive, cut):
+    """One row of one head holds a value that is not finite: no softmax of its scores exists, so the row is NaN (its scores are
+    NaN, or some are +infinity, or, where all keys are positive, all are -infinity).  All other rows keep their bits."""
+    cache, table, lens, q = laid_out(dt, cut, positive)
+    batch, n_q, heads, dim = len(cut[0]), cut[1], cut[2] * cut[3], cut[4]
+    want = B.attention_kv4(q, cache, table, lens, batch, n_q, heads)
+    assert torch.isfinite(want).all()
+    for b in {0, batch - 1, batch // 2}:
+        for h in {0, heads - 1}:
+            q2 = q.clone()
+            q2[b * n_q + n_q - 1, h * dim + dim // 3] = bad
+            got = B.attention_kv4(q2, cache, table, lens, batch, n_q, heads)
+            expect = want.clone()
+            if cut[0][b] > 0:
+                expect[b * n_q + n_q - 1, h * dim:(h + 1) * dim] = math.nan
+            assert torch.equal(torch.isnan(got), torch.isnan(expect)), (b, h)
+            assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), (b, h)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("cut", CUTS)
+def test_attention_kv4_newest_token_that_is_not_finite(dt, cut):
+    """The newest token's key or value of one key/value head is stored as NaN, alone in its chunk where the length is 64 k + 1:
+    the newest query of that head's group is NaN.  Queries before it, other heads and other sequences keep their bits."""
+    lens, n_q, hk, g, dim, page = cut
+    batch, heads = len(lens), hk * g
+    for what in ("key", "value"):
+        cache, table, lt, q = laid_out(dt, cut)
+        want = B.attention_kv4(q, cache, table, lt, batch, n_q, heads)
+        for b in {0, batch - 1}:
+            if lens[b] == 0:
+                continue
+            at = table[b, (lens[b] - 1) // page].long().view(1) * page + (lens[b] - 1) % page
+            pages = cache.pages.clone()
+            k, v = B.kv4_read(cache, at)
+            (k if what == "key" else v)[0, (hk - 1) * dim + 5] = math.nan
+            hit = B.Kv4Cache(pages, page, hk, dim, dt)
+            B.kv4_append(hit, k, v, at)
+            kept = cache.pages.clone().view(cache.pages.shape[0], hk, -1)
+            kept[:, hk - 1] = pages.view(cache.pages.shape[0], hk, -1)[:, hk - 1]       # the other heads as they were, to the bit
+            got = B.attention_kv4(q, B.Kv4Cache(kept.view_as(pages), page, hk, dim, dt), table, lt, batch, n_q, heads)
+            expect = want.clone()
+            expect[b * n_q + n_q - 1, (hk - 1) * g * dim:] = math.nan
+            assert torch.equal(torch.isnan(got), torch.isnan(expect)), (what, b)
+            assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), (what, b)
