@@ -459,8 +459,8 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
  * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.
  * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; its first word is the status word of
- * bitlinear_ws_status: the kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means o of
- * this call is not valid); calls that may overlap need workspaces of their own. */
+ * bitlinear_ws_status: the kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means that
+ * one ran out; the rows of o that miss tokens for it are NaN); calls that may overlap need workspaces of their own. */
 bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, int64_t ld_q, const bl_kv4_cache* cache,
                                   const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
                                   int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,

@@ -22,9 +22,10 @@
 // Work.  The visible tokens of all sequences, in chunks of 64, times key/value heads (times blocks of query rows)
 // form one list that is cut into equal parts, one per warp: ragged batches and single long sequences balance
 // alike.  A warp runs on its own: its chunks stream into its part of shared memory by bulk copies, one or two ahead
-// (104 or 139 KB in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is reported in
-// the workspace's status word.  A warp that owns all chunks of a head writes the output; else its
-// unnormalised sums go to the workspace, two slots per warp, and a second kernel joins them in list order.
+// (104 or 139 KB in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is
+// reported in the workspace's status word, and the rows that the warp still had to work on become NaN.  A warp that owns
+// all chunks of a head writes the output; else its unnormalised sums go to the workspace, two slots per warp, and a second
+// kernel joins them in list order.
 // Few and short lists go to clusters of CTAs instead, one per list (a sequence, key/value head and block of rows), which
 // join their parts through each other's shared memory: one kernel (launch_dim gives the rule).
 #include <algorithm>
@@ -235,6 +236,55 @@ template <> __device__ __forceinline__ void load_words<4>(const char* p, uint32_
 template <> __device__ __forceinline__ void load_words<2>(const char* p, uint32_t (&w)[2]) {
   const uint2 r = *reinterpret_cast<const uint2*>(p);
   w[0] = r.x; w[1] = r.y;
+}
+
+// The two numbers by which the join finds a row block's parts: the slot of the first chunk's, the warp of the last chunk's.
+__device__ __forceinline__ int* ends_at(const Kv4AttnArgs& a, const Plan& plan, int b, int hk, int blk) {
+  return ends_of(a, plan) + 2 * (((int64_t)b * a.cache.kv_heads + hk) * plan.blocks + blk);
+}
+
+// Warp w's copies did not come: the rows of its items from `item` on (later: an item before it ended a segment; from_start: the
+// segment that it goes on with began with its list's first chunk) become NaN, a part's sum where they are not the warp's alone,
+// which goes through every join.  Out of line, with a walk of its own: the loop over the chunks has no register to spare for it.
+template <typename T, int kDim>
+__device__ __noinline__ void lose_items(Kv4AttnArgs a, Plan plan, int w, int item, bool later, bool from_start, bool fresh) {
+  const int lane = threadIdx.x & 31;
+  const float nan = __int_as_float(0x7FC00000);
+  Spread spread(a);
+  const Cut cut(spread.all * plan.heads_blocks, plan);
+  const int64_t end = cut.begin(w + 1);
+  int64_t at = cut.begin(w) + item, rest;
+  Walk x;
+  x.b = spread.find(a, plan.heads_blocks, at, rest);
+  x.s = make_seq(a, x.b);
+  const int hb = (int)(rest / x.s.chunks);
+  x.c = (int)(rest - (int64_t)hb * x.s.chunks);
+  x.hk = hb / plan.blocks;
+  x.blk = hb - x.hk * plan.blocks;
+  while (at < end) {                                   // a segment each time: all that is left of a list, or of the warp's items
+    if (fresh) from_start = x.c == 0;
+    const int n = (int)min((int64_t)(x.s.chunks - x.c), end - at);
+    const bool last = x.c + n == x.s.chunks;
+    float* slot = slots_of(a) + (2 * w + later) * slot_floats(plan, kDim);
+    if (lane == 0) {
+      int* where = ends_at(a, plan, x.b, x.hk, x.blk);
+      if (from_start) where[0] = 2 * w + later;
+      if (last) where[1] = w;
+    }
+    for (int rr = 0; rr < min(plan.rows_per_block, plan.rows - x.blk * plan.rows_per_block); ++rr) {
+      const int r = x.blk * plan.rows_per_block + rr, i_q = r / plan.group;
+      T* out = reinterpret_cast<T*>(a.o) + ((int64_t)x.b * a.n_q + i_q) * a.ld_o + (int64_t)(x.hk * plan.group + r - i_q * plan.group) * kDim;
+      if (from_start && last) {
+        for (int d = lane; d < kDim; d += 32) out[d] = out_cast<T>(nan);
+      } else if (lane == 0) {
+        *reinterpret_cast<float2*>(slot + rr * (kDim + 4) + kDim) = make_float2(-INFINITY, nan);
+      }
+    }
+    later = fresh = true;
+    at += n;
+    x.c += n - 1;
+    if (at < end) x.next(a, plan);
+  }
 }
 
 // What a chunk in flight is, written beside its bytes when its copies are issued.
@@ -549,7 +599,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
     const bool whole = !kCluster && from_start && it.last;
     // where the join finds the row block's parts: that of the first chunk (slot), that of the last (warp)
     if (!kCluster && lane == 0) {
-      int* where = ends_of(a, plan) + 2 * (((int64_t)it.b * a.cache.kv_heads + it.hk) * plan.blocks + it.rows0 / plan.rows_per_block);
+      int* where = ends_at(a, plan, it.b, it.hk, it.rows0 / plan.rows_per_block);
       if (from_start) where[0] = 2 * w + later;
       if (it.last) where[1] = w;
     }
@@ -615,11 +665,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   if (!kCluster || items > 0) begin_segment(items_of[0]);   // while the first chunk is on its way
   bool fresh = false;
   for (int item = 0; item < items; ++item) {
-    if (!arrived(item, polls)) {                       // the copies did not come: reported, nothing more is done
+    if (!arrived(item, polls)) {                       // the copies did not come: reported, and the rows that miss them become NaN
       if (lane == 0) *reinterpret_cast<volatile uint32_t*>(a.ws) = BL_ERR_TIMEOUT;
       for (int i = item; i < min(issued, items); ++i) arrived(i, tc::kSpinLimit);   // those in flight end before the CTA does (bounded)
-      if (!kCluster) return;
-      items = 0;
+      if (!kCluster) {
+        lose_items<T, kDim>(a, plan, w, item, later, from_start, fresh);
+        return;
+      }
+      __syncwarp();                                    // the part's sums take the place of its chunks, where the copies have ended
+      if (lane < plan.rows_per_block)
+        *reinterpret_cast<float2*>(reinterpret_cast<float*>(ring) + lane * (kDim + 4) + kDim) = make_float2(-INFINITY, __int_as_float(0x7FC00000));
       break;
     }
     const Item it = items_of[item % kStages];
@@ -638,7 +693,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   // ---- the parts of the CTA's warps become one, then those of the cluster's CTAs
   constexpr int kRow = kDim + 4;                       // a row's sums, its maximum, the sum of its probabilities
   float* joined = reinterpret_cast<float*>(smem + kWarps * kStages * (kStageBytes + (int)sizeof(Item) + 8));
-  if (items == 0 && lane < plan.rows_per_block)        // nothing, or not all of it came
+  if (items == 0 && lane < plan.rows_per_block)        // nothing
     *reinterpret_cast<float2*>(reinterpret_cast<float*>(ring) + lane * kRow + kDim) = make_float2(-INFINITY, 0.f);
   __syncthreads();
   const int rows0 = ahead.blk * plan.rows_per_block, rows = min(plan.rows_per_block, plan.rows - rows0);
@@ -725,7 +780,7 @@ template <typename T, int kDim> __device__ __forceinline__ JoinRow<T> join_row(c
     return x;
   }
   const int w0 = ends.x >> 1, parts = part_count(ends.x, ends.y, plan.parts);
-  if (parts == 0) return x;                            // never written: the first kernel gave up (status word)
+  if (parts == 0) return x;                            // cannot be: the first kernel's warps end every list, also one whose copies did not come
   // the first part may be in its warp's second slot; the others are in first slots
   x.parts = parts;
   x.stride = 2 * slot_floats(plan, kDim);

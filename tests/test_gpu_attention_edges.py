@@ -79,3 +79,29 @@ def test_attention_kv4_newest_token_that_is_not_finite(dt, cut):
             expect[b * n_q + n_q - 1, (hk - 1) * g * dim:] = math.nan
             assert torch.equal(torch.isnan(got), torch.isnan(expect)), (what, b)
             assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), (what, b)
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("given", [False, True])
+def test_attention_kv4_rows_are_nan_where_waits_run_out(given, cut):
+    """With no polls allowed no chunk arrives: rows that miss tokens are NaN, whether or not the caller can ask for the status, and
+    whatever the workspace held.  A sequence without tokens waits for nothing."""
+    lens, n_q, hk, g, dim, page = cut
+    batch, heads = len(lens), hk * g
+    cache, table, lt, q = laid_out(BF16, cut)
+    want = B.attention_kv4(q, cache, table, lt, batch, n_q, heads)
+    size = B.attention_kv4_ws_bytes(batch, n_q, heads, hk, dim)
+    ws = torch.randint(0, 256, (size,), device=DEV, dtype=torch.uint8) if given else None
+    o = torch.full_like(want, 3.0)
+    B.debug_wait_limit(0)
+    try:
+        B.attention_kv4(q, cache, table, lt, batch, n_q, heads, o=o, ws=ws)
+        if given:
+            assert B.ws_status(ws) == B.ERR_TIMEOUT
+        torch.cuda.synchronize()
+    finally:
+        B.debug_wait_limit(-1)
+    some = (lt > 0).repeat_interleave(n_q)
+    assert torch.isnan(o[some]).all() and not o[~some].any()
+    assert torch.equal(B.attention_kv4(q, cache, table, lt, batch, n_q, heads, o=o, ws=ws), want)
+    assert not given or B.ws_status(ws) == B.OK
