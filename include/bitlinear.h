@@ -458,9 +458,9 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
  * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
  * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.
- * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; its first word is the status word of
- * bitlinear_ws_status: the kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means that
- * one ran out; the rows of o that miss tokens for it are NaN); calls that may overlap need workspaces of their own. */
+ * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; bitlinear_ws_status reads its start: the
+ * kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means that one ran out; the rows of o
+ * that miss tokens for it are NaN); calls that may overlap need workspaces of their own. */
 bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, int64_t ld_q, const bl_kv4_cache* cache,
                                   const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
                                   int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,
@@ -476,8 +476,9 @@ size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_he
 bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
                                    const int32_t* pairs, int64_t n, void* stream);
 
-/* Synchronises `stream`, then reads the status word a previous bitlinear_forward or
- * bitlinear_matmul_i32 call left in `ws`.  BL_OK, BL_ERR_TIMEOUT, or BL_ERR_CUDA. */
+/* Synchronises `stream`, then reads the status that a previous bitlinear_forward,
+ * bitlinear_matmul_i32 or other call that names it left at the start of `ws` (a word, or words
+ * of which any may report).  BL_OK, BL_ERR_TIMEOUT, or BL_ERR_CUDA. */
 bl_status bitlinear_ws_status(const void* ws, void* stream);
 
 /* Test and diagnostic hook: caps the number of polls that the bounded device-side waits of

@@ -544,8 +544,8 @@ def attention_kv4_ws_bytes(batch, n_q, heads, kv_heads, head_dim) -> int:
 def attention_kv4(q, cache, block_table, lens, batch, n_q, heads, window=0, sinks=0, scale=0.0, o=None, ws=None):
     """bitlinear_attention_kv4.  q [batch*n_q, heads*head_dim] of the cache's dtype; block_table int32 [batch, max_pages];
     lens int32 [batch], the n_q new tokens included.  Returns o like q.  `ws` may carry a workspace of
-    attention_kv4_ws_bytes() bytes (its first word is the status word); with or without it, rows that miss tokens because a
-    bounded wait ran out are NaN."""
+    attention_kv4_ws_bytes() bytes, of which ws_status() then tells whether a bounded wait ran out; with or without it, rows
+    that miss tokens for that reason are NaN."""
     r = (_fast or _marshal()).kv4(*cache._args, q, block_table, lens, batch, n_q, heads, window, sinks, scale, o, ws)
     if type(r) is int:
         _check(r, "bitlinear_attention_kv4")

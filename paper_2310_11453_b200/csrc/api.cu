@@ -643,7 +643,14 @@ bl_status bitlinear_ws_status(const void* ws, void* stream) {
   uint32_t word = 0;
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return BL_ERR_CUDA;
   if (cudaMemcpy(&word, ws, sizeof(word), cudaMemcpyDeviceToHost) != cudaSuccess) return BL_ERR_CUDA;
-  return word == 0 ? BL_OK : BL_ERR_TIMEOUT;
+  const uint32_t n = word - kStatusPerWarp;            // words that follow
+  if (n > kMostStatusWords) return word == 0 ? BL_OK : BL_ERR_TIMEOUT;
+  uint32_t words[kMostStatusWords];
+  if (n > 0 && cudaMemcpy(words, reinterpret_cast<const uint32_t*>(ws) + 1, n * sizeof(uint32_t), cudaMemcpyDeviceToHost) != cudaSuccess)
+    return BL_ERR_CUDA;
+  for (uint32_t i = 0; i < n; ++i)
+    if (words[i] != 0) return BL_ERR_TIMEOUT;
+  return BL_OK;
 }
 
 int64_t bitlinear_debug_decode_fallbacks(void* stream) {

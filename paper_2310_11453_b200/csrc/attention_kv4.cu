@@ -23,7 +23,7 @@
 // form one list that is cut into equal parts, one per warp: ragged batches and single long sequences balance
 // alike.  A warp runs on its own: its chunks stream into its part of shared memory by bulk copies, one or two ahead
 // (104 or 139 KB in flight per SM), with no barrier between warps.  The wait for a chunk is bounded; one that runs out is
-// reported in the workspace's status word, and the rows that the warp still had to work on become NaN.  A warp that owns
+// reported in the warp's status word, and the rows that the warp still had to work on become NaN.  A warp that owns
 // all chunks of a head writes the output; else its unnormalised sums go to the workspace, two slots per warp, and a second
 // kernel joins them in list order.
 // Few and short lists go to clusters of CTAs instead, one per list (a sequence, key/value head and block of rows), which
@@ -46,7 +46,8 @@ constexpr int kMaxSms = 160;
 constexpr int kMostClusterLog2 = 3, kMostCluster = 1 << kMostClusterLog2;   // CTAs of a cluster
 constexpr int kCtaRows = 4;                // rows of the result per SM up to which the join has a CTA for each
 constexpr int kClusterChunks = 4;          // chunks per warp up to which a cluster takes a list
-constexpr size_t kStatusBytes = 256;       // the status word lies at the start of the workspace
+constexpr size_t kStatusBytes = 7936;      // the status words lie at the start of the workspace
+static_assert((1 + kMaxSms * kMostWarps) * 4 <= kStatusBytes && kMaxSms * kMostWarps <= (int)kMostStatusWords, "more warps than status words");
 
 struct Plan {                              // how the list is laid out; made on the host, the same for both kernels
   int group, rows, rows_per_block, blocks; // query heads per key/value head; query rows; rows per block; blocks
@@ -126,12 +127,16 @@ struct Spread {
   }
 };
 
-// Workspace: the status word, the parts (two slots per warp), then two numbers per sequence, head and block of rows.
+// Workspace: the status words (one per warp), the parts (two slots per warp), then two numbers per sequence, head and block of rows.
 __host__ __device__ inline int64_t slot_floats(const Plan& plan, int head_dim) { return (int64_t)plan.rows_per_block * (head_dim + 4); }
 __device__ __forceinline__ float* slots_of(const Kv4AttnArgs& a) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kStatusBytes); }
 __device__ __forceinline__ int* ends_of(const Kv4AttnArgs& a, const Plan& plan) {
   return reinterpret_cast<int*>(slots_of(a) + 2 * plan.parts * slot_floats(plan, a.cache.head_dim));
 }
+
+// The warps of the launch in one row of numbers (those of a CTA far apart: short lists spread over the SMs), and a warp's status word.
+__device__ __forceinline__ int warp_number() { return (int)((threadIdx.x >> 5) * gridDim.x + blockIdx.x); }
+__device__ __forceinline__ void set_status(void* ws, uint32_t status) { reinterpret_cast<volatile uint32_t*>(ws)[1 + warp_number()] = status; }
 
 // a / b for a >= 0, b > 0: the 32-bit division (a fifth of the instructions) where it serves.
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
@@ -243,12 +248,12 @@ __device__ __forceinline__ int* ends_at(const Kv4AttnArgs& a, const Plan& plan, 
   return ends_of(a, plan) + 2 * (((int64_t)b * a.cache.kv_heads + hk) * plan.blocks + blk);
 }
 
-// Warp w's copies did not come: the rows of its items from `item` on (later: an item before it ended a segment; from_start: the
+// The warp's copies did not come: the rows of its items from `item` on (later: an item before it ended a segment; from_start: the
 // segment that it goes on with began with its list's first chunk) become NaN, a part's sum where they are not the warp's alone,
 // which goes through every join.  Out of line, with a walk of its own: the loop over the chunks has no register to spare for it.
 template <typename T, int kDim>
-__device__ __noinline__ void lose_items(Kv4AttnArgs a, Plan plan, int w, int item, bool later, bool from_start, bool fresh) {
-  const int lane = threadIdx.x & 31;
+__device__ __noinline__ void lose_items(Kv4AttnArgs a, Plan plan, int item, bool later, bool from_start, bool fresh) {
+  const int lane = threadIdx.x & 31, w = warp_number();
   const float nan = __int_as_float(0x7FC00000);
   Spread spread(a);
   const Cut cut(spread.all * plan.heads_blocks, plan);
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   extern __shared__ __align__(16) char smem[];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, qd = lane & 3;
-  const int w = warp * gridDim.x + blockIdx.x;         // short lists spread over the SMs
+  const int w = warp_number();
   const int ps = a.cache.page_size, pl = plan.page_log2, block_bytes = Block<kDim>::bytes(ps), subs = kChunk >> pl;
   char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
@@ -316,7 +321,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   __syncwarp();
 
   pdl_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.ws) = 0;   // the status word
+  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.ws) = kStatusPerWarp + gridDim.x * kWarps;
+  if (lane == 0) set_status(a.ws, 0);
   // ---- loads: the page numbers of a chunk are fetched one chunk before its copies are issued
   Walk ahead;
   int items;
@@ -666,10 +672,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
   bool fresh = false;
   for (int item = 0; item < items; ++item) {
     if (!arrived(item, polls)) {                       // the copies did not come: reported, and the rows that miss them become NaN
-      if (lane == 0) *reinterpret_cast<volatile uint32_t*>(a.ws) = BL_ERR_TIMEOUT;
+      if (lane == 0) set_status(a.ws, BL_ERR_TIMEOUT);
       for (int i = item; i < min(issued, items); ++i) arrived(i, tc::kSpinLimit);   // those in flight end before the CTA does (bounded)
       if (!kCluster) {
-        lose_items<T, kDim>(a, plan, w, item, later, from_start, fresh);
+        lose_items<T, kDim>(a, plan, item, later, from_start, fresh);
         return;
       }
       __syncwarp();                                    // the part's sums take the place of its chunks, where the copies have ended
@@ -936,7 +942,7 @@ cudaError_t launch_clusters(const Kv4AttnArgs& a, int dev, int64_t lists, int64_
       if (e != cudaSuccess) return e;
       if (dev < 64) known[dev][i].store(fit + 1, std::memory_order_relaxed);
     }
-    if (lists <= fit) size = i;
+    if (lists <= fit && lists << i <= kMaxSms) size = i;       // (no more warps than the workspace has status words for)
   }
   if (size < 0 || chunks > kClusterChunks * 8 << size) return cudaSuccess;
   *done = true;

@@ -19,6 +19,12 @@ namespace bl {
 extern std::atomic<long long> g_debug_wait_polls;
 extern std::atomic<int> g_debug_meet_skew;
 
+// The start of a workspace is what bitlinear_ws_status reads: a status word, 0 or a bl_status, or kStatusPerWarp plus the number
+// of such words that follow it, one per warp of the kernel.  The latter is for a kernel whose warps all may report and which
+// nothing runs in front of: each warp clears its own word and sets it, so that no report can be cleared by another warp.
+constexpr uint32_t kStatusPerWarp = 0x5A570000u;
+constexpr uint32_t kMostStatusWords = 2047;
+
 // Programmatic dependent launch.  A kernel launched through launch_pdl() may be scheduled while
 // the kernel before it on the stream is still running: it calls pdl_wait() before its first
 // access to global memory (after set-up that touches only its own shared memory), which blocks

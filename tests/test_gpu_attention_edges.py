@@ -105,3 +105,34 @@ def test_attention_kv4_rows_are_nan_where_waits_run_out(given, cut):
     assert torch.isnan(o[some]).all() and not o[~some].any()
     assert torch.equal(B.attention_kv4(q, cache, table, lt, batch, n_q, heads, o=o, ws=ws), want)
     assert not given or B.ws_status(ws) == B.OK
+
+
+@pytest.mark.parametrize("lens", [[0, 300], [0, 64 * 270], [0] * 90 + [1]])
+def test_attention_kv4_a_report_stays(lens):
+    """Warps report waits that ran out each in a word of its own: the first CTA, which has nothing to do here, clears nobody else's.
+    Every such word counts, and a call that ends well clears them all."""
+    hk, heads, dim, page = 2, 4, 64, 64
+    cut = (lens, 1, hk, heads // hk, dim, page)
+    batch = len(lens)
+    cache, table, lt, q = laid_out(F16, cut)
+    ws = torch.randint(0, 256, (B.attention_kv4_ws_bytes(batch, 1, heads, hk, dim),), device=DEV, dtype=torch.uint8)
+    B.debug_wait_limit(0)
+    try:
+        for _ in range(100):
+            B.attention_kv4(q, cache, table, lt, batch, 1, heads, ws=ws)
+            assert B.ws_status(ws) == B.ERR_TIMEOUT
+    finally:
+        B.debug_wait_limit(-1)
+    B.attention_kv4(q, cache, table, lt, batch, 1, heads, ws=ws)
+    assert B.ws_status(ws) == B.OK
+    words = ws.view(torch.int32)
+    n = int(words[0]) & 0x7FF
+    assert n % 8 == 0 and not words[1:1 + n].any()
+    for i in (1, 2, n // 2, n - 1, n):
+        words[i] = B.ERR_TIMEOUT
+        assert B.ws_status(ws) == B.ERR_TIMEOUT
+        words[i] = 0
+    assert B.ws_status(ws) == B.OK
+    words[1:1 + n] = B.ERR_TIMEOUT
+    B.attention_kv4(q, cache, table, lt, batch, 1, heads, ws=ws)
+    assert B.ws_status(ws) == B.OK
