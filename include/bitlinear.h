@@ -399,7 +399,8 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
  *   must not decrease (else which rows are processed is not defined).
  *   A sequence with fewer query rows than key rows has its queries at the last positions (a chunk
  *   behind tokens that are already known); with more, the first ones see nothing.  A query that sees
- *   nothing gets zeros.  Rows of o outside every sequence are left as they were.
+ *   nothing gets zeros; one whose visible scores have no softmax (a NaN or +infinity among them, or nothing
+ *   but -infinity) NaN.  Rows of o outside every sequence are left as they were.
  *   head_dim 64 or 128; heads a multiple of kv_heads; scale 0 means 1 / sqrt(head_dim).
  * Values in invisible places have no influence, whatever they are (infinities and NaN included).
  * fp32 softmax statistics and accumulators; probabilities are rounded to the type of v for the

@@ -479,8 +479,10 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     if (ok) {
       // Through shared memory (the query tile's, which no product reads any more), each warp its own rows: whole rows leave
       // together.  Written from the registers, 16 bytes of each of 32 rows at a time, the whole kernel took 2 % longer.
-      const bool mine = row < job.rows;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      // A row in front of the first key sees nothing and gets zeros; another whose sum is 0 sees nothing but scores of
+      // -infinity: 1 / 0 makes it NaN.
+      const bool mine = row < job.rows, none = pos < 0;
+      const float inv = none ? 0.f : 1.f / l;
       unsigned char* stage = sq + warp * 32 * kDim * 2;
       float check = 0.f;
 #pragma unroll
@@ -493,7 +495,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float x = l == 0.f ? 0.f : v[2 * i] * inv, y = l == 0.f ? 0.f : v[2 * i + 1] * inv;
+          const float x = none ? 0.f : v[2 * i] * inv, y = none ? 0.f : v[2 * i + 1] * inv;
           check = fmaf(x, 0.f, fmaf(y, 0.f, check));           // NaN once a value is not finite
           w[i] = pack2<T>(x, y);
         }
@@ -512,8 +514,8 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           *reinterpret_cast<uint4*>(o + (int64_t)i * a.ld_o + part * 8) = *reinterpret_cast<const uint4*>(stage + i * kDim * 2 + (part ^ (i & 7)) * 16);
       }
       __syncwarp();
-      // (a sum l that is not finite comes from scores that are seen: the row's result is NaN by definition)
-      unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f) && l - l == 0.f);
+      // (a sum l that is 0 or not finite comes from scores that are seen: the row's result is NaN by definition)
+      unsigned bad = __ballot_sync(0xFFFFFFFFu, mine && !(check == 0.f) && l > 0.f && l - l == 0.f);
       while (bad) {
         const int i = __ffs(bad) - 1;
         bad &= bad - 1;

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2310_11453_b200 import binding as B
-from tests.test_gpu_attention_ops import BF16, DEV, F16, fill, randn
+from tests.test_gpu_attention_ops import BF16, DEV, F16, fill, packed, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +136,25 @@ def test_attention_kv4_a_report_stays(lens):
     words[1:1 + n] = B.ERR_TIMEOUT
     B.attention_kv4(q, cache, table, lt, batch, 1, heads, ws=ws)
     assert B.ws_status(ws) == B.OK
+
+
+# ---- prompts with a window -------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_attention_window_query_that_is_not_finite(dt, dim, bad):
+    """Every key is positive where the query is not finite, so -infinity makes every score -infinity: no softmax exists."""
+    heads, hk, lens = 2, 1, [1, 300, 70]
+    cu, at = packed(lens)
+    q, v = randn(1, at[-1], heads * dim, dtype=dt), randn(3, at[-1], hk * dim, dtype=dt)
+    k = randn(2, at[-1], hk * dim, dtype=dt)
+    k[:, 7] = k[:, 7].abs() + 0.5
+    want = B.attention_window(q, k, v, 3, 300, heads, hk, dim, window=100, sinks=2, cu_q=cu)
+    for row in (0, 1, 200, at[-1] - 1):
+        q2 = q.clone()
+        q2[row, dim + 7] = bad
+        got = B.attention_window(q2, k, v, 3, 300, heads, hk, dim, window=100, sinks=2, cu_q=cu)
+        expect = want.clone()
+        expect[row, dim:] = math.nan
+        assert torch.equal(torch.isnan(got), torch.isnan(expect)), row
+        assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), row
