@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2310_11453_b200 import binding as B
-from tests.test_gpu_attention_ops import BF16, DEV, F16, fill, packed, randn
+from tests import attention_ref as R
+from tests.test_gpu_attention_ops import BF16, DEV, F16, F32, fill, packed, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +159,26 @@ def test_attention_window_query_that_is_not_finite(dt, dim, bad):
         expect[row, dim:] = math.nan
         assert torch.equal(torch.isnan(got), torch.isnan(expect)), row
         assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), row
+
+
+# ---- norm and rotation -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", [F16, BF16, F32])
+@pytest.mark.parametrize("dim,rot", [(128, 64), (80, 32), (256, 16), (64, 0)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_norm_rope_values_that_do_not_turn_stay_apart(dt, dim, rot, inter):
+    """An infinity or NaN behind rot_dim says nothing about other values (without the norm; with it, the mean is infinite)."""
+    T, heads, kv = 9, 3, 2
+    q, k = randn(1, T, heads * dim, dtype=dt), randn(2, T, kv * dim, dtype=dt)
+    for x, n in ((q, heads), (k, kv)):
+        x.view(T, n, dim)[1, 0, rot] = math.inf
+        x.view(T, n, dim)[2, n - 1, dim - 1] = -math.inf
+        x.view(T, n, dim)[3, 1, rot + (dim - rot) // 2] = math.nan
+        x.view(T, n, dim)[4, 0, rot + 8] = math.inf
+    pos = torch.arange(T, device=DEV).int() * 77
+    freq = (10000.0 ** (-torch.arange(0, rot, 2, device=DEV, dtype=torch.float64) / max(rot, 1))).float()
+    for x, y in zip((q, k), B.qk_norm_rope(q, k, pos, freq, heads, kv, dim, eps=-1.0, interleaved=inter)):
+        x, y = x.view(T, -1, dim)[..., rot:], y.view(T, -1, dim)[..., rot:]
+        assert torch.equal(torch.isnan(y), torch.isnan(x)) and torch.equal(torch.nan_to_num(y, nan=1.5), torch.nan_to_num(x, nan=1.5))
+    for x, y in zip((q, k), B.qk_norm_rope(q, k, pos, freq, heads, kv, dim, eps=1e-6, interleaved=inter)):
+        want = R.norm_rope(x, None, pos, freq, dim, 1e-6, inter)[0]
+        assert torch.equal(torch.isnan(y), torch.isnan(want))
