@@ -490,9 +490,10 @@ def attention_window(q, k, v, batch, seq, heads, kv_heads=None, head_dim=128, wi
                      seq_k=None, scale=0.0, o=None):
     """bitlinear_attention_window.  q [rows, heads*head_dim], k, v [rows_k, kv_heads*head_dim] fp16 or bf16 (may be
     column blocks of one buffer).  `seq` (and `seq_k`, default the same) is the common length, or with cu_q (cu_k)
-    int32 [batch+1], packed sequences, an upper bound of their lengths.  Returns o [rows, heads*head_dim]."""
+    int32 [batch+1], packed sequences, an upper bound of their lengths (with cu_k, `seq_k` defaults to the rows of k).
+    Returns o [rows, heads*head_dim]."""
     r = (_fast or _marshal()).window(q, k, v, batch, seq, heads, heads if kv_heads is None else kv_heads, head_dim, window, sinks,
-                                     cu_q, cu_k, seq if seq_k is None else seq_k, scale, o)
+                                     cu_q, cu_k, seq_k, scale, o)
     if type(r) is int:
         _check(r, "bitlinear_attention_window")
     return r

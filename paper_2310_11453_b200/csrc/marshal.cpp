@@ -166,13 +166,16 @@ PyObject* window(PyObject*, PyObject* const* a, Py_ssize_t n) {
     want(n, 15);
     const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v");
     const int batch = small(a[3], "batch");
-    const int64_t seq = whole(a[4], "seq"), seq_k = whole(a[12], "seq_k");
+    const int64_t seq = whole(a[4], "seq");
     const int heads = small(a[5], "heads"), kv = small(a[6], "kv_heads"), dim = small(a[7], "head_dim");
     const int win = small(a[8], "window"), sinks = small(a[9], "sinks");
     const c10::Device dev = cuda_device(q, "q");
     const auto type = q.scalar_type();
     const bl_dtype code = type_code(type);
     const int64_t rows = q.dim() > 0 ? q.size(0) : 0, rows_k = k.dim() > 0 ? k.size(0) : 0;
+    // Keys with offsets of their own are bounded by the rows of k: the bound of the queries would cut their last tokens off and
+    // shift every position.
+    const int64_t seq_k = a[12] != Py_None ? whole(a[12], "seq_k") : a[11] == Py_None ? seq : rows_k;
     const int64_t wide = (int64_t)heads * dim, narrow = (int64_t)kv * dim;
     const int64_t ld_q = rows_of(q, "q", dev, type, rows, wide), ld_k = rows_of(k, "k", dev, type, rows_k, narrow);
     const int64_t ld_v = rows_of(v, "v", dev, type, rows_k, narrow);

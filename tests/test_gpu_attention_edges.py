@@ -6,7 +6,7 @@ import torch
 
 from paper_2310_11453_b200 import binding as B
 from tests import attention_ref as R
-from tests.test_gpu_attention_ops import BF16, DEV, F16, F32, fill, packed, randn
+from tests.test_gpu_attention_ops import BF16, DEV, F16, F32, check_window, fill, packed, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -159,6 +159,17 @@ def test_attention_window_query_that_is_not_finite(dt, dim, bad):
         expect[row, dim:] = math.nan
         assert torch.equal(torch.isnan(got), torch.isnan(expect)), row
         assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(expect)), row
+
+
+def test_attention_window_packed_chunks_behind_known_tokens_need_no_bound_of_the_keys():
+    heads, hk, dim, dt = 4, 2, 128, F16
+    lq, lk = [16, 1, 40, 16], [100, 700, 41, 16]
+    cq, aq = packed(lq)
+    ck, ak = packed(lk)
+    q, k, v = randn(1, aq[-1], heads * dim, dtype=dt), randn(2, ak[-1], hk * dim, dtype=dt), randn(3, ak[-1], hk * dim, dtype=dt)
+    o = B.attention_window(q, k, v, 4, 40, heads, hk, dim, window=64, sinks=3, cu_q=cq, cu_k=ck)
+    check_window(q, k, v, o, list(zip(aq, lq, ak, lk)), heads, hk, dim, 64, 3)
+    assert torch.equal(o, B.attention_window(q, k, v, 4, 40, heads, hk, dim, window=64, sinks=3, cu_q=cq, cu_k=ck, seq_k=700))
 
 
 # ---- norm and rotation -----------------------------------------------------------------------------
