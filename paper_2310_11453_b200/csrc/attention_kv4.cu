@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attention_kv4_kernel(Kv4AttnAr
         qf[nt][i][2] = half2_bits(v[i][2] * up, v[i][6] * up);
         qf[nt][i][3] = half2_bits(v[i][3] * up * 0.0625f, v[i][7] * up * 0.0625f);
       }
-      const float fr = sl * pow2i(min(24 - max(e, -114), 127)), sr = sum * sl;
+      const float fr = sl * pow2i(-max(e, -114)) * 16777216.f, sr = sum * sl;   // (2^(24 - e) itself may pass 2^127)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         f[nt][j] = __shfl_sync(0xFFFFFFFFu, fr, 4 * (2 * qd + j));

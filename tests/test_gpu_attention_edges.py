@@ -6,7 +6,7 @@ import torch
 
 from paper_2310_11453_b200 import binding as B
 from tests import attention_ref as R
-from tests.test_gpu_attention_ops import BF16, DEV, F16, F32, check_window, fill, packed, randn
+from tests.test_gpu_attention_ops import BF16, DEV, F16, F32, check_kv4, check_window, fill, packed, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -137,6 +137,16 @@ def test_attention_kv4_a_report_stays(lens):
     words[1:1 + n] = B.ERR_TIMEOUT
     B.attention_kv4(q, cache, table, lt, batch, 1, heads, ws=ws)
     assert B.ws_status(ws) == B.OK
+
+
+@pytest.mark.parametrize("size,step", [(2.0 ** 117, 1e-35), (2.0 ** 110, 1e-33), (2.0 ** -100, 2.0 ** 100)])
+def test_attention_kv4_sizes_of_the_query_at_the_ends_of_bf16(size, step):
+    hk, g, dim, page, n = 1, 2, 128, 32, 300
+    cache = B.Kv4Cache.empty(10, page, hk, dim, BF16, DEV)
+    B.kv4_append(cache, (randn(1, 320, hk * dim) * step).to(BF16), randn(2, 320, hk * dim, dtype=BF16), torch.arange(320, device=DEV))
+    q = (randn(3, 1, g * hk * dim) * size).to(BF16)
+    table, lens = torch.arange(10, device=DEV).int().view(1, 10), torch.tensor([n], device=DEV).int()
+    check_kv4(q, cache, table, [n], 1, 1, g * hk, 0, 0, 0.0, B.attention_kv4(q, cache, table, lens, 1, 1, g * hk))
 
 
 # ---- prompts with a window -------------------------------------------------------------------------
