@@ -52,13 +52,13 @@ void check_place(const Tensor& t, const char* name, c10::Device dev, at::ScalarT
   if (t.scalar_type() != type)
     throw TypeError(std::string(name) + " is " + c10::toString(t.scalar_type()) + ", expected " + c10::toString(type));
 }
-// A token matrix [rows, width] whose rows are contiguous; returns its row stride.
+// A token matrix [rows, width] whose rows are contiguous; returns its row stride (of a single row, which has none, any that serves).
 int64_t rows_of(const Tensor& t, const char* name, c10::Device dev, at::ScalarType type, int64_t rows, int64_t width) {
   check_place(t, name, dev, type);
   if (t.dim() != 2 || t.size(0) != rows || t.size(1) != width || t.stride(1) != 1)
     throw std::invalid_argument(std::string(name) + " has shape " + shape_of(t) + ", expected (" + std::to_string(rows) + ", " +
                                 std::to_string(width) + ") with the values of a row contiguous");
-  return rows > 1 ? t.stride(0) : std::max(t.stride(0), (width + 7) / 8 * 8);
+  return rows > 1 ? t.stride(0) : (width + 7) / 8 * 8;
 }
 // A contiguous tensor of n values in the given shape (second < 0: one dimension).
 void* flat(const Tensor& t, const char* name, c10::Device dev, at::ScalarType type, int64_t first, int64_t second = -1) {

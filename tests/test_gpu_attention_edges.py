@@ -203,3 +203,26 @@ def test_norm_rope_values_that_do_not_turn_stay_apart(dt, dim, rot, inter):
     for x, y in zip((q, k), B.qk_norm_rope(q, k, pos, freq, heads, kv, dim, eps=1e-6, interleaved=inter)):
         want = R.norm_rope(x, None, pos, freq, dim, 1e-6, inter)[0]
         assert torch.equal(torch.isnan(y), torch.isnan(want))
+
+
+# ---- the binding -----------------------------------------------------------------------------------
+def test_a_single_row_may_have_any_stride():
+    heads, hk, dim, page, dt = 4, 2, 64, 16, F16
+
+    def odd(seed, width):                                              # one row out of rows of an odd length
+        x = torch.empty((1, width + 5), device=DEV, dtype=dt)
+        x[:, :width] = randn(seed, 1, width, dtype=dt)
+        return x[:, :width]
+    q, k, v = odd(1, heads * dim), odd(2, hk * dim), odd(3, hk * dim)
+    dense = [x.clone(memory_format=torch.contiguous_format) for x in (q, k, v)]
+    pos, freq = torch.tensor([7], device=DEV).int(), torch.ones(dim // 2, device=DEV)
+    for a, b in zip(B.qk_norm_rope(q, k, pos, freq, heads, hk, dim), B.qk_norm_rope(*dense[:2], pos, freq, heads, hk, dim)):
+        assert torch.equal(a, b)
+    assert torch.equal(B.attention_window(q, k, v, 1, 1, heads, hk, dim), B.attention_window(*dense, 1, 1, heads, hk, dim))
+    cache = B.Kv4Cache.empty(2, page, hk, dim, dt, DEV)
+    B.kv4_append(cache, k, v, torch.tensor([5], device=DEV))
+    outs = [odd(4, hk * dim), odd(5, hk * dim)]
+    for a, b in zip(B.kv4_read(cache, torch.tensor([5], device=DEV), k=outs[0], v=outs[1]), B.kv4_read(cache, torch.tensor([5], device=DEV))):
+        assert torch.equal(a, b)
+    table, lens = torch.zeros((1, 1), device=DEV, dtype=torch.int32), torch.tensor([6], device=DEV).int()
+    assert torch.equal(B.attention_kv4(q, cache, table, lens, 1, 1, heads, o=odd(6, heads * dim)), B.attention_kv4(dense[0], cache, table, lens, 1, 1, heads))
