@@ -466,7 +466,7 @@ bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, 
                                   const int32_t* block_table, int64_t max_pages, const int32_t* lens, int window,
                                   int sinks, float scale, void* o, int64_t ld_o, void* ws, size_t ws_bytes,
                                   void* stream);
-size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim);
+size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim);   /* 0 if a size is not supported */
 
 /* Copies whole pages inside the cache, in every layer: for each pair (src, dst) of pairs int32 [n][2],
  * page dst becomes a copy of page src (a forked sequence's last page, a copy on write, the moves of a

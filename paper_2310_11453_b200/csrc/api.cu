@@ -94,6 +94,11 @@ inline bool attention_dtype(int t) { return t == BL_F16 || t == BL_BF16; }
 // 0: no window; one that no position can leave is none.
 inline int clip_window(int window) { return window > 0 && window < kMaxRows ? window : 0; }
 inline bool aligned_to(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// Query rows of attention_kv4: batch x n_q tokens of `heads` heads.
+inline bool query_rows(int batch, int n_q, int heads) {
+  return batch >= 0 && n_q >= 1 && heads >= 1 && heads <= kMaxHeads && (int64_t)batch * n_q <= kMaxRows &&
+         (int64_t)batch * n_q * heads <= kMaxRows && (int64_t)n_q * heads <= kMaxRows;
+}
 // A row stride takes the row and keeps every row 16-byte aligned.
 inline bool row_stride(int64_t ld, int heads, int head_dim) { return ld >= (int64_t)heads * head_dim && ld % 8 == 0; }
 
@@ -598,7 +603,7 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
 }
 
 size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim) {
-  if (batch < 0 || n_q < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0) return 0;
+  if (!query_rows(batch, n_q, heads) || kv_heads < 1 || heads % kv_heads != 0) return 0;
   if (head_dim != 64 && head_dim != 128) return 0;
   return round256(attention_kv4_ws_bytes(batch, n_q, heads, kv_heads, head_dim));
 }
@@ -609,9 +614,8 @@ bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, 
                                   void* stream) {
   const bl_status st = check_cache(cache);
   if (st != BL_OK) return st;
-  if (batch < 0 || n_q < 1 || heads < 1 || heads > kMaxHeads || heads % cache->kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
+  if (!query_rows(batch, n_q, heads) || heads % cache->kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
   if (max_pages < 0 || max_pages > kMaxRows / cache->page_size) return BL_ERR_SHAPE;
-  if ((int64_t)batch * n_q > kMaxRows || (int64_t)batch * n_q * heads > kMaxRows) return BL_ERR_SHAPE;
   if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
   if (!row_stride(ld_q, heads, cache->head_dim) || !row_stride(ld_o, heads, cache->head_dim)) return BL_ERR_SHAPE;
   if (batch == 0) return BL_OK;

@@ -1,6 +1,7 @@
 """What the attention operators refuse, on the host and before any launch, and their sizes."""
 import ctypes as C
 import subprocess
+import sys
 
 import pytest
 import torch
@@ -159,3 +160,15 @@ def test_parts_named_by_any_bits_stay_within_the_workspace(tmp_path):
     for (first, last, warps), n in zip(args, map(int, out), strict=True):
         w0 = first // 2
         assert n == (last - w0 + 1 if 0 <= w0 <= last < warps else 0), (first, last, warps)
+
+
+def test_workspace_sizes_that_do_not_fit_are_refused():
+    """Sizes that attention_kv4 refuses have no workspace; sums and products of them may pass 32 bits.  In a process of its own: a
+    division by a count of rows that wrapped around to 0 ends it."""
+    sizes = [(1, 1 << 20, 4096, 1, 128), (0, 1 << 20, 4096, 1, 128), (1, 1 << 30, 4, 1, 64), (1, 2 ** 31 - 1, 1, 1, 128), (1, 1, 8192, 1, 128),
+             (2 ** 31 - 1, 1, 4096, 4096, 128), (1 << 20, 1 << 11, 1, 1, 64), (1, 1, 2 ** 31 - 1, 1, 64), (1, 5, 2 ** 30, 2, 64)]
+    code = f"from paper_2310_11453_b200 import binding as B\nprint([B.attention_kv4_ws_bytes(*s) for s in {sizes}])"
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
+    assert done.returncode == 0, done
+    assert done.stdout.strip() == str([0] * len(sizes))
+    assert B.attention_kv4_ws_bytes(1, 1 << 18, 4096, 1, 128) > 0 and B.attention_kv4_ws_bytes(1 << 18, 1, 4096, 4096, 128) > 0
