@@ -401,7 +401,7 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
  *   behind tokens that are already known); with more, the first ones see nothing.  A query that sees
  *   nothing gets zeros; one whose visible scores have no softmax (a NaN or +infinity among them, or nothing
  *   but -infinity) NaN.  Rows of o outside every sequence are left as they were.
- *   head_dim 64 or 128; heads a multiple of kv_heads; scale 0 means 1 / sqrt(head_dim).
+ *   head_dim 64 or 128; heads a multiple of kv_heads; scale 0..2e38, 0 means 1 / sqrt(head_dim).
  * Values in invisible places have no influence, whatever they are (infinities and NaN included).
  * fp32 softmax statistics and accumulators; probabilities are rounded to the type of v for the
  * product, and one rounding on output.  The kernel's waits are bounded; if one ever ran out, the rows concerned are
@@ -456,7 +456,7 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   0..max_pages * page_size).  Query i of n_q stands at position lens - n_q + i; one that sees nothing
  *   (negative position, empty sequence) gets zeros.
  *   A query whose visible scores have no softmax (a NaN or +infinity among them, or nothing but -infinity) gets NaN.
- *   scale 0 means 1 / sqrt(head_dim).  n_q >= 1, any number; made for few.
+ *   scale as there.  n_q >= 1, any number; made for few.
  * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
  * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.
  * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; bitlinear_ws_status reads its start: the

@@ -94,6 +94,8 @@ inline bool attention_dtype(int t) { return t == BL_F16 || t == BL_BF16; }
 // 0: no window; one that no position can leave is none.
 inline int clip_window(int window) { return window > 0 && window < kMaxRows ? window : 0; }
 inline bool aligned_to(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// The kernels multiply scores by scale . log2(e), which has to be finite.
+inline bool score_scale(float scale) { return scale >= 0.f && scale <= 2.0e38f; }
 // Query rows of attention_kv4: batch x n_q tokens of `heads` heads.
 inline bool query_rows(int batch, int n_q, int heads) {
   return batch >= 0 && n_q >= 1 && heads >= 1 && heads <= kMaxHeads && (int64_t)batch * n_q <= kMaxRows &&
@@ -551,7 +553,7 @@ bl_status bitlinear_attention_window(const void* q, const void* k, const void* v
   if (batch < 0 || seq_q < 0 || seq_k < 0 || rows_q < 0 || rows_k < 0) return BL_ERR_SHAPE;
   if (seq_q > kMaxRows || seq_k > kMaxRows || rows_q > kMaxRows || rows_k > kMaxRows) return BL_ERR_SHAPE;
   if (heads < 1 || kv_heads < 1 || heads > kMaxHeads || heads % kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
-  if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
+  if (!score_scale(scale)) return BL_ERR_SHAPE;
   if (cu_k && !cu_q) return BL_ERR_NULL;
   if (!cu_q && ((int64_t)batch * seq_q > rows_q || (int64_t)batch * seq_k > rows_k)) return BL_ERR_SHAPE;
   if (!row_stride(ld_q, heads, head_dim) || !row_stride(ld_o, heads, head_dim) || !row_stride(ld_k, kv_heads, head_dim) ||
@@ -616,7 +618,7 @@ bl_status bitlinear_attention_kv4(const void* q, int batch, int n_q, int heads, 
   if (st != BL_OK) return st;
   if (!query_rows(batch, n_q, heads) || heads % cache->kv_heads != 0 || sinks < 0) return BL_ERR_SHAPE;
   if (max_pages < 0 || max_pages > kMaxRows / cache->page_size) return BL_ERR_SHAPE;
-  if (!(scale >= 0.f) || scale > 3.0e38f) return BL_ERR_SHAPE;
+  if (!score_scale(scale)) return BL_ERR_SHAPE;
   if (!row_stride(ld_q, heads, cache->head_dim) || !row_stride(ld_o, heads, cache->head_dim)) return BL_ERR_SHAPE;
   if (batch == 0) return BL_OK;
   if (!q || !o || !lens || (max_pages > 0 && !block_table)) return BL_ERR_NULL;

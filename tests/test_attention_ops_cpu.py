@@ -172,3 +172,11 @@ def test_workspace_sizes_that_do_not_fit_are_refused():
     assert done.returncode == 0, done
     assert done.stdout.strip() == str([0] * len(sizes))
     assert B.attention_kv4_ws_bytes(1, 1 << 18, 4096, 1, 128) > 0 and B.attention_kv4_ws_bytes(1 << 18, 1, 4096, 4096, 128) > 0
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.0e38, -0.0])
+def test_scales_that_pass_fp32_in_the_exponent_are_refused(scale):
+    """Scores are taken times log2(e): 2.4e38 and more would be an infinite factor, and NaN of a score of 0."""
+    assert window(scale=scale, batch=0) == (B.ERR_SHAPE if scale > 0 else B.OK)
+    assert kv4(scale=scale, batch=0) == (B.ERR_SHAPE if scale > 0 else B.OK)
+    assert window(scale=2e38, batch=0) == B.OK and kv4(scale=2e38, batch=0) == B.OK
