@@ -370,7 +370,7 @@ bl_status bitlinear_block_forward(const void* x, int batch, int seq, int heads, 
  * one out of range is stated, and no access leaves the buffers described by the arguments. */
 
 /* Norm of each query and key head with the position rotation, in one pass:
- *   x^ = w . x / sqrt(mean(x^2) + eps)   over the head's head_dim values (eps < 0: no norm, no weight)
+ *   x^ = w . x / sqrt(mean(x^2) + eps)   over the head's head_dim values (eps < 0: no norm, no weight; not NaN)
  *   (x^_a, x^_b) -> (x^_a cos t - x^_b sin t, x^_b cos t + x^_a sin t),   t = position . inv_freq[i]
  * for the pairs i < rot_dim / 2: a = i, b = i + rot_dim / 2, or a = 2i, b = 2i + 1 when interleaved
  * != 0; values from rot_dim on are only normalised.  fp32 throughout, angles reduced in fp64 (so far

@@ -529,7 +529,7 @@ bl_status bitlinear_qk_norm_rope(const void* q, const void* k, bl_dtype dt, int6
   if (!valid_dtype(dt)) return BL_ERR_UNSUPPORTED;
   if (T < 0 || T > kMaxRows || heads < 1 || kv_heads < 1 || heads > kMaxHeads || kv_heads > kMaxHeads) return BL_ERR_SHAPE;
   if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0) return BL_ERR_SHAPE;
-  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16 != 0) return BL_ERR_SHAPE;
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16 != 0 || eps != eps) return BL_ERR_SHAPE;
   if (!row_stride(ld_q, heads, head_dim) || !row_stride(ld_qo, heads, head_dim) || !row_stride(ld_k, kv_heads, head_dim) ||
       !row_stride(ld_ko, kv_heads, head_dim))
     return BL_ERR_SHAPE;

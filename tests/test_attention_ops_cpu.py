@@ -180,3 +180,10 @@ def test_scales_that_pass_fp32_in_the_exponent_are_refused(scale):
     assert window(scale=scale, batch=0) == (B.ERR_SHAPE if scale > 0 else B.OK)
     assert kv4(scale=scale, batch=0) == (B.ERR_SHAPE if scale > 0 else B.OK)
     assert window(scale=2e38, batch=0) == B.OK and kv4(scale=2e38, batch=0) == B.OK
+
+
+def test_norm_rope_refuses_an_eps_that_is_no_number():
+    """A negative eps means no norm; NaN compares like one, and would leave the norm out in silence."""
+    assert norm_rope(eps=float("nan"), T=0) == B.ERR_SHAPE
+    for eps in (-1.0, 0.0, 1e-6, float("-inf")):
+        assert norm_rope(eps=eps, T=0) == B.OK
