@@ -505,14 +505,21 @@ def kv4_page_bytes(page_size, kv_heads, head_dim) -> int:
 
 class Kv4Cache:
     """One layer's 4-bit key/value cache (bl_kv4_cache): pages u8 [num_pages, page bytes], contiguous, e.g. one
-    layer of a [layers, num_pages, page bytes] tensor.  Holds no state of its own."""
+    layer of a [layers, num_pages, page bytes] tensor.  Holds no state of its own; other pages take another object."""
 
     def __init__(self, pages, page_size, kv_heads, head_dim, dtype):
         if dtype not in (torch.float16, torch.bfloat16):
             raise TypeError(f"unsupported dtype {dtype}")
-        self.pages, self.page_size, self.kv_heads, self.head_dim, self.dtype = pages, page_size, kv_heads, head_dim, dtype
+        self._dtype = dtype
         self._args = (pages, page_size, kv_heads, head_dim, _DTYPES[dtype])
         (_fast or _marshal()).cache(*self._args)
+
+    # read-only: the calls pass _args
+    pages = property(lambda self: self._args[0])
+    page_size = property(lambda self: self._args[1])
+    kv_heads = property(lambda self: self._args[2])
+    head_dim = property(lambda self: self._args[3])
+    dtype = property(lambda self: self._dtype)
 
     @staticmethod
     def empty(num_pages, page_size, kv_heads, head_dim, dtype, device):

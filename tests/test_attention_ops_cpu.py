@@ -187,3 +187,11 @@ def test_norm_rope_refuses_an_eps_that_is_no_number():
     assert norm_rope(eps=float("nan"), T=0) == B.ERR_SHAPE
     for eps in (-1.0, 0.0, 1e-6, float("-inf")):
         assert norm_rope(eps=eps, T=0) == B.OK
+
+
+def test_a_cache_object_cannot_be_pointed_elsewhere():
+    """The calls use what the constructor checked: an assignment afterwards would be ignored by them, so it is refused."""
+    cache = object.__new__(B.Kv4Cache)
+    for name in ("pages", "page_size", "kv_heads", "head_dim", "dtype"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, 1)
