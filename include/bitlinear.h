@@ -457,7 +457,9 @@ bl_status bitlinear_kv4_read(const bl_kv4_cache* cache, void* k, void* v, int64_
  *   (negative position, empty sequence) gets zeros.
  *   A query whose visible scores have no softmax (a NaN or +infinity among them, or nothing but -infinity) gets NaN.
  *   scale as there.  n_q >= 1, any number; made for few.
- * Sums and statistics in fp32; the work is split along the sequences over the whole GPU and joined in a
+ * Sums and statistics in fp32.  Rounded for the products: the query to fp16 after a power of two per row (exact
+ * but for values 2^-24 of the row's largest and less), probability times value step to fp16 (after a power of
+ * two); one rounding on output.  The work is split along the sequences over the whole GPU and joined in a
  * fixed order (same inputs and sizes, same bits).  o must not overlap q or the cache.  batch = 0 does nothing.
  * Workspace: bitlinear_attention_kv4_ws_bytes() (16-byte aligned; bitlinear_ws_status reads its start: the
  * kernel's waits for its copies are bounded, and BL_ERR_TIMEOUT there means that one ran out; the rows of o
@@ -484,10 +486,11 @@ bl_status bitlinear_ws_status(const void* ws, void* stream);
 
 /* Test and diagnostic hook: caps the number of polls that the bounded device-side waits of
  * kernels launched afterwards by this process may make (bitlinear_gemv_decode's wait for its
- * weight copies; the waits of bitlinear_attention_window and bitlinear_attention_kv4; the meeting between the two passes of the cooperative per-tensor kernel of
- * bitlinear_quant_act).  polls < 0 restores the built-in limits; 0 means a single poll (for
+ * weight copies; the waits of bitlinear_attention_window and bitlinear_attention_kv4; the meeting between the
+ * two passes of the cooperative per-tensor kernel of bitlinear_quant_act).  polls < 0 restores the built-in limits; 0 means a single poll (for
  * bitlinear_gemv_decode and bitlinear_attention_window: none at all, weights are read from global
- * memory, rows are computed one by one; for bitlinear_attention_kv4: none, it reports the timeout).
+ * memory, rows are computed one by one; for bitlinear_attention_kv4: none, it reports the timeout and its rows
+ * are NaN).
  * meet_skew != 0 additionally makes the cooperative kernel wait for an arrival tag that no CTA
  * publishes, so that its wait runs out by construction: the kernel then records
  * BL_ERR_TIMEOUT in the status word, writes no codes and returns (nothing hangs, traps or

@@ -479,7 +479,8 @@ def qk_norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq=None, 
                  q_out=None, k_out=None):
     """bitlinear_qk_norm_rope.  q [T, heads*head_dim], k [T, kv_heads*head_dim] (may be column blocks of one
     buffer); positions int32 [T] (negative: padding, left as it is); inv_freq f32 [rot_dim/2]; wq, wk
-    [head_dim] or None; eps < 0 skips the norm.  Returns (q_out, k_out), which may be given (q, k for in place)."""
+    [head_dim] or None; eps < 0 skips the norm.  Returns (q_out, k_out), which may be given (q, k for in place); rows of
+    padding of new ones hold anything."""
     r = (_fast or _marshal()).norm_rope(q, k, positions, inv_freq, heads, kv_heads, head_dim, wq, wk, eps, interleaved, q_out, k_out)
     if type(r) is int:
         _check(r, "bitlinear_qk_norm_rope")
@@ -491,7 +492,7 @@ def attention_window(q, k, v, batch, seq, heads, kv_heads=None, head_dim=128, wi
     """bitlinear_attention_window.  q [rows, heads*head_dim], k, v [rows_k, kv_heads*head_dim] fp16 or bf16 (may be
     column blocks of one buffer).  `seq` (and `seq_k`, default the same) is the common length, or with cu_q (cu_k)
     int32 [batch+1], packed sequences, an upper bound of their lengths (with cu_k, `seq_k` defaults to the rows of k).
-    Returns o [rows, heads*head_dim]."""
+    Returns o [rows, heads*head_dim]; rows of a new one outside every sequence hold anything."""
     r = (_fast or _marshal()).window(q, k, v, batch, seq, heads, heads if kv_heads is None else kv_heads, head_dim, window, sinks,
                                      cu_q, cu_k, seq_k, scale, o)
     if type(r) is int:
