@@ -58,7 +58,7 @@ typedef enum {
   BL_ERR_TOO_LARGE = 8    /* the problem exceeds the built-in scratch of a *_noalloc entry point */
 } bl_status;
 
-typedef enum { BL_F32 = 0, BL_F16 = 1, BL_BF16 = 2 } bl_dtype;
+typedef enum { BL_F32 = 0, BL_F16 = 1, BL_BF16 = 2, BL_I8 = 3 /* codes, where a call says so */ } bl_dtype;
 
 /* Eq. 4-5 (signed codes in [-127,127]) or Eq. 6 (eta-shifted codes in [0,127]). */
 typedef enum { BL_ABSMAX = 0, BL_ETA = 1 } bl_quant_mode;
@@ -478,6 +478,85 @@ size_t bitlinear_attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_he
  * are multiples of 16, layer_stride >= num_pages * page_bytes (any value for one layer).  n = 0 does nothing. */
 bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_pages, int layers, size_t layer_stride,
                                    const int32_t* pairs, int64_t n, void* stream);
+
+/* ---- layers held in 8 bits, and experts made of them -------------------------------------------
+ * The layers of a BitNet that are not binarised (Sec. 2 keeps its other components "high-precision, e.g.
+ * 8-bit": the output layer first of all), and a feed-forward block of experts of which each token visits a few.
+ *   matrix of codes  int8 [rows, K], a scale (fp32) per row: value = scale . code, code in -127..127
+ *   tokens' rows come from bitlinear_rms_norm_quant; a weight matrix [N, K] is one too, a scale per output channel,
+ *   and bitlinear_rms_norm_quant with eps < 0 quantises it.
+ * Indices in device memory (rows, offsets, places) cannot be checked on the host: what each kernel does with
+ * one out of range is stated, and no access leaves the buffers described by the arguments.  Rows of a token that are
+ * not finite stay visible as NaN. */
+
+/* Residual's addition, root-mean-square norm, 8-bit codes with a scale per token, in one pass:
+ *   h_t = residual_t + x_t,  or with rows:  h_t = residual_t + sum_j row_weights[t, j] . x[rows[t, j]]   (j < top_k)
+ *   y_t = weight . h_t / sqrt(mean(h_t^2) + eps)         (eps < 0: y = h, no norm, no weight; not NaN)
+ *   scale_t = max |y_t| / 127,   code = round(y_t / scale_t)       (half to even)
+ *   x [x_rows, K] stride ld_x, dtype dt (BL_F32, BL_F16, BL_BF16; residual, weight, h, y likewise).  Without rows x_rows >= T.
+ *   rows int32 [T, top_k] (an entry outside 0..x_rows-1, e.g. -1, adds nothing), row_weights fp32 [T, top_k] or NULL (ones);
+ *   top_k 1..64, the places and weights of bitlinear_route_topk serve: x is then what the experts left.
+ *   residual [T, K] stride ld_res, or NULL.  weight [K] or NULL (ones).
+ *   h, y [T, K] strides ld_h, ld_y, x_q int8 [T, K] stride ld_q with scale fp32 [T]: each may be NULL if not wanted,
+ *   but not all.  h and y may be residual, or without rows x, themselves (same stride), else outputs overlap nothing.
+ *   K a multiple of 8, 8..32768; strides multiples of 8.
+ * fp32 throughout; the codes are those of h before it is rounded to dt, and those of exact arithmetic where y / scale is
+ * further than 2^-13 from a border between two codes (with rows: and further than the roundings of the sum of top_k + 1 terms).  A row of zeros has codes and scale 0; a row in which a value is not
+ * finite has scale NaN and codes 0.  T = 0 does nothing.  No workspace. */
+bl_status bitlinear_rms_norm_quant(const void* x, bl_dtype dt, int64_t x_rows, int64_t T, int64_t K, int64_t ld_x,
+                                   const int32_t* rows, const float* row_weights, int top_k, const void* residual,
+                                   int64_t ld_res, const void* weight, float eps, void* h, int64_t ld_h, void* y,
+                                   int64_t ld_y, int8_t* x_q, int64_t ld_q, float* scale, void* stream);
+
+/* Matrix product of codes with a scale per token and per output channel:
+ *   y[m, n] = (sum_k x_q[m, k] w_q[n, k]) . x_scale[m] . w_scale[n] + bias[n],  ReLU,  + residual[m, n]
+ *   x_q int8 [M, K] stride ld_x, w_q int8 [N, K] stride ld_w: K a multiple of 16, 16..131056, strides multiples of 16
+ *   (codes may be -128..127: no sum leaves 32 bits).  x_scale fp32 [M], w_scale fp32 [N], either NULL: ones.
+ *   bias [N] or NULL, residual [M, N] stride ld_res or NULL, y [M, N] stride ld_y, all of dtype yt (BL_F32, BL_F16,
+ *   BL_BF16), element-aligned.  y may be residual itself (same stride), else overlaps nothing.  N 1..2^24.
+ * The sums are exact; then fp32, one rounding on output.  A NaN stays one through the ReLU.  Waits are bounded; were one
+ * to run out, the rows concerned are NaN.  M = 0 does nothing.  No workspace. */
+bl_status bitlinear_matmul_i8(const int8_t* x_q, int64_t M, int64_t K, int64_t N, int64_t ld_x, const float* x_scale,
+                              const int8_t* w_q, int64_t ld_w, const float* w_scale, const void* bias, int relu,
+                              const void* residual, int64_t ld_res, void* y, bl_dtype yt, int64_t ld_y, void* stream);
+
+/* The experts of each token, and the lists of rows that they make.
+ *   logits [T, experts] stride ld, dtype dt (BL_F32, BL_F16, BL_BF16), element-aligned; experts 1..512.
+ *   chosen   int32 [T, top_k]: the experts with the top_k largest scores, largest first; of equal scores the lowest index
+ *            (-0 and 0 are equal, a NaN counts as less than -infinity).  top_k 1..32, at most experts.
+ *   weights  fp32 [T, top_k]: exp(z - max z) of the chosen over its sum over the chosen (normalise != 0) or over all
+ *            experts.  Where that is no number (a NaN anywhere, +infinity, nothing but -infinity): NaN.
+ *   offsets  int32 [experts + 1]: rows offsets[e] .. offsets[e + 1] - 1 of the list belong to expert e.
+ *   rows     int32 [T * top_k]: the token of each row of the list, ordered by expert, then by token.
+ *   places   int32 [T, top_k]: the row of the list that belongs to each choice.
+ *   positions int32 [T] or NULL: a negative one marks a row of padding (as in bitlinear_qk_norm_rope), which visits no expert:
+ *            chosen and places -1, weights 0; entries of rows behind offsets[experts] are then left as they were.
+ * T = 0 sets offsets to 0.  T * top_k <= 2^30.  Workspace: bitlinear_route_topk_ws_bytes() (0 for up to 64 tokens: ws may
+ * be NULL), 16-byte aligned; calls that may overlap need workspaces of their own. */
+bl_status bitlinear_route_topk(const void* logits, bl_dtype dt, int64_t T, int experts, int64_t ld, int top_k,
+                               int normalise, const int32_t* positions, int32_t* chosen, float* weights,
+                               int32_t* offsets, int32_t* rows, int32_t* places, void* ws, size_t ws_bytes,
+                               void* stream);
+size_t bitlinear_route_topk_ws_bytes(int64_t T, int experts);      /* 0 if a size is not supported, too */
+
+/* Matrix products of lists of rows, each with the weights of its expert:
+ *   y[r, n] = (sum_k x[rows[r], k] w[e, n, k]) . x_scale[rows[r]] . w_scale[e, n] + bias[e, n],  ReLU
+ * for the rows r of expert e, offsets[e] <= r < offsets[e + 1].  Lists may be empty or hold every row.
+ *   x [x_rows, K] stride ld_x, w [experts, N, K] with row stride ld_w and expert_stride a
+ *   multiple of it (at least N ld_w; any for one expert), both of type `operand`:
+ *     BL_I8    codes; x_scale fp32 [x_rows], w_scale fp32 [experts, N], either NULL: ones.  K as in bitlinear_matmul_i8.
+ *     BL_F16, BL_BF16   values (x_scale and w_scale NULL): fp32 sums.  K a multiple of 8, 8..2^20, strides multiples of 8.
+ *   offsets int32 [experts + 1], experts 1..1024: clamped to 0..R; they must not decrease (else which rows are processed is
+ *   not defined).  rows int32 [R] (clamped to 0..x_rows-1), or NULL: row r of x itself, x_rows >= R.
+ *   bias [experts, N] or NULL, y [R, N] stride ld_y, of dtype yt (BL_F32, BL_F16, BL_BF16), element-aligned; y overlaps nothing.
+ *   N 1..2^24.  Rows of y outside every list are left as they were.
+ * fp32 sums are formed in an order that the sizes alone decide (same inputs, same bits).  One rounding on output; NaN and
+ * waits as in bitlinear_matmul_i8.  R = 0 does nothing.  No workspace. */
+bl_status bitlinear_matmul_grouped(const void* x, bl_dtype operand, int64_t x_rows, int64_t K, int64_t N, int64_t ld_x,
+                                   const float* x_scale, const void* w, int64_t ld_w, int64_t expert_stride,
+                                   const float* w_scale, int experts, const int32_t* offsets, const int32_t* rows,
+                                   int64_t R, const void* bias, int relu, void* y, bl_dtype yt, int64_t ld_y,
+                                   void* stream);
 
 /* Synchronises `stream`, then reads the status that a previous bitlinear_forward,
  * bitlinear_matmul_i32 or other call that names it left at the start of `ws` (a word, or words

@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libbitlinear_b200.so")
 
 # enums of include/bitlinear.h
 OK = 0
-F32, F16, BF16 = 0, 1, 2
+F32, F16, BF16, I8 = 0, 1, 2, 3
 ABSMAX, ETA = 0, 1
 PER_TENSOR, PER_TOKEN = 0, 1
 CANONICAL, PREFILL, DECODE = 0, 1, 2
@@ -36,6 +36,8 @@ EXPORTS = [
     "bitlinear_qk_norm_rope", "bitlinear_attention_window", "bitlinear_kv4_page_bytes", "bitlinear_kv4_append",
     "bitlinear_kv4_read", "bitlinear_attention_kv4", "bitlinear_attention_kv4_ws_bytes", "bitlinear_kv4_copy_pages",
     "bitlinear_debug_window_fallbacks",
+    "bitlinear_rms_norm_quant", "bitlinear_matmul_i8", "bitlinear_route_topk", "bitlinear_route_topk_ws_bytes",
+    "bitlinear_matmul_grouped",
 ]
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -116,6 +118,18 @@ def lib():
         L.bitlinear_attention_window.restype = ci
         L.bitlinear_attention_window.argtypes = [vp, vp, vp, vp, ci, ci, vp, vp, i64, i64, i64, i64, ci, ci, ci, i64, i64,
                                                  i64, i64, ci, ci, C.c_float, vp]
+        L.bitlinear_rms_norm_quant.restype = ci
+        L.bitlinear_rms_norm_quant.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, vp, i64, vp, C.c_float, vp, i64, vp, i64,
+                                               vp, i64, vp, vp]
+        L.bitlinear_matmul_i8.restype = ci
+        L.bitlinear_matmul_i8.argtypes = [vp, i64, i64, i64, i64, vp, vp, i64, vp, vp, ci, vp, i64, vp, ci, i64, vp]
+        L.bitlinear_route_topk.restype = ci
+        L.bitlinear_route_topk.argtypes = [vp, ci, i64, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.bitlinear_route_topk_ws_bytes.restype = sz
+        L.bitlinear_route_topk_ws_bytes.argtypes = [i64, ci]
+        L.bitlinear_matmul_grouped.restype = ci
+        L.bitlinear_matmul_grouped.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, i64, i64, vp, ci, vp, vp, i64, vp, ci, vp, ci,
+                                               i64, vp]
         L.bitlinear_kv4_page_bytes.restype = sz
         L.bitlinear_kv4_page_bytes.argtypes = [ci, ci, ci]
         L.bitlinear_kv4_append.restype = ci
@@ -470,7 +484,8 @@ def _marshal():
             raise ImportError(f"_marshal.so is missing or does not load: run `python -m paper_2310_11453_b200.build` ({e})")
         m.bind(*(C.cast(getattr(L, "bitlinear_" + n), C.c_void_p).value for n in
                  ("qk_norm_rope", "attention_window", "kv4_page_bytes", "kv4_append", "kv4_read", "attention_kv4",
-                  "attention_kv4_ws_bytes", "kv4_copy_pages")))
+                  "attention_kv4_ws_bytes", "kv4_copy_pages", "rms_norm_quant", "matmul_i8", "route_topk",
+                  "route_topk_ws_bytes", "matmul_grouped")))
         _fast = m
     return _fast
 
@@ -567,6 +582,54 @@ def kv4_copy_pages(pages, pairs):
     r = (_fast or _marshal()).copy_pages(pages, pairs)
     if type(r) is int:
         _check(r, "bitlinear_kv4_copy_pages")
+    return r
+
+
+# ---- layers held in 8 bits, and experts made of them -----------------------------------------------
+# Marshalled like the attention operators, with the same rules for devices, types and streams.
+def rms_norm_quant(x, weight=None, eps=1e-6, residual=None, rows=None, row_weights=None, h=None, y=None, x_q=True, scale=None):
+    """bitlinear_rms_norm_quant.  x [T, K] f32, fp16 or bf16, or with rows int32 [T, top_k] (and row_weights f32 of that shape) the
+    rows [x_rows, K] to be summed up; weight [K]; residual [T, K]; eps < 0 leaves the norm and the weight out (x is only quantised:
+    a weight matrix [N, K] gets a scale per output channel).  h (the sum), y (the normed values) and x_q (the codes, with `scale`
+    f32 [T]) are outputs: a tensor to write to, True for a new one, None for none.  Returns (x_q, scale, h, y)."""
+    r = (_fast or _marshal()).norm_quant(x, weight, eps, residual, rows, row_weights, h, y, x_q, scale)
+    if type(r) is int:
+        _check(r, "bitlinear_rms_norm_quant")
+    return r
+
+
+def matmul_i8(x_q, x_scale, w_q, w_scale, out_dtype=torch.bfloat16, bias=None, relu=False, residual=None, y=None):
+    """bitlinear_matmul_i8.  x_q int8 [M, K] with x_scale f32 [M], w_q int8 [N, K] with w_scale f32 [N] (scales may be None: ones);
+    bias [N] and residual [M, N] of the output's dtype.  Returns y [M, N] (a given one sets the dtype)."""
+    r = (_fast or _marshal()).matmul_i8(x_q, x_scale, w_q, w_scale, _DTYPES.get(out_dtype, -1), bias, relu, residual, y)
+    if type(r) is int:
+        _check(r, "bitlinear_matmul_i8")
+    return r
+
+
+def route_topk_ws_bytes(T, experts) -> int:
+    return int(lib().bitlinear_route_topk_ws_bytes(T, experts))
+
+
+def route_topk(logits, top_k, normalise=True, positions=None, ws=None, chosen=None, weights=None, offsets=None, rows=None, places=None):
+    """bitlinear_route_topk.  logits [T, experts] f32, fp16 or bf16; positions int32 [T] or None (negative: padding, which visits no
+    expert).  Returns (chosen int32 [T, top_k], weights f32 [T, top_k], offsets int32 [experts+1], rows int32 [T*top_k], places int32
+    [T, top_k]), each of which may be given; with padding, entries of new rows behind offsets[-1] hold anything."""
+    r = (_fast or _marshal()).route(logits, top_k, normalise, positions, ws, chosen, weights, offsets, rows, places)
+    if type(r) is int:
+        _check(r, "bitlinear_route_topk")
+    return r
+
+
+def matmul_grouped(x, w, offsets, rows=None, x_scale=None, w_scale=None, bias=None, relu=False, out_dtype=None, y=None):
+    """bitlinear_matmul_grouped.  w [experts, N, K], x [x_rows, K], both int8 (with x_scale f32 [x_rows], w_scale f32 [experts, N], or
+    None: ones), fp16 or bf16; offsets int32 [experts+1] into the list rows int32 [R] of rows of x (None: x's rows in order).  bias
+    [experts, N] of the output's dtype (default: x's, bf16 for int8).  Returns y [R, N]; rows of a new one outside every list hold
+    anything."""
+    r = (_fast or _marshal()).grouped(x, w, offsets, rows, x_scale, w_scale, bias, relu,
+                                      None if out_dtype is None else _DTYPES.get(out_dtype, -1), y)
+    if type(r) is int:
+        _check(r, "bitlinear_matmul_grouped")
     return r
 
 

@@ -2,6 +2,9 @@
 // Nothing here allocates device memory or synchronises (bitlinear_ws_status excepted).
 #include <math.h>
 
+#include <initializer_list>
+#include <utility>
+
 #include "common.cuh"
 
 namespace bl {
@@ -103,6 +106,20 @@ inline bool query_rows(int batch, int n_q, int heads) {
 }
 // A row stride takes the row and keeps every row 16-byte aligned.
 inline bool row_stride(int64_t ld, int heads, int head_dim) { return ld >= (int64_t)heads * head_dim && ld % 8 == 0; }
+
+// ---- checks of the 8-bit layers ------------------------------------------------------------------
+constexpr int kMaxRouted = 512, kMaxExperts = 1024;
+constexpr int64_t kMaxStride = (int64_t)1 << 38;     // tensor maps take strides of up to 2^40 bytes
+constexpr int64_t kMaxFeatures = 1 << 24;
+
+// The sizes of a matrix product of R rows.
+bl_status check_product(int operand, int64_t R, int64_t K, int64_t N, int64_t ld_x, int64_t ld_w, int64_t ld_y) {
+  const int64_t unit = operand == BL_I8 ? 16 : 8;     // values in 16 bytes
+  if (R < 0 || R > kMaxRows || N < 1 || N > kMaxFeatures) return BL_ERR_SHAPE;
+  if (K < unit || K % unit != 0 || K > (operand == BL_I8 ? 131056 : 1 << 20)) return BL_ERR_SHAPE;
+  if (ld_x < K || ld_x % unit != 0 || ld_x > kMaxStride || ld_w < K || ld_w % unit != 0 || ld_w > kMaxStride) return BL_ERR_SHAPE;
+  return ld_y < N || ld_y > kMaxStride ? BL_ERR_SHAPE : BL_OK;
+}
 
 bl_status check_cache(const bl_kv4_cache* c) {
   if (!c) return BL_ERR_NULL;
@@ -642,6 +659,90 @@ bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_p
   if (!aligned16(pages) || !aligned_to(pairs, 8)) return BL_ERR_ALIGN;
   return launch_kv4_copy_pages(pages, page_bytes, num_pages, layers, layers > 1 ? layer_stride : 0, pairs, n,
                                (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_rms_norm_quant(const void* x, bl_dtype dt, int64_t x_rows, int64_t T, int64_t K, int64_t ld_x,
+                                   const int32_t* rows, const float* row_weights, int top_k, const void* residual,
+                                   int64_t ld_res, const void* weight, float eps, void* h, int64_t ld_h, void* y,
+                                   int64_t ld_y, int8_t* x_q, int64_t ld_q, float* scale, void* stream) {
+  if (!valid_dtype(dt)) return BL_ERR_UNSUPPORTED;
+  if (T < 0 || T > kMaxRows || x_rows < 0 || x_rows > kMaxRows || K < 8 || K > 32768 || K % 8 != 0 || eps != eps) return BL_ERR_SHAPE;
+  if (rows ? (top_k < 1 || top_k > 64) : x_rows < T) return BL_ERR_SHAPE;
+  if (row_weights && !rows) return BL_ERR_NULL;
+  auto stride = [K](const void* p, int64_t ld) { return !p || (ld >= K && ld % 8 == 0 && ld <= kMaxStride); };
+  if (ld_x < K || ld_x % 8 != 0 || ld_x > kMaxStride || !stride(residual, ld_res) || !stride(h, ld_h) || !stride(y, ld_y) || !stride(x_q, ld_q)) return BL_ERR_SHAPE;
+  if (T == 0) return BL_OK;
+  if ((!x && x_rows > 0) || (!h && !y && !x_q) || (x_q && !scale)) return BL_ERR_NULL;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(h) || !aligned16(y) || !aligned_to(x_q, 8) ||
+      !aligned_to(rows, 4) || !aligned_to(row_weights, 4) || !aligned_to(scale, 4))
+    return BL_ERR_ALIGN;
+  for (const auto& o : {std::make_pair((const void*)h, ld_h), std::make_pair((const void*)y, ld_y)})
+    if (o.first && ((o.first == residual && o.second != ld_res) || (o.first == x && (rows || o.second != ld_x)))) return BL_ERR_SHAPE;
+  NormQuantArgs a{x, dt, x_rows, T, K, ld_x, rows, row_weights, top_k, residual, ld_res, weight, eps, h, ld_h, y, ld_y, x_q, ld_q, scale};
+  return launch_rms_norm_quant(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_matmul_i8(const int8_t* x_q, int64_t M, int64_t K, int64_t N, int64_t ld_x, const float* x_scale,
+                              const int8_t* w_q, int64_t ld_w, const float* w_scale, const void* bias, int relu,
+                              const void* residual, int64_t ld_res, void* y, bl_dtype yt, int64_t ld_y, void* stream) {
+  if (!valid_dtype(yt)) return BL_ERR_UNSUPPORTED;
+  const bl_status st = check_product(BL_I8, M, K, N, ld_x, ld_w, ld_y);
+  if (st != BL_OK) return st;
+  if (residual && (ld_res < N || ld_res > kMaxStride)) return BL_ERR_SHAPE;
+  if (M == 0) return BL_OK;
+  if (!x_q || !w_q || !y) return BL_ERR_NULL;
+  const unsigned es = yt == BL_F32 ? 4 : 2;
+  if (!aligned16(x_q) || !aligned16(w_q) || !aligned_to(y, es) || !aligned_to(bias, es) || !aligned_to(residual, es) ||
+      !aligned_to(x_scale, 4) || !aligned_to(w_scale, 4))
+    return BL_ERR_ALIGN;
+  if (y == residual && ld_y != ld_res) return BL_ERR_SHAPE;
+  MatmulArgs a{BL_I8, x_q, M, K, N, ld_x, x_scale, w_q, ld_w, 0, w_scale, 1, nullptr, nullptr, M, bias, relu ? 1 : 0, residual, ld_res, y, yt, ld_y};
+  return launch_matmul(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+size_t bitlinear_route_topk_ws_bytes(int64_t T, int experts) {
+  if (T < 0 || T > kMaxRows || experts < 1 || experts > kMaxRouted) return 0;
+  return round256(route_topk_ws_bytes(T, experts));
+}
+
+bl_status bitlinear_route_topk(const void* logits, bl_dtype dt, int64_t T, int experts, int64_t ld, int top_k,
+                               int normalise, const int32_t* positions, int32_t* chosen, float* weights,
+                               int32_t* offsets, int32_t* rows, int32_t* places, void* ws, size_t ws_bytes,
+                               void* stream) {
+  if (!valid_dtype(dt)) return BL_ERR_UNSUPPORTED;
+  if (T < 0 || experts < 1 || experts > kMaxRouted || top_k < 1 || top_k > 32 || top_k > experts) return BL_ERR_SHAPE;
+  if (T > kMaxRows / top_k || ld < experts || ld > kMaxStride) return BL_ERR_SHAPE;
+  if (!offsets || (T > 0 && (!logits || !chosen || !weights || !rows || !places))) return BL_ERR_NULL;
+  if (!aligned_to(logits, dt == BL_F32 ? 4 : 2) || !aligned_to(positions, 4) || !aligned_to(chosen, 4) || !aligned_to(weights, 4) ||
+      !aligned_to(offsets, 4) || !aligned_to(rows, 4) || !aligned_to(places, 4))
+    return BL_ERR_ALIGN;
+  const size_t need = bitlinear_route_topk_ws_bytes(T, experts);
+  if (need > 0 && (!ws || ws_bytes < need)) return BL_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BL_ERR_ALIGN;
+  RouteArgs a{logits, dt, T, experts, ld, top_k, normalise ? 1 : 0, positions, chosen, weights, offsets, rows, places, nullptr, nullptr, nullptr, 0};
+  return launch_route_topk(a, ws, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
+}
+
+bl_status bitlinear_matmul_grouped(const void* x, bl_dtype operand, int64_t x_rows, int64_t K, int64_t N, int64_t ld_x,
+                                   const float* x_scale, const void* w, int64_t ld_w, int64_t expert_stride,
+                                   const float* w_scale, int experts, const int32_t* offsets, const int32_t* rows,
+                                   int64_t R, const void* bias, int relu, void* y, bl_dtype yt, int64_t ld_y,
+                                   void* stream) {
+  if ((operand != BL_I8 && operand != BL_F16 && operand != BL_BF16) || !valid_dtype(yt)) return BL_ERR_UNSUPPORTED;
+  if (operand != BL_I8 && (x_scale || w_scale)) return BL_ERR_UNSUPPORTED;
+  const bl_status st = check_product(operand, R, K, N, ld_x, ld_w, ld_y);
+  if (st != BL_OK) return st;
+  if (experts < 1 || experts > kMaxExperts || x_rows < 0 || x_rows > kMaxRows || (rows ? x_rows < 1 && R > 0 : x_rows < R)) return BL_ERR_SHAPE;
+  if (experts > 1 && (expert_stride % ld_w != 0 || expert_stride / ld_w < N || expert_stride > kMaxStride)) return BL_ERR_SHAPE;
+  if (R == 0) return BL_OK;
+  if (!x || !w || !offsets || !y) return BL_ERR_NULL;
+  const unsigned es = yt == BL_F32 ? 4 : 2;
+  if (!aligned16(x) || !aligned16(w) || !aligned_to(y, es) || !aligned_to(bias, es) || !aligned_to(x_scale, 4) ||
+      !aligned_to(w_scale, 4) || !aligned_to(offsets, 4) || !aligned_to(rows, 4))
+    return BL_ERR_ALIGN;
+  MatmulArgs a{operand, x, x_rows, K, N, ld_x, x_scale, w, ld_w, expert_stride, w_scale, experts, offsets, rows, R, bias, relu ? 1 : 0,
+               nullptr, 0, y, yt, ld_y};
+  return launch_matmul(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
 }
 
 bl_status bitlinear_ws_status(const void* ws, void* stream) {

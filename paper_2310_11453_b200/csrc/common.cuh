@@ -266,6 +266,35 @@ struct Kv4AttnArgs {
 size_t attention_kv4_ws_bytes(int batch, int n_q, int heads, int kv_heads, int head_dim);
 cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s);
 
+// 8-bit layers and experts (rms_norm_quant.cu, route_topk.cu, matmul.cu with matmul_narrow.cu and matmul_wide.cu).
+struct NormQuantArgs {
+  const void* x; bl_dtype dt; int64_t x_rows, T, K, ld_x; const int32_t* rows; const float* row_weights; int top_k;
+  const void* residual; int64_t ld_res; const void* weight; float eps;
+  void* h; int64_t ld_h; void* y; int64_t ld_y; int8_t* x_q; int64_t ld_q; float* scale;
+};
+cudaError_t launch_rms_norm_quant(const NormQuantArgs& a, cudaStream_t s);
+
+struct RouteArgs {
+  const void* logits; bl_dtype dt; int64_t T; int experts; int64_t ld; int top_k, normalise; const int32_t* positions;
+  int32_t* chosen; float* weights; int32_t* offsets; int32_t* rows; int32_t* places;
+  unsigned long long* members; uint8_t* counts; int32_t* sums; int stride;     // in the workspace, set by the launcher
+};
+size_t route_topk_ws_bytes(int64_t T, int experts);
+cudaError_t launch_route_topk(RouteArgs a, void* ws, cudaStream_t s);
+
+// y[r, n] = (sum_k x[source of r, k] w[expert of r, n, k]) x_scale w_scale + bias, ReLU, + residual.
+struct MatmulArgs {
+  bl_dtype operand;                                // BL_I8, BL_F16 or BL_BF16
+  const void* x; int64_t x_rows, K, N, ld_x; const float* x_scale;
+  const void* w; int64_t ld_w, expert_stride; const float* w_scale; int experts;
+  const int32_t* offsets;                          // nullptr: one expert, every row
+  const int32_t* rows; int64_t R;                  // rows of y
+  const void* bias; int relu; const void* residual; int64_t ld_res;
+  void* y; bl_dtype yt; int64_t ld_y;
+};
+cudaError_t launch_matmul(const MatmulArgs& a, cudaStream_t s);
+cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int splits, cudaStream_t s);
+
 // Host-side layout maps (also exported through bitlinear_layout_index).
 int64_t prefill_bytes(int64_t N, int64_t K);
 void prefill_index(int64_t K, int64_t n, int64_t k, int64_t* byte_off, int* bit);

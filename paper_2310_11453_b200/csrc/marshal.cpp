@@ -1,4 +1,4 @@
-// Compiled argument marshalling for the attention operators (module _marshal, used by binding.py).
+// Compiled argument marshalling for the attention operators and the 8-bit layers (module _marshal, used by binding.py).
 //
 // A decode step makes several of these calls per layer, each a few microseconds of device time; looking at seven tensors,
 // allocating outputs and converting twenty arguments costs 10 microseconds from Python and about 3 from here.  The
@@ -33,6 +33,11 @@ struct Entry {
   decltype(&bitlinear_attention_kv4) kv4;
   decltype(&bitlinear_attention_kv4_ws_bytes) kv4_ws;
   decltype(&bitlinear_kv4_copy_pages) copy_pages;
+  decltype(&bitlinear_rms_norm_quant) norm_quant;
+  decltype(&bitlinear_matmul_i8) matmul_i8;
+  decltype(&bitlinear_route_topk) route;
+  decltype(&bitlinear_route_topk_ws_bytes) route_ws;
+  decltype(&bitlinear_matmul_grouped) grouped;
 } entry;
 
 struct TypeError : std::runtime_error { using std::runtime_error::runtime_error; };
@@ -308,12 +313,206 @@ PyObject* copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+bool given(PyObject* o) { return o != Py_None; }
+// An output: a given tensor, a new one for True, none for None or False.
+Tensor output(PyObject* o, const char* name, int64_t rows, int64_t width, at::TensorOptions options) {
+  if (o == Py_None || o == Py_False) return Tensor();
+  if (o == Py_True) return at::empty({rows, width}, options);
+  return tensor(o, name);
+}
+// Like rows_of, for a matrix whose rows take any stride; a stride that no row uses is the width, rounded up to `unit`.
+int64_t any_rows_of(const Tensor& t, const char* name, c10::Device dev, at::ScalarType type, int64_t rows, int64_t width, int64_t unit) {
+  check_place(t, name, dev, type);
+  if (t.dim() != 2 || t.size(0) != rows || t.size(1) != width || (t.stride(1) != 1 && width > 1))
+    throw std::invalid_argument(std::string(name) + " has shape " + shape_of(t) + ", expected (" + std::to_string(rows) + ", " +
+                                std::to_string(width) + ") with the values of a row contiguous");
+  return rows > 1 ? t.stride(0) : (width + unit - 1) / unit * unit;
+}
+PyObject* wrapped(PyObject* o, const Tensor& t) {
+  if (o == Py_True) return THPVariable_Wrap(t);
+  if (o == Py_False) o = Py_None;
+  Py_INCREF(o);
+  return o;
+}
+at::ScalarType scalar_type(PyObject* o) {                       // of a BL_* code
+  switch (small(o, "dtype")) {
+    case BL_F32: return at::kFloat;
+    case BL_F16: return at::kHalf;
+    case BL_BF16: return at::kBFloat16;
+    default: throw TypeError("unsupported dtype");
+  }
+}
+int truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v;
+}
+
+// x, weight, eps, residual, rows, row_weights, h, y, x_q, scale
+PyObject* norm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 10);
+    const Tensor& x = tensor(a[0], "x");
+    const c10::Device dev = cuda_device(x, "x");
+    const auto type = x.scalar_type();
+    const bl_dtype code = type_code(type);
+    if (x.dim() != 2) throw std::invalid_argument("x has shape " + shape_of(x) + ", expected (rows, K)");
+    const int64_t x_rows = x.size(0), K = x.size(1), ld_x = any_rows_of(x, "x", dev, type, x_rows, K, 8);
+    const float eps = real(a[2]);
+    int64_t T = x_rows, top_k = 0;
+    void *rp = nullptr, *wp = nullptr;
+    if (given(a[4])) {
+      const Tensor& rows = tensor(a[4], "rows");
+      if (rows.dim() != 2) throw std::invalid_argument("rows has shape " + shape_of(rows) + ", expected (T, top_k)");
+      T = rows.size(0); top_k = rows.size(1);
+      rp = flat(rows, "rows", dev, at::kInt, T, top_k);
+      if (T > 0 && top_k > INT32_MAX) throw std::invalid_argument("rows is too wide");
+      if (given(a[5])) wp = flat(tensor(a[5], "row_weights"), "row_weights", dev, at::kFloat, T, top_k);
+    } else if (given(a[5])) {
+      throw std::invalid_argument("row_weights without rows");
+    }
+    void* weight = given(a[1]) ? flat(tensor(a[1], "weight"), "weight", dev, type, K) : nullptr;
+    const void* res = nullptr;
+    int64_t ld_res = 0;
+    if (given(a[3])) {
+      const Tensor& r = tensor(a[3], "residual");
+      ld_res = any_rows_of(r, "residual", dev, type, T, K, 8);
+      res = r.data_ptr();
+    }
+    const c10::cuda::CUDAGuard guard(dev);
+    const Tensor h = output(a[6], "h", T, K, x.options()), y = output(a[7], "y", T, K, x.options());
+    const Tensor q = output(a[8], "x_q", T, K, x.options().dtype(at::kChar));
+    const Tensor scale = !q.defined() ? Tensor() : given(a[9]) ? tensor(a[9], "scale") : at::empty({T}, x.options().dtype(at::kFloat));
+    const int64_t ld_h = h.defined() ? any_rows_of(h, "h", dev, type, T, K, 8) : 0, ld_y = y.defined() ? any_rows_of(y, "y", dev, type, T, K, 8) : 0;
+    const int64_t ld_q = q.defined() ? any_rows_of(q, "x_q", dev, at::kChar, T, K, 8) : 0;
+    void* sp = q.defined() ? flat(scale, "scale", dev, at::kFloat, T) : nullptr;
+    auto at_of = [](const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const bl_status st = entry.norm_quant(x.data_ptr(), code, x_rows, T, K, ld_x, (const int32_t*)rp, (const float*)wp, (int)top_k, res, ld_res,
+                                          weight, eps, at_of(h), ld_h, at_of(y), ld_y, (int8_t*)at_of(q), ld_q, (float*)sp, stream_of(dev));
+    if (st != BL_OK) return status(st);
+    PyObject* r = PyTuple_New(4);
+    if (!r) throw python_error();
+    PyTuple_SET_ITEM(r, 0, wrapped(a[8], q));
+    PyTuple_SET_ITEM(r, 1, q.defined() ? given_or(a[9], scale) : wrapped(Py_None, Tensor()));
+    PyTuple_SET_ITEM(r, 2, wrapped(a[6], h));
+    PyTuple_SET_ITEM(r, 3, wrapped(a[7], y));
+    return r;
+  });
+}
+
+// x_q, x_scale, w_q, w_scale, dtype, bias, relu, residual, y
+PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 9);
+    const Tensor &x = tensor(a[0], "x_q"), &w = tensor(a[2], "w_q");
+    const c10::Device dev = cuda_device(x, "x_q");
+    if (x.dim() != 2 || w.dim() != 2) throw std::invalid_argument("x_q and w_q must have two dimensions");
+    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+    const int64_t ld_x = any_rows_of(x, "x_q", dev, at::kChar, M, K, 16), ld_w = any_rows_of(w, "w_q", dev, at::kChar, N, K, 16);
+    void* xs = given(a[1]) ? flat(tensor(a[1], "x_scale"), "x_scale", dev, at::kFloat, M) : nullptr;
+    void* ws = given(a[3]) ? flat(tensor(a[3], "w_scale"), "w_scale", dev, at::kFloat, N) : nullptr;
+    const auto type = given(a[8]) ? tensor(a[8], "y").scalar_type() : scalar_type(a[4]);
+    void* bias = given(a[5]) ? flat(tensor(a[5], "bias"), "bias", dev, type, N) : nullptr;
+    const int relu = truth(a[6]);
+    const void* res = nullptr;
+    int64_t ld_res = 0;
+    if (given(a[7])) {
+      const Tensor& r = tensor(a[7], "residual");
+      ld_res = any_rows_of(r, "residual", dev, type, M, N, 1);
+      res = r.data_ptr();
+    }
+    const c10::cuda::CUDAGuard guard(dev);
+    const Tensor y = given(a[8]) ? tensor(a[8], "y") : at::empty({M, N}, x.options().dtype(type));
+    const int64_t ld_y = any_rows_of(y, "y", dev, type, M, N, 1);
+    const bl_status st = entry.matmul_i8((const int8_t*)x.data_ptr(), M, K, N, ld_x, (const float*)xs, (const int8_t*)w.data_ptr(), ld_w,
+                                         (const float*)ws, bias, relu, res, ld_res, y.data_ptr(), type_code(type), ld_y, stream_of(dev));
+    return st != BL_OK ? status(st) : given_or(a[8], y);
+  });
+}
+
+// logits, top_k, normalise, positions, ws, chosen, weights, offsets, rows, places
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 10);
+    const Tensor& z = tensor(a[0], "logits");
+    const c10::Device dev = cuda_device(z, "logits");
+    const auto type = z.scalar_type();
+    const bl_dtype code = type_code(type);
+    if (z.dim() != 2) throw std::invalid_argument("logits has shape " + shape_of(z) + ", expected (T, experts)");
+    const int64_t T = z.size(0), E = z.size(1), ld = any_rows_of(z, "logits", dev, type, T, E, 1);
+    const int k = small(a[1], "top_k"), normalise = truth(a[2]);
+    if (E > INT32_MAX || k < 1 || k > E || k > 32) throw std::invalid_argument("top_k must be 1..32 and at most the number of experts");
+    void* pos = given(a[3]) ? flat(tensor(a[3], "positions"), "positions", dev, at::kInt, T) : nullptr;
+    const c10::cuda::CUDAGuard guard(dev);
+    const auto ints = z.options().dtype(at::kInt);
+    const Tensor chosen = given(a[5]) ? tensor(a[5], "chosen") : at::empty({T, k}, ints);
+    const Tensor weights = given(a[6]) ? tensor(a[6], "weights") : at::empty({T, k}, z.options().dtype(at::kFloat));
+    const Tensor offsets = given(a[7]) ? tensor(a[7], "offsets") : at::empty({E + 1}, ints);
+    const Tensor rows = given(a[8]) ? tensor(a[8], "rows") : at::empty({T * k}, ints);
+    const Tensor places = given(a[9]) ? tensor(a[9], "places") : at::empty({T, k}, ints);
+    void *cp = flat(chosen, "chosen", dev, at::kInt, T, k), *wp = flat(weights, "weights", dev, at::kFloat, T, k);
+    void *op = flat(offsets, "offsets", dev, at::kInt, E + 1), *rp = flat(rows, "rows", dev, at::kInt, T * k);
+    void* pp = flat(places, "places", dev, at::kInt, T, k);
+    const int64_t need = (int64_t)entry.route_ws(T, (int)E);
+    Tensor ws;
+    if (given(a[4])) { ws = tensor(a[4], "ws"); (void)flat(ws, "ws", dev, at::kByte, ws.numel()); }
+    else if (need > 0) ws = at::empty({need}, z.options().dtype(at::kByte));
+    const bl_status st = entry.route(z.data_ptr(), code, T, (int)E, ld, k, normalise, (const int32_t*)pos, (int32_t*)cp, (float*)wp, (int32_t*)op,
+                                     (int32_t*)rp, (int32_t*)pp, ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0,
+                                     stream_of(dev));
+    if (st != BL_OK) return status(st);
+    PyObject* r = PyTuple_New(5);
+    if (!r) throw python_error();
+    PyTuple_SET_ITEM(r, 0, given_or(a[5], chosen));
+    PyTuple_SET_ITEM(r, 1, given_or(a[6], weights));
+    PyTuple_SET_ITEM(r, 2, given_or(a[7], offsets));
+    PyTuple_SET_ITEM(r, 3, given_or(a[8], rows));
+    PyTuple_SET_ITEM(r, 4, given_or(a[9], places));
+    return r;
+  });
+}
+
+// x, w, offsets, rows, x_scale, w_scale, bias, relu, dtype, y
+PyObject* grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    want(n, 10);
+    const Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w"), &offsets = tensor(a[2], "offsets");
+    const c10::Device dev = cuda_device(x, "x");
+    const auto type = x.scalar_type();
+    const bool codes = type == at::kChar;
+    if (!codes && type != at::kHalf && type != at::kBFloat16) throw TypeError(std::string("x is ") + c10::toString(type) + ", expected int8, fp16 or bf16");
+    const int64_t unit = codes ? 16 : 8;
+    if (x.dim() != 2 || w.dim() != 3) throw std::invalid_argument("x must have two dimensions and w three");
+    const int64_t x_rows = x.size(0), K = x.size(1), E = w.size(0), N = w.size(1);
+    const int64_t ld_x = any_rows_of(x, "x", dev, type, x_rows, K, unit);
+    check_place(w, "w", dev, type);
+    if (w.size(2) != K || w.stride(2) != 1) throw std::invalid_argument("w has shape " + shape_of(w) + ", expected (experts, N, K) with the values of a row contiguous");
+    if (E < 1 || E > INT32_MAX) throw std::invalid_argument("w has no experts, or too many");
+    const int64_t ld_w = N > 1 ? w.stride(1) : E > 1 ? w.stride(0) : (K + unit - 1) / unit * unit;
+    void* op = flat(offsets, "offsets", dev, at::kInt, E + 1);
+    const int64_t R = given(a[3]) ? tensor(a[3], "rows").numel() : x_rows;
+    void* rp = given(a[3]) ? flat(tensor(a[3], "rows"), "rows", dev, at::kInt, R) : nullptr;
+    void* xs = given(a[4]) ? flat(tensor(a[4], "x_scale"), "x_scale", dev, at::kFloat, x_rows) : nullptr;
+    void* ws = given(a[5]) ? flat(tensor(a[5], "w_scale"), "w_scale", dev, at::kFloat, E, N) : nullptr;
+    const auto ytype = given(a[9]) ? tensor(a[9], "y").scalar_type() : given(a[8]) ? scalar_type(a[8]) : codes ? at::kBFloat16 : type;
+    void* bias = given(a[6]) ? flat(tensor(a[6], "bias"), "bias", dev, ytype, E, N) : nullptr;
+    const int relu = truth(a[7]);
+    const c10::cuda::CUDAGuard guard(dev);
+    const Tensor y = given(a[9]) ? tensor(a[9], "y") : at::empty({R, N}, x.options().dtype(ytype));
+    const int64_t ld_y = any_rows_of(y, "y", dev, ytype, R, N, 1);
+    const bl_status st = entry.grouped(x.data_ptr(), codes ? BL_I8 : type_code(type), x_rows, K, N, ld_x, (const float*)xs, w.data_ptr(), ld_w,
+                                       w.stride(0), (const float*)ws, (int)E, (const int32_t*)op, (const int32_t*)rp, R, bias, relu, y.data_ptr(),
+                                       type_code(ytype), ld_y, stream_of(dev));
+    return st != BL_OK ? status(st) : given_or(a[9], y);
+  });
+}
+
 // Addresses of the C entry points, in the order of Entry.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    want(n, 8);
-    void* p[8];
-    for (int i = 0; i < 8; ++i) {
+    want(n, 13);
+    void* p[13];
+    for (int i = 0; i < 13; ++i) {
       p[i] = PyLong_AsVoidPtr(a[i]);
       if (PyErr_Occurred()) throw python_error();
       if (!p[i]) throw std::invalid_argument("no address");
@@ -326,6 +525,11 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     entry.kv4 = reinterpret_cast<decltype(entry.kv4)>(p[5]);
     entry.kv4_ws = reinterpret_cast<decltype(entry.kv4_ws)>(p[6]);
     entry.copy_pages = reinterpret_cast<decltype(entry.copy_pages)>(p[7]);
+    entry.norm_quant = reinterpret_cast<decltype(entry.norm_quant)>(p[8]);
+    entry.matmul_i8 = reinterpret_cast<decltype(entry.matmul_i8)>(p[9]);
+    entry.route = reinterpret_cast<decltype(entry.route)>(p[10]);
+    entry.route_ws = reinterpret_cast<decltype(entry.route_ws)>(p[11]);
+    entry.grouped = reinterpret_cast<decltype(entry.grouped)>(p[12]);
     Py_RETURN_NONE;
   });
 }
@@ -339,8 +543,12 @@ PyMethodDef methods[] = {FAST(bind, "Hands over the addresses of the C entry poi
                          FAST(read, "bitlinear_kv4_read"),
                          FAST(kv4, "bitlinear_attention_kv4"),
                          FAST(copy_pages, "bitlinear_kv4_copy_pages"),
+                         FAST(norm_quant, "bitlinear_rms_norm_quant"),
+                         FAST(matmul_i8, "bitlinear_matmul_i8"),
+                         FAST(route, "bitlinear_route_topk"),
+                         FAST(grouped, "bitlinear_matmul_grouped"),
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled argument marshalling of the attention operators.", -1, methods};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled argument marshalling of the attention operators and the 8-bit layers.", -1, methods};
 
 }  // namespace
 

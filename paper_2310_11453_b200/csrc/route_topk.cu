@@ -1,0 +1,279 @@
+// The experts of each token, and the lists of rows that they make.
+//   chosen   the top_k largest of a token's scores; of equals the lowest index first (a NaN counts as less than -infinity)
+//   weights  exp(z_e - max z) over their sum, over the chosen or over all experts
+//   offsets  first row of each expert in the list of all (token, choice) pairs ordered by expert, then by token
+//   rows     the token of each row of that list;  places: the row of each (token, choice)
+// Latency, not bandwidth: the scores of 8191 tokens over 128 experts are 2 MB.  A warp holds a token's scores as keys
+// whose unsigned order is theirs (lane l has experts l, l + 32, ..), and picks by warp-wide integer maxima.
+// The order of the list comes without sorting: each block of kRun tokens notes, per expert, the set of its tokens
+// as bits, so a token's rank is a count of lower bits, whatever the order in which warps set them.  With one block that
+// is all; with more, each leaves its counts (a byte per expert) and a second kernel adds up those of the
+// blocks before its own.  Beyond kDirect blocks, whose counts every block would read, a kernel in between sums them up.
+#include "common.cuh"
+
+namespace bl {
+
+namespace {
+
+constexpr int kRun = 64;                       // tokens per block; a count fits a byte
+constexpr int kWarps = 16;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxExperts = 512;
+constexpr int kDirect = 512;                   // blocks whose counts the placing kernel adds up itself
+
+// Unsigned order of the keys = order of the values; -0 and 0 are equal, NaN is lowest.
+__device__ __forceinline__ uint32_t key_of(float z) {
+  return z != z ? 0u : enc_ordered(z + 0.f);
+}
+
+template <typename T, int kPer>                // kPer scores per lane
+__global__ void __launch_bounds__(kThreads) route_pick_kernel(RouteArgs a) {
+  __shared__ unsigned long long members[kMaxExperts];      // tokens of the run that chose the expert
+  __shared__ int first[kMaxExperts + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool alone = gridDim.x == 1;
+  pdl_launch_dependents();
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) members[e] = 0ull;
+  __syncthreads();
+  pdl_wait();
+  const int64_t t0 = (int64_t)blockIdx.x * kRun;
+  const T* logits = reinterpret_cast<const T*>(a.logits);
+  for (int local = warp; local < kRun; local += kWarps) {
+    const int64_t t = t0 + local;
+    if (t >= a.T) break;
+    const bool padding = a.positions && a.positions[t] < 0;
+    float z[kPer];
+    uint32_t key[kPer];
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = lane + 32 * i;
+      z[i] = e < a.experts ? in_cast(logits[t * a.ld + e]) : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = lane + 32 * i;
+      key[i] = e < a.experts ? key_of(z[i]) + 1u : 0u;     // +1: no expert lies under every score (no key is 2^32 - 1)
+      nan |= z[i] != z[i];
+    }
+    nan = __any_sync(0xFFFFFFFFu, nan);
+    // top_k times: the largest key, and of the experts that have it the lowest
+    int mine = -1;                             // lane j keeps choice j
+    float mine_z = -INFINITY, top_z = 0.f;
+    uint32_t local_top = 0u;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) local_top = max(local_top, key[i]);
+    for (int j = 0; j < a.top_k; ++j) {
+      const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, local_top);
+      int at = INT32_MAX;
+      if (local_top == best) {
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i) if (key[i] == best) at = lane + 32 * i;
+      }
+      const int e = __reduce_min_sync(0xFFFFFFFFu, at);
+      float ez = 0.f;
+      if (at == e) {                           // the owner takes it out
+        local_top = 0u;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (lane + 32 * i == e) { ez = z[i]; key[i] = 0u; }
+          local_top = max(local_top, key[i]);
+        }
+      }
+      ez = __shfl_sync(0xFFFFFFFFu, ez, e & 31);
+      if (j == 0) top_z = ez;
+      if (lane == j) { mine = e; mine_z = ez; }
+    }
+    float p = lane < a.top_k ? expf(mine_z - top_z) : 0.f, total = p;
+    if (!a.normalise) {
+      total = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) if (lane + 32 * i < a.experts) total += expf(z[i] - top_z);
+    }
+    total = warp_sum(total);
+    if (lane < a.top_k) {
+      a.chosen[t * a.top_k + lane] = padding ? -1 : mine;
+      a.weights[t * a.top_k + lane] = padding ? 0.f : nan ? __uint_as_float(0x7FC00000u) : p / total;
+      if (!padding) atomicOr(&members[mine], 1ull << local);
+    }
+  }
+  __syncthreads();
+  if (!alone) {
+    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+      a.members[(int64_t)blockIdx.x * a.experts + e] = members[e];
+      a.counts[(int64_t)blockIdx.x * a.stride + e] = (uint8_t)__popcll(members[e]);
+    }
+    return;
+  }
+  // one block: its own prefix sums
+  if (warp == 0) {
+    int sum = 0;
+    for (int base = 0; base < a.experts; base += 32) {
+      const int e = base + lane;
+      const int n = e < a.experts ? __popcll(members[e]) : 0;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (e < a.experts) first[e] = sum + upto - n;
+      sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    if (lane == 0) first[a.experts] = sum;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = first[e];
+  for (int c = threadIdx.x; c < (int)a.T * a.top_k; c += kThreads) {
+    const int local = c / a.top_k, e = a.chosen[c];
+    int place = -1;
+    if (e >= 0) {
+      place = first[e] + __popcll(members[e] & ((1ull << local) - 1ull));
+      a.rows[place] = local;
+    }
+    a.places[c] = place;
+  }
+}
+
+// Many blocks: counts summed over all blocks before each, per expert.  One block per expert.
+__global__ void __launch_bounds__(256) route_sum_kernel(RouteArgs a, int runs) {
+  __shared__ int part[8];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int e = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int before = 0;
+  for (int base = 0; base < runs; base += 256) {
+    const int r = base + threadIdx.x;
+    const int n = r < runs ? a.counts[(int64_t)r * a.stride + e] : 0;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) part[warp] = upto;
+    __syncthreads();
+    int lower = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { if (w < warp) lower += part[w]; all += part[w]; }
+    if (r < runs) a.sums[(int64_t)r * a.experts + e] = before + lower + upto - n;
+    before += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.sums[(int64_t)runs * a.experts + e] = before;
+}
+
+// Rows and places of a run, and the offsets.
+template <bool kSummed>
+__global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, int runs) {
+  __shared__ int total[kMaxExperts], before[kMaxExperts];
+  __shared__ int first[kMaxExperts + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) { total[e] = 0; before[e] = 0; }
+  __syncthreads();
+  pdl_wait();
+  if (kSummed) {
+    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+      total[e] = a.sums[(int64_t)runs * a.experts + e];
+      before[e] = a.sums[(int64_t)blockIdx.x * a.experts + e];
+    }
+  } else {
+    // four experts a thread (the rows of counts are padded to words), the runs shared out over the warps
+    const int words = a.stride / 4;
+    for (int w0 = 0; w0 < words; w0 += 32) {
+      const int w = w0 + lane;
+      if (w >= words) continue;
+      int all[4] = {0, 0, 0, 0}, low[4] = {0, 0, 0, 0};
+#pragma unroll 8
+      for (int r = warp; r < runs; r += kWarps) {
+        const uint32_t c = *reinterpret_cast<const uint32_t*>(a.counts + (int64_t)r * a.stride + 4 * w);
+        const bool mine = r < (int)blockIdx.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = (c >> (8 * i)) & 255;
+          all[i] += n;
+          low[i] += mine ? n : 0;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * w + i < a.experts) { atomicAdd(&total[4 * w + i], all[i]); atomicAdd(&before[4 * w + i], low[i]); }   // whole numbers: any order
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {
+    int sum = 0;
+    for (int base = 0; base < a.experts; base += 32) {
+      const int e = base + lane;
+      const int n = e < a.experts ? total[e] : 0;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (e < a.experts) first[e] = sum + upto - n;
+      sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    if (lane == 0) first[a.experts] = sum;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = first[e];
+  const int64_t t0 = (int64_t)blockIdx.x * kRun;
+  const int here = (int)min((int64_t)kRun, a.T - t0);
+  const unsigned long long* members = a.members + (int64_t)blockIdx.x * a.experts;
+  for (int c = threadIdx.x; c < here * a.top_k; c += kThreads) {
+    const int local = c / a.top_k, e = a.chosen[t0 * a.top_k + c];
+    int place = -1;
+    if (e >= 0) {
+      place = first[e] + before[e] + __popcll(members[e] & ((1ull << local) - 1ull));
+      a.rows[place] = (int)(t0 + local);
+    }
+    a.places[t0 * a.top_k + c] = place;
+  }
+}
+
+template <typename T>
+cudaError_t pick(const RouteArgs& a, unsigned runs, cudaStream_t s) {
+  if (a.experts <= 32) return launch_pdl(route_pick_kernel<T, 1>, runs, kThreads, 0, s, a);
+  if (a.experts <= 64) return launch_pdl(route_pick_kernel<T, 2>, runs, kThreads, 0, s, a);
+  if (a.experts <= 128) return launch_pdl(route_pick_kernel<T, 4>, runs, kThreads, 0, s, a);
+  if (a.experts <= 256) return launch_pdl(route_pick_kernel<T, 8>, runs, kThreads, 0, s, a);
+  return launch_pdl(route_pick_kernel<T, 16>, runs, kThreads, 0, s, a);
+}
+
+size_t round16(size_t v) { return (v + 15) & ~size_t(15); }
+
+struct Carve { size_t members, counts, sums, total; };
+Carve carve(int64_t T, int experts) {
+  Carve c{0, 0, 0, 0};
+  const size_t runs = (size_t)((T + kRun - 1) / kRun);
+  if (runs <= 1) return c;
+  const size_t stride = (size_t)((experts + 3) / 4 * 4);
+  c.counts = round16(runs * (size_t)experts * 8);
+  c.sums = c.counts + round16(runs * stride);
+  c.total = c.sums + (runs > kDirect ? (runs + 1) * (size_t)experts * 4 : 0);
+  return c;
+}
+
+}  // namespace
+
+size_t route_topk_ws_bytes(int64_t T, int experts) { return carve(T, experts).total; }
+
+cudaError_t launch_route_topk(RouteArgs a, void* ws, cudaStream_t s) {
+  const Carve c = carve(a.T, a.experts);
+  const unsigned runs = a.T > 0 ? (unsigned)((a.T + kRun - 1) / kRun) : 1u;
+  a.stride = (a.experts + 3) / 4 * 4;
+  a.members = reinterpret_cast<unsigned long long*>(ws);
+  a.counts = reinterpret_cast<uint8_t*>(ws) + c.counts;
+  a.sums = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(ws) + c.sums);
+  cudaError_t e = a.dt == BL_F32 ? pick<float>(a, runs, s) : a.dt == BL_F16 ? pick<__half>(a, runs, s) : pick<__nv_bfloat16>(a, runs, s);
+  if (e != cudaSuccess || runs == 1) return e;
+  if (runs <= kDirect) return launch_pdl(route_place_kernel<false>, runs, kThreads, 0, s, a, (int)runs);
+  if ((e = launch_pdl(route_sum_kernel, (unsigned)a.experts, 256, 0, s, a, (int)runs)) != cudaSuccess) return e;
+  return launch_pdl(route_place_kernel<true>, runs, kThreads, 0, s, a, (int)runs);
+}
+
+}  // namespace bl
