@@ -5,6 +5,8 @@ namespace bl {
 
 cudaError_t launch_matmul(const MatmulArgs& a, cudaStream_t s) {
   const int64_t mean = a.offsets ? (a.R + a.experts - 1) / a.experts : a.R;
+  if (mean > 160) return launch_matmul_wide(a, 256, s);
+  if (mean > 64) return launch_matmul_wide(a, 128, s);
   const int tokens = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
   const int64_t token_tiles = a.offsets ? a.R / tokens + (a.experts < a.R ? a.experts : a.R) : (a.R + tokens - 1) / tokens;
   const int64_t tiles = token_tiles * ((a.N + 127) / 128);
