@@ -17,12 +17,18 @@ using namespace tc;
 constexpr int kRowBytes = 128;             // bytes of K per stage and row: one swizzle atom
 constexpr int kMaxExperts = 1024;
 
-// A wait with a limit: 0 polls for a limit of 0.
+// A wait with a limit (a number of polls, or below 0 two seconds).  The clock is only read once a wait is long: reading it takes longer than most
+// waits last.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long polls) {
-  if (polls < 0) return mbar_wait(bar, parity, abort_flag);
-  for (long long i = 0; i < polls; ++i) {
+  unsigned long long t0 = 0;
+  for (long long it = 0; polls < 0 || it < polls; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
+    if ((it & 255) == 255) {
+      if (*abort_flag) return false;
+      const unsigned long long now = global_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > kWaitNs) break;
+    }
   }
   *abort_flag = 1;
   return false;
@@ -60,6 +66,17 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 // Four rows of the matrix, wherever they lie, one under the other.
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int c0, const int (&r)[4], uint32_t bar) {
   asm volatile(
@@ -72,10 +89,10 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -120,24 +137,28 @@ __device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int R) {
   return v < 0 ? 0 : v > R ? R : v;
 }
 
-struct Tile { int expert, row0, rows; };   // rows: 0 where there is no such tile
+// The tiles of a launch, in the order in which every role of every CTA takes them: expert by expert, within one all row tiles of a
+// feature tile first, so that CTAs that run at once share its weights.  The plan lies in shared memory: per expert the first row
+// tile (and behind the last their number), the first row, the number of rows.
+inline size_t plan_bytes(int experts) { return (size_t)(3 * experts + 1) * sizeof(int); }
 
-// The i-th tile of up to kTile rows in the order of the experts.  All lanes of a warp call it.
-__device__ inline Tile find_tile(const MatmulArgs& a, int i, int tile_rows) {
-  Tile t{0, i * tile_rows, 0};
-  if (!a.offsets) {
-    const int64_t left = a.R - (int64_t)i * tile_rows;
-    t.rows = left < 0 ? 0 : left > tile_rows ? tile_rows : (int)left;
-    return t;
-  }
+// One warp makes the plan.
+__device__ inline void make_plan(const MatmulArgs& a, int* plan, int tile_rows) {
   const int lane = threadIdx.x & 31;
+  int *first = plan, *start = plan + a.experts + 1, *count = plan + 2 * a.experts + 1;
   int seen = 0;
   for (int base = 0; base < a.experts; base += 32) {
     const int e = base + lane;
     int from = 0, n = 0;
     if (e < a.experts) {
-      from = offset_of(a.offsets, e, (int)a.R);
-      n = max(0, offset_of(a.offsets, e + 1, (int)a.R) - from);
+      if (a.offsets) {
+        from = offset_of(a.offsets, e, (int)a.R);
+        n = max(0, offset_of(a.offsets, e + 1, (int)a.R) - from);
+      } else {
+        n = (int)a.R;
+      }
+      start[e] = from;
+      count[e] = n;
     }
     const int tiles = (n + tile_rows - 1) / tile_rows;
     int upto = tiles;
@@ -146,20 +167,31 @@ __device__ inline Tile find_tile(const MatmulArgs& a, int i, int tile_rows) {
       const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += v;
     }
-    const uint32_t hit = __ballot_sync(0xFFFFFFFFu, seen + upto > i);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      const int before = seen + upto - tiles;
-      const int r0 = (i - before) * tile_rows;
-      t.expert = base + l;
-      t.row0 = __shfl_sync(0xFFFFFFFFu, from + r0, l);
-      t.rows = __shfl_sync(0xFFFFFFFFu, min(tile_rows, n - r0), l);
-      return t;
-    }
+    if (e < a.experts) first[e] = seen + upto - tiles;
     seen += __shfl_sync(0xFFFFFFFFu, upto, 31);
   }
-  return t;
+  if (lane == 0) first[a.experts] = seen;
 }
+
+struct Walk {
+  const int *first, *start, *count;
+  uint32_t t, total, stride, feature_tiles;
+  int e, row0, rows, f;                    // of the tile: expert, first row, rows, feature tile
+  __device__ Walk(const int* plan, int experts, int feature_tiles_, uint32_t from, uint32_t stride_)
+      : first(plan), start(plan + experts + 1), count(plan + 2 * experts + 1), t(from), total((uint32_t)plan[experts] * (uint32_t)feature_tiles_),
+        stride(stride_), feature_tiles((uint32_t)feature_tiles_), e(0), row0(0), rows(0), f(0) {}
+  __device__ bool valid() const { return t < total; }
+  __device__ void next() { t += stride; }
+  // An expert's rows are shared out evenly over its tiles, in multiples of `unit` rows.
+  __device__ void locate(int unit) {
+    while (t >= feature_tiles * (uint32_t)first[e + 1]) ++e;
+    const uint32_t local = t - feature_tiles * (uint32_t)first[e], n = (uint32_t)(first[e + 1] - first[e]);
+    f = (int)(local / n);
+    const int each = (int)(((uint32_t)count[e] + n - 1) / n + unit - 1) / unit * unit, skip = (int)(local - (uint32_t)f * n) * each;
+    row0 = start[e] + skip;
+    rows = min(each, count[e] - skip);
+  }
+};
 
 // The row of x behind a row of the list; one that does not exist reads as the nearest that does.
 __device__ __forceinline__ int source_row(const MatmulArgs& a, int row) {
@@ -217,15 +249,19 @@ inline cudaError_t encode_rows(CUtensorMap* map, const void* base, int64_t row_b
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess : cudaErrorInvalidValue;
 }
-inline cudaError_t encode_weights(CUtensorMap* map, const MatmulArgs& a, int box_rows) {
+// A matrix (of several experts, if experts > 0) as boxes of box_rows x 128 bytes: of `sub` consecutive blocks of K at once, which
+// lie behind each other in shared memory (sub > 0: K has to be a whole number of blocks), or of one at any byte of K (sub = 0).
+// Coordinates: byte, row, block, expert.
+inline cudaError_t encode_blocks(CUtensorMap* map, const void* base, int64_t row_bytes, int64_t rows, int64_t stride_bytes, int experts,
+                                 int64_t expert_bytes, int box_rows, int sub) {
   EncodeFn enc = encode_fn();
   if (!enc) return cudaErrorNotSupported;
-  const int es = a.operand == BL_I8 ? 1 : 2;
-  const cuuint64_t dims[3] = {(cuuint64_t)(a.K * es), (cuuint64_t)a.N, (cuuint64_t)a.experts};
-  const cuuint64_t strides[2] = {(cuuint64_t)(a.ld_w * es), (cuuint64_t)((a.experts > 1 ? a.expert_stride : a.ld_w) * es)};
-  const cuuint32_t box[3] = {(cuuint32_t)kRowBytes, (cuuint32_t)box_rows, 1};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(a.w), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t dims[4] = {(cuuint64_t)(sub > 0 ? kRowBytes : row_bytes), (cuuint64_t)rows, (cuuint64_t)(sub > 0 ? row_bytes / kRowBytes : 1),
+                              (cuuint64_t)(experts > 0 ? experts : 1)};
+  const cuuint64_t strides[3] = {(cuuint64_t)stride_bytes, (cuuint64_t)kRowBytes, (cuuint64_t)(experts > 1 ? expert_bytes : stride_bytes)};
+  const cuuint32_t box[4] = {(cuuint32_t)kRowBytes, (cuuint32_t)box_rows, (cuuint32_t)(sub > 0 ? sub : 1), 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, experts > 0 ? 4 : 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess : cudaErrorInvalidValue;
 }

@@ -1,10 +1,15 @@
 // 8-bit (and fp16, bf16) matrix products of few rows: decode steps and short lists of rows.  Bound by the weights' bytes.
-// A tile is 128 output features x kTokens rows; a cluster of `splits` CTAs shares the K axis of one tile, so that the loads
-// of few tiles spread over the GPU, and joins its sums through shared memory (the whole numbers exactly, fp32 in the order of the
-// CTAs).  One tile per cluster: what a CTA spends on its start and its end is covered by the others on the SM.
-// Warp 0 loads (weights as boxes of 128 rows x 128 bytes; tokens as boxes, or four rows at a time where a list says which),
-// warp 1 multiplies, warps 2-5 take a quarter of the lanes each to y.
-// Waits are bounded; a tile whose wait runs out is written as NaN.
+// A tile is `features` output features (128, 64 or 32, as few as it takes to give every SM a share of the loads) x kTokens rows.
+// The instruction always multiplies 128 rows of weights; those behind the tile's are whatever lies there, and nobody reads
+// their sums.  Where even that leaves SMs without work, a cluster of `splits` CTAs shares the K axis of a tile and joins its
+// sums through shared memory (whole numbers exactly, fp32 in the order of the CTAs); there is a cluster per tile then.  Without,
+// the grid is persistent: loads run ahead from tile to tile, and two accumulators take turns.
+// A ring slot holds `sub` blocks of 128 bytes of K.  Where K is a whole number of blocks one tensor copy brings the weights of
+// a slot, and one the tokens: a copy costs about 70 clocks and 3.4 per row of 128 bytes (measured on one SM), so small
+// ones are dear.  Without lists the weights do not depend on what comes before on the stream: the first slots of them are
+// asked for ahead of its order.
+// Warp 0 loads (tokens four rows at a time where a list says which), warp 1 multiplies, warps 2-5 take a quarter of the lanes
+// each to y.  Waits are bounded; a tile whose wait runs out is written as NaN.
 #include "matmul_common.cuh"
 
 namespace bl {
@@ -14,204 +19,283 @@ namespace {
 using namespace mm;
 
 constexpr int kThreads = 192;
-constexpr int kFeatures = 128;
-constexpr int kABytes = kFeatures * kRowBytes;
+constexpr int kLanes = 128;                 // rows of weights per instruction
 constexpr int kMaxSlots = 8;
-constexpr size_t kBudget = 113 * 1024;      // two CTAs per SM
 
 struct Control {
-  unsigned long long full[kMaxSlots], empty[kMaxSlots], done, drained;
+  unsigned long long full[kMaxSlots], empty[kMaxSlots], done[2], taken[2], drained;
   uint32_t tmem_base;
   int abort_flag, peer_abort;
-  Tile tile;
-  float x_scale[64];
+  alignas(16) float x_scale[4][64];
 };
 
-template <int kTokens>
-__host__ __device__ constexpr int slots_for(bool join) {
-  const size_t n = (kBudget - 1024 - sizeof(Control) - (join ? (size_t)kTokens * kFeatures * 4 : 0)) / (kABytes + kTokens * kRowBytes);
-  return n > kMaxSlots ? kMaxSlots : (int)n;
-}
-template <int kTokens>
-constexpr size_t smem_bytes(bool join) {
-  return 1024 + (size_t)slots_for<kTokens>(join) * (kABytes + kTokens * kRowBytes) + (join ? (size_t)kTokens * kFeatures * 4 : 0) + sizeof(Control);
-}
+// How a launch cuts its work and its shared memory.
+struct Cut {
+  int features, feature_tiles, splits, sub, slots, packed;   // packed: a slot's weights come in one copy, its tokens in another
+  int x_block;                                               // bytes of a block of tokens: of those that there can be, in eights
+  int w_bytes, x_bytes;                                      // of a copy
+  int behind;                                                // bytes that an instruction may read behind the last slot
+  uint32_t idesc;
+};
 
 template <int kTokens, bool kInt, typename TY>
 __global__ void __launch_bounds__(kThreads)
-matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, MatmulArgs a, uint32_t idesc,
-                     int feature_tiles, int splits, int tx_bytes, long long polls) {
-  constexpr int kStage = kABytes + kTokens * kRowBytes;
-  constexpr int kCols = kTokens < 32 ? 32 : kTokens;          // of tensor memory
+matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, MatmulArgs a, Cut cut, long long polls) {
+  constexpr int kCols = 2 * kTokens;                          // of tensor memory: two accumulators
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const int slots = splits > 1 ? slots_for<kTokens>(true) : slots_for<kTokens>(false);
-  uint32_t* parts = reinterpret_cast<uint32_t*>(smem + (size_t)slots * kStage);      // [CTA][token of mine][feature]
-  Control* ctl = reinterpret_cast<Control*>(reinterpret_cast<unsigned char*>(parts) + (splits > 1 ? (size_t)kTokens * kFeatures * 4 : 0));
+  const int splits = cut.splits, sub = cut.sub, slots = cut.slots;
+  const int w_block = cut.features * kRowBytes, slot_bytes = sub * (w_block + cut.x_block);
+  // slots, then room for what an instruction reads behind the last one, then the other CTAs' sums [CTA][token of mine][feature]
+  uint32_t* parts = reinterpret_cast<uint32_t*>(smem + slots * slot_bytes + cut.behind);
+  Control* ctl = reinterpret_cast<Control*>(reinterpret_cast<unsigned char*>(parts) + (splits > 1 ? kTokens * cut.features * 4 : 0));
+  int* plan = reinterpret_cast<int*>(ctl + 1);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = splits > 1 ? (int)(blockIdx.x % (unsigned)splits) : 0;
-  const unsigned item = blockIdx.x / (unsigned)splits;
+  const uint32_t item = blockIdx.x / (uint32_t)splits, items = gridDim.x / (uint32_t)splits;
+  const int es = kInt ? 1 : 2;
+  const int blocks = (int)((a.K * es + kRowBytes - 1) / kRowBytes);
+  const int steps = (blocks + sub - 1) / sub;                // slots' worth of K; this CTA's:
+  const int s0 = (int)((int64_t)steps * rank / splits), s1 = (int)((int64_t)steps * (rank + 1) / splits);
   pdl_launch_dependents();
+  auto load_weights = [&](int step, int slot, int n0, int expert) {
+    const uint32_t dst = smem_u32(smem + slot * slot_bytes), bar = smem_u32(&ctl->full[slot]);
+    if (cut.packed) {
+      tma_load_4d(dst, &map_w, 0, n0, step * sub, expert, bar);
+    } else {
+      for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_load_4d(dst + b * w_block, &map_w, (step * sub + b) * kRowBytes, n0, 0, expert, bar);
+    }
+  };
+  auto copies = [&](int step) { return cut.packed ? 1 : min(sub, blocks - step * sub); };
+  int ahead = 0;                                             // slots whose weights are on their way before the stream's order is waited for
   if (threadIdx.x == 0) {
     prefetch_map(&map_w);
     prefetch_map(&map_x);
     for (int s = 0; s < slots; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-    mbar_init(smem_u32(&ctl->done), 1);
+    for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->done[b]), 1); mbar_init(smem_u32(&ctl->taken[b]), 4); }
     mbar_init(smem_u32(&ctl->drained), 1);
     ctl->abort_flag = polls == 0;
     ctl->peer_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (!a.offsets && polls != 0) {
+      // one expert: the feature tile of the first tile of this CTA
+      const int row_tiles = (int)((a.R + kTokens - 1) / kTokens), first_n0 = (int)(item / (uint32_t)row_tiles) * cut.features;
+      ahead = min(slots, s1 - s0);
+      for (int i = 0; i < ahead; ++i) {
+        mbar_expect_tx(smem_u32(&ctl->full[i]), (uint32_t)(cut.w_bytes * copies(s0 + i)));
+        load_weights(s0 + i, i, first_n0, 0);
+      }
+    }
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  __syncwarp();
   pdl_wait();
-  const int n0 = (int)(item % (unsigned)feature_tiles) * kFeatures;
-  if (warp == 2) {
-    const Tile t = find_tile(a, (int)(item / (unsigned)feature_tiles), kTokens);
-    if (lane == 0) ctl->tile = t;
-  }
+  if (warp == 2) make_plan(a, plan, kTokens);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (splits > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // this CTA is there: its memory may be written
-  const Tile tile = ctl->tile;
   const uint32_t tmem_base = ctl->tmem_base;
-  const int es = kInt ? 1 : 2;
-  const int blocks = (int)((a.K * es + kRowBytes - 1) / kRowBytes);
-  const int kb0 = (int)((int64_t)blocks * rank / splits), kb1 = (int)((int64_t)blocks * (rank + 1) / splits);
-
-  if (tile.rows == 0 || *abort_flag) {
-    // no such tile (the whole cluster sees the same), or no waits allowed
-  } else if (warp == 0) {
-    int r[4] = {0, 0, 0, 0};
-    if (a.rows && lane < kTokens / 4) {
+  const Walk from(plan, a.experts, cut.feature_tiles, item, items);
+  const int quarter = warp & 3, f = quarter * 32 + lane;
+  const bool writer = warp >= 2 && quarter * 32 < cut.features;
+  TY* y = reinterpret_cast<TY*>(a.y);
+  const TY* res = reinterpret_cast<const TY*>(a.residual);
+  // What a warp needs of a tile before its sums are there.
+  auto take_scales = [&](const Walk& w) {
+    __syncwarp();
+    for (int j = lane; j < kTokens; j += 32) ctl->x_scale[quarter][j] = a.x_scale && j < w.rows ? a.x_scale[source_row(a, w.row0 + j)] : 1.f;
+    __syncwarp();
+  };
+  // Sums of up to kN rows on their way out, without a branch between them: their loads and conversions overlap.
+  auto put = [&](const Feature<TY>& feature, int64_t row, int n, int rows, const auto& sums, const float* x_scale, bool good) {
+    constexpr int kN = sizeof(sums) / sizeof(sums[0]);
+    Raw<TY> add[kN];
+    if (res) {
+      const TY* r = res + row * a.ld_res + n;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = source_row(a, tile.row0 + min(4 * lane + i, tile.rows - 1));
+      for (int j = 0; j < kN; ++j) add[j] = load_raw(r + min(j, rows - 1) * a.ld_res);
     }
-    int slot = 0;
+    float v[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = good ? feature.finish(a, sum_value<kInt>(sums[j]), x_scale[j]) : __uint_as_float(0x7FC00000u);
+    if (res) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] += raw_value<TY>(add[j]);
+    }
+    TY* out = y + row * a.ld_y + n;
+    if (rows >= kN) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) out[j * a.ld_y] = out_cast<TY>(v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+        if (j < rows) out[j * a.ld_y] = out_cast<TY>(v[j]);
+    }
+  };
+
+  if (warp == 0) {
+    int slot = 0, issued = 0;
     uint32_t phase = 0;
-    int kb = kb0;
-    for (; kb < kb1; ++kb) {
-      bool ok = true;
-      if (lane == 0) {
-        ok = wait_for(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
-        if (ok) mbar_arrive_expect_tx(smem_u32(&ctl->full[slot]), (uint32_t)tx_bytes);
+    bool ok = polls != 0;
+    for (Walk w = from; ok && w.valid(); w.next()) {
+      w.locate(kTokens);
+      const int n0 = w.f * cut.features;
+      int r[4] = {0, 0, 0, 0};
+      if (a.rows && lane < kTokens / 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = source_row(a, w.row0 + min(4 * lane + i, w.rows - 1));
       }
-      if (!__shfl_sync(0xFFFFFFFFu, ok, 0)) break;
-      const uint32_t dst = smem_u32(smem + (size_t)slot * kStage), bar = smem_u32(&ctl->full[slot]);
-      if (lane == 0) tma_load_3d(dst, &map_w, kb * kRowBytes, n0, tile.expert, bar);
-      if (a.rows) {
-        if (lane < kTokens / 4) tma_gather4(dst + kABytes + lane * 4 * kRowBytes, &map_x, kb * kRowBytes, r, bar);
-      } else if (lane == 0) {
-        tma_load_2d(dst + kABytes, &map_x, kb * kRowBytes, tile.row0, bar);
+      for (int step = s0; step < s1; ++step) {
+        const uint32_t bar = smem_u32(&ctl->full[slot]);
+        if (lane == 0) {
+          ok = wait_for(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+          if (ok) {
+            const bool asked = issued < ahead;
+            const int x_bytes = a.rows ? cut.x_block * min(sub, blocks - step * sub) : cut.x_bytes * copies(step);
+            mbar_arrive_expect_tx(bar, (uint32_t)(x_bytes + (asked ? 0 : cut.w_bytes * copies(step))));
+            if (!asked) load_weights(step, slot, n0, w.e);
+          }
+        }
+        if (a.rows) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+        if (!ok || (!a.rows && lane != 0)) break;
+        const uint32_t dst = smem_u32(smem + slot * slot_bytes) + (uint32_t)(sub * w_block);
+        if (!a.rows && cut.packed) {
+          tma_load_3d(dst, &map_x, 0, w.row0, step * sub, bar);
+        } else {
+          for (int b = 0; b < sub && step * sub + b < blocks; ++b) {
+            const int c = (step * sub + b) * kRowBytes;
+            if (!a.rows) tma_load_3d(dst + b * cut.x_block, &map_x, c, w.row0, 0, bar);
+            else if (lane < kTokens / 4) tma_gather4(dst + b * cut.x_block + lane * 4 * kRowBytes, &map_x, c, r, bar);
+          }
+        }
+        ++issued;
+        if (++slot == slots) { slot = 0; phase ^= 1u; }
       }
-      if (++slot == slots) { slot = 0; phase ^= 1u; }
     }
-    // Copies that nobody waits for any more must not land in a CTA that is gone.
-    if (*abort_flag && lane == 0) {
-      for (int i = max(kb0, kb - slots); i < kb; ++i)
-        wait_quiet(smem_u32(&ctl->full[(i - kb0) % slots]), (uint32_t)((i - kb0) / slots & 1));
+    // Copies that nobody waits for any more must not land in a CTA that is gone, nor those asked for ahead.
+    if (lane == 0 && *abort_flag) {
+      for (int i = max(0, issued - slots); i < issued; ++i) wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
+      for (int i = issued; i < ahead; ++i) {
+        mbar_arrive(smem_u32(&ctl->full[i]));
+        wait_quiet(smem_u32(&ctl->full[i]), 0);
+      }
     }
+    __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
       int slot = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!(ok = wait_for(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
+      uint32_t phase = 0, pass = 0;
+      bool ok = polls != 0;
+      for (Walk w = from; ok && w.valid(); w.next(), ++pass) {
+        const uint32_t buf = pass & 1u, d = tmem_base + buf * (uint32_t)kTokens;
+        if (!(ok = wait_for(smem_u32(&ctl->taken[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
         tc_fence_after();
-        const uint32_t at = smem_u32(smem + (size_t)slot * kStage);
-        const uint64_t adesc = smem_desc_sw128(at), bdesc = smem_desc_sw128(at + kABytes);
+        for (int step = s0; step < s1; ++step) {
+          if (!(ok = wait_for(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
+          tc_fence_after();
+          const uint32_t at = smem_u32(smem + slot * slot_bytes);
+          for (int b = 0; b < sub && step * sub + b < blocks; ++b) {
+            const uint64_t adesc = smem_desc_sw128(at + (uint32_t)(b * w_block)), bdesc = smem_desc_sw128(at + (uint32_t)(sub * w_block + b * cut.x_block));
 #pragma unroll
-        for (int j = 0; j < kRowBytes / 32; ++j)
-          mma<kInt, 1>(tmem_base, adesc + (uint64_t)(2 * j), bdesc + (uint64_t)(2 * j), idesc, kb > kb0 || j > 0);
-        mma_commit(smem_u32(&ctl->empty[slot]));
-        if (++slot == slots) { slot = 0; phase ^= 1u; }
+            for (int j = 0; j < kRowBytes / 32; ++j)
+              mma<kInt, 1>(d, adesc + (uint64_t)(2 * j), bdesc + (uint64_t)(2 * j), cut.idesc, step > s0 || b > 0 || j > 0);
+          }
+          mma_commit(smem_u32(&ctl->empty[slot]));
+          if (++slot == slots) { slot = 0; phase ^= 1u; }
+        }
+        if (ok) mma_commit(smem_u32(&ctl->done[buf]));
       }
       // The products are over before this CTA gives its memory back, whoever gave up waiting for them.
-      mma_commit(smem_u32(ok ? &ctl->done : &ctl->drained));
-      wait_quiet(smem_u32(ok ? &ctl->done : &ctl->drained), 0);
+      mma_commit(smem_u32(&ctl->drained));
+      wait_quiet(smem_u32(&ctl->drained), 0);
     }
     __syncwarp();
-  } else {
-    const int e = threadIdx.x - 64;                           // 0..127
-    if (e < kTokens) ctl->x_scale[e] = a.x_scale && e < tile.rows ? a.x_scale[source_row(a, tile.row0 + e)] : 1.f;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+  } else if (splits == 1) {
+    bool ok = polls != 0;
+    uint32_t pass = 0;
+    for (Walk w = from; w.valid(); w.next(), ++pass) {
+      w.locate(kTokens);
+      const uint32_t buf = pass & 1u;
+      const int n = w.f * cut.features + f;
+      const Feature<TY> feature(a, w.e, writer && f < cut.features ? n : (int)a.N);
+      take_scales(w);
+      if (ok) {
+        if (lane == 0) ok = wait_for(smem_u32(&ctl->done[buf]), (pass >> 1) & 1u, abort_flag, polls);
+        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+      }
+      tc_fence_after();
+      if (writer) {
+        const uint32_t taddr = tmem_base + buf * (uint32_t)kTokens + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+        for (int c = 0; c < kTokens && c < w.rows; c += 16) {
+          uint32_t r[16];
+          tmem_ld16(taddr + (uint32_t)c, r);
+          if (feature.on) put(feature, w.row0 + c, n, w.rows - c, r, ctl->x_scale[quarter] + c, ok);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->taken[buf]));
+    }
   }
 
-  if (splits > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  const int quarter = warp & 3, f = quarter * 32 + lane, n = n0 + f;
-  const bool writer = warp >= 2 && tile.rows > 0;
-  TY* y = reinterpret_cast<TY*>(a.y);
-  const TY* res = reinterpret_cast<const TY*>(a.residual);
-  auto put = [&](const Feature<TY>& feature, int j, float sum) {
-    const int64_t row = tile.row0 + j;
-    float v = feature.finish(a, sum, ctl->x_scale[j]);
-    if (res) v += in_cast(res[row * a.ld_res + n]);
-    y[row * a.ld_y + n] = out_cast<TY>(v);
-  };
-  if (writer) {
-    bool ok = !*abort_flag;
-    if (ok) {
-      if (lane == 0) ok = wait_for(smem_u32(&ctl->done), 0, abort_flag, polls);
-      ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-    }
-    tc_fence_after();
-    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    if (splits == 1) {
-      const Feature<TY> feature(a, tile.expert, n);
+  if (splits > 1) {
+    // One tile for the cluster, if any; every thread of it takes part in its barriers.
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    const int shift = __ffs(kTokens / splits) - 1, each = 1 << shift;      // tokens that a CTA finishes
+    Walk w = from;
+    const bool mine = writer && w.valid();
+    if (w.valid()) w.locate(kTokens);
+    const int n = w.f * cut.features + f;
+    const Feature<TY> feature(a, w.e, mine && f < cut.features ? n : (int)a.N);
+    if (mine) {
+      take_scales(w);
+      bool ok = polls != 0;
+      if (ok) {
+        if (lane == 0) ok = wait_for(smem_u32(&ctl->done[0]), 0, abort_flag, polls);
+        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+      }
+      tc_fence_after();
 #pragma unroll 1
-      for (int c = 0; c < kTokens && c < tile.rows; c += 16) {
+      for (int c = 0; c < kTokens && c < w.rows; c += 16) {
         uint32_t r[16];
-        tmem_ld16(taddr + (uint32_t)c, r);
-        if (feature.on) {
+        tmem_ld16(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, r);
+        if (f < cut.features) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c + j < tile.rows) put(feature, c + j, ok ? sum_value<kInt>(r[j]) : __uint_as_float(0x7FC00000u));
-        }
-      }
-    } else {
-      const int each = kTokens / splits;                      // tokens that a CTA finishes
-#pragma unroll 1
-      for (int c = 0; c < kTokens && c < tile.rows; c += 16) {
-        uint32_t r[16];
-        tmem_ld16(taddr + (uint32_t)c, r);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int token = c + j, owner = token / each;
-          uint32_t dst;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst)
-                       : "r"(smem_u32(parts + (rank * each + token - owner * each) * kFeatures + f)), "r"(owner));
-          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(dst), "r"(r[j]) : "memory");
-        }
-      }
-      if (!ok && lane == 0) {
-        for (int o = 0; o < splits; ++o) {
-          uint32_t dst;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(smem_u32(&ctl->peer_abort)), "r"(o));
-          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(dst), "r"(1) : "memory");
-        }
-      }
-    }
-  }
-  if (splits > 1 && tile.rows > 0) {
-    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-    if (writer) {
-      const int each = kTokens / splits;
-      const bool bad = *reinterpret_cast<volatile int*>(&ctl->peer_abort) != 0;
-      const Feature<TY> feature(a, tile.expert, n);
-      if (feature.on) {
-        for (int j = 0; j < each && rank * each + j < tile.rows; ++j) {
-          uint32_t sum = parts[j * kFeatures + f];
-          for (int s = 1; s < splits; ++s) {
-            const uint32_t v = parts[(s * each + j) * kFeatures + f];
-            sum = kInt ? sum + v : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v));
+          for (int j = 0; j < 16; ++j) {
+            const int token = c + j, owner = token >> shift;
+            if (token < w.rows) st_cluster(map_to_rank(smem_u32(parts + ((rank << shift) + (token & (each - 1))) * cut.features + f), (uint32_t)owner), r[j]);
           }
-          put(feature, rank * each + j, bad ? __uint_as_float(0x7FC00000u) : sum_value<kInt>(sum));
         }
+      }
+      if (!ok && lane == 0)
+        for (int o = 0; o < splits; ++o) st_cluster(map_to_rank(smem_u32(&ctl->peer_abort), (uint32_t)o), 1u);
+    }
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+    if (mine && feature.on) {
+      const bool bad = *reinterpret_cast<volatile int*>(&ctl->peer_abort) != 0;
+      const int t0 = rank << shift, here = min(each, w.rows - t0);
+#pragma unroll 1
+      for (int j = 0; j < here; j += 4) {
+        uint32_t sums[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = min(j + i, here - 1);
+          sums[i] = parts[at * cut.features + f];
+#pragma unroll
+          for (int s = 1; s < 8; ++s) {
+            if (s < splits) {
+              const uint32_t v = parts[((s << shift) + at) * cut.features + f];
+              sums[i] = kInt ? sums[i] + v : __float_as_uint(__uint_as_float(sums[i]) + __uint_as_float(v));
+            }
+          }
+        }
+        put(feature, w.row0 + t0 + j, n, here - j, sums, ctl->x_scale[quarter] + t0 + j, !bad);
       }
     }
   }
@@ -224,48 +308,71 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 }
 
 template <int kTokens, bool kInt, typename TY>
-cudaError_t launch(const MatmulArgs& a, int splits, cudaStream_t s) {
+cudaError_t launch(const MatmulArgs& a, int features, int splits, int per_sm, cudaStream_t s) {
   const int es = kInt ? 1 : 2;
-  const int64_t feature_tiles = (a.N + kFeatures - 1) / kFeatures;
+  const int64_t blocks = (a.K * es + kRowBytes - 1) / kRowBytes;
+  const int64_t feature_tiles = (a.N + features - 1) / features;
   int64_t token_tiles = (a.R + kTokens - 1) / kTokens;
   if (a.offsets) token_tiles = a.R / kTokens + (a.experts < a.R ? a.experts : a.R);    // at most: one that is not full per expert
-  const int64_t grid = token_tiles * feature_tiles * splits;
-  if (grid > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  if (token_tiles * feature_tiles * splits > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  // Slots of up to four blocks of K, as many as leave room for three slots at least.
+  Cut cut;
+  const int box_t = a.rows || a.x_rows > kTokens - 8 ? kTokens : ((int)a.x_rows + 7) / 8 * 8;
+  const int block = (features + box_t) * kRowBytes;
+  cut.x_block = box_t * kRowBytes;
+  cut.behind = (kLanes - features > kTokens - box_t ? kLanes - features : kTokens - box_t) * kRowBytes;
+  const int budget = (227 - per_sm) * 1024 / per_sm;          // an SM's shared memory, less what the system keeps per CTA
+  const int fixed = 1024 + (int)sizeof(Control) + (int)plan_bytes(a.experts) + cut.behind + (splits > 1 ? kTokens * features * 4 : 0);
+  cut.sub = 4;
+  while (cut.sub > 1 && (budget - fixed) / (cut.sub * block) < 3) cut.sub /= 2;
+  cut.slots = (budget - fixed) / (cut.sub * block);
+  if (cut.slots > kMaxSlots) cut.slots = kMaxSlots;
+  cut.features = features;
+  cut.feature_tiles = (int)feature_tiles;
+  while (splits > 1 && (blocks + cut.sub - 1) / cut.sub < splits) splits /= 2;       // no CTA without a slot's worth of K
+  cut.splits = splits;
+  cut.packed = a.K * es % kRowBytes == 0;
+  cut.w_bytes = features * kRowBytes * (cut.packed ? cut.sub : 1);
+  cut.x_bytes = box_t * kRowBytes * (cut.packed ? cut.sub : 1);
+  cut.idesc = instr_desc(a.operand, kLanes, kTokens);
   CUtensorMap map_w, map_x;
-  const int box_n = a.N < kFeatures ? (int)a.N : kFeatures, box_t = a.rows ? 1 : a.x_rows < kTokens ? (int)a.x_rows : kTokens;
-  cudaError_t e = encode_weights(&map_w, a, box_n);
-  if (e == cudaSuccess) e = encode_rows(&map_x, a.x, a.K * es, a.x_rows, a.ld_x * es, box_t);
+  cudaError_t e = encode_blocks(&map_w, a.w, a.K * es, a.N, a.ld_w * es, a.experts, a.expert_stride * es, features, cut.packed ? cut.sub : 0);
   if (e != cudaSuccess) return e;
-  const int tx = (box_n + (a.rows ? kTokens : box_t)) * kRowBytes;
+  if (a.rows) e = encode_rows(&map_x, a.x, a.K * es, a.x_rows, a.ld_x * es, 1);
+  else e = encode_blocks(&map_x, a.x, a.K * es, a.x_rows, a.ld_x * es, 0, 0, box_t, cut.packed ? cut.sub : 0);
+  if (e != cudaSuccess) return e;
   const auto kern = matmul_narrow_kernel<kTokens, kInt, TY>;
-  const size_t smem = smem_bytes<kTokens>(splits > 1);
   static std::atomic<uint64_t> ready{0};                     // devices on which the kernel's shared memory limit is set
   int dev = 0;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
   if (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
-    const size_t most = smem_bytes<kTokens>(false) > smem_bytes<kTokens>(true) ? smem_bytes<kTokens>(false) : smem_bytes<kTokens>(true);
-    if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024)) != cudaSuccess) return e;
     if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_acq_rel);
   }
+  int sms = 0;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+  int64_t clusters = token_tiles * feature_tiles;
+  if (splits == 1 && clusters > (int64_t)sms * per_sm) clusters = (int64_t)sms * per_sm;
+  const size_t smem = (size_t)fixed + (size_t)cut.slots * cut.sub * block;
   const long long polls = g_debug_wait_polls.load(std::memory_order_relaxed);
-  return launch_pdl_clusters(kern, dim3((unsigned)grid), splits > 1 ? (unsigned)splits : 0u, kThreads, smem, s, map_w, map_x, a,
-                             instr_desc(a.operand, kFeatures, kTokens), (int)feature_tiles, splits, tx, polls);
+  return launch_pdl_clusters(kern, dim3((unsigned)(clusters * splits)), splits > 1 ? (unsigned)splits : 0u, kThreads, smem, s, map_w, map_x, a, cut, polls);
 }
 
 template <int kTokens>
-cudaError_t launch_type(const MatmulArgs& a, int splits, cudaStream_t s) {
+cudaError_t launch_type(const MatmulArgs& a, int features, int splits, int per_sm, cudaStream_t s) {
   const bool whole = a.operand == BL_I8;
   switch (a.yt) {
-    case BL_F32: return whole ? launch<kTokens, true, float>(a, splits, s) : launch<kTokens, false, float>(a, splits, s);
-    case BL_F16: return whole ? launch<kTokens, true, __half>(a, splits, s) : launch<kTokens, false, __half>(a, splits, s);
-    default: return whole ? launch<kTokens, true, __nv_bfloat16>(a, splits, s) : launch<kTokens, false, __nv_bfloat16>(a, splits, s);
+    case BL_F32: return whole ? launch<kTokens, true, float>(a, features, splits, per_sm, s) : launch<kTokens, false, float>(a, features, splits, per_sm, s);
+    case BL_F16: return whole ? launch<kTokens, true, __half>(a, features, splits, per_sm, s) : launch<kTokens, false, __half>(a, features, splits, per_sm, s);
+    default: return whole ? launch<kTokens, true, __nv_bfloat16>(a, features, splits, per_sm, s) : launch<kTokens, false, __nv_bfloat16>(a, features, splits, per_sm, s);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int splits, cudaStream_t s) {
-  return tokens == 16 ? launch_type<16>(a, splits, s) : tokens == 32 ? launch_type<32>(a, splits, s) : launch_type<64>(a, splits, s);
+cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int features, int splits, int per_sm, cudaStream_t s) {
+  return tokens == 16 ? launch_type<16>(a, features, splits, per_sm, s) : tokens == 32 ? launch_type<32>(a, features, splits, per_sm, s)
+                                                                               : launch_type<64>(a, features, splits, per_sm, s);
 }
 
 }  // namespace bl

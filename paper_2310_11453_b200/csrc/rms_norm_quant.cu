@@ -99,7 +99,9 @@ struct RowThreads {
 template <typename T, int kChunks, bool kJoin>
 __global__ void __launch_bounds__(1024) rms_norm_quant_kernel(NormQuantArgs a, int row_threads) {
   __shared__ float2 part[2 * kMaxWarps];
-  pdl_launch_dependents();
+  // Weights are quantised without the norm, and bitlinear_matmul_i8 reads weights ahead of the stream's order: what follows then starts
+  // when these are written.
+  if (a.eps >= 0.f) pdl_launch_dependents();
   const int in_block = threadIdx.x / row_threads, i = threadIdx.x - in_block * row_threads;
   RowThreads rt;
   rt.warps = row_threads / 32; rt.warp = i / 32; rt.lane = i & 31; rt.id = in_block + 1; rt.turn = 0;
