@@ -678,7 +678,7 @@ bl_status bitlinear_rms_norm_quant(const void* x, bl_dtype dt, int64_t x_rows, i
     return BL_ERR_ALIGN;
   for (const auto& o : {std::make_pair((const void*)h, ld_h), std::make_pair((const void*)y, ld_y)})
     if (o.first && ((o.first == residual && o.second != ld_res) || (o.first == x && (rows || o.second != ld_x)))) return BL_ERR_SHAPE;
-  NormQuantArgs a{x, dt, x_rows, T, K, ld_x, rows, row_weights, top_k, residual, ld_res, weight, eps, h, ld_h, y, ld_y, x_q, ld_q, scale};
+  NormQuantArgs a{x, dt, x_rows, T, K, ld_x, rows, row_weights, top_k, residual, ld_res, weight, eps, h, ld_h, y, ld_y, x_q, ld_q, scale, (float)(1.0 / (double)K)};
   return launch_rms_norm_quant(a, (cudaStream_t)stream) == cudaSuccess ? BL_OK : BL_ERR_CUDA;
 }
 

@@ -270,7 +270,7 @@ cudaError_t launch_attention_kv4(const Kv4AttnArgs& a, cudaStream_t s);
 struct NormQuantArgs {
   const void* x; bl_dtype dt; int64_t x_rows, T, K, ld_x; const int32_t* rows; const float* row_weights; int top_k;
   const void* residual; int64_t ld_res; const void* weight; float eps;
-  void* h; int64_t ld_h; void* y; int64_t ld_y; int8_t* x_q; int64_t ld_q; float* scale;
+  void* h; int64_t ld_h; void* y; int64_t ld_y; int8_t* x_q; int64_t ld_q; float* scale; float inv_k;
 };
 cudaError_t launch_rms_norm_quant(const NormQuantArgs& a, cudaStream_t s);
 

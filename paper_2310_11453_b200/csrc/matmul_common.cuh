@@ -17,30 +17,6 @@ using namespace tc;
 constexpr int kRowBytes = 128;             // bytes of K per stage and row: one swizzle atom
 constexpr int kMaxExperts = 1024;
 
-// A wait with a limit (a number of polls, or below 0 two seconds).  The clock is only read once a wait is long: reading it takes longer than most
-// waits last.
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long polls) {
-  unsigned long long t0 = 0;
-  for (long long it = 0; polls < 0 || it < polls; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 255) == 255) {
-      if (*abort_flag) return false;
-      const unsigned long long now = global_ns();
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > kWaitNs) break;
-    }
-  }
-  *abort_flag = 1;
-  return false;
-}
-
-// Waits for something that is sure to come (its own copies and products), whether or not others gave up; bounded all the same.
-__device__ __forceinline__ void wait_quiet(uint32_t bar, uint32_t parity) {
-  const unsigned long long t0 = global_ns();
-  while (!mbar_try_wait(bar, parity))
-    if (global_ns() - t0 > kWaitNs) return;
-}
-
 // Instruction descriptor: both operands K-major; s8 x s8 -> s32, or fp16 / bf16 -> fp32.
 __host__ __device__ constexpr uint32_t instr_desc(int operand, int m, int n) {
   return (operand == BL_I8 ? (2u << 4) | (1u << 7) | (1u << 10)

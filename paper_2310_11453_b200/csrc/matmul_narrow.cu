@@ -153,7 +153,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       for (int step = s0; step < s1; ++step) {
         const uint32_t bar = smem_u32(&ctl->full[slot]);
         if (lane == 0) {
-          ok = wait_for(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+          ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
           if (ok) {
             const bool asked = issued < ahead;
             const int x_bytes = a.rows ? cut.x_block * min(sub, blocks - step * sub) : cut.x_bytes * copies(step);
@@ -179,10 +179,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     }
     // Copies that nobody waits for any more must not land in a CTA that is gone, nor those asked for ahead.
     if (lane == 0 && *abort_flag) {
-      for (int i = max(0, issued - slots); i < issued; ++i) wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
+      for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
       for (int i = issued; i < ahead; ++i) {
         mbar_arrive(smem_u32(&ctl->full[i]));
-        wait_quiet(smem_u32(&ctl->full[i]), 0);
+        mbar_wait_quiet(smem_u32(&ctl->full[i]), 0);
       }
     }
     __syncwarp();
@@ -193,10 +193,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       bool ok = polls != 0;
       for (Walk w = from; ok && w.valid(); w.next(), ++pass) {
         const uint32_t buf = pass & 1u, d = tmem_base + buf * (uint32_t)kTokens;
-        if (!(ok = wait_for(smem_u32(&ctl->taken[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
+        if (!(ok = mbar_wait_polls(smem_u32(&ctl->taken[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
         tc_fence_after();
         for (int step = s0; step < s1; ++step) {
-          if (!(ok = wait_for(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
+          if (!(ok = mbar_wait_polls(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem + slot * slot_bytes);
           for (int b = 0; b < sub && step * sub + b < blocks; ++b) {
@@ -212,7 +212,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       }
       // The products are over before this CTA gives its memory back, whoever gave up waiting for them.
       mma_commit(smem_u32(&ctl->drained));
-      wait_quiet(smem_u32(&ctl->drained), 0);
+      mbar_wait_quiet(smem_u32(&ctl->drained), 0);
     }
     __syncwarp();
   } else if (splits == 1) {
@@ -225,7 +225,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       const Feature<TY> feature(a, w.e, writer && f < cut.features ? n : (int)a.N);
       take_scales(w);
       if (ok) {
-        if (lane == 0) ok = wait_for(smem_u32(&ctl->done[buf]), (pass >> 1) & 1u, abort_flag, polls);
+        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->done[buf]), (pass >> 1) & 1u, abort_flag, polls);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
       }
       tc_fence_after();
@@ -257,7 +257,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       take_scales(w);
       bool ok = polls != 0;
       if (ok) {
-        if (lane == 0) ok = wait_for(smem_u32(&ctl->done[0]), 0, abort_flag, polls);
+        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->done[0]), 0, abort_flag, polls);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
       }
       tc_fence_after();

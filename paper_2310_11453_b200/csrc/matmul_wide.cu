@@ -94,7 +94,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       for (int kb = 0; kb < blocks; kb += kSub) {
         const int n = min(kSub, blocks - kb);
         const uint32_t bar = full0 + 8u * (uint32_t)slot;
-        ok = wait_for(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+        ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
         if (!ok) break;
         mbar_arrive_expect_tx_cluster(bar, (uint32_t)(tx_bytes * n));
         for (int b = 0; b < n; ++b) {
@@ -125,10 +125,10 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const uint32_t buf = pass & 1u, d = tmem_base + buf * (uint32_t)kMostRows;
         w.locate(kUnit);
         const uint32_t desc = idesc | (uint32_t)(padded(w.rows) >> 3) << 17;
-        if (!(ok = wait_for(smem_u32(&ctl->tmem_empty[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
+        if (!(ok = mbar_wait_polls(smem_u32(&ctl->tmem_empty[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
         tc_fence_after();
         for (int kb = 0; kb < blocks; kb += kSub) {
-          if (!(ok = wait_for(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
+          if (!(ok = mbar_wait_polls(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem + (size_t)slot * kSlotBytes);
           const int n = min(kSub, blocks - kb);
@@ -148,7 +148,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       }
       // The products are over before the memory that they use is given back, whoever gave up waiting for them.
       mma_commit_pair(map_to_rank(smem_u32(&ctl->drained), 0));
-      wait_quiet(smem_u32(&ctl->drained), 0);
+      mbar_wait_quiet(smem_u32(&ctl->drained), 0);
     }
     __syncwarp();
   } else if (warp >= 4 + kEpiWarps) {
@@ -172,7 +172,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       }
       for (int kb = 0; kb < blocks; kb += kSub) {
         const int n = min(kSub, blocks - kb);
-        if (lane == 0) ok = wait_for(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
         if (!ok) break;
         for (int b = 0; b < n; ++b) {
@@ -202,7 +202,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       const uint32_t full0 = map_to_rank(smem_u32(&ctl->full[0]), 0);
       for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); ok && w.valid(); w.next()) {
         for (int kb = 0; kb < blocks; kb += kSub) {
-          if (!(ok = wait_for(smem_u32(&ctl->gathered[slot]), phase, abort_flag, polls))) break;
+          if (!(ok = mbar_wait_polls(smem_u32(&ctl->gathered[slot]), phase, abort_flag, polls))) break;
           fence_proxy_async_smem();
           mbar_arrive_cluster(full0 + 8u * (uint32_t)slot);
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
@@ -231,7 +231,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
           scale_of[i] = a.x_scale && c0 + 64 * i + lane < w.rows ? a.x_scale[source_row(a, w.row0 + c0 + 64 * i + lane)] : 1.f;
       }
       if (ok) {
-        if (lane == 0) ok = wait_for(smem_u32(&ctl->tmem_full[buf]), (pass >> 1) & 1u, abort_flag, polls);
+        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->tmem_full[buf]), (pass >> 1) & 1u, abort_flag, polls);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
       }
       tc_fence_after();

@@ -1,12 +1,14 @@
 // Residual's addition, root-mean-square norm and 8-bit codes with a scale per token, in one pass:
 //   h = residual + x   (or residual + sum_j p_j x[r_j]: the rows that a token's experts left, weighed)
 //   y = w . h / sqrt(mean h^2 + eps),   scale = max |y| / 127,   code = round(y / scale).
-// Bound by memory: x and the residual are read once, h and the codes written once, and a row stays in the registers of
-// its threads in between.  The norm's factor is the same for the whole row and positive, so it cancels in the codes:
+// Bound by memory (and by instructions for the 16-bit types): x and the residual are read once, h and the codes written once, and a
+// row stays in the registers of its threads in between.  The norm's factor is the same for the whole row and positive, so it cancels in the codes:
 //   code = round(h w . 127 / max |h w|),   scale = max |h w| / (127 sqrt(mean h^2 + eps)),
 // and one reduction that carries the sum of squares and the largest |h w| together serves both.
-// Rows whose squares, or whose products with w, leave the range of fp32 go through a second pair of reductions over
-// values scaled by a power of two (exact).
+// Rows whose squares, or whose products with w, leave the range of fp32 go round again, scaled by a power of two (exact); they are
+// loaded anew for it, by the same code, so that this costs the others neither registers nor instructions.
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace bl {
@@ -24,39 +26,66 @@ template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T* p)
   if constexpr (sizeof(T) == 4) v.r2 = *(reinterpret_cast<const uint4*>(p) + 1);
   return v;
 }
-__device__ __forceinline__ void floats(const Eight<float>& e, float (&v)[8]) {
-  v[0] = __uint_as_float(e.r.x); v[1] = __uint_as_float(e.r.y); v[2] = __uint_as_float(e.r.z); v[3] = __uint_as_float(e.r.w);
-  v[4] = __uint_as_float(e.r2.x); v[5] = __uint_as_float(e.r2.y); v[6] = __uint_as_float(e.r2.z); v[7] = __uint_as_float(e.r2.w);
+// Values are held and worked on in pairs (packed fp32 arithmetic).
+__device__ __forceinline__ float2 bits2(uint32_t a, uint32_t b) { return make_float2(__uint_as_float(a), __uint_as_float(b)); }
+__device__ __forceinline__ void floats(const Eight<float>& e, float2 (&v)[4]) {
+  v[0] = bits2(e.r.x, e.r.y); v[1] = bits2(e.r.z, e.r.w); v[2] = bits2(e.r2.x, e.r2.y); v[3] = bits2(e.r2.z, e.r2.w);
 }
-__device__ __forceinline__ void floats(const Eight<__half>& e, float (&v)[8]) {
+__device__ __forceinline__ void floats(const Eight<__half>& e, float2 (&v)[4]) {
   const __half2* h = reinterpret_cast<const __half2*>(&e.r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(h[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+  for (int i = 0; i < 4; ++i) v[i] = __half22float2(h[i]);
 }
-__device__ __forceinline__ void floats(const Eight<__nv_bfloat16>& e, float (&v)[8]) {
+__device__ __forceinline__ void floats(const Eight<__nv_bfloat16>& e, float2 (&v)[4]) {
   const uint32_t w[4] = {e.r.x, e.r.y, e.r.z, e.r.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  for (int i = 0; i < 4; ++i) v[i] = bits2(w[i] << 16, w[i] & 0xFFFF0000u);
 }
-__device__ __forceinline__ void store_eight(float* p, const float (&v)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store_eight(float* p, const float2 (&v)[4]) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
 }
-__device__ __forceinline__ void store_eight(__half* p, const float (&v)[8]) {
+__device__ __forceinline__ void store_eight(__half* p, const float2 (&v)[4]) {
   uint4 r;
   __half2* h = reinterpret_cast<__half2*>(&r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+  for (int i = 0; i < 4; ++i) h[i] = __float22half2_rn(v[i]);
   *reinterpret_cast<uint4*>(p) = r;
 }
-__device__ __forceinline__ void store_eight(__nv_bfloat16* p, const float (&v)[8]) {
+__device__ __forceinline__ void store_eight(__nv_bfloat16* p, const float2 (&v)[4]) {
   uint4 r;
   __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+  for (int i = 0; i < 4; ++i) h[i] = __float22bfloat162_rn(v[i]);
   *reinterpret_cast<uint4*>(p) = r;
 }
-
+__device__ __forceinline__ float2 both(float f) { return make_float2(f, f); }
+template <typename T> __device__ __forceinline__ void add_eight(float2 (&h)[4], const Eight<T>& v) {
+  float2 f[4];
+  floats(v, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = __fadd2_rn(h[e], f[e]);
+}
+template <typename T> __device__ __forceinline__ void add_eight(float2 (&h)[4], const Eight<T>& v, float p) {
+  float2 f[4];
+  floats(v, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = __ffma2_rn(both(p), f[e], h[e]);
+}
+// Eight ones, as stored.
+template <typename T> __device__ __forceinline__ Eight<T> ones() {
+  Eight<T> v;
+  const uint32_t w = sizeof(T) == 4 ? 0x3F800000u : std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
+  v.r = make_uint4(w, w, w, w);
+  if constexpr (sizeof(T) == 4) v.r2 = v.r;
+  return v;
+}
+// The largest of one and the sizes of a pair; a NaN stays.
+__device__ __forceinline__ float max_of(float a, float2 v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(v.x)), "f"(fabsf(v.y)));
+  return r;
+}
 // max that keeps a NaN
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -70,9 +99,14 @@ __device__ __forceinline__ bool finite(float f) { return (__float_as_uint(f) & 0
 struct RowThreads {
   float2* part;              // [2][warps], in turns so that one barrier per reduction is enough
   int warps, warp, lane, id, turn;
+  __device__ RowThreads(float2* parts, int in_block, int i, int row_threads)
+      : part(parts + in_block * 2 * (row_threads / 32)), warps(row_threads / 32), warp(i / 32), lane(i & 31), id(in_block + 1), turn(0) {}
   __device__ void sync() const {
+    // Barriers by number as constants: with one in a register a block is taken to use all sixteen, and four blocks fit on an SM.  A
+    // block has two groups of two warps, or one of any size.
     if (warps == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
+    else if (id == 1) asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+    else asm volatile("bar.sync 2, %0;" ::"r"(warps * 32) : "memory");
   }
   __device__ void reduce(float& sum, float& top) {
 #pragma unroll
@@ -95,177 +129,196 @@ struct RowThreads {
   }
 };
 
-// Thread i of a row holds the chunks of eight values i, i + threads, ..., kChunks of them at most.
+// What the outputs of a chunk are made from.
+struct RowResult { float factor, inv; bool fine; };
+
+template <typename T>
+__device__ __forceinline__ void store_chunk(const NormQuantArgs& a, int t, int at, const float2 (&h)[4], const float2 (&w)[4], const RowResult& r) {
+  float2 p[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = __fmul2_rn(w[e], h[e]);
+  if (a.y) {
+    float2 v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __fmul2_rn(p[e], both(r.factor));
+    store_eight(reinterpret_cast<T*>(a.y) + (int64_t)t * a.ld_y + at * 8, v);
+  }
+  if (a.x_q) {
+    // 1.5 2^23 + v has round(v), half to even, in its low bits; |v| <= 127 (1 + 2^-22) rounds into -127..127
+    uint32_t q[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float2 u = __ffma2_rn(p[2 * e], both(r.inv), both(12582912.f)), v = __ffma2_rn(p[2 * e + 1], both(r.inv), both(12582912.f));
+      q[e] = __byte_perm(__byte_perm(__float_as_uint(u.x), __float_as_uint(u.y), 0x0040),
+                         __byte_perm(__float_as_uint(v.x), __float_as_uint(v.y), 0x0040), 0x5410);
+    }
+    *reinterpret_cast<uint2*>(a.x_q + (int64_t)t * a.ld_q + at * 8) = r.fine ? make_uint2(q[0], q[1]) : make_uint2(0u, 0u);
+  }
+}
+__device__ __forceinline__ RowResult result_of(const NormQuantArgs& a, int t, int i, float top, float factor) {
+  RowResult r;
+  r.fine = finite(top);
+  r.factor = factor;
+  r.inv = r.fine && top > 0.f ? 127.f / top : 0.f;
+  if (a.x_q && i == 0) a.scale[t] = r.fine ? top * factor * (1.f / 127.f) : __uint_as_float(0x7FC00000u);
+  return r;
+}
+
+// Squares or products out of fp32's range, or so small that they lost bits.
+__device__ __forceinline__ bool out_of_range(float f) {          // below 1e-30 (of the positive), infinite or NaN
+  return __float_as_uint(f) - 0x0DA24260u >= 0x7F800000u - 0x0DA24260u;
+}
+
+template <int kChunks> __device__ __forceinline__ void scale_row(float2 (&h)[kChunks][4], float f) {
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[c][e] = __fmul2_rn(h[c][e], both(f));
+}
+
+// The chunks of h (zeros behind the row).
 template <typename T, int kChunks, bool kJoin>
-__global__ void __launch_bounds__(1024) rms_norm_quant_kernel(NormQuantArgs a, int row_threads) {
-  __shared__ float2 part[2 * kMaxWarps];
-  // Weights are quantised without the norm, and bitlinear_matmul_i8 reads weights ahead of the stream's order: what follows then starts
-  // when these are written.
-  if (a.eps >= 0.f) pdl_launch_dependents();
-  const int in_block = threadIdx.x / row_threads, i = threadIdx.x - in_block * row_threads;
-  RowThreads rt;
-  rt.warps = row_threads / 32; rt.warp = i / 32; rt.lane = i & 31; rt.id = in_block + 1; rt.turn = 0;
-  rt.part = part + in_block * 2 * rt.warps;
-  const int64_t t = (int64_t)blockIdx.x * (blockDim.x / row_threads) + in_block;
-  if (t >= a.T) return;                              // whole rows of threads: none waits for another's
-  pdl_wait();
-  const int chunks = (int)(a.K / 8);
-  const bool norm = a.eps >= 0.f;
+__device__ __forceinline__ void fetch(const NormQuantArgs& a, int t, int i, int row_threads, int chunks, float2 (&h)[kChunks][4]) {
   const T* x = reinterpret_cast<const T*>(a.x);
-  const T* res = a.residual ? reinterpret_cast<const T*>(a.residual) + t * a.ld_res : nullptr;
-  const T* weight = norm ? reinterpret_cast<const T*>(a.weight) : nullptr;
-
-  float h[kChunks][8];
-  if constexpr (kJoin) {
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int at = i + c * row_threads;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) h[c][e] = 0.f;
-      if (at < chunks && res) floats(load_eight(res + at * 8), h[c]);
-    }
-    const int32_t* rows = a.rows + t * a.top_k;
-    const float* shares = a.row_weights ? a.row_weights + t * a.top_k : nullptr;
-#pragma unroll 4
-    for (int j = 0; j < a.top_k; ++j) {
-      const int32_t r = rows[j];
-      if (r < 0 || r >= a.x_rows) continue;          // no row: nothing is added
-      const float p = shares ? shares[j] : 1.f;
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        const int at = i + c * row_threads;
-        if (at < chunks) {
-          float v[8];
-          floats(load_eight(x + (int64_t)r * a.ld_x + at * 8), v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[c][e] = fmaf(p, v[e], h[c][e]);
-        }
-      }
-    }
-  } else {
-    Eight<T> xs[kChunks], rs[kChunks];
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int at = i + c * row_threads;
-      if (at < chunks) {
-        xs[c] = load_eight(x + t * a.ld_x + at * 8);
-        if (res) rs[c] = load_eight(res + at * 8);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int at = i + c * row_threads;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) h[c][e] = 0.f;
-      if (at < chunks) {
-        floats(xs[c], h[c]);
-        if (res) {
-          float v[8];
-          floats(rs[c], v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[c][e] += v[e];
-        }
-      }
-    }
-  }
-  if (a.h) {
-    T* out = reinterpret_cast<T*>(a.h) + t * a.ld_h;
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      if (i + c * row_threads < chunks) store_eight(out + (i + c * row_threads) * 8, h[c]);
-  }
-  if (!a.y && !a.x_q) return;
-
-  // The sum of squares and the largest |h w|.  The products are formed again for the outputs: the weights come from L1, and
-  // the registers serve more rows in flight.
-  float sum = 0.f, top = 0.f;
-  auto weights = [&](int at, float (&w)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = 1.f;
-    if (weight) floats(load_eight(weight + at * 8), w);
-  };
-  auto measure = [&]() {
-    sum = 0.f; top = 0.f;
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      const int at = i + c * row_threads;
-      if (at < chunks) {
-        float w[8];
-        weights(at, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sum = fmaf(h[c][e], h[c][e], sum);
-          top = max_nan(top, fabsf(h[c][e] * w[e]));
-        }
-      }
-    }
-    rt.reduce(sum, top);
-  };
-  measure();
-  const float inv_k = 1.f / (float)a.K;
-  float factor = norm ? rsqrtf(fmaf(sum, inv_k, a.eps)) : 1.f;
-  bool divide = false;                               // codes by division rather than by 127 / top
-  // Squares or products out of fp32's range, or so small that they lost bits.
-  if (!finite(top) || top < 1e-30f || (norm && (!finite(sum) || fmaf(sum, inv_k, a.eps) < 1e-30f))) {
-    float most = 0.f, none = 0.f;
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = max_nan(most, fabsf(h[c][e]));
-    rt.reduce(none, most);
-    if (finite(most) && most > 0.f) {
-      // h <- f h, f the power of two that brings the largest into [1, 2), or as near as a factor of 2^100 comes
-      const int up = min(100, 127 - max(1, (int)(__float_as_uint(most) >> 23)));
-      const float f = up >= -126 ? __uint_as_float((uint32_t)(127 + up) << 23) : __uint_as_float(0x00400000u);   // 2^-127 is denormal
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[c][e] *= f;
-      measure();
-      // w h / sqrt(mean h^2 + eps) = w (f h) / sqrt(mean (f h)^2 + f^2 eps); where f^2 eps passes fp32, the mean is nothing beside it
-      const float scaled_eps = a.eps * f * f;
-      factor = !norm ? 1.f / f : finite(scaled_eps) ? rsqrtf(fmaf(sum, inv_k, scaled_eps)) : rsqrtf(a.eps) / f;
-      divide = true;
-    } else if (most == 0.f) {
-      factor = 0.f;                                  // a row of zeros stays one, with eps = 0 too
-    }
-  }
-  const bool fine = finite(top);
-  const float inv = fine && top > 0.f ? 127.f / top : 0.f;
-  if (a.x_q && i == 0) a.scale[t] = fine ? top * factor * (1.f / 127.f) : __uint_as_float(0x7FC00000u);
+  Eight<T> xs[kJoin ? 1 : kChunks];
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     const int at = i + c * row_threads;
-    if (at >= chunks) continue;
-    float w[8];
-    weights(at, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] *= h[c][e];
-    if (a.y) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = w[e] * factor;
-      store_eight(reinterpret_cast<T*>(a.y) + t * a.ld_y + at * 8, v);
+    Eight<T> r{};
+    if constexpr (!kJoin) xs[c] = Eight<T>{};
+    if (at < chunks) {
+      if constexpr (!kJoin) xs[c] = load_eight(x + (int64_t)t * a.ld_x + at * 8);
+      if (a.residual) r = load_eight(reinterpret_cast<const T*>(a.residual) + (int64_t)t * a.ld_res + at * 8);
     }
-    if (a.x_q) {
-      uint32_t q[8];
+    floats(r, h[c]);
+  }
+  if constexpr (!kJoin) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {                  // |w / top| 127 <= 127 (1 + 2^-22): rounds into -127..127
-        const float v = divide ? (top > 0.f ? w[e] / top * 127.f : 0.f) : w[e] * inv;
-        q[e] = fine ? (uint32_t)__float2int_rn(v) : 0u;
+    for (int c = 0; c < kChunks; ++c) add_eight(h[c], xs[c]);
+  } else {
+    // Four rows at a time, all on their way together; one that is not there is a row of zeros with the weight 0.
+    const int32_t* rows = a.rows + (int64_t)t * a.top_k;
+    const float* shares = a.row_weights ? a.row_weights + (int64_t)t * a.top_k : nullptr;
+#pragma unroll 1
+    for (int j0 = 0; j0 < a.top_k; j0 += 4) {
+      int32_t r[4];
+      float p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        r[j] = j0 + j < a.top_k ? rows[j0 + j] : -1;
+        p[j] = shares && j0 + j < a.top_k ? shares[j0 + j] : 1.f;
+        if (r[j] >= a.x_rows) r[j] = -1;
+        if (r[j] < 0) p[j] = 0.f;
       }
-      *reinterpret_cast<uint2*>(a.x_q + t * a.ld_q + at * 8) =
-          make_uint2((q[0] & 255u) | (q[1] & 255u) << 8 | (q[2] & 255u) << 16 | q[3] << 24,
-                     (q[4] & 255u) | (q[5] & 255u) << 8 | (q[6] & 255u) << 16 | q[7] << 24);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const int at = i + c * row_threads;
+        Eight<T> v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[j] = Eight<T>{};
+          if (at < chunks && r[j] >= 0) v[j] = load_eight(x + (int64_t)r[j] * a.ld_x + at * 8);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add_eight(h[c], v[j], p[j]);
+      }
     }
   }
 }
 
-template <typename T, int kChunks>
+// Thread i of a row holds the chunks of eight values i, i + threads, ..., kChunks of them at most.
+template <typename T, int kChunks, int kThreads, bool kJoin>
+__global__ void __launch_bounds__(kThreads, kChunks == 2 ? 2 : 1) rms_norm_quant_kernel(NormQuantArgs a, int row_threads) {
+  __shared__ float2 part[2 * kMaxWarps];
+  // Weights are quantised without the norm, and bitlinear_matmul_i8 reads weights ahead of the stream's order: what follows then starts
+  // when these are written.
+  if (a.eps >= 0.f) pdl_launch_dependents();
+  const int per_block = blockDim.x == row_threads ? 1 : blockDim.x / row_threads;
+  const int in_block = per_block == 1 ? 0 : threadIdx.x / row_threads, i = threadIdx.x - in_block * row_threads;
+  RowThreads rt(part, in_block, i, row_threads);
+  const int t = (int)blockIdx.x * per_block + in_block;
+  if (t >= (int)a.T) return;                              // whole rows of threads: none waits for another's
+  pdl_wait();
+  const int chunks = (int)(a.K / 8);
+  const float inv_k = a.inv_k;
+  const bool norm = a.eps >= 0.f;
+  // Once round for nearly every row.  One that leaves the range: its largest size, then once more scaled by f (twice, with tiny
+  // weights), and once to have the values themselves again.
+  enum { kPlain, kMost, kScaled, kRescaled, kLast };
+  int round = kPlain;
+  float f = 1.f;
+  RowResult result{1.f, 0.f, true};
+  float2 h[kChunks][4];
+  auto weight_of = [&](int c, bool want) {
+    return want && norm && a.weight && i + c * row_threads < chunks ? load_eight(reinterpret_cast<const T*>(a.weight) + (i + c * row_threads) * 8) : ones<T>();
+  };
+#pragma unroll 1
+  for (;;) {
+    Eight<T> weight[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) weight[c] = weight_of(c, round != kMost);
+    fetch<T, kChunks, kJoin>(a, t, i, row_threads, chunks, h);
+    if (round == kLast || (!a.y && !a.x_q)) break;
+    if (f != 1.f) scale_row(h, f);
+    // the sum of squares and the largest |h w|
+    float2 s[2] = {both(0.f), both(0.f)};
+    float m[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      float2 w[4];
+      floats(weight[c], w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e & 1] = __ffma2_rn(h[c][e], h[c][e], s[e & 1]);
+        m[e & 1] = max_of(m[e & 1], __fmul2_rn(h[c][e], w[e]));
+      }
+    }
+    float sum = (s[0].x + s[0].y) + (s[1].x + s[1].y), top = max_nan(m[0], m[1]);
+    rt.reduce(sum, top);
+    if (round == kPlain) {
+      const float mean = fmaf(sum, inv_k, a.eps);
+      result = result_of(a, t, i, top, norm ? rsqrtf(mean) : 1.f);
+      if (!out_of_range(top) && !(norm && out_of_range(mean))) break;
+      round = kMost;
+    } else if (round == kMost) {
+      if (top == 0.f) result.factor = 0.f;             // a row of zeros stays one, with eps = 0 too
+      if (top == 0.f && a.x_q && i == 0 && result.fine) a.scale[t] = 0.f;
+      if (top == 0.f || !finite(top)) { round = kLast; continue; }
+      // f: the power of two that brings the largest into [1, 2), or as near as a factor of 2^100 comes
+      const int up = min(100, 127 - max(1, (int)(__float_as_uint(top) >> 23)));
+      f = up >= -126 ? __uint_as_float((uint32_t)(127 + up) << 23) : __uint_as_float(0x00400000u);   // 2^-127 is denormal
+      round = kScaled;
+    } else {
+      // w h / sqrt(mean h^2 + eps) = w (f h) / sqrt(mean (f h)^2 + f^2 eps); where f^2 eps passes fp32, the mean is nothing beside it
+      const float scaled_eps = a.eps * f * f;
+      result = result_of(a, t, i, top, !norm ? 1.f / f : finite(scaled_eps) ? rsqrtf(fmaf(sum, inv_k, scaled_eps)) : rsqrtf(a.eps) / f);
+      const bool again = round == kScaled && top < 1e-30f && top > 0.f && f < 1.3e8f;      // tiny weights
+      if (again) f *= 1.2676506e30f;                   // 2^100
+      round = again ? kRescaled : kLast;
+    }
+  }
+  if (a.h) {
+    T* out = reinterpret_cast<T*>(a.h) + (int64_t)t * a.ld_h;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      if (i + c * row_threads < chunks) store_eight(out + (i + c * row_threads) * 8, h[c]);
+  }
+  if (f != 1.f) scale_row(h, f);
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int at = i + c * row_threads;
+    if (at >= chunks) continue;
+    float2 w[4];
+    floats(weight_of(c, true), w);                     // again, from L1: registers are worth more
+    store_chunk<T>(a, t, at, h[c], w, result);
+  }
+}
+
+template <typename T, int kChunks, int kThreads>
 cudaError_t launch_chunks(const NormQuantArgs& a, int row_threads, cudaStream_t s) {
   const int per_block = row_threads >= 128 ? 1 : 128 / row_threads;
   const int64_t blocks = (a.T + per_block - 1) / per_block;
-  const auto kern = a.rows ? rms_norm_quant_kernel<T, kChunks, true> : rms_norm_quant_kernel<T, kChunks, false>;
+  const auto kern = a.rows ? rms_norm_quant_kernel<T, kChunks, kThreads, true> : rms_norm_quant_kernel<T, kChunks, kThreads, false>;
   return launch_pdl(kern, (unsigned)blocks, (unsigned)(row_threads * per_block), 0, s, a, row_threads);
 }
 
@@ -273,9 +326,12 @@ template <typename T>
 cudaError_t launch_type(const NormQuantArgs& a, cudaStream_t s) {
   const int chunks = (int)(a.K / 8);
   auto threads = [&](int per) { return ((chunks + per - 1) / per + 31) / 32 * 32; };
-  if (threads(1) <= 256 || (a.T <= 148 && threads(1) <= 1024)) return launch_chunks<T, 1>(a, threads(1), s);
-  if (threads(2) <= 1024) return launch_chunks<T, 2>(a, threads(2), s);
-  return launch_chunks<T, 4>(a, threads(4), s);
+  // Few rows: as many threads as there are chunks (1 x 4096: 1.9 us).  Many: two chunks a thread share what every thread does once
+  // per row (8191 x 4096 bf16: one chunk 72 us, two 45.6, four 48).
+  if (threads(1) <= 64 || (a.T <= 148 && threads(1) <= 1024)) return launch_chunks<T, 1, 1024>(a, threads(1), s);
+  if (threads(2) <= 512) return launch_chunks<T, 2, 512>(a, threads(2), s);
+  if (threads(4) <= 512) return launch_chunks<T, 4, 512>(a, threads(4), s);
+  return launch_chunks<T, 4, 1024>(a, threads(4), s);
 }
 
 }  // namespace

@@ -54,6 +54,28 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *abort_flag = 1;
   return false;
 }
+// The same with a number of polls (below 0: two seconds).  The clock is only read once a wait is long: reading it takes longer than
+// most waits last.
+__device__ __forceinline__ bool mbar_wait_polls(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long polls) {
+  unsigned long long t0 = 0;
+  for (long long it = 0; polls < 0 || it < polls; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 255) == 255) {
+      if (*abort_flag) return false;
+      const unsigned long long now = global_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > kWaitNs) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
+}
+// Waits for something that is sure to come (one's own copies and products), whether or not others gave up; bounded all the same.
+__device__ __forceinline__ void mbar_wait_quiet(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = global_ns();
+  while (!mbar_try_wait(bar, parity))
+    if (global_ns() - t0 > kWaitNs) return;
+}
 __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
