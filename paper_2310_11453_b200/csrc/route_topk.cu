@@ -4,7 +4,8 @@
 //   offsets  first row of each expert in the list of all (token, choice) pairs ordered by expert, then by token
 //   rows     the token of each row of that list;  places: the row of each (token, choice)
 // Latency, not bandwidth: the scores of 8191 tokens over 128 experts are 2 MB.  A warp holds a token's scores as keys
-// whose unsigned order is theirs (lane l has experts l, l + 32, ..), and picks by warp-wide integer maxima.
+// whose unsigned order is theirs (lane l has experts l, l + 32, ..), and picks by warp-wide integer maxima; a 16-bit score and its
+// expert share a key, so that one maximum finds both.  A warp's tokens are loaded before the first is looked at.
 // The order of the list comes without sorting: each block of kRun tokens notes, per expert, the set of its tokens
 // as bits, so a token's rank is a count of lower bits, whatever the order in which warps set them.  With one block that
 // is all; with more, each leaves its counts (a byte per expert) and a second kernel adds up those of the
@@ -16,20 +17,49 @@ namespace bl {
 namespace {
 
 constexpr int kRun = 64;                       // tokens per block; a count fits a byte
-constexpr int kWarps = 16;
+constexpr int kWarps = 32;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxExperts = 512;
 constexpr int kDirect = 512;                   // blocks whose counts the placing kernel adds up itself
 
-// Unsigned order of the keys = order of the values; -0 and 0 are equal, NaN is lowest.
-__device__ __forceinline__ uint32_t key_of(float z) {
-  return z != z ? 0u : enc_ordered(z + 0.f);
+// Unsigned order of the keys = order of the values; -0 and 0 are equal, NaN is lowest.  Nothing is 0, the key of what is taken or was
+// never there.
+__device__ __forceinline__ uint32_t key_of(float z) { return (z != z ? 0u : enc_ordered(z + 0.f)) + 1u; }
+__device__ __forceinline__ float value_of(uint32_t key) { return dec_ordered(key - 1u); }      // of any but NaN
+
+// Key and expert of a score of 16 bits: equal scores in the order of their experts, lowest first.
+template <typename T> __device__ __forceinline__ uint32_t short_key(T v, int e) {
+  const float z = in_cast(v) + 0.f;
+  const uint32_t b = (uint32_t)*reinterpret_cast<const uint16_t*>(&v);
+  const uint32_t order = z != z ? 0u : z == 0.f ? 0x8000u : (b & 0x8000u) ? 0xFFFFu - b : b + 0x8000u;   // +0 is 0x8000, the largest 0xFC00 or less
+  return ((order + 1u) << 16) | (uint32_t)(0xFFFF - e);
 }
+
+// One warp: first[e] = sum of count[0..e-1].
+__device__ __forceinline__ void prefix_sums(int experts, const int* count, int* first) {
+  const int lane = threadIdx.x & 31;
+  int sum = 0;
+  for (int base = 0; base < experts; base += 32) {
+    const int e = base + lane, n = e < experts ? count[e] : 0;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (e < experts) first[e] = sum + upto - n;
+    sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
+  }
+  if (lane == 0) first[experts] = sum;
+}
+
+constexpr int kPerWarp = kRun / kWarps;        // tokens
 
 template <typename T, int kPer>                // kPer scores per lane
 __global__ void __launch_bounds__(kThreads) route_pick_kernel(RouteArgs a) {
   __shared__ unsigned long long members[kMaxExperts];      // tokens of the run that chose the expert
-  __shared__ int first[kMaxExperts + 1];
+  __shared__ int count[kMaxExperts], first[kMaxExperts + 1];
+  constexpr bool kShort = sizeof(T) == 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool alone = gridDim.x == 1;
   pdl_launch_dependents();
@@ -38,57 +68,78 @@ __global__ void __launch_bounds__(kThreads) route_pick_kernel(RouteArgs a) {
   pdl_wait();
   const int64_t t0 = (int64_t)blockIdx.x * kRun;
   const T* logits = reinterpret_cast<const T*>(a.logits);
-  for (int local = warp; local < kRun; local += kWarps) {
+  T raw[kPerWarp][kPer];
+  int32_t position[kPerWarp];
+#pragma unroll
+  for (int n = 0; n < kPerWarp; ++n) {
+    const int64_t t = t0 + warp + n * kWarps;
+    position[n] = a.positions && t < a.T ? a.positions[t] : 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = lane + 32 * i;
+      raw[n][i] = t < a.T && e < a.experts ? logits[t * a.ld + e] : T(-INFINITY);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kPerWarp; ++n) {
+    const int local = warp + n * kWarps;
     const int64_t t = t0 + local;
     if (t >= a.T) break;
-    const bool padding = a.positions && a.positions[t] < 0;
-    float z[kPer];
-    uint32_t key[kPer];
+    const bool padding = position[n] < 0;
+    uint32_t key[kPer], local_top = 0u;
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = lane + 32 * i;
-      z[i] = e < a.experts ? in_cast(logits[t * a.ld + e]) : -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 32 * i;
-      key[i] = e < a.experts ? key_of(z[i]) + 1u : 0u;     // +1: no expert lies under every score (no key is 2^32 - 1)
-      nan |= z[i] != z[i];
+      const float z = in_cast(raw[n][i]);
+      nan |= z != z;
+      if constexpr (kShort) key[i] = e < a.experts ? short_key(raw[n][i], e) : 0u;
+      else key[i] = e < a.experts ? key_of(z) : 0u;
+      local_top = max(local_top, key[i]);
     }
     nan = __any_sync(0xFFFFFFFFu, nan);
     // top_k times: the largest key, and of the experts that have it the lowest
     int mine = -1;                             // lane j keeps choice j
-    float mine_z = -INFINITY, top_z = 0.f;
-    uint32_t local_top = 0u;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) local_top = max(local_top, key[i]);
+    uint32_t mine_key = 0u, top_key = 0u;
     for (int j = 0; j < a.top_k; ++j) {
       const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, local_top);
-      int at = INT32_MAX;
-      if (local_top == best) {
+      int e;
+      if constexpr (kShort) {
+        e = 0xFFFF - (int)(best & 0xFFFFu);
+      } else {
+        int at = INT32_MAX;
+        if (local_top == best) {
 #pragma unroll
-        for (int i = kPer - 1; i >= 0; --i) if (key[i] == best) at = lane + 32 * i;
+          for (int i = kPer - 1; i >= 0; --i) if (key[i] == best) at = lane + 32 * i;
+        }
+        e = __reduce_min_sync(0xFFFFFFFFu, at);
       }
-      const int e = __reduce_min_sync(0xFFFFFFFFu, at);
-      float ez = 0.f;
-      if (at == e) {                           // the owner takes it out
+      if (local_top == best) {                 // it is taken out
         local_top = 0u;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          if (lane + 32 * i == e) { ez = z[i]; key[i] = 0u; }
+          if (lane + 32 * i == e) key[i] = 0u;
           local_top = max(local_top, key[i]);
         }
       }
-      ez = __shfl_sync(0xFFFFFFFFu, ez, e & 31);
-      if (j == 0) top_z = ez;
-      if (lane == j) { mine = e; mine_z = ez; }
+      if (j == 0) top_key = best;
+      if (lane == j) { mine = e; mine_key = best; }
     }
-    float p = lane < a.top_k ? expf(mine_z - top_z) : 0.f, total = p;
+    auto value = [](uint32_t k) {              // of a key; of one that stands for NaN, anything
+      if constexpr (kShort) {
+        const uint32_t o = (k >> 16) - 1u;
+        const uint16_t b = (uint16_t)(o >= 0x8000u ? o - 0x8000u : 0xFFFFu - o);
+        return in_cast(*reinterpret_cast<const T*>(&b));
+      } else {
+        return value_of(k);
+      }
+    };
+    const float top_z = value(top_key);
+    float p = lane < a.top_k ? expf(value(mine_key) - top_z) : 0.f, total = p;
     if (!a.normalise) {
       total = 0.f;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) if (lane + 32 * i < a.experts) total += expf(z[i] - top_z);
+      for (int i = 0; i < kPer; ++i) if (lane + 32 * i < a.experts) total += expf(in_cast(raw[n][i]) - top_z);
     }
     total = warp_sum(total);
     if (lane < a.top_k) {
@@ -106,22 +157,9 @@ __global__ void __launch_bounds__(kThreads) route_pick_kernel(RouteArgs a) {
     return;
   }
   // one block: its own prefix sums
-  if (warp == 0) {
-    int sum = 0;
-    for (int base = 0; base < a.experts; base += 32) {
-      const int e = base + lane;
-      const int n = e < a.experts ? __popcll(members[e]) : 0;
-      int upto = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (e < a.experts) first[e] = sum + upto - n;
-      sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
-    }
-    if (lane == 0) first[a.experts] = sum;
-  }
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) count[e] = __popcll(members[e]);
+  __syncthreads();
+  if (warp == 0) prefix_sums(a.experts, count, first);
   __syncthreads();
   for (int e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = first[e];
   for (int c = threadIdx.x; c < (int)a.T * a.top_k; c += kThreads) {
@@ -168,66 +206,59 @@ template <bool kSummed>
 __global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, int runs) {
   __shared__ int total[kMaxExperts], before[kMaxExperts];
   __shared__ int first[kMaxExperts + 1];
+  __shared__ unsigned long long members[kMaxExperts];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
   for (int e = threadIdx.x; e < a.experts; e += kThreads) { total[e] = 0; before[e] = 0; }
   __syncthreads();
   pdl_wait();
+  // What the end needs is asked for first.
+  const int64_t t0 = (int64_t)blockIdx.x * kRun;
+  const int here = (int)min((int64_t)kRun, a.T - t0) * a.top_k;      // choices of the run, at most two for each thread
+  const int32_t* chosen = a.chosen + t0 * a.top_k;
+  const int e0 = threadIdx.x < here ? chosen[threadIdx.x] : -1, e1 = threadIdx.x + kThreads < here ? chosen[threadIdx.x + kThreads] : -1;
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) members[e] = a.members[(int64_t)blockIdx.x * a.experts + e];
   if (kSummed) {
     for (int e = threadIdx.x; e < a.experts; e += kThreads) {
       total[e] = a.sums[(int64_t)runs * a.experts + e];
       before[e] = a.sums[(int64_t)blockIdx.x * a.experts + e];
     }
   } else {
-    // four experts a thread (the rows of counts are padded to words), the runs shared out over the warps
+    // four experts a thread (the rows of counts are padded to words), the runs shared out over the warps; sums of up to 16 runs of 64
+    // tokens, two in a word
     const int words = a.stride / 4;
     for (int w0 = 0; w0 < words; w0 += 32) {
       const int w = w0 + lane;
-      if (w >= words) continue;
-      int all[4] = {0, 0, 0, 0}, low[4] = {0, 0, 0, 0};
-#pragma unroll 8
-      for (int r = warp; r < runs; r += kWarps) {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(a.counts + (int64_t)r * a.stride + 4 * w);
-        const bool mine = r < (int)blockIdx.x;
+      uint32_t all[2] = {0u, 0u}, low[2] = {0u, 0u};
+      if (w < words) {
+#pragma unroll 4
+        for (int r = warp; r < runs; r += kWarps) {
+          const uint32_t c = *reinterpret_cast<const uint32_t*>(a.counts + (int64_t)r * a.stride + 4 * w);
+          const uint32_t even = c & 0x00FF00FFu, odd = (c >> 8) & 0x00FF00FFu;
+          all[0] += even; all[1] += odd;
+          if (r < (int)blockIdx.x) { low[0] += even; low[1] += odd; }
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int n = (c >> (8 * i)) & 255;
-          all[i] += n;
-          low[i] += mine ? n : 0;
+        for (int i = 0; i < 4; ++i) {                  // whole numbers: any order
+          if (4 * w + i >= a.experts) break;
+          atomicAdd(&total[4 * w + i], (int)(all[i & 1] >> (16 * (i >> 1)) & 0xFFFFu));
+          atomicAdd(&before[4 * w + i], (int)(low[i & 1] >> (16 * (i >> 1)) & 0xFFFFu));
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (4 * w + i < a.experts) { atomicAdd(&total[4 * w + i], all[i]); atomicAdd(&before[4 * w + i], low[i]); }   // whole numbers: any order
     }
   }
   __syncthreads();
-  if (warp == 0) {
-    int sum = 0;
-    for (int base = 0; base < a.experts; base += 32) {
-      const int e = base + lane;
-      const int n = e < a.experts ? total[e] : 0;
-      int upto = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (e < a.experts) first[e] = sum + upto - n;
-      sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
-    }
-    if (lane == 0) first[a.experts] = sum;
-  }
+  if (warp == 0) prefix_sums(a.experts, total, first);
   __syncthreads();
   if (blockIdx.x == 0)
     for (int e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = first[e];
-  const int64_t t0 = (int64_t)blockIdx.x * kRun;
-  const int here = (int)min((int64_t)kRun, a.T - t0);
-  const unsigned long long* members = a.members + (int64_t)blockIdx.x * a.experts;
-  for (int c = threadIdx.x; c < here * a.top_k; c += kThreads) {
-    const int local = c / a.top_k, e = a.chosen[t0 * a.top_k + c];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = threadIdx.x + k * kThreads, e = k ? e1 : e0;
+    if (c >= here) break;
     int place = -1;
     if (e >= 0) {
+      const int local = c / a.top_k;
       place = first[e] + before[e] + __popcll(members[e] & ((1ull << local) - 1ull));
       a.rows[place] = (int)(t0 + local);
     }
