@@ -198,19 +198,19 @@ template <typename TY> __device__ __forceinline__ float raw_value(Raw<TY> v) { r
 // What a feature's outputs have in common.
 template <typename TY>
 struct Feature {
-  float scale, bias;
+  float scale, bias, least;                // least: 0 with a ReLU
   bool on;
-  __device__ Feature(const MatmulArgs& a, int expert, int n) : scale(1.f), bias(0.f), on(n < a.N) {
+  __device__ Feature(const MatmulArgs& a, int expert, int n) : scale(1.f), bias(0.f), least(a.relu ? 0.f : -INFINITY), on(n < a.N) {
     if (!on) return;
     const int64_t at = (int64_t)expert * a.N + n;
     if (a.w_scale) scale = a.w_scale[at];
     if (a.bias) bias = in_cast(reinterpret_cast<const TY*>(a.bias)[at]);
   }
-  // (sum sx) sw: the factors alone may leave fp32's range.  A NaN stays one through the ReLU.
-  __device__ float finish(const MatmulArgs& a, float sum, float x_scale) const {
-    float v = sum * x_scale * scale + bias;
-    if (a.relu) v = v < 0.f ? 0.f : v;
-    return v;
+  // (sum sx) sw + bias, of two rows: the product of the factors alone may leave fp32's range.  A NaN stays one through the ReLU.
+  __device__ void finish2(float sum0, float sum1, float sx0, float sx1, float& v0, float& v1) const {
+    const float2 v = __ffma2_rn(__fmul2_rn(make_float2(sum0, sum1), make_float2(sx0, sx1)), make_float2(scale, scale), make_float2(bias, bias));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v0) : "f"(v.x), "f"(least));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v1) : "f"(v.y), "f"(least));
   }
 };
 

@@ -93,8 +93,9 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   __syncwarp();
+  if (warp == 2 && !a.offsets) make_plan(a, plan, kTokens);
   pdl_wait();
-  if (warp == 2) make_plan(a, plan, kTokens);
+  if (warp == 2 && a.offsets) make_plan(a, plan, kTokens);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -122,7 +123,11 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     }
     float v[kN];
 #pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = good ? feature.finish(a, sum_value<kInt>(sums[j]), x_scale[j]) : __uint_as_float(0x7FC00000u);
+    for (int j = 0; j < kN; j += 2) feature.finish2(sum_value<kInt>(sums[j]), sum_value<kInt>(sums[j + 1]), x_scale[j], x_scale[j + 1], v[j], v[j + 1]);
+    if (!good) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] = __uint_as_float(0x7FC00000u);
+    }
     if (res) {
 #pragma unroll
       for (int j = 0; j < kN; ++j) v[j] += raw_value<TY>(add[j]);

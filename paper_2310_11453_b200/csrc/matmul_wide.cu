@@ -71,12 +71,17 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
-  if (warp == 3) make_plan(a, plan, tile_rows);
+  if (warp == 3 && !a.offsets) make_plan(a, plan, tile_rows);
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();                                // both CTAs' barriers exist before any remote arrival
   tc_fence_after();
+  // So far nothing that the kernel before this one on the stream could have written was read.
+  pdl_wait();
+  if (a.offsets) {
+    if (warp == 3) make_plan(a, plan, tile_rows);
+    __syncthreads();
+  }
   const uint32_t tmem_base = ctl->tmem_base;
   const int blocks = (int)((a.K * (kInt ? 1 : 2) + kRowBytes - 1) / kRowBytes);
 
@@ -264,10 +269,8 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
           const float4 s = kInt ? *reinterpret_cast<const float4*>(x_scale + j) : make_float4(1.f, 1.f, 1.f, 1.f);
-          v[j] = feature.finish(a, sum_value<kInt>(r[j]), s.x);
-          v[j + 1] = feature.finish(a, sum_value<kInt>(r[j + 1]), s.y);
-          v[j + 2] = feature.finish(a, sum_value<kInt>(r[j + 2]), s.z);
-          v[j + 3] = feature.finish(a, sum_value<kInt>(r[j + 3]), s.w);
+          feature.finish2(sum_value<kInt>(r[j]), sum_value<kInt>(r[j + 1]), s.x, s.y, v[j], v[j + 1]);
+          feature.finish2(sum_value<kInt>(r[j + 2]), sum_value<kInt>(r[j + 3]), s.z, s.w, v[j + 2], v[j + 3]);
         }
         if (res) {
 #pragma unroll
