@@ -293,7 +293,7 @@ struct MatmulArgs {
   void* y; bl_dtype yt; int64_t ld_y;
 };
 cudaError_t launch_matmul(const MatmulArgs& a, cudaStream_t s);
-cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int features, int splits, int per_sm, cudaStream_t s);   // tokens 16, 32 or 64; features 128, 64 or 32
+cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int splits, int per_sm, cudaStream_t s);   // tokens 16, 32 or 64
 cudaError_t launch_matmul_wide(const MatmulArgs& a, int tile_rows, cudaStream_t s);              // 32..256, in steps of 32
 
 // Host-side layout maps (also exported through bitlinear_layout_index).

@@ -49,7 +49,7 @@ cudaError_t launch_matmul(const MatmulArgs& a, cudaStream_t s) {
   // Two CTAs per SM where there is a tile or two for each (16 experts met, 2048 x 2048, 256 tiles: 16.1 us, one per SM 17.0), one
   // with twice the room for loads where there is only one tile, or one runs through many (1024 tiles: 48 and 50).
   const int per_sm = tiles * splits <= sms || tiles > 3 * sms ? 1 : 2;
-  return launch_matmul_narrow(a, tokens, 128, splits, per_sm, s);
+  return launch_matmul_narrow(a, tokens, splits, per_sm, s);
 }
 
 }  // namespace bl

@@ -107,7 +107,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// Rows of the list [0, R) that belong to expert e, from offsets that may be anything.
+// offsets[e], cut to the list [0, R).
 __device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int R) {
   const int v = offsets[e];
   return v < 0 ? 0 : v > R ? R : v;
@@ -118,23 +118,35 @@ __device__ __forceinline__ int offset_of(const int32_t* offsets, int e, int R) {
 // tile (and behind the last their number), the first row, the number of rows.
 inline size_t plan_bytes(int experts) { return (size_t)(3 * experts + 1) * sizeof(int); }
 
-// One warp makes the plan.
+// One warp makes the plan.  An offset below one before it counts as that one: whatever they are, the lists do not overlap, and there are no
+// more tiles than the host reckoned with.
 __device__ inline void make_plan(const MatmulArgs& a, int* plan, int tile_rows) {
   const int lane = threadIdx.x & 31;
   int *first = plan, *start = plan + a.experts + 1, *count = plan + 2 * a.experts + 1;
-  int seen = 0;
+  int seen = 0, reached = 0;                 // tiles and rows of the experts before
   for (int base = 0; base < a.experts; base += 32) {
     const int e = base + lane;
     int from = 0, n = 0;
-    if (e < a.experts) {
-      if (a.offsets) {
-        from = offset_of(a.offsets, e, (int)a.R);
-        n = max(0, offset_of(a.offsets, e + 1, (int)a.R) - from);
-      } else {
-        n = (int)a.R;
+    if (a.offsets) {
+      from = e < a.experts ? offset_of(a.offsets, e, (int)a.R) : 0;
+      int to = e < a.experts ? offset_of(a.offsets, e + 1, (int)a.R) : 0;
+      from = max(from, reached);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, from, o);
+        if (lane >= o) from = max(from, v);
       }
+      to = max(to, from);
+      n = to - from;
+      reached = __shfl_sync(0xFFFFFFFFu, to, 31);
+    } else if (e == 0) {
+      n = (int)a.R;
+    }
+    if (e < a.experts) {
       start[e] = from;
       count[e] = n;
+    } else {
+      n = 0;
     }
     const int tiles = (n + tile_rows - 1) / tile_rows;
     int upto = tiles;

@@ -1,7 +1,5 @@
 // 8-bit (and fp16, bf16) matrix products of few rows: decode steps and short lists of rows.  Bound by the weights' bytes.
-// A tile is `features` output features (128, 64 or 32, as few as it takes to give every SM a share of the loads) x kTokens rows.
-// The instruction always multiplies 128 rows of weights; those behind the tile's are whatever lies there, and nobody reads
-// their sums.  Where even that leaves SMs without work, a cluster of `splits` CTAs shares the K axis of a tile and joins its
+// A tile is 128 output features x kTokens rows.  Where that leaves SMs without work, a cluster of `splits` CTAs shares the K axis of a tile and joins its
 // sums through shared memory (whole numbers exactly, fp32 in the order of the CTAs); there is a cluster per tile then.  Without,
 // the grid is persistent: loads run ahead from tile to tile, and two accumulators take turns.
 // A ring slot holds `sub` blocks of 128 bytes of K.  Where K is a whole number of blocks one tensor copy brings the weights of
@@ -19,7 +17,8 @@ namespace {
 using namespace mm;
 
 constexpr int kThreads = 192;
-constexpr int kLanes = 128;                 // rows of weights per instruction
+constexpr int kFeatures = 128;              // of a tile: rows of weights per instruction
+constexpr int kWBlock = kFeatures * kRowBytes;
 constexpr int kMaxSlots = 8;
 
 struct Control {
@@ -31,10 +30,10 @@ struct Control {
 
 // How a launch cuts its work and its shared memory.
 struct Cut {
-  int features, feature_tiles, splits, sub, slots, packed;   // packed: a slot's weights come in one copy, its tokens in another
+  int feature_tiles, splits, sub, slots, packed;   // packed: a slot's weights come in one copy, its tokens in another
   int x_block;                                               // bytes of a block of tokens: of those that there can be, in eights
   int w_bytes, x_bytes;                                      // of a copy
-  int behind;                                                // bytes that an instruction may read behind the last slot
+  int behind;                                                // bytes that an instruction may read behind the last slot: tokens that there are not
   uint32_t idesc;
 };
 
@@ -45,10 +44,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int splits = cut.splits, sub = cut.sub, slots = cut.slots;
-  const int w_block = cut.features * kRowBytes, slot_bytes = sub * (w_block + cut.x_block);
+  const int slot_bytes = sub * (kWBlock + cut.x_block);
   // slots, then room for what an instruction reads behind the last one, then the other CTAs' sums [CTA][token of mine][feature]
   uint32_t* parts = reinterpret_cast<uint32_t*>(smem + slots * slot_bytes + cut.behind);
-  Control* ctl = reinterpret_cast<Control*>(reinterpret_cast<unsigned char*>(parts) + (splits > 1 ? kTokens * cut.features * 4 : 0));
+  Control* ctl = reinterpret_cast<Control*>(reinterpret_cast<unsigned char*>(parts) + (splits > 1 ? kTokens * kFeatures * 4 : 0));
   int* plan = reinterpret_cast<int*>(ctl + 1);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -64,7 +63,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (cut.packed) {
       tma_load_4d(dst, &map_w, 0, n0, step * sub, expert, bar);
     } else {
-      for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_load_4d(dst + b * w_block, &map_w, (step * sub + b) * kRowBytes, n0, 0, expert, bar);
+      for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_load_4d(dst + b * kWBlock, &map_w, (step * sub + b) * kRowBytes, n0, 0, expert, bar);
     }
   };
   auto copies = [&](int step) { return cut.packed ? 1 : min(sub, blocks - step * sub); };
@@ -80,7 +79,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (!a.offsets && polls != 0) {
       // one expert: the feature tile of the first tile of this CTA
-      const int row_tiles = (int)((a.R + kTokens - 1) / kTokens), first_n0 = (int)(item / (uint32_t)row_tiles) * cut.features;
+      const int row_tiles = (int)((a.R + kTokens - 1) / kTokens), first_n0 = (int)(item / (uint32_t)row_tiles) * kFeatures;
       ahead = min(slots, s1 - s0);
       for (int i = 0; i < ahead; ++i) {
         mbar_expect_tx(smem_u32(&ctl->full[i]), (uint32_t)(cut.w_bytes * copies(s0 + i)));
@@ -103,7 +102,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   const uint32_t tmem_base = ctl->tmem_base;
   const Walk from(plan, a.experts, cut.feature_tiles, item, items);
   const int quarter = warp & 3, f = quarter * 32 + lane;
-  const bool writer = warp >= 2 && quarter * 32 < cut.features;
+  const bool writer = warp >= 2;
   TY* y = reinterpret_cast<TY*>(a.y);
   const TY* res = reinterpret_cast<const TY*>(a.residual);
   // What a warp needs of a tile before its sums are there.
@@ -149,7 +148,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     bool ok = polls != 0;
     for (Walk w = from; ok && w.valid(); w.next()) {
       w.locate(kTokens);
-      const int n0 = w.f * cut.features;
+      const int n0 = w.f * kFeatures;
       int r[4] = {0, 0, 0, 0};
       if (a.rows && lane < kTokens / 4) {
 #pragma unroll
@@ -168,7 +167,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         }
         if (a.rows) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
         if (!ok || (!a.rows && lane != 0)) break;
-        const uint32_t dst = smem_u32(smem + slot * slot_bytes) + (uint32_t)(sub * w_block);
+        const uint32_t dst = smem_u32(smem + slot * slot_bytes) + (uint32_t)(sub * kWBlock);
         if (!a.rows && cut.packed) {
           tma_load_3d(dst, &map_x, 0, w.row0, step * sub, bar);
         } else {
@@ -205,7 +204,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
           tc_fence_after();
           const uint32_t at = smem_u32(smem + slot * slot_bytes);
           for (int b = 0; b < sub && step * sub + b < blocks; ++b) {
-            const uint64_t adesc = smem_desc_sw128(at + (uint32_t)(b * w_block)), bdesc = smem_desc_sw128(at + (uint32_t)(sub * w_block + b * cut.x_block));
+            const uint64_t adesc = smem_desc_sw128(at + (uint32_t)(b * kWBlock)), bdesc = smem_desc_sw128(at + (uint32_t)(sub * kWBlock + b * cut.x_block));
 #pragma unroll
             for (int j = 0; j < kRowBytes / 32; ++j)
               mma<kInt, 1>(d, adesc + (uint64_t)(2 * j), bdesc + (uint64_t)(2 * j), cut.idesc, step > s0 || b > 0 || j > 0);
@@ -226,22 +225,20 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     for (Walk w = from; w.valid(); w.next(), ++pass) {
       w.locate(kTokens);
       const uint32_t buf = pass & 1u;
-      const int n = w.f * cut.features + f;
-      const Feature<TY> feature(a, w.e, writer && f < cut.features ? n : (int)a.N);
+      const int n = w.f * kFeatures + f;
+      const Feature<TY> feature(a, w.e, n);
       take_scales(w);
       if (ok) {
         if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->done[buf]), (pass >> 1) & 1u, abort_flag, polls);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
       }
       tc_fence_after();
-      if (writer) {
-        const uint32_t taddr = tmem_base + buf * (uint32_t)kTokens + ((uint32_t)(quarter * 32) << 16);
+      const uint32_t taddr = tmem_base + buf * (uint32_t)kTokens + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
-        for (int c = 0; c < kTokens && c < w.rows; c += 16) {
-          uint32_t r[16];
-          tmem_ld16(taddr + (uint32_t)c, r);
-          if (feature.on) put(feature, w.row0 + c, n, w.rows - c, r, ctl->x_scale[quarter] + c, ok);
-        }
+      for (int c = 0; c < kTokens && c < w.rows; c += 16) {
+        uint32_t r[16];
+        tmem_ld16(taddr + (uint32_t)c, r);
+        if (feature.on) put(feature, w.row0 + c, n, w.rows - c, r, ctl->x_scale[quarter] + c, ok);
       }
       tc_fence_before();
       __syncwarp();
@@ -256,8 +253,8 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     Walk w = from;
     const bool mine = writer && w.valid();
     if (w.valid()) w.locate(kTokens);
-    const int n = w.f * cut.features + f;
-    const Feature<TY> feature(a, w.e, mine && f < cut.features ? n : (int)a.N);
+    const int n = w.f * kFeatures + f;
+    const Feature<TY> feature(a, w.e, mine ? n : (int)a.N);
     if (mine) {
       take_scales(w);
       bool ok = polls != 0;
@@ -270,12 +267,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       for (int c = 0; c < kTokens && c < w.rows; c += 16) {
         uint32_t r[16];
         tmem_ld16(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, r);
-        if (f < cut.features) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int token = c + j, owner = token >> shift;
-            if (token < w.rows) st_cluster(map_to_rank(smem_u32(parts + ((rank << shift) + (token & (each - 1))) * cut.features + f), (uint32_t)owner), r[j]);
-          }
+        for (int j = 0; j < 16; ++j) {
+          const int token = c + j, owner = token >> shift;
+          if (token < w.rows) st_cluster(map_to_rank(smem_u32(parts + ((rank << shift) + (token & (each - 1))) * kFeatures + f), (uint32_t)owner), r[j]);
         }
       }
       if (!ok && lane == 0)
@@ -291,11 +286,11 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int at = min(j + i, here - 1);
-          sums[i] = parts[at * cut.features + f];
+          sums[i] = parts[at * kFeatures + f];
 #pragma unroll
           for (int s = 1; s < 8; ++s) {
             if (s < splits) {
-              const uint32_t v = parts[((s << shift) + at) * cut.features + f];
+              const uint32_t v = parts[((s << shift) + at) * kFeatures + f];
               sums[i] = kInt ? sums[i] + v : __float_as_uint(__uint_as_float(sums[i]) + __uint_as_float(v));
             }
           }
@@ -313,35 +308,34 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 }
 
 template <int kTokens, bool kInt, typename TY>
-cudaError_t launch(const MatmulArgs& a, int features, int splits, int per_sm, cudaStream_t s) {
+cudaError_t launch(const MatmulArgs& a, int splits, int per_sm, cudaStream_t s) {
   const int es = kInt ? 1 : 2;
   const int64_t blocks = (a.K * es + kRowBytes - 1) / kRowBytes;
-  const int64_t feature_tiles = (a.N + features - 1) / features;
+  const int64_t feature_tiles = (a.N + kFeatures - 1) / kFeatures;
   int64_t token_tiles = (a.R + kTokens - 1) / kTokens;
   if (a.offsets) token_tiles = a.R / kTokens + (a.experts < a.R ? a.experts : a.R);    // at most: one that is not full per expert
   if (token_tiles * feature_tiles * splits > 0x7FFFFFFF) return cudaErrorInvalidValue;
   // Slots of up to four blocks of K, as many as leave room for three slots at least.
   Cut cut;
   const int box_t = a.rows || a.x_rows > kTokens - 8 ? kTokens : ((int)a.x_rows + 7) / 8 * 8;
-  const int block = (features + box_t) * kRowBytes;
+  const int block = (kFeatures + box_t) * kRowBytes;
   cut.x_block = box_t * kRowBytes;
-  cut.behind = (kLanes - features > kTokens - box_t ? kLanes - features : kTokens - box_t) * kRowBytes;
+  cut.behind = (kTokens - box_t) * kRowBytes;
   const int budget = (227 - per_sm) * 1024 / per_sm;          // an SM's shared memory, less what the system keeps per CTA
-  const int fixed = 1024 + (int)sizeof(Control) + (int)plan_bytes(a.experts) + cut.behind + (splits > 1 ? kTokens * features * 4 : 0);
+  const int fixed = 1024 + (int)sizeof(Control) + (int)plan_bytes(a.experts) + cut.behind + (splits > 1 ? kTokens * kFeatures * 4 : 0);
   cut.sub = 4;
   while (cut.sub > 1 && (budget - fixed) / (cut.sub * block) < 3) cut.sub /= 2;
   cut.slots = (budget - fixed) / (cut.sub * block);
   if (cut.slots > kMaxSlots) cut.slots = kMaxSlots;
-  cut.features = features;
   cut.feature_tiles = (int)feature_tiles;
   while (splits > 1 && (blocks + cut.sub - 1) / cut.sub < splits) splits /= 2;       // no CTA without a slot's worth of K
   cut.splits = splits;
   cut.packed = a.K * es % kRowBytes == 0;
-  cut.w_bytes = features * kRowBytes * (cut.packed ? cut.sub : 1);
+  cut.w_bytes = kWBlock * (cut.packed ? cut.sub : 1);
   cut.x_bytes = box_t * kRowBytes * (cut.packed ? cut.sub : 1);
-  cut.idesc = instr_desc(a.operand, kLanes, kTokens);
+  cut.idesc = instr_desc(a.operand, kFeatures, (box_t + 15) / 16 * 16);
   CUtensorMap map_w, map_x;
-  cudaError_t e = encode_blocks(&map_w, a.w, a.K * es, a.N, a.ld_w * es, a.experts, a.expert_stride * es, features, cut.packed ? cut.sub : 0);
+  cudaError_t e = encode_blocks(&map_w, a.w, a.K * es, a.N, a.ld_w * es, a.experts, a.expert_stride * es, kFeatures, cut.packed ? cut.sub : 0);
   if (e != cudaSuccess) return e;
   if (a.rows) e = encode_rows(&map_x, a.x, a.K * es, a.x_rows, a.ld_x * es, 1);
   else e = encode_blocks(&map_x, a.x, a.K * es, a.x_rows, a.ld_x * es, 0, 0, box_t, cut.packed ? cut.sub : 0);
@@ -364,20 +358,20 @@ cudaError_t launch(const MatmulArgs& a, int features, int splits, int per_sm, cu
 }
 
 template <int kTokens>
-cudaError_t launch_type(const MatmulArgs& a, int features, int splits, int per_sm, cudaStream_t s) {
+cudaError_t launch_type(const MatmulArgs& a, int splits, int per_sm, cudaStream_t s) {
   const bool whole = a.operand == BL_I8;
   switch (a.yt) {
-    case BL_F32: return whole ? launch<kTokens, true, float>(a, features, splits, per_sm, s) : launch<kTokens, false, float>(a, features, splits, per_sm, s);
-    case BL_F16: return whole ? launch<kTokens, true, __half>(a, features, splits, per_sm, s) : launch<kTokens, false, __half>(a, features, splits, per_sm, s);
-    default: return whole ? launch<kTokens, true, __nv_bfloat16>(a, features, splits, per_sm, s) : launch<kTokens, false, __nv_bfloat16>(a, features, splits, per_sm, s);
+    case BL_F32: return whole ? launch<kTokens, true, float>(a, splits, per_sm, s) : launch<kTokens, false, float>(a, splits, per_sm, s);
+    case BL_F16: return whole ? launch<kTokens, true, __half>(a, splits, per_sm, s) : launch<kTokens, false, __half>(a, splits, per_sm, s);
+    default: return whole ? launch<kTokens, true, __nv_bfloat16>(a, splits, per_sm, s) : launch<kTokens, false, __nv_bfloat16>(a, splits, per_sm, s);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int features, int splits, int per_sm, cudaStream_t s) {
-  return tokens == 16 ? launch_type<16>(a, features, splits, per_sm, s) : tokens == 32 ? launch_type<32>(a, features, splits, per_sm, s)
-                                                                               : launch_type<64>(a, features, splits, per_sm, s);
+cudaError_t launch_matmul_narrow(const MatmulArgs& a, int tokens, int splits, int per_sm, cudaStream_t s) {
+  return tokens == 16 ? launch_type<16>(a, splits, per_sm, s) : tokens == 32 ? launch_type<32>(a, splits, per_sm, s)
+                                                                               : launch_type<64>(a, splits, per_sm, s);
 }
 
 }  // namespace bl

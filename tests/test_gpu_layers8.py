@@ -390,6 +390,89 @@ def test_grouped_many_experts_and_refusals():
     assert B.matmul_grouped(x[:0], w, lists([0] * e)).shape == (0, N)
 
 
+@pytest.mark.parametrize("values", [[0, 300, 5, 700, 2, 900, 900, 20], [900, 0, 900, 0, 900, 0, 900, 0], [5, 4, 3, 2, 1, 0, -1, -2]])
+def test_grouped_offsets_that_decrease_touch_nothing_twice_and_nothing_else(values):
+    e, K, N, R_ = 7, 64, 300, 900
+    x, w = whole(1, -9, 9, R_, K), whole(2, -9, 9, e, N, K)
+    y = torch.full((R_ + 2, N), 9.25, device=DEV)
+    B.matmul_grouped(x, w, torch.tensor(values, dtype=torch.int32, device=DEV), y=y[1:-1])
+    assert bool((y[0] == 9.25).all()) and bool((y[-1] == 9.25).all())
+    every = torch.einsum("rk,enk->ern", x.double(), w.double())
+    known = (y[1:-1].double() == every).all(-1).any(0) | (y[1:-1] == 9.25).all(-1)
+    assert bool(known.all())                                       # a row is some expert's product, or untouched
+
+
+def test_results_beyond_32_bits():
+    M, K, N = 140001, 32, 32768                                    # 4.6e9 outputs
+    x, w = whole(1, -9, 9, M, K), whole(2, -9, 9, N, K)
+    got = B.matmul_i8(x, None, w, None)
+    for rows in (slice(0, 3), slice(65534, 65540), slice(131070, 131075), slice(M - 300, M)):
+        check_product(got[rows], x[rows], w, BF16)
+    off = torch.tensor([0, 70000, M], dtype=torch.int32, device=DEV)
+    got = B.matmul_grouped(x, torch.stack((w, -w)), off, y=got)
+    check_product(got[65530:65545], x[65530:65545], w, BF16)
+    check_product(got[M - 300:], x[M - 300:], -w, BF16)
+    del got
+    T, K = 530001, 4096                                            # 2.2e9 values
+    x = torch.zeros((T, K), dtype=F16, device=DEV)
+    x[-5:] = randn(3, 5, K, dtype=F16)
+    codes, scale, _, _ = B.rms_norm_quant(x)
+    want = B.rms_norm_quant(x[-5:].clone())
+    assert torch.equal(codes[-5:], want[0]) and torch.equal(scale[-5:], want[1]) and not codes[:-5].any()
+
+
+def test_weights_quantised_just_before_they_are_used():
+    """Weights are read ahead of the stream's order, but not ahead of the kernel that quantises them."""
+    x, xs = whole(1, -127, 127, 3, 2048), torch.ones(3, device=DEV)
+    latent = [randn(i, 4096, 2048, dtype=BF16) for i in range(6)]
+    want = []
+    for w in latent:
+        q, s, _, _ = B.rms_norm_quant(w, eps=-1.0)
+        torch.cuda.synchronize()
+        want.append(B.matmul_i8(x, xs, q, s, out_dtype=F32))
+    q, s = torch.empty((4096, 2048), dtype=I8, device=DEV), torch.empty(4096, device=DEV)
+    for _ in range(3):
+        got = []
+        for w in latent:                                           # the same buffer again and again
+            B.rms_norm_quant(w, eps=-1.0, x_q=q, scale=s)
+            got.append(B.matmul_i8(x, xs, q, s, out_dtype=F32))
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_norm_of_nothing_but_rows_that_are_not_there():
+    x, res = randn(1, 0, 256, dtype=BF16), randn(2, 5, 256, dtype=BF16)
+    rows = torch.tensor([[-1, 0], [7, -1], [-1, -1], [1 << 30, 3], [0, 0]], dtype=torch.int32, device=DEV)
+    q, s, h, _ = B.rms_norm_quant(x, None, 1e-6, res, rows, torch.full((5, 2), math.nan, device=DEV), h=True)
+    want = B.rms_norm_quant(res, None, 1e-6)
+    assert torch.equal(h, res) and torch.equal(q, want[0]) and torch.equal(s, want[1])
+
+
+@pytest.mark.parametrize("T,E_", [(7, 8), (200, 24)])
+def test_captured_without_a_call_before(T, E_):
+    z = randn(3, T, E_)
+    x, w = whole(1, -9, 9, T, 208), whole(2, -9, 9, E_, 104, 208)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(g, stream=s):
+            chosen, weights, offsets, rows, places = B.route_topk(z, 2)
+            up = B.matmul_grouped(x, w, offsets, rows, out_dtype=F32)
+            q, sc, _, _ = B.rms_norm_quant(up, rows=places, row_weights=weights)
+    for _ in range(2):
+        z.copy_(randn(9, T, E_))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+    check_route(z, 2, True)
+    c = R.route(z, 2, True)
+    assert chosen.tolist() == c[0]
+    counts = [b - a for a, b in zip(c[2], c[2][1:])]
+    check_grouped(up, x, w, counts, rows, F32)
+    want = B.rms_norm_quant(up, rows=places, row_weights=weights)
+    assert torch.equal(q, want[0]) and torch.equal(sc, want[1])
+
+
 # ---- together --------------------------------------------------------------------------------------------
 def block(x, res, p):
     """A feed-forward block of experts in 8 bits between two norms, as a decoder of such layers runs it."""
