@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/TensorImpl.h>
 #include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -348,6 +349,22 @@ int truth(PyObject* o) {
   return v;
 }
 
+// One allocation for several small tensors that belong together: an allocation costs about as much as the rest of a call's marshalling.
+struct Pool {
+  Tensor bytes;
+  int64_t used = 0;
+  static int64_t room(int64_t n) { return (n + 15) / 16 * 16; }
+  Tensor take(at::IntArrayRef sizes, at::ScalarType type) {
+    int64_t n = c10::elementSize(type);
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_storage_offset(used / n);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    for (const int64_t s : sizes) n *= s;
+    used += room(n);
+    return t;
+  }
+};
+
 // x, weight, eps, residual, rows, row_weights, h, y, x_q, scale
 PyObject* norm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -381,8 +398,15 @@ PyObject* norm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const c10::cuda::CUDAGuard guard(dev);
     const Tensor h = output(a[6], "h", T, K, x.options()), y = output(a[7], "y", T, K, x.options());
-    const Tensor q = output(a[8], "x_q", T, K, x.options().dtype(at::kChar));
-    const Tensor scale = !q.defined() ? Tensor() : given(a[9]) ? tensor(a[9], "scale") : at::empty({T}, x.options().dtype(at::kFloat));
+    Tensor q, scale;
+    if (a[8] == Py_True && !given(a[9])) {                      // new codes and new scales
+      Pool pool{at::empty({Pool::room(T * K) + Pool::room(4 * T)}, x.options().dtype(at::kByte))};
+      q = pool.take({T, K}, at::kChar);
+      scale = pool.take({T}, at::kFloat);
+    } else {
+      q = output(a[8], "x_q", T, K, x.options().dtype(at::kChar));
+      if (q.defined()) scale = given(a[9]) ? tensor(a[9], "scale") : at::empty({T}, x.options().dtype(at::kFloat));
+    }
     const int64_t ld_h = h.defined() ? any_rows_of(h, "h", dev, type, T, K, 8) : 0, ld_y = y.defined() ? any_rows_of(y, "y", dev, type, T, K, 8) : 0;
     const int64_t ld_q = q.defined() ? any_rows_of(q, "x_q", dev, at::kChar, T, K, 8) : 0;
     void* sp = q.defined() ? flat(scale, "scale", dev, at::kFloat, T) : nullptr;
@@ -444,16 +468,20 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (E > INT32_MAX || k < 1 || k > E || k > 32) throw std::invalid_argument("top_k must be 1..32 and at most the number of experts");
     void* pos = given(a[3]) ? flat(tensor(a[3], "positions"), "positions", dev, at::kInt, T) : nullptr;
     const c10::cuda::CUDAGuard guard(dev);
-    const auto ints = z.options().dtype(at::kInt);
-    const Tensor chosen = given(a[5]) ? tensor(a[5], "chosen") : at::empty({T, k}, ints);
-    const Tensor weights = given(a[6]) ? tensor(a[6], "weights") : at::empty({T, k}, z.options().dtype(at::kFloat));
-    const Tensor offsets = given(a[7]) ? tensor(a[7], "offsets") : at::empty({E + 1}, ints);
-    const Tensor rows = given(a[8]) ? tensor(a[8], "rows") : at::empty({T * k}, ints);
-    const Tensor places = given(a[9]) ? tensor(a[9], "places") : at::empty({T, k}, ints);
+    const int64_t need = (int64_t)entry.route_ws(T, (int)E), pairs = Pool::room(4 * T * k), list = Pool::room(4 * (E + 1));
+    // new outputs come from one allocation
+    const bool news[5] = {!given(a[5]), !given(a[6]), !given(a[7]), !given(a[8]), !given(a[9])};
+    const int64_t room = (news[0] + news[1] + news[3] + news[4]) * pairs + news[2] * list;
+    Pool pool;
+    if (room > 0) pool.bytes = at::empty({room}, z.options().dtype(at::kByte));
+    const Tensor chosen = news[0] ? pool.take({T, k}, at::kInt) : tensor(a[5], "chosen");
+    const Tensor weights = news[1] ? pool.take({T, k}, at::kFloat) : tensor(a[6], "weights");
+    const Tensor offsets = news[2] ? pool.take({E + 1}, at::kInt) : tensor(a[7], "offsets");
+    const Tensor rows = news[3] ? pool.take({T * k}, at::kInt) : tensor(a[8], "rows");
+    const Tensor places = news[4] ? pool.take({T, k}, at::kInt) : tensor(a[9], "places");
     void *cp = flat(chosen, "chosen", dev, at::kInt, T, k), *wp = flat(weights, "weights", dev, at::kFloat, T, k);
     void *op = flat(offsets, "offsets", dev, at::kInt, E + 1), *rp = flat(rows, "rows", dev, at::kInt, T * k);
     void* pp = flat(places, "places", dev, at::kInt, T, k);
-    const int64_t need = (int64_t)entry.route_ws(T, (int)E);
     Tensor ws;
     if (given(a[4])) { ws = tensor(a[4], "ws"); (void)flat(ws, "ws", dev, at::kByte, ws.numel()); }
     else if (need > 0) ws = at::empty({need}, z.options().dtype(at::kByte));

@@ -86,41 +86,47 @@ __global__ void __launch_bounds__(kThreads) route_pick_kernel(RouteArgs a) {
     const int64_t t = t0 + local;
     if (t >= a.T) break;
     const bool padding = position[n] < 0;
-    uint32_t key[kPer], local_top = 0u;
+    uint32_t key[kPer];
+    int expert[kPer];
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = lane + 32 * i;
       const float z = in_cast(raw[n][i]);
       nan |= z != z;
+      expert[i] = e;
       if constexpr (kShort) key[i] = e < a.experts ? short_key(raw[n][i], e) : 0u;
       else key[i] = e < a.experts ? key_of(z) : 0u;
-      local_top = max(local_top, key[i]);
     }
     nan = __any_sync(0xFFFFFFFFu, nan);
+    // A lane's scores in order, largest first, equal ones by their experts: a round then looks at the first only.
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) {
+#pragma unroll
+      for (int j = i; j > 0; --j) {
+        if (key[j] > key[j - 1]) {
+          const uint32_t k = key[j]; key[j] = key[j - 1]; key[j - 1] = k;
+          if constexpr (!kShort) { const int x = expert[j]; expert[j] = expert[j - 1]; expert[j - 1] = x; }
+        }
+      }
+    }
     // top_k times: the largest key, and of the experts that have it the lowest
     int mine = -1;                             // lane j keeps choice j
     uint32_t mine_key = 0u, top_key = 0u;
     for (int j = 0; j < a.top_k; ++j) {
-      const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, local_top);
+      const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key[0]);
       int e;
+      bool taken = key[0] == best;
       if constexpr (kShort) {
         e = 0xFFFF - (int)(best & 0xFFFFu);
       } else {
-        int at = INT32_MAX;
-        if (local_top == best) {
-#pragma unroll
-          for (int i = kPer - 1; i >= 0; --i) if (key[i] == best) at = lane + 32 * i;
-        }
-        e = __reduce_min_sync(0xFFFFFFFFu, at);
+        e = __reduce_min_sync(0xFFFFFFFFu, taken ? expert[0] : INT32_MAX);
+        taken = taken && expert[0] == e;
       }
-      if (local_top == best) {                 // it is taken out
-        local_top = 0u;
+      if (taken) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          if (lane + 32 * i == e) key[i] = 0u;
-          local_top = max(local_top, key[i]);
-        }
+        for (int i = 0; i + 1 < kPer; ++i) { key[i] = key[i + 1]; if constexpr (!kShort) expert[i] = expert[i + 1]; }
+        key[kPer - 1] = 0u;
       }
       if (j == 0) top_key = best;
       if (lane == j) { mine = e; mine_key = best; }
@@ -266,13 +272,32 @@ __global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, int 
   }
 }
 
+// Many blocks: one per SM.  They need few registers, and two on an SM while another has none take as long as two (8191 tokens over 128
+// experts 12.2 us, so 8.7): each asks for more than half of the shared memory.
+constexpr size_t kAlone = 120 * 1024;
+
+template <typename T, int kPer>
+cudaError_t pick_per(const RouteArgs& a, unsigned runs, cudaStream_t s) {
+  const auto kern = route_pick_kernel<T, kPer>;
+  if (runs == 1) return launch_pdl(kern, runs, kThreads, 0, s, a);
+  static std::atomic<uint64_t> ready{0};                     // devices on which the kernel's shared memory limit is set
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+    if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAlone)) != cudaSuccess) return e;
+    if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_acq_rel);
+  }
+  return launch_pdl(kern, runs, kThreads, kAlone, s, a);
+}
+
 template <typename T>
 cudaError_t pick(const RouteArgs& a, unsigned runs, cudaStream_t s) {
-  if (a.experts <= 32) return launch_pdl(route_pick_kernel<T, 1>, runs, kThreads, 0, s, a);
-  if (a.experts <= 64) return launch_pdl(route_pick_kernel<T, 2>, runs, kThreads, 0, s, a);
-  if (a.experts <= 128) return launch_pdl(route_pick_kernel<T, 4>, runs, kThreads, 0, s, a);
-  if (a.experts <= 256) return launch_pdl(route_pick_kernel<T, 8>, runs, kThreads, 0, s, a);
-  return launch_pdl(route_pick_kernel<T, 16>, runs, kThreads, 0, s, a);
+  if (a.experts <= 32) return pick_per<T, 1>(a, runs, s);
+  if (a.experts <= 64) return pick_per<T, 2>(a, runs, s);
+  if (a.experts <= 128) return pick_per<T, 4>(a, runs, s);
+  if (a.experts <= 256) return pick_per<T, 8>(a, runs, s);
+  return pick_per<T, 16>(a, runs, s);
 }
 
 size_t round16(size_t v) { return (v + 15) & ~size_t(15); }
