@@ -548,8 +548,7 @@ size_t bitlinear_route_topk_ws_bytes(int64_t T, int experts);      /* 0 if a siz
  *   multiple of it (at least N ld_w; any for one expert), both of type `operand`:
  *     BL_I8    codes; x_scale fp32 [x_rows], w_scale fp32 [experts, N], either NULL: ones.  K as in bitlinear_matmul_i8.
  *     BL_F16, BL_BF16   values (x_scale and w_scale NULL): fp32 sums.  K a multiple of 8, 8..2^20, strides multiples of 8.
- *   offsets int32 [experts + 1], experts 1..1024: clamped to 0..R; they must not decrease (else which rows are processed is
- *   not defined).  rows int32 [R] (clamped to 0..x_rows-1), or NULL: row r of x itself, x_rows >= R.
+ *   offsets int32 [experts + 1], experts 1..1024: clamped to 0..R; one below an offset before it counts as that one.  rows int32 [R] (clamped to 0..x_rows-1), or NULL: row r of x itself, x_rows >= R.
  *   bias [experts, N] or NULL, y [R, N] stride ld_y, of dtype yt (BL_F32, BL_F16, BL_BF16), element-aligned; y overlaps nothing.
  *   N 1..2^24.  Rows of y outside every list are left as they were.
  * fp32 sums are formed in an order that the sizes alone decide (same inputs, same bits).  One rounding on output; NaN and
