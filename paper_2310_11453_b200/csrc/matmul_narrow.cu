@@ -149,8 +149,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     for (Walk w = from; ok && w.valid(); w.next()) {
       w.locate(kTokens);
       const int n0 = w.f * kFeatures;
+      // Listed rows four at a time, as many as there are (places behind them hold what was there, and nobody reads their sums).
+      const int fours = (w.rows + 3) / 4;
       int r[4] = {0, 0, 0, 0};
-      if (a.rows && lane < kTokens / 4) {
+      if (a.rows && lane < fours) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = source_row(a, w.row0 + min(4 * lane + i, w.rows - 1));
       }
@@ -160,7 +162,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
           ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
           if (ok) {
             const bool asked = issued < ahead;
-            const int x_bytes = a.rows ? cut.x_block * min(sub, blocks - step * sub) : cut.x_bytes * copies(step);
+            const int x_bytes = a.rows ? fours * 4 * kRowBytes * min(sub, blocks - step * sub) : cut.x_bytes * copies(step);
             mbar_arrive_expect_tx(bar, (uint32_t)(x_bytes + (asked ? 0 : cut.w_bytes * copies(step))));
             if (!asked) load_weights(step, slot, n0, w.e);
           }
@@ -174,7 +176,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
           for (int b = 0; b < sub && step * sub + b < blocks; ++b) {
             const int c = (step * sub + b) * kRowBytes;
             if (!a.rows) tma_load_3d(dst + b * cut.x_block, &map_x, c, w.row0, 0, bar);
-            else if (lane < kTokens / 4) tma_gather4(dst + b * cut.x_block + lane * 4 * kRowBytes, &map_x, c, r, bar);
+            else if (lane < fours) tma_gather4(dst + b * cut.x_block + lane * 4 * kRowBytes, &map_x, c, r, bar);
           }
         }
         ++issued;

@@ -158,7 +158,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     __syncwarp();
   } else if (warp >= 4 + kEpiWarps) {
     // Rows by a list: 16-byte copies, eight lanes to a row of 128 bytes (a tensor copy of four listed rows takes 65 clocks, three
-    // times what the tensor cores leave: 8192 rows x 2048 x 8192 over 16 experts 316 us, with these copies @@ us).
+    // times what the tensor cores leave: 8192 rows x 2048 x 8192, 512 for each of 16 experts, 316 us, with these copies 127).
     constexpr int kPer = kMostRows / 2 * 8 / (32 * kGatherWarps);  // copies per thread and block of K, at most
     const int u = threadIdx.x - 32 * (4 + kEpiWarps), part = u & 7;
     const int64_t row_bytes = a.K * (kInt ? 1 : 2);
