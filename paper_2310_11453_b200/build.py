@@ -1,5 +1,5 @@
 """Compile the CUDA sources into paper_2310_11453_b200/libbitlinear_b200.so for sm_100a, and the argument
-marshalling of the attention operators into paper_2310_11453_b200/_marshal.so.
+marshalling of the attention operators and the 8-bit layers into paper_2310_11453_b200/_marshal.so.
 
 nvcc cross-compiles without a GPU.  The library links the static CUDA runtime and nothing else,
 so it loads in any process (with or without torch) on a box that has the driver; _marshal is a Python

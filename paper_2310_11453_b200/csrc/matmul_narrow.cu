@@ -1,7 +1,7 @@
 // 8-bit (and fp16, bf16) matrix products of few rows: decode steps and short lists of rows.  Bound by the weights' bytes.
-// A tile is 128 output features x kTokens rows.  Where that leaves SMs without work, a cluster of `splits` CTAs shares the K axis of a tile and joins its
-// sums through shared memory (whole numbers exactly, fp32 in the order of the CTAs); there is a cluster per tile then.  Without,
-// the grid is persistent: loads run ahead from tile to tile, and two accumulators take turns.
+// A tile is 128 output features x kTokens rows.  Where that leaves SMs without work, a cluster of `splits` CTAs shares the K axis of a
+// tile and joins its sums through shared memory (whole numbers exactly, fp32 in the order of the CTAs); there is a cluster per
+// tile then.  Without, the grid is persistent: loads run ahead from tile to tile, and two accumulators take turns.
 // A ring slot holds `sub` blocks of 128 bytes of K.  Where K is a whole number of blocks one tensor copy brings the weights of
 // a slot, and one the tokens: a copy costs about 70 clocks and 3.4 per row of 128 bytes (measured on one SM), so small
 // ones are dear.  Without lists the weights do not depend on what comes before on the stream: the first slots of them are
@@ -31,9 +31,9 @@ struct Control {
 // How a launch cuts its work and its shared memory.
 struct Cut {
   int feature_tiles, splits, sub, slots, packed;   // packed: a slot's weights come in one copy, its tokens in another
-  int x_block;                                               // bytes of a block of tokens: of those that there can be, in eights
-  int w_bytes, x_bytes;                                      // of a copy
-  int behind;                                                // bytes that an instruction may read behind the last slot: tokens that there are not
+  int x_block;                                     // bytes of a block of tokens: of those that there can be, in eights
+  int w_bytes, x_bytes;                            // of a copy
+  int behind;                                      // bytes that an instruction may read behind the last slot: tokens that there are not
   uint32_t idesc;
 };
 

@@ -5,8 +5,11 @@
 // tiles of one expert follow each other with its row tiles first, so that the CTAs that run at once share its weights.
 // Which tiles there are is worked out by every cluster from the experts' offsets, which the host does not know.
 // Roles per CTA: warp 0 loads, warp 1 (of CTA 0) multiplies, warp 2 allocates tensor memory, warp 3 plans, warps 4-11 write y:
-// warp w the features of quarter w % 4, every other 32 rows; warps 12-15, where a list says which rows of x, bring those.  Accumulators alternate, so that writing one overlaps the next.
-// A ring slot holds kSub blocks of 128 bytes of K: one round of barriers per 8 instructions.
+// warp w the features of quarter w % 4, every other 32 rows; warps 12-15, where a list says which rows of x, bring those.
+// Accumulators alternate, so that writing one overlaps the next.
+// A ring slot holds kSub blocks of 128 bytes of K: one round of barriers per 8 instructions (with a block per slot and six slots
+// 8192 x 4096 x 4096 takes 97 us, so 89).  The instruction takes as long for few rows as for 256 (a block of K 0.28 us with 32 rows, 0.40
+// with 256, at which point 32 KB per SM and block come out of L2 at 11 TB/s): few full tiles beat many small ones.
 // Waits are bounded; a tile whose wait runs out is written as NaN.
 #include "matmul_common.cuh"
 
@@ -32,9 +35,9 @@ constexpr int kSlots = 3;
 __device__ __forceinline__ int padded(int rows) { return (rows + kUnit - 1) / kUnit * kUnit; }
 
 struct Control {
-  unsigned long long full[kSlots], empty[kSlots];          // full: rank 0's, for the bytes of both
-  unsigned long long gathered[kSlots];                        // this CTA's rows by a list
-  unsigned long long tmem_full[2], tmem_empty[2], drained;       // tmem_empty: rank 0's, for the warps of both
+  unsigned long long full[kSlots], empty[kSlots];               // full: rank 0's, for the bytes of both
+  unsigned long long gathered[kSlots];                          // this CTA's rows by a list
+  unsigned long long tmem_full[2], tmem_empty[2], drained;      // tmem_empty: rank 0's, for the warps of both
   uint32_t tmem_base;
   int abort_flag;
   alignas(16) float x_scale[kEpiWarps][32];
@@ -89,34 +92,34 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     // no waits allowed: nothing is started
   } else if (warp == 0) {
     if (lane == 0) {
-    int slot = 0;
-    uint32_t phase = 0;
-    const uint32_t full0 = map_to_rank(smem_u32(&ctl->full[0]), 0);
-    bool ok = true;
-    for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); ok && w.valid(); w.next()) {
-      w.locate(kUnit);
-      const int n0 = w.f * kPairFeatures + (int)rank * kHalf, mine = (int)rank * (padded(w.rows) / 2);     // this CTA's features and rows of the tile
-      for (int kb = 0; kb < blocks; kb += kSub) {
-        const int n = min(kSub, blocks - kb);
-        const uint32_t bar = full0 + 8u * (uint32_t)slot;
-        ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
-        if (!ok) break;
-        mbar_arrive_expect_tx_cluster(bar, (uint32_t)(tx_bytes * n));
-        for (int b = 0; b < n; ++b) {
-          const uint32_t dst = smem_u32(smem + (size_t)slot * kSlotBytes + (size_t)b * kStage);
-          const int c = (kb + b) * kRowBytes;
-          tma_load_4d_pair(dst, &map_w, c, n0, 0, w.e, bar);
-          if (!a.rows) tma_load_2d_pair(dst + kABytes, &map_x, c, w.row0 + mine, bar);
+      int slot = 0;
+      uint32_t phase = 0;
+      const uint32_t full0 = map_to_rank(smem_u32(&ctl->full[0]), 0);
+      bool ok = true;
+      for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); ok && w.valid(); w.next()) {
+        w.locate(kUnit);
+        const int n0 = w.f * kPairFeatures + (int)rank * kHalf, mine = (int)rank * (padded(w.rows) / 2);     // this CTA's features and rows of the tile
+        for (int kb = 0; kb < blocks; kb += kSub) {
+          const int n = min(kSub, blocks - kb);
+          const uint32_t bar = full0 + 8u * (uint32_t)slot;
+          ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+          if (!ok) break;
+          mbar_arrive_expect_tx_cluster(bar, (uint32_t)(tx_bytes * n));
+          for (int b = 0; b < n; ++b) {
+            const uint32_t dst = smem_u32(smem + (size_t)slot * kSlotBytes + (size_t)b * kStage);
+            const int c = (kb + b) * kRowBytes;
+            tma_load_4d_pair(dst, &map_w, c, n0, 0, w.e, bar);
+            if (!a.rows) tma_load_2d_pair(dst + kABytes, &map_x, c, w.row0 + mine, bar);
+          }
+          if (++slot == kSlots) { slot = 0; phase ^= 1u; }
         }
-        if (++slot == kSlots) { slot = 0; phase ^= 1u; }
       }
-    }
-    // Every copy is read by a product that the epilogue waits for.  Where a wait ran out, copies may be on their way that nobody
-    // waits for, counted on the partner's barrier: they get the time of a thousand copies.
-    if (*abort_flag && polls != 0) {
-      const unsigned long long t0 = global_ns();
-      while (global_ns() - t0 < 5000000ull) {}
-    }
+      // Every copy is read by a product that the epilogue waits for.  Where a wait ran out, copies may be on their way that nobody
+      // waits for, counted on the partner's barrier: they get the time of a thousand copies.
+      if (*abort_flag && polls != 0) {
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 5000000ull) {}
+      }
     }
     __syncwarp();
   } else if (warp == 1) {
