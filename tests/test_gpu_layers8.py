@@ -161,6 +161,17 @@ def test_norm_in_place_on_other_streams_and_with_nothing_to_do():
         B.rms_norm_quant(x, weight, x_q=None)
 
 
+@pytest.mark.parametrize("T,K", [(3, 512), (40, 8192), (200, 3000)])
+def test_norm_of_which_one_output_is_wanted(T, K):
+    x, res, weight = randn(1, T, K, dtype=F16), randn(2, T, K, dtype=F16), randn(3, K, dtype=F16)
+    codes, scale, h, y = B.rms_norm_quant(x, weight, residual=res, h=True, y=True)
+    only = B.rms_norm_quant(x, weight, residual=res, h=True, x_q=None)
+    assert torch.equal(only[2], h) and only[0] is None and only[1] is None and only[3] is None
+    assert torch.equal(B.rms_norm_quant(x, weight, residual=res, x_q=None, y=True)[3], y)
+    q, s, none, none2 = B.rms_norm_quant(x, weight, residual=res)
+    assert torch.equal(q, codes) and torch.equal(s, scale) and none is None and none2 is None
+
+
 # ---- matrix product of codes -------------------------------------------------------------------------
 def check_product(got, x, w, yt, xs=None, ws=None, bias=None, relu=False, residual=None, exact=True):
     want, size = R.product(x, w, xs, ws, bias, relu, residual)
@@ -390,6 +401,56 @@ def test_grouped_many_experts_and_refusals():
     assert B.matmul_grouped(x[:0], w, lists([0] * e)).shape == (0, N)
 
 
+@pytest.mark.parametrize("dt", [I8, F16])
+@pytest.mark.parametrize("counts", [[2, 0, 3], [90, 0, 333]])
+def test_grouped_strides(counts, dt):
+    K, N, T, n = 336, 150, 50, sum(counts)
+    xb, wb = whole(1, -8, 8, max(T, n), K + 64, dtype=dt), whole(2, -8, 8, len(counts), N + 2, K + 16, dtype=dt)
+    x, w = xb[:, 32:32 + K], wb[:, :N, :K]
+    rows = whole(3, 0, T - 1, n, dtype=torch.int32)
+    check_grouped(B.matmul_grouped(x[:T], w, lists(counts), rows, out_dtype=F32), x, w, counts, rows, F32, whole=True)
+    check_grouped(B.matmul_grouped(x[:n], w, lists(counts), out_dtype=F32), x, w, counts, None, F32, whole=True)
+
+
+def test_grouped_many_long_lists_and_the_longest_rows():
+    e, K, N = 1024, 64, 260
+    counts = [17 + (i * 11) % 23 for i in range(e)]
+    n = sum(counts)
+    x, w = whole(1, -9, 9, 500, K), whole(2, -9, 9, e, N, K)
+    rows = whole(3, 0, 499, n, dtype=torch.int32)
+    got = B.matmul_grouped(x, w, lists(counts), rows, out_dtype=F32)
+    expert = torch.repeat_interleave(torch.arange(e, device=DEV), torch.tensor(counts, device=DEV))
+    want = torch.cat([torch.einsum("rk,rnk->rn", x[rows[a:a + 4000].long()].double(), w[expert[a:a + 4000]].double()) for a in range(0, n, 4000)])
+    assert torch.equal(got.double(), want)
+    K = 1 << 20
+    for counts in ([3, 0, 2], [130, 5]):
+        x, w = whole(4, -2, 2, 20, K, dtype=BF16), whole(5, -2, 2, len(counts), 140, K, dtype=BF16)      # sums up to 2^22: exact
+        rows = whole(6, 0, 19, sum(counts), dtype=torch.int32)
+        got, at = B.matmul_grouped(x, w, lists(counts), rows, out_dtype=F32), 0
+        for i, c in enumerate(counts):
+            assert torch.equal(got[at:at + c].double(), (x.double() @ w[i].double().t())[rows[at:at + c].long()])
+            at += c
+
+
+@pytest.mark.parametrize("polls", [0, 1, 3])
+@pytest.mark.parametrize("counts", [[3, 0, 9], [300, 77]])
+def test_grouped_waits_that_run_out(counts, polls):
+    x, w = whole(1, -9, 9, 64, 2048), whole(2, -9, 9, len(counts), 600, 2048)
+    rows = whole(3, 0, 63, sum(counts), dtype=torch.int32)
+    want = B.matmul_grouped(x, w, lists(counts), rows, out_dtype=F32)
+    offsets = lists(counts)
+    torch.cuda.synchronize()
+    B.debug_wait_limit(polls)
+    try:
+        got = B.matmul_grouped(x, w, offsets, rows, out_dtype=F32)
+        torch.cuda.synchronize()
+    finally:
+        B.debug_wait_limit(-1)
+    bad = torch.isnan(got)
+    assert torch.equal(got[~bad], want[~bad]) and (polls > 0 or bool(bad.all()))
+    assert torch.equal(B.matmul_grouped(x, w, offsets, rows, out_dtype=F32), want)
+
+
 @pytest.mark.parametrize("values", [[0, 300, 5, 700, 2, 900, 900, 20], [900, 0, 900, 0, 900, 0, 900, 0], [5, 4, 3, 2, 1, 0, -1, -2]])
 def test_grouped_offsets_that_decrease_touch_nothing_twice_and_nothing_else(values):
     e, K, N, R_ = 7, 64, 300, 900
@@ -515,6 +576,29 @@ def test_block_of_experts(T, d, ffn, e, k):
     check_grouped(r["down"], mid, p["down"], counts, None, BF16, xs=ms, ws=p["down_scale"])
     wh, size = R.summed(r["down"], r["h"], r["places"], r["weights"])
     check(r["out"], wh, (k + 2) * E * size + R.half_step(BF16) * wh.abs() + 1e-40)
+
+
+@pytest.mark.parametrize("T", [13, 150])
+def test_block_of_a_padded_batch(T):
+    """Rows of padding visit no expert and change nobody's result."""
+    p = parameters(512, 768, 8, 2)
+    x, res = randn(41, T, 512, dtype=BF16), randn(42, T, 512, dtype=BF16)
+    real = torch.arange(T, device=DEV) % 3 != 1
+    pos = torch.where(real, torch.arange(T, device=DEV), -1).int()
+
+    def run(x, res, pos):
+        codes, scale, h, _ = B.rms_norm_quant(x, p["norm"], residual=res, h=True)
+        logits = B.matmul_i8(codes, scale, p["gate"], p["gate_scale"], out_dtype=F32)
+        _, weights, offsets, rows, places = B.route_topk(logits, 2, positions=pos)
+        up = B.matmul_grouped(codes, p["up"], offsets, rows, scale, p["up_scale"], relu=True)
+        mid, mid_scale, _, _ = B.rms_norm_quant(up, eps=-1.0)
+        down = B.matmul_grouped(mid, p["down"], offsets, None, mid_scale, p["down_scale"])
+        return B.rms_norm_quant(down, p["norm2"], residual=h, rows=places, row_weights=weights, h=True), h
+
+    (q, s, h, _), first = run(x, res, pos)
+    (wq, ws, wh, _), _ = run(x[real], res[real], None)
+    assert torch.equal(q[real], wq) and torch.equal(s[real], ws) and torch.equal(h[real], wh)
+    assert torch.equal(h[~real], first[~real])                     # padding: the residual alone
 
 
 def test_block_in_graphs_that_run_at_once():
