@@ -283,10 +283,10 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
       const bool bad = *reinterpret_cast<volatile int*>(&ctl->peer_abort) != 0;
       const int t0 = rank << shift, here = min(each, w.rows - t0);
 #pragma unroll 1
-      for (int j = 0; j < here; j += 4) {
-        uint32_t sums[4];
+      for (int j = 0; j < here; j += 8) {
+        uint32_t sums[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
           const int at = min(j + i, here - 1);
           sums[i] = parts[at * kFeatures + f];
 #pragma unroll
