@@ -501,8 +501,9 @@ bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_p
  *   but not all.  h and y may be residual, or without rows x, themselves (same stride), else outputs overlap nothing.
  *   K a multiple of 8, 8..32768; strides multiples of 8.
  * fp32 throughout; the codes are those of h before it is rounded to dt, and those of exact arithmetic where y / scale is
- * further than 2^-13 from a border between two codes (with rows: and further than the roundings of the sum of top_k + 1 terms).  A row of zeros has codes and scale 0; a row in which a value is not
- * finite has scale NaN and codes 0.  T = 0 does nothing.  No workspace. */
+ * further than 2^-13 from a border between two codes (with rows: and further than the roundings of the sum of
+ * top_k + 1 terms).  A row of zeros has codes and scale 0; a row in which a value is not finite has scale NaN and codes 0.
+ * T = 0 does nothing.  No workspace. */
 bl_status bitlinear_rms_norm_quant(const void* x, bl_dtype dt, int64_t x_rows, int64_t T, int64_t K, int64_t ld_x,
                                    const int32_t* rows, const float* row_weights, int top_k, const void* residual,
                                    int64_t ld_res, const void* weight, float eps, void* h, int64_t ld_h, void* y,
@@ -548,7 +549,8 @@ size_t bitlinear_route_topk_ws_bytes(int64_t T, int experts);      /* 0 if a siz
  *   multiple of it (at least N ld_w; any for one expert), both of type `operand`:
  *     BL_I8    codes; x_scale fp32 [x_rows], w_scale fp32 [experts, N], either NULL: ones.  K as in bitlinear_matmul_i8.
  *     BL_F16, BL_BF16   values (x_scale and w_scale NULL): fp32 sums.  K a multiple of 8, 8..2^20, strides multiples of 8.
- *   offsets int32 [experts + 1], experts 1..1024: clamped to 0..R; one below an offset before it counts as that one.  rows int32 [R] (clamped to 0..x_rows-1), or NULL: row r of x itself, x_rows >= R.
+ *   offsets int32 [experts + 1], experts 1..1024: clamped to 0..R; one below an offset before it counts as that one.
+ *   rows int32 [R] (clamped to 0..x_rows-1), or NULL: row r of x itself, x_rows >= R.
  *   bias [experts, N] or NULL, y [R, N] stride ld_y, of dtype yt (BL_F32, BL_F16, BL_BF16), element-aligned; y overlaps nothing.
  *   N 1..2^24.  Rows of y outside every list are left as they were.
  * fp32 sums are formed in an order that the sizes alone decide (same inputs, same bits).  One rounding on output; NaN and
@@ -566,11 +568,12 @@ bl_status bitlinear_ws_status(const void* ws, void* stream);
 
 /* Test and diagnostic hook: caps the number of polls that the bounded device-side waits of
  * kernels launched afterwards by this process may make (bitlinear_gemv_decode's wait for its
- * weight copies; the waits of bitlinear_attention_window and bitlinear_attention_kv4; the meeting between the
+ * weight copies; the waits of bitlinear_attention_window, bitlinear_attention_kv4, bitlinear_matmul_i8 and
+ * bitlinear_matmul_grouped; the meeting between the
  * two passes of the cooperative per-tensor kernel of bitlinear_quant_act).  polls < 0 restores the built-in limits; 0 means a single poll (for
  * bitlinear_gemv_decode and bitlinear_attention_window: none at all, weights are read from global
  * memory, rows are computed one by one; for bitlinear_attention_kv4: none, it reports the timeout and its rows
- * are NaN).
+ * are NaN; for the two matrix products: none, their rows are NaN).
  * meet_skew != 0 additionally makes the cooperative kernel wait for an arrival tag that no CTA
  * publishes, so that its wait runs out by construction: the kernel then records
  * BL_ERR_TIMEOUT in the status word, writes no codes and returns (nothing hangs, traps or

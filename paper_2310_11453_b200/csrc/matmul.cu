@@ -38,10 +38,10 @@ Choice choose(const MatmulArgs& a, int64_t sms) {
     if (tile == 64 || cost < least) { c.wide = tile; least = cost; }
   }
   if (mean > 256) return c;
-  // Narrow: 0.24 us a block of K (listed rows 0.035 more for every four), two CTAs on an SM 1.6 times that each; weights at 6.5 TB/s at most.  K shared by a
-  // cluster: as much less of it for each CTA, and a join that grows with the rows (1 x 4096 x 4096 12.6 us in one piece, 7.6 in four;
-  // 64 x 4096 x 4096 13.0 and 10.5; 40 x 2048 x 8192 9.0 in one, 10.9 in two).  Clusters of eight need GPCs with room for them: one CTA per SM takes 17 us
-  // for 40 x 8192 x 2048, two per SM 9.9.
+  // Narrow: 0.24 us a block of K (listed rows 0.035 more for every four), two CTAs on an SM 1.6 times that each; weights at 6.5 TB/s at
+  // most.  K shared by a cluster: as much less of it for each CTA, and a join that grows with the rows (1 x 4096 x 4096 12.6 us in one
+  // piece, 7.6 in four; 64 x 4096 x 4096 13.0 and 10.5; 40 x 2048 x 8192 9.0 in one, 10.9 in two).  Clusters of eight need GPCs with room
+  // for them: one CTA per SM takes 17 us for 40 x 8192 x 2048, two per SM 9.9.
   for (int tokens = mean <= 16 ? 16 : 32; tokens <= (mean <= 16 ? 16 : 64); tokens *= 2) {
     const int64_t tiles = row_tiles(tokens) * features;
     const int64_t most = (a.offsets ? a.R / tokens + met : ceil_div(a.R, tokens)) * features;      // that there can be
