@@ -5,8 +5,9 @@
 // row stays in the registers of its threads in between.  The norm's factor is the same for the whole row and positive, so it cancels in the codes:
 //   code = round(h w . 127 / max |h w|),   scale = max |h w| / (127 sqrt(mean h^2 + eps)),
 // and one reduction that carries the sum of squares and the largest |h w| together serves both.
-// Rows whose squares, or whose products with w, leave the range of fp32 go round again, scaled by a power of two (exact); they are
-// loaded anew for it, by the same code, so that this costs the others neither registers nor instructions.
+// Rows whose squares, or whose products with w, leave the range of fp32 go round again: once for the mean, scaled by the power of two
+// that their largest value asks for, and once for the products, scaled by one that those ask for (a value that dwarfs the others may have
+// a small weight).  They are loaded anew for it, a chunk of eight values at a time, so that this costs the others no registers.
 #include <type_traits>
 
 #include "common.cuh"
@@ -129,14 +130,23 @@ struct RowThreads {
   }
 };
 
-// What the outputs of a chunk are made from.
+// What the outputs are made from: the products of values and weights times factor (y) and inv (codes).
 struct RowResult { float factor, inv; bool fine; };
 
-template <typename T>
-__device__ __forceinline__ void store_chunk(const NormQuantArgs& a, int t, int at, const float2 (&h)[4], const float2 (&w)[4], const RowResult& r) {
-  float2 p[4];
+__device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }        // n in -126..127
+__device__ __forceinline__ double pow2_wide(int n) { return __hiloint2double((1023 + n) << 20, 0); }       // n in -1022..1023
+// v 2^n; what would pass fp32's largest stays there (scaled up, it belongs to a factor of 0 or to a product that is nothing beside the largest).
+__device__ __forceinline__ void scale_eight(float2 (&v)[4], int n) {
+  const float f = pow2(n), most = n > 0 ? 3.4028234e38f : INFINITY;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) p[e] = __fmul2_rn(w[e], h[e]);
+  for (int e = 0; e < 4; ++e) {
+    v[e] = __fmul2_rn(v[e], both(f));
+    if (n > 0) v[e] = make_float2(fminf(fmaxf(v[e].x, -most), most), fminf(fmaxf(v[e].y, -most), most));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_products(const NormQuantArgs& a, int t, int at, const float2 (&p)[4], const RowResult& r) {
   if (a.y) {
     float2 v[4];
 #pragma unroll
@@ -169,12 +179,10 @@ __device__ __forceinline__ bool out_of_range(float f) {          // below 1e-30 
   return __float_as_uint(f) - 0x0DA24260u >= 0x7F800000u - 0x0DA24260u;
 }
 
-template <int kChunks> __device__ __forceinline__ void scale_row(float2 (&h)[kChunks][4], float f) {
-#pragma unroll
-  for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) h[c][e] = __fmul2_rn(h[c][e], both(f));
-}
+// Powers of two by which the values and the weights of a row whose products leave the range are multiplied, both, so that a product that
+// counts has two factors in range: products that overflow are 2^128 to 2^256, those that are too small 2^-99 at most (in a second step
+// those below 2^-250).  Scaled up, a factor that passes fp32's range had 2^53 (2^8) or more, and a partner of 0: as 2^-149 is the least.
+constexpr int kDown = -65, kUp = 75, kFurtherUp = 120;
 
 // The chunks of h (zeros behind the row).
 template <typename T, int kChunks, bool kJoin>
@@ -226,6 +234,83 @@ __device__ __forceinline__ void fetch(const NormQuantArgs& a, int t, int i, int 
   }
 }
 
+template <typename T>
+__device__ __forceinline__ Eight<T> load_weight(const NormQuantArgs& a, int at, int chunks) {
+  return a.weight && a.eps >= 0.f && at < chunks ? load_eight(reinterpret_cast<const T*>(a.weight) + at * 8) : ones<T>();
+}
+
+// A row whose mean or whose largest product left the range; result is what the first round made of it.
+template <typename T, bool kJoin>
+__device__ __forceinline__ void far_row(const NormQuantArgs& a, int t, int i, int row_threads, int chunks, float top, RowResult result, RowThreads& rt) {
+  const bool norm = a.eps >= 0.f;
+  // its largest size, the mean of its squares scaled by 2^mean_scale, the largest product of values and weights scaled by 2^scale each
+  // (once or twice), and its outputs from products scaled by 2^shift
+  enum { kMost, kMean, kProducts, kLast };
+  int round = kMost, mean_scale = 0, scale = !out_of_range(top) ? 0 : top < 1e-30f ? kUp : kDown, shift = 0;
+  float root = 1.f;                                    // 1 / sqrt(mean of the scaled squares and eps)
+#pragma unroll 1
+  for (;;) {
+    float sum = 0.f;
+    top = 0.f;
+#pragma unroll 1
+    for (int at = i; at < chunks; at += row_threads) {
+      float2 h[1][4], w[4];
+      fetch<T, 1, kJoin>(a, t, at, row_threads, chunks, h);
+      if (round == kLast && a.h) store_eight(reinterpret_cast<T*>(a.h) + (int64_t)t * a.ld_h + at * 8, h[0]);
+      floats(round >= kProducts ? load_weight<T>(a, at, chunks) : ones<T>(), w);
+      if (round == kMean) scale_eight(h[0], mean_scale);
+      if (round >= kProducts && scale != 0) {
+        scale_eight(h[0], scale);
+        scale_eight(w, scale);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum = fmaf(h[0][e].x, h[0][e].x, fmaf(h[0][e].y, h[0][e].y, sum));
+        w[e] = __fmul2_rn(h[0][e], w[e]);
+        top = max_of(top, w[e]);
+      }
+      if (round == kLast) {
+        if (shift != 0) {                              // up to 2^126 either way: in two steps
+          scale_eight(w, shift / 2);
+          scale_eight(w, shift - shift / 2);
+        }
+        store_products<T>(a, t, at, w, result);
+      }
+    }
+    if (round == kLast) return;
+    rt.reduce(sum, top);
+    if (round == kMost) {
+      if (top == 0.f) result.factor = 0.f;             // a row of zeros stays one, with eps = 0 too
+      if (top == 0.f && a.x_q && i == 0 && result.fine) a.scale[t] = 0.f;
+      if (top == 0.f || !finite(top)) scale = 0;
+      // the largest goes to [1, 2) or [1, 4), or as near as a factor of 2^100 comes
+      mean_scale = max(-126, min(100, 127 - max(1, (int)(__float_as_uint(top) >> 23))));
+      round = top == 0.f || !finite(top) ? kLast : norm ? kMean : kProducts;
+    } else if (round == kMean) {
+      // 1 / sqrt(mean h^2 + eps) = f / sqrt(mean (f h)^2 + f^2 eps), f = 2^mean_scale; where f^2 eps passes fp32, the mean is nothing beside it
+      const float f = pow2(mean_scale), scaled_eps = a.eps * f * f;
+      root = finite(scaled_eps) ? rsqrtf(fmaf(sum, a.inv_k, scaled_eps)) : rsqrtf(a.eps);
+      if (!finite(scaled_eps)) mean_scale = 0;
+      round = kProducts;
+    } else if (scale == kUp && top > 0.f && top < 7.8886091e-31f) {       // 2^-100
+      scale = kFurtherUp;
+    } else {
+      // The products are brought to [1, 2) at their largest, and what is left of the powers of two goes into one factor: that of y is
+      // about the largest y, and that of the codes 127 or less.  With a weight that is not finite the others' y are as they are.
+      const bool apply = finite(top) && top > 0.f;
+      if (!finite(top)) scale = 0;
+      shift = apply ? 127 - max(1, (int)(__float_as_uint(top) >> 23)) : 0;
+      const double factor = (double)root * pow2_wide((norm ? mean_scale : 0) - 2 * scale - shift);
+      const float normal = apply ? top * pow2(shift / 2) * pow2(shift - shift / 2) : 0.f;
+      result.fine = finite(top);
+      result.factor = top == 0.f ? 0.f : (float)factor;
+      result.inv = apply ? 127.f / normal : 0.f;
+      if (a.x_q && i == 0) a.scale[t] = !result.fine ? __uint_as_float(0x7FC00000u) : (float)(factor * normal * (1. / 127.));
+      round = kLast;
+    }
+  }
+}
+
 // Thread i of a row holds the chunks of eight values i, i + threads, ..., kChunks of them at most.
 template <typename T, int kChunks, int kThreads, bool kJoin>
 __global__ void __launch_bounds__(kThreads, kChunks == 2 ? 2 : 1) rms_norm_quant_kernel(NormQuantArgs a, int row_threads) {
@@ -240,61 +325,36 @@ __global__ void __launch_bounds__(kThreads, kChunks == 2 ? 2 : 1) rms_norm_quant
   if (t >= (int)a.T) return;                              // whole rows of threads: none waits for another's
   pdl_wait();
   const int chunks = (int)(a.K / 8);
-  const float inv_k = a.inv_k;
   const bool norm = a.eps >= 0.f;
-  // Once round for nearly every row.  One that leaves the range: its largest size, then once more scaled by f (twice, with tiny
-  // weights), and once to have the values themselves again.
-  enum { kPlain, kMost, kScaled, kRescaled, kLast };
-  int round = kPlain;
-  float f = 1.f;
   RowResult result{1.f, 0.f, true};
   float2 h[kChunks][4];
-  auto weight_of = [&](int c, bool want) {
-    return want && norm && a.weight && i + c * row_threads < chunks ? load_eight(reinterpret_cast<const T*>(a.weight) + (i + c * row_threads) * 8) : ones<T>();
-  };
-#pragma unroll 1
-  for (;;) {
+  {
     Eight<T> weight[kChunks];
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) weight[c] = weight_of(c, round != kMost);
+    for (int c = 0; c < kChunks; ++c) weight[c] = load_weight<T>(a, i + c * row_threads, chunks);
     fetch<T, kChunks, kJoin>(a, t, i, row_threads, chunks, h);
-    if (round == kLast || (!a.y && !a.x_q)) break;
-    if (f != 1.f) scale_row(h, f);
-    // the sum of squares and the largest |h w|
-    float2 s[2] = {both(0.f), both(0.f)};
-    float m[2] = {0.f, 0.f};
+    if (a.y || a.x_q) {
+      // the sum of squares and the largest |h w|
+      float2 s[2] = {both(0.f), both(0.f)};
+      float m[2] = {0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      float2 w[4];
-      floats(weight[c], w);
+      for (int c = 0; c < kChunks; ++c) {
+        float2 w[4];
+        floats(weight[c], w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[e & 1] = __ffma2_rn(h[c][e], h[c][e], s[e & 1]);
-        m[e & 1] = max_of(m[e & 1], __fmul2_rn(h[c][e], w[e]));
+        for (int e = 0; e < 4; ++e) {
+          s[e & 1] = __ffma2_rn(h[c][e], h[c][e], s[e & 1]);
+          m[e & 1] = max_of(m[e & 1], __fmul2_rn(h[c][e], w[e]));
+        }
       }
-    }
-    float sum = (s[0].x + s[0].y) + (s[1].x + s[1].y), top = max_nan(m[0], m[1]);
-    rt.reduce(sum, top);
-    if (round == kPlain) {
-      const float mean = fmaf(sum, inv_k, a.eps);
+      float sum = (s[0].x + s[0].y) + (s[1].x + s[1].y), top = max_nan(m[0], m[1]);
+      rt.reduce(sum, top);
+      const float mean = fmaf(sum, a.inv_k, a.eps);
       result = result_of(a, t, i, top, norm ? rsqrtf(mean) : 1.f);
-      if (!out_of_range(top) && !(norm && out_of_range(mean))) break;
-      round = kMost;
-    } else if (round == kMost) {
-      if (top == 0.f) result.factor = 0.f;             // a row of zeros stays one, with eps = 0 too
-      if (top == 0.f && a.x_q && i == 0 && result.fine) a.scale[t] = 0.f;
-      if (top == 0.f || !finite(top)) { round = kLast; continue; }
-      // f: the power of two that brings the largest into [1, 2), or as near as a factor of 2^100 comes
-      const int up = min(100, 127 - max(1, (int)(__float_as_uint(top) >> 23)));
-      f = up >= -126 ? __uint_as_float((uint32_t)(127 + up) << 23) : __uint_as_float(0x00400000u);   // 2^-127 is denormal
-      round = kScaled;
-    } else {
-      // w h / sqrt(mean h^2 + eps) = w (f h) / sqrt(mean (f h)^2 + f^2 eps); where f^2 eps passes fp32, the mean is nothing beside it
-      const float scaled_eps = a.eps * f * f;
-      result = result_of(a, t, i, top, !norm ? 1.f / f : finite(scaled_eps) ? rsqrtf(fmaf(sum, inv_k, scaled_eps)) : rsqrtf(a.eps) / f);
-      const bool again = round == kScaled && top < 1e-30f && top > 0.f && f < 1.3e8f;      // tiny weights
-      if (again) f *= 1.2676506e30f;                   // 2^100
-      round = again ? kRescaled : kLast;
+      if (out_of_range(top) || (norm && out_of_range(mean))) {
+        far_row<T, kJoin>(a, t, i, row_threads, chunks, top, result, rt);
+        return;
+      }
     }
   }
   if (a.h) {
@@ -303,14 +363,15 @@ __global__ void __launch_bounds__(kThreads, kChunks == 2 ? 2 : 1) rms_norm_quant
     for (int c = 0; c < kChunks; ++c)
       if (i + c * row_threads < chunks) store_eight(out + (i + c * row_threads) * 8, h[c]);
   }
-  if (f != 1.f) scale_row(h, f);
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     const int at = i + c * row_threads;
     if (at >= chunks) continue;
     float2 w[4];
-    floats(weight_of(c, true), w);                     // again, from L1: registers are worth more
-    store_chunk<T>(a, t, at, h[c], w, result);
+    floats(load_weight<T>(a, at, chunks), w);             // again, from L1: registers are worth more
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __fmul2_rn(w[e], h[c][e]);
+    store_products<T>(a, t, at, w, result);
   }
 }
 

@@ -1,0 +1,71 @@
+"""Calls of the 8-bit layers that the ordinary ranges do not reach.
+
+Tolerances as in test_gpu_layers8: e = 2^-24 is one rounding of fp32, u(T) = eps(T) / 2 one to T.  Scaling by powers of two is exact, so
+rows that leave the range have those of the others: the sum h 2 e of its terms, the norm's factor 40 e with the products, one rounding on
+output.  Where an output is below the smallest normal number of its type the rounding is half of the smallest denormal one (bf16:
+2^-134, under 1e-40; fp32: 2^-150, with one more for the factor, under 1e-44)."""
+
+import pytest
+import torch
+
+from paper_2310_11453_b200 import binding as B
+from tests import layers8_ref as R
+from tests.test_gpu_layers8 import BF16, DEV, E, F32, check, randn, whole
+
+pytestmark = pytest.mark.gpu
+LEAST = {BF16: 1e-40, F32: 1e-44}
+
+
+# ---- norm: weights and values at the ends of the range -------------------------------------------------
+def check_range(x, weight, eps, rows=None, row_weights=None):
+    """y, scale and codes of rows without cancellation (one term, or terms of one sign)."""
+    dt = x.dtype
+    codes, scale, h, y = B.rms_norm_quant(x, weight, eps, rows=rows, row_weights=row_weights, h=True, y=True)
+    wh, _ = R.summed(x, None, rows, row_weights)
+    n = 2 + (rows.shape[1] if rows is not None else 0)
+    want = R.normed(wh, weight, eps)
+    near = (40 + 2 * n) * E
+    check(y, want, (near + R.half_step(dt)) * want.abs() + LEAST[dt], "y")
+    top = want.abs().amax(-1)
+    check(scale, top / 127, (near + 4 * E) * top / 127 + 1e-44, "scale")
+    v = torch.where(top[:, None] > 0, want / top[:, None].clamp(min=1e-300) * 127, torch.zeros_like(want))
+    slack = 2.0 ** -13 + 127 * 2 * n * E
+    worst = float(((codes.double() - v).abs() - 0.5 - slack).max())
+    assert worst <= 0, f"codes: {worst} beyond half a step"
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("T,K", [(5, 1024), (200, 1024), (3, 16392)])
+@pytest.mark.parametrize("weight", [1e-32, 1e-35, 1e-37, 1e30])
+@pytest.mark.parametrize("size", [1.0, 1e-10, 1e-25, 3e5, 1e25])
+def test_norm_of_weights_at_the_ends_of_the_range(dt, T, K, weight, size):
+    x = randn(K, T, K, scale=size).to(dt)
+    w = ((1 + 0.2 * randn(3, K)) * weight).to(dt)
+    for eps in (0.0, 1e-6):
+        check_range(x, w, eps)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_norm_of_a_value_that_dwarfs_the_others(dt):
+    """A weight of 0 hides the largest value from the codes, which are those of the others whatever it takes to hold its square."""
+    K = 1024
+    x = randn(1, 6, K)
+    x[:, 17] = torch.tensor([1e38, -3e38, 1e30, 1e20, 3e19, 2.0], device=DEV)
+    x, w = x.to(dt), (1 + 0.2 * randn(2, K)).to(dt)
+    w[17] = 0
+    check_range(x, w, 0.0)
+    check_range(x, w, 1e-6)
+    w2 = w.clone()                                                 # and weights that bring the others back
+    w2[torch.arange(K, device=DEV) != 17] *= 1e30
+    check_range(x, w2, 1e-6)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_norm_of_summed_rows_at_the_ends_of_the_range(dt):
+    K, T = 1024, 7
+    rows = whole(1, 0, 11, T, 2, dtype=torch.int32)
+    p = torch.softmax(randn(2, T, 2), -1)
+    for size, weight in ((1.0, 1e-33), (1e-20, 1e-30), (1e-30, 1.0), (1e25, 1.0), (1e30, 1e-20), (1e30, 1e20)):
+        x = (randn(3, 12, K).abs() * size).to(dt)
+        check_range(x, ((1 + 0.2 * randn(4, K)) * weight).to(dt), 1e-6, rows, p)
+        check_range(x, ((1 + 0.2 * randn(4, K)) * weight).to(dt), 0.0, rows, p)
