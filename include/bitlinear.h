@@ -515,8 +515,7 @@ bl_status bitlinear_rms_norm_quant(const void* x, bl_dtype dt, int64_t x_rows, i
  *   (codes may be -128..127: no sum leaves 32 bits).  x_scale fp32 [M], w_scale fp32 [N], either NULL: ones.
  *   bias [N] or NULL, residual [M, N] stride ld_res or NULL, y [M, N] stride ld_y, all of dtype yt (BL_F32, BL_F16,
  *   BL_BF16), element-aligned.  y may be residual itself (same stride), else overlaps nothing.  N 1..2^24.
- * The weights are read ahead of stream order, like those of bitlinear_gemv_decode: whatever wrote w_q must have completed before
- * the call, or must be bitlinear_rms_norm_quant with eps < 0 or a kernel of another library, on the same stream.
+ * All inputs are read in the stream's order: w_q may be written just before the call by any kernel on the same stream.
  * The sums are exact; then fp32, one rounding on output.  A NaN stays one through the ReLU.  Waits are bounded; were one
  * to run out, the rows concerned are NaN.  M = 0 does nothing.  No workspace. */
 bl_status bitlinear_matmul_i8(const int8_t* x_q, int64_t M, int64_t K, int64_t N, int64_t ld_x, const float* x_scale,

@@ -4,8 +4,8 @@
 // tile then.  Without, the grid is persistent: loads run ahead from tile to tile, and two accumulators take turns.
 // A ring slot holds `sub` blocks of 128 bytes of K.  Where K is a whole number of blocks one tensor copy brings the weights of
 // a slot, and one the tokens: a copy costs about 70 clocks and 3.4 per row of 128 bytes (measured on one SM), so small
-// ones are dear.  Without lists the weights do not depend on what comes before on the stream: the first slots of them are
-// asked for ahead of its order.
+// ones are dear.  Without lists it is known at once which weights come first: those of a ring are brought into L2 while the kernel
+// before this one on the stream still runs, and copied from there in the stream's order, so that weights may be written just before.
 // Warp 0 loads (tokens four rows at a time where a list says which), warp 1 multiplies, warps 2-5 take a quarter of the lanes
 // each to y.  Waits are bounded; a tile whose wait runs out is written as NaN.
 #include "matmul_common.cuh"
@@ -58,16 +58,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   const int steps = (blocks + sub - 1) / sub;                // slots' worth of K; this CTA's:
   const int s0 = (int)((int64_t)steps * rank / splits), s1 = (int)((int64_t)steps * (rank + 1) / splits);
   pdl_launch_dependents();
-  auto load_weights = [&](int step, int slot, int n0, int expert) {
-    const uint32_t dst = smem_u32(smem + slot * slot_bytes), bar = smem_u32(&ctl->full[slot]);
-    if (cut.packed) {
-      tma_load_4d(dst, &map_w, 0, n0, step * sub, expert, bar);
-    } else {
-      for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_load_4d(dst + b * kWBlock, &map_w, (step * sub + b) * kRowBytes, n0, 0, expert, bar);
-    }
-  };
   auto copies = [&](int step) { return cut.packed ? 1 : min(sub, blocks - step * sub); };
-  int ahead = 0;                                             // slots whose weights are on their way before the stream's order is waited for
   if (threadIdx.x == 0) {
     prefetch_map(&map_w);
     prefetch_map(&map_x);
@@ -80,10 +71,12 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (!a.offsets && polls != 0) {
       // one expert: the feature tile of the first tile of this CTA
       const int row_tiles = (int)((a.R + kTokens - 1) / kTokens), first_n0 = (int)(item / (uint32_t)row_tiles) * kFeatures;
-      ahead = min(slots, s1 - s0);
-      for (int i = 0; i < ahead; ++i) {
-        mbar_expect_tx(smem_u32(&ctl->full[i]), (uint32_t)(cut.w_bytes * copies(s0 + i)));
-        load_weights(s0 + i, i, first_n0, 0);
+      for (int step = s0; step < min(s0 + slots, s1); ++step) {
+        if (cut.packed) {
+          tma_prefetch_4d(&map_w, 0, first_n0, step * sub, 0);
+        } else {
+          for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_prefetch_4d(&map_w, (step * sub + b) * kRowBytes, first_n0, 0, 0);
+        }
       }
     }
   }
@@ -161,10 +154,14 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         if (lane == 0) {
           ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
           if (ok) {
-            const bool asked = issued < ahead;
             const int x_bytes = a.rows ? fours * 4 * kRowBytes * min(sub, blocks - step * sub) : cut.x_bytes * copies(step);
-            mbar_arrive_expect_tx(bar, (uint32_t)(x_bytes + (asked ? 0 : cut.w_bytes * copies(step))));
-            if (!asked) load_weights(step, slot, n0, w.e);
+            mbar_arrive_expect_tx(bar, (uint32_t)(x_bytes + cut.w_bytes * copies(step)));
+            const uint32_t dst = smem_u32(smem + slot * slot_bytes);
+            if (cut.packed) {
+              tma_load_4d(dst, &map_w, 0, n0, step * sub, w.e, bar);
+            } else {
+              for (int b = 0; b < sub && step * sub + b < blocks; ++b) tma_load_4d(dst + b * kWBlock, &map_w, (step * sub + b) * kRowBytes, n0, 0, w.e, bar);
+            }
           }
         }
         if (a.rows) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
@@ -183,14 +180,9 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         if (++slot == slots) { slot = 0; phase ^= 1u; }
       }
     }
-    // Copies that nobody waits for any more must not land in a CTA that is gone, nor those asked for ahead.
-    if (lane == 0 && *abort_flag) {
+    // Copies that nobody waits for any more must not land in a CTA that is gone.
+    if (lane == 0 && *abort_flag)
       for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
-      for (int i = issued; i < ahead; ++i) {
-        mbar_arrive(smem_u32(&ctl->full[i]));
-        mbar_wait_quiet(smem_u32(&ctl->full[i]), 0);
-      }
-    }
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {

@@ -69,3 +69,42 @@ def test_norm_of_summed_rows_at_the_ends_of_the_range(dt):
         x = (randn(3, 12, K).abs() * size).to(dt)
         check_range(x, ((1 + 0.2 * randn(4, K)) * weight).to(dt), 1e-6, rows, p)
         check_range(x, ((1 + 0.2 * randn(4, K)) * weight).to(dt), 0.0, rows, p)
+
+
+# ---- weights written just before they are used --------------------------------------------------------------
+@pytest.mark.parametrize("M", [1, 40, 300])
+@pytest.mark.parametrize("eps", [-1.0, 1e-6])
+def test_weights_written_by_the_kernel_before(M, eps):
+    """Whatever writes the weights on the stream, a norm that lets its successor start early included, the product sees what it wrote."""
+    N, K = 4096, 2048
+    x, xs = whole(1, -127, 127, M, K), torch.ones(M, device=DEV)
+    latent = [randn(i, N, K, dtype=BF16) for i in range(6)]
+    want = []
+    for w in latent:
+        q, s, _, _ = B.rms_norm_quant(w, eps=eps)
+        torch.cuda.synchronize()
+        want.append(B.matmul_i8(x, xs, q, s, out_dtype=F32))
+    q, s = torch.empty((N, K), dtype=torch.int8, device=DEV), torch.empty(N, device=DEV)
+
+    def run():
+        got = []
+        for w in latent:                                           # the same buffer again and again
+            B.rms_norm_quant(w, eps=eps, x_q=q, scale=s)
+            got.append(B.matmul_i8(x, xs, q, s, out_dtype=F32))
+        for w in latent:                                           # the product before is still running when this one's weights are written
+            B.matmul_i8(x, xs, q, s, out_dtype=F32)
+            B.rms_norm_quant(w, eps=eps, x_q=q, scale=s)
+            got.append(B.matmul_i8(x, xs, q, s, out_dtype=F32))
+        return got
+    for _ in range(3):
+        for a, b in zip(run(), want + want):
+            assert torch.equal(a, b)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = run()
+    for _ in range(3):
+        q.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want + want):
+            assert torch.equal(a, b)
