@@ -315,9 +315,7 @@ __device__ __forceinline__ void far_row(const NormQuantArgs& a, int t, int i, in
 template <typename T, int kChunks, int kThreads, bool kJoin>
 __global__ void __launch_bounds__(kThreads, kChunks == 2 ? 2 : 1) rms_norm_quant_kernel(NormQuantArgs a, int row_threads) {
   __shared__ float2 part[2 * kMaxWarps];
-  // Weights are quantised without the norm, and bitlinear_matmul_i8 reads weights ahead of the stream's order: what follows then starts
-  // when these are written.
-  if (a.eps >= 0.f) pdl_launch_dependents();
+  pdl_launch_dependents();
   const int per_block = blockDim.x == row_threads ? 1 : blockDim.x / row_threads;
   const int in_block = per_block == 1 ? 0 : threadIdx.x / row_threads, i = threadIdx.x - in_block * row_threads;
   RowThreads rt(part, in_block, i, row_threads);
