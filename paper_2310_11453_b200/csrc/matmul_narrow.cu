@@ -135,8 +135,9 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     }
   };
 
+  int issued = 0;                                            // slots that thread 0 filled
   if (warp == 0) {
-    int slot = 0, issued = 0;
+    int slot = 0;
     uint32_t phase = 0;
     bool ok = polls != 0;
     for (Walk w = from; ok && w.valid(); w.next()) {
@@ -180,9 +181,6 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         if (++slot == slots) { slot = 0; phase ^= 1u; }
       }
     }
-    // Copies that nobody waits for any more must not land in a CTA that is gone.
-    if (lane == 0 && *abort_flag)
-      for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
@@ -295,6 +293,11 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   }
   tc_fence_before();
   __syncthreads();
+  // Where a wait ran out, whichever role's and however late, copies may be on their way that nobody waits for any more: they must not
+  // land in a CTA that is gone.  Now that every role is through, thread 0 waits for the last round of the ring; those before it were
+  // waited for to fill the slots again.
+  if (threadIdx.x == 0 && *abort_flag)
+    for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait_quiet(smem_u32(&ctl->full[i % slots]), (uint32_t)(i / slots & 1));
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kCols) : "memory");

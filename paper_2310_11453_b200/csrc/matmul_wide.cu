@@ -40,6 +40,7 @@ struct Control {
   unsigned long long tmem_full[2], tmem_empty[2], drained;      // tmem_empty: rank 0's, for the warps of both
   uint32_t tmem_base;
   int abort_flag;
+  uint32_t filled, relayed;                                     // slots that warp 0, and with listed rows warp 3, reported to full
   alignas(16) float x_scale[kEpiWarps][32];
 };
 inline size_t smem_bytes(int experts) { return 1024 + (size_t)kSlots * kSlotBytes + sizeof(Control) + plan_bytes(experts); }
@@ -68,6 +69,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tmem_full[b]), 1); mbar_init(smem_u32(&ctl->tmem_empty[b]), 2 * kEpiWarps); }
     mbar_init(smem_u32(&ctl->drained), 1);
     ctl->abort_flag = polls == 0;
+    ctl->filled = ctl->relayed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
@@ -86,14 +88,21 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     __syncthreads();
   }
   const uint32_t tmem_base = ctl->tmem_base;
+  // Bounded; who gives up lets both CTAs know.
+  const uint32_t partner_flag = map_to_rank(smem_u32(&ctl->abort_flag), rank ^ 1u);
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_wait_polls(bar, parity, abort_flag, polls)) return true;
+    st_cluster(partner_flag, 1u);
+    return false;
+  };
   const int blocks = (int)((a.K * (kInt ? 1 : 2) + kRowBytes - 1) / kRowBytes);
 
-  if (*abort_flag && (warp < 4 || warp >= 4 + kEpiWarps)) {
+  if (polls == 0 && (warp < 4 || warp >= 4 + kEpiWarps)) {
     // no waits allowed: nothing is started
   } else if (warp == 0) {
     if (lane == 0) {
       int slot = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, filled = 0;
       const uint32_t full0 = map_to_rank(smem_u32(&ctl->full[0]), 0);
       bool ok = true;
       for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); ok && w.valid(); w.next()) {
@@ -102,7 +111,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         for (int kb = 0; kb < blocks; kb += kSub) {
           const int n = min(kSub, blocks - kb);
           const uint32_t bar = full0 + 8u * (uint32_t)slot;
-          ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+          ok = wait(smem_u32(&ctl->empty[slot]), phase ^ 1u);
           if (!ok) break;
           mbar_arrive_expect_tx_cluster(bar, (uint32_t)(tx_bytes * n));
           for (int b = 0; b < n; ++b) {
@@ -111,15 +120,13 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
             tma_load_4d_pair(dst, &map_w, c, n0, 0, w.e, bar);
             if (!a.rows) tma_load_2d_pair(dst + kABytes, &map_x, c, w.row0 + mine, bar);
           }
+          ++filled;
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
         }
       }
-      // Every copy is read by a product that the epilogue waits for.  Where a wait ran out, copies may be on their way that nobody
-      // waits for, counted on the partner's barrier: they get the time of a thousand copies.
-      if (*abort_flag && polls != 0) {
-        const unsigned long long t0 = global_ns();
-        while (global_ns() - t0 < 5000000ull) {}
-      }
+      ctl->filled = filled;
+      // The last products report their slots to both CTAs: this one is there until they have.
+      for (uint32_t i = filled > kSlots ? filled - kSlots : 0u; ok && i < filled; ++i) ok = wait(smem_u32(&ctl->empty[i % kSlots]), i / kSlots & 1u);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -133,10 +140,10 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const uint32_t buf = pass & 1u, d = tmem_base + buf * (uint32_t)kMostRows;
         w.locate(kUnit);
         const uint32_t desc = idesc | (uint32_t)(padded(w.rows) >> 3) << 17;
-        if (!(ok = mbar_wait_polls(smem_u32(&ctl->tmem_empty[buf]), ((pass >> 1) & 1u) ^ 1u, abort_flag, polls))) break;
+        if (!(ok = wait(smem_u32(&ctl->tmem_empty[buf]), ((pass >> 1) & 1u) ^ 1u))) break;
         tc_fence_after();
         for (int kb = 0; kb < blocks; kb += kSub) {
-          if (!(ok = mbar_wait_polls(smem_u32(&ctl->full[slot]), phase, abort_flag, polls))) break;
+          if (!(ok = wait(smem_u32(&ctl->full[slot]), phase))) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem + (size_t)slot * kSlotBytes);
           const int n = min(kSub, blocks - kb);
@@ -180,7 +187,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       }
       for (int kb = 0; kb < blocks; kb += kSub) {
         const int n = min(kSub, blocks - kb);
-        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->empty[slot]), phase ^ 1u, abort_flag, polls);
+        if (lane == 0) ok = wait(smem_u32(&ctl->empty[slot]), phase ^ 1u);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
         if (!ok) break;
         for (int b = 0; b < n; ++b) {
@@ -205,17 +212,19 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     // Rows by a list: hands the copies of a slot over to the tensor cores' side of memory and reports them.
     if (lane == 0 && a.rows) {
       int slot = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, relayed = 0;
       bool ok = true;
       const uint32_t full0 = map_to_rank(smem_u32(&ctl->full[0]), 0);
       for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); ok && w.valid(); w.next()) {
         for (int kb = 0; kb < blocks; kb += kSub) {
-          if (!(ok = mbar_wait_polls(smem_u32(&ctl->gathered[slot]), phase, abort_flag, polls))) break;
+          if (!(ok = wait(smem_u32(&ctl->gathered[slot]), phase))) break;
           fence_proxy_async_smem();
           mbar_arrive_cluster(full0 + 8u * (uint32_t)slot);
+          ++relayed;
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
         }
       }
+      ctl->relayed = relayed;
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -224,7 +233,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     float* x_scale = ctl->x_scale[warp - 4];
     TY* y = reinterpret_cast<TY*>(a.y);
     const TY* res = reinterpret_cast<const TY*>(a.residual);
-    bool ok = !*abort_flag;
+    bool ok = polls != 0;
     uint32_t pass = 0;
     const uint32_t release = map_to_rank(smem_u32(&ctl->tmem_empty[0]), 0);
     for (Walk w(plan, a.experts, feature_tiles, blockIdx.x >> 1, gridDim.x >> 1); w.valid(); w.next(), ++pass) {
@@ -239,7 +248,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
           scale_of[i] = a.x_scale && c0 + 64 * i + lane < w.rows ? a.x_scale[source_row(a, w.row0 + c0 + 64 * i + lane)] : 1.f;
       }
       if (ok) {
-        if (lane == 0) ok = mbar_wait_polls(smem_u32(&ctl->tmem_full[buf]), (pass >> 1) & 1u, abort_flag, polls);
+        if (lane == 0) ok = wait(smem_u32(&ctl->tmem_full[buf]), (pass >> 1) & 1u);
         ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
       }
       tc_fence_after();
@@ -302,6 +311,23 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();                                // the partner no longer touches this CTA's memory
+  if (*abort_flag && polls != 0) {
+    // A wait ran out, whichever role's and however late, and both CTAs know it: copies may be on their way that no product waited for.
+    // They are counted on rank 0's barriers, whose phases still lack the reports that nobody made: rank 0 makes those, then waits.  Only
+    // the last round of the ring can be open: a slot is filled again when the products have read it.
+    if (rank == 0 && threadIdx.x == 0) {
+      const uint32_t reports[4] = {ctl->filled, ld_cluster(map_to_rank(smem_u32(&ctl->filled), 1)), ctl->relayed,
+                                   ld_cluster(map_to_rank(smem_u32(&ctl->relayed), 1))};
+      const uint32_t most = max(max(reports[0], reports[1]), max(reports[2], reports[3]));
+      for (uint32_t i = most > kSlots ? most - kSlots : 0u; i < most; ++i) {
+        const uint32_t bar = smem_u32(&ctl->full[i % kSlots]);
+        for (int r = 0; r < (a.rows ? 4 : 2); ++r)
+          if (reports[r] <= i) mbar_arrive(bar);
+        mbar_wait_quiet(bar, i / kSlots & 1u);
+      }
+    }
+    cluster_sync_all();
+  }
   if (warp == 2) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");

@@ -10,7 +10,7 @@ import torch
 
 from paper_2310_11453_b200 import binding as B
 from tests import layers8_ref as R
-from tests.test_gpu_layers8 import BF16, DEV, E, F32, check, randn, whole
+from tests.test_gpu_layers8 import BF16, DEV, E, F32, check, lists, randn, whole
 
 pytestmark = pytest.mark.gpu
 LEAST = {BF16: 1e-40, F32: 1e-44}
@@ -108,3 +108,41 @@ def test_weights_written_by_the_kernel_before(M, eps):
         torch.cuda.synchronize()
         for a, b in zip(got, want + want):
             assert torch.equal(a, b)
+
+
+# ---- waits that run out ---------------------------------------------------------------------------------------
+def limited(polls, call):
+    B.debug_wait_limit(polls)
+    try:
+        return call()
+    finally:
+        B.debug_wait_limit(-1)
+
+
+def right_or_nan(got, want):
+    bad = torch.isnan(got)
+    return torch.equal(got[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("polls", [1, 2, 5, 30])
+@pytest.mark.parametrize("M,K,N,listed", [(2, 4096, 600, False), (50, 2048, 600, False), (50, 8192, 128, False), (300, 1024, 512, False), (300, 4096, 2048, False),
+                                          (9, 1024, 600, True), (300, 2048, 1024, True)])
+def test_copies_of_a_call_that_gave_up_do_not_reach_the_next(polls, M, K, N, listed):
+    """A call whose waits run out leaves nothing on its way: calls right behind it, on the same SMs and the same shared memory, are right."""
+    x, w = whole(1, -9, 9, M, K), whole(2, -9, 9, N, K)
+    rows, offsets = whole(3, 0, M - 1, M, dtype=torch.int32), lists([M])
+    y = torch.empty((M, N), device=DEV)
+
+    def call(y):
+        return B.matmul_grouped(x, w[None], offsets, rows, y=y) if listed else B.matmul_i8(x, None, w, None, y=y)
+    want = call(torch.empty((M, N), device=DEV))
+    z = randn(5, 100, 64)
+    chosen = B.route_topk(z, 4)[0].clone()
+    codes = B.rms_norm_quant(z)[0].clone()
+    torch.cuda.synchronize()
+    for _ in range(12):
+        got = limited(polls, lambda: call(y))
+        after = call(torch.empty((M, N), device=DEV))
+        route, q = B.route_topk(z, 4)[0], B.rms_norm_quant(z)[0]
+        assert torch.equal(after, want) and torch.equal(route, chosen) and torch.equal(q, codes)
+        assert right_or_nan(got, want)
