@@ -232,9 +232,11 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         tmem_ld16(taddr + (uint32_t)c, r);
         if (feature.on) put(feature, w.row0 + c, n, w.rows - c, r, ctl->x_scale[quarter] + c, ok);
       }
+      // One that gave up reports nothing more: its report would stand for a warp that still reads, and the next products would go over
+      // what that one reads.  The multiplying warp gives up as well then, and every tile from here on is NaN.
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->taken[buf]));
+      if (ok && lane == 0) mbar_arrive(smem_u32(&ctl->taken[buf]));
     }
   }
 

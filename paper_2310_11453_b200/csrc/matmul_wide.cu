@@ -302,9 +302,11 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
             if (j < here) out[j * a.ld_y] = out_cast<TY>(v[j]);
         }
       }
+      // One that gave up reports nothing more: its report would stand for a warp, of either CTA, that still reads, and the next products
+      // would go over what that one reads.  The multiplying warp gives up as well then, and every tile from here on is NaN.
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(release + 8u * buf);
+      if (ok && lane == 0) mbar_arrive_cluster(release + 8u * buf);
     }
   }
 

@@ -146,3 +146,19 @@ def test_copies_of_a_call_that_gave_up_do_not_reach_the_next(polls, M, K, N, lis
         route, q = B.route_topk(z, 4)[0], B.rms_norm_quant(z)[0]
         assert torch.equal(after, want) and torch.equal(route, chosen) and torch.equal(q, codes)
         assert right_or_nan(got, want)
+
+
+@pytest.mark.parametrize("polls", [1, 2, 4, 10, 30, 100])
+@pytest.mark.parametrize("M,K,N,listed", [(4096, 256, 8192, False), (2500, 512, 4096, True), (64, 128, 120000, False), (40, 512, 100000, True)])
+def test_waits_that_run_out_with_many_tiles_to_come(polls, M, K, N, listed):
+    """Some warps give up while others still read their sums: every value is right or NaN, whichever tile it is of."""
+    x, w = whole(1, -9, 9, M, K), whole(2, -9, 9, N, K)
+    rows, offsets = whole(3, 0, M - 1, M, dtype=torch.int32), lists([M])
+
+    def call():
+        return B.matmul_grouped(x, w[None], offsets, rows, out_dtype=F32) if listed else B.matmul_i8(x, None, w, None, out_dtype=F32)
+    want = call()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        assert right_or_nan(limited(polls, call), want)
+        assert torch.equal(call(), want)
