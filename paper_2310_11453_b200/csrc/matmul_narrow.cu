@@ -57,7 +57,6 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   const int blocks = (int)((a.K * es + kRowBytes - 1) / kRowBytes);
   const int steps = (blocks + sub - 1) / sub;                // slots' worth of K; this CTA's:
   const int s0 = (int)((int64_t)steps * rank / splits), s1 = (int)((int64_t)steps * (rank + 1) / splits);
-  pdl_launch_dependents();
   auto copies = [&](int step) { return cut.packed ? 1 : min(sub, blocks - step * sub); };
   if (threadIdx.x == 0) {
     prefetch_map(&map_w);
@@ -83,6 +82,7 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    pdl_launch_dependents();                       // not before the tensor memory is ours: a kernel behind this one may take some, then wait for this one
   }
   __syncwarp();
   if (warp == 2 && !a.offsets) make_plan(a, plan, kTokens);

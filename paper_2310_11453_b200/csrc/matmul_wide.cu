@@ -57,7 +57,6 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  pdl_launch_dependents();
   if (threadIdx.x == 0) {
     prefetch_map(&map_w);
     prefetch_map(&map_x);
@@ -75,6 +74,7 @@ matmul_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   if (warp == 2) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    pdl_launch_dependents();                       // not before the tensor memory is ours: a kernel behind this one may take some, then wait for this one
   }
   if (warp == 3 && !a.offsets) make_plan(a, plan, tile_rows);
   tc_fence_before();
