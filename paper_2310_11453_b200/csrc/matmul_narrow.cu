@@ -85,14 +85,14 @@ matmul_narrow_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     pdl_launch_dependents();                       // not before the tensor memory is ours: a kernel behind this one may take some, then wait for this one
   }
   __syncwarp();
-  if (warp == 2 && !a.offsets) make_plan(a, plan, kTokens);
-  pdl_wait();
-  if (warp == 2 && a.offsets) make_plan(a, plan, kTokens);
+  if (a.offsets) pdl_wait();
+  if (warp == 2) make_plan(a, plan, kTokens);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (splits > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // this CTA is there: its memory may be written
   const uint32_t tmem_base = ctl->tmem_base;
+  if (!a.offsets) pdl_wait();                        // so far nothing that the kernel before could have written was read
   const Walk from(plan, a.experts, cut.feature_tiles, item, items);
   const int quarter = warp & 3, f = quarter * 32 + lane;
   const bool writer = warp >= 2;
