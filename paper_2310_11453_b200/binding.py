@@ -591,7 +591,8 @@ def rms_norm_quant(x, weight=None, eps=1e-6, residual=None, rows=None, row_weigh
     """bitlinear_rms_norm_quant.  x [T, K] f32, fp16 or bf16, or with rows int32 [T, top_k] (and row_weights f32 of that shape) the
     rows [x_rows, K] to be summed up; weight [K]; residual [T, K]; eps < 0 leaves the norm and the weight out (x is only quantised:
     a weight matrix [N, K] gets a scale per output channel).  h (the sum), y (the normed values) and x_q (the codes, with `scale`
-    f32 [T]) are outputs: a tensor to write to, True for a new one, None for none.  Returns (x_q, scale, h, y)."""
+    f32 [T]) are outputs: a tensor to write to, True for a new one, None for none.  Returns (x_q, scale, h, y).  New codes and scales
+    of up to 1 MiB together share one storage, which lives as long as either."""
     r = (_fast or _marshal()).norm_quant(x, weight, eps, residual, rows, row_weights, h, y, x_q, scale)
     if type(r) is int:
         _check(r, "bitlinear_rms_norm_quant")
@@ -614,7 +615,8 @@ def route_topk_ws_bytes(T, experts) -> int:
 def route_topk(logits, top_k, normalise=True, positions=None, ws=None, chosen=None, weights=None, offsets=None, rows=None, places=None):
     """bitlinear_route_topk.  logits [T, experts] f32, fp16 or bf16; positions int32 [T] or None (negative: padding, which visits no
     expert).  Returns (chosen int32 [T, top_k], weights f32 [T, top_k], offsets int32 [experts+1], rows int32 [T*top_k], places int32
-    [T, top_k]), each of which may be given; with padding, entries of new rows behind offsets[-1] hold anything."""
+    [T, top_k]), each of which may be given; with padding, entries of new rows behind offsets[-1] hold anything.  New ones of up to
+    1 MiB together share one storage, which lives as long as any of them."""
     r = (_fast or _marshal()).route(logits, top_k, normalise, positions, ws, chosen, weights, offsets, rows, places)
     if type(r) is int:
         _check(r, "bitlinear_route_topk")

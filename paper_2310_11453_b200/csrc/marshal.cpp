@@ -350,6 +350,8 @@ int truth(PyObject* o) {
 }
 
 // One allocation for several small tensors that belong together: an allocation costs about as much as the rest of a call's marshalling.
+// Each keeps the memory of all alive, so only up to kPooled bytes.
+constexpr int64_t kPooled = 1 << 20;
 struct Pool {
   Tensor bytes;
   int64_t used = 0;
@@ -399,7 +401,7 @@ PyObject* norm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::cuda::CUDAGuard guard(dev);
     const Tensor h = output(a[6], "h", T, K, x.options()), y = output(a[7], "y", T, K, x.options());
     Tensor q, scale;
-    if (a[8] == Py_True && !given(a[9])) {                      // new codes and new scales
+    if (a[8] == Py_True && !given(a[9]) && T * K + 4 * T <= kPooled) {      // new codes and new scales
       Pool pool{at::empty({Pool::room(T * K) + Pool::room(4 * T)}, x.options().dtype(at::kByte))};
       q = pool.take({T, K}, at::kChar);
       scale = pool.take({T}, at::kFloat);
@@ -472,13 +474,15 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
     // new outputs come from one allocation
     const bool news[5] = {!given(a[5]), !given(a[6]), !given(a[7]), !given(a[8]), !given(a[9])};
     const int64_t room = (news[0] + news[1] + news[3] + news[4]) * pairs + news[2] * list;
+    const bool pooled = room > 0 && room <= kPooled;
     Pool pool;
-    if (room > 0) pool.bytes = at::empty({room}, z.options().dtype(at::kByte));
-    const Tensor chosen = news[0] ? pool.take({T, k}, at::kInt) : tensor(a[5], "chosen");
-    const Tensor weights = news[1] ? pool.take({T, k}, at::kFloat) : tensor(a[6], "weights");
-    const Tensor offsets = news[2] ? pool.take({E + 1}, at::kInt) : tensor(a[7], "offsets");
-    const Tensor rows = news[3] ? pool.take({T * k}, at::kInt) : tensor(a[8], "rows");
-    const Tensor places = news[4] ? pool.take({T, k}, at::kInt) : tensor(a[9], "places");
+    if (pooled) pool.bytes = at::empty({room}, z.options().dtype(at::kByte));
+    auto out = [&](int i, const char* name, at::IntArrayRef sizes, at::ScalarType type) {
+      return !news[i] ? tensor(a[5 + i], name) : pooled ? pool.take(sizes, type) : at::empty(sizes, z.options().dtype(type));
+    };
+    const Tensor chosen = out(0, "chosen", {T, k}, at::kInt), weights = out(1, "weights", {T, k}, at::kFloat);
+    const Tensor offsets = out(2, "offsets", {E + 1}, at::kInt), rows = out(3, "rows", {T * k}, at::kInt);
+    const Tensor places = out(4, "places", {T, k}, at::kInt);
     void *cp = flat(chosen, "chosen", dev, at::kInt, T, k), *wp = flat(weights, "weights", dev, at::kFloat, T, k);
     void *op = flat(offsets, "offsets", dev, at::kInt, E + 1), *rp = flat(rows, "rows", dev, at::kInt, T * k);
     void* pp = flat(places, "places", dev, at::kInt, T, k);

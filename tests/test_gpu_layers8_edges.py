@@ -162,3 +162,16 @@ def test_waits_that_run_out_with_many_tiles_to_come(polls, M, K, N, listed):
     for _ in range(4):
         assert right_or_nan(limited(polls, call), want)
         assert torch.equal(call(), want)
+
+
+# ---- what outputs keep alive ----------------------------------------------------------------------------------
+def test_outputs_keep_little_more_than_themselves_alive():
+    """New outputs may share a storage, of 1 MiB at most: a scale kept does not keep a matrix of codes."""
+    def bytes_of(t):
+        return t.untyped_storage().nbytes()
+    for T, K in ((4096, 2048), (64, 16384), (3, 64)):
+        q, s, _, _ = B.rms_norm_quant(randn(1, T, K, dtype=BF16), eps=-1.0)
+        assert bytes_of(q) <= max(1 << 20, q.numel()) and bytes_of(s) <= max(1 << 20, 4 * T)
+    for T, e, k in ((40000, 64, 8), (20, 8, 2)):
+        out = B.route_topk(randn(1, T, e), k)
+        assert all(bytes_of(t) <= max(1 << 20, 4 * t.numel()) for t in out)
