@@ -164,6 +164,27 @@ def test_waits_that_run_out_with_many_tiles_to_come(polls, M, K, N, listed):
         assert torch.equal(call(), want)
 
 
+# ---- offsets that decrease ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("values", [[0, 300, 5, 700, 2, 900, 900, 20], [900, 0, 900, 0, 900, 0, 900, 0], [5, 4, 3, 2, 1, 0, -1, -2], [-9, 40, 30, 41, 2000, 50, 60, 70],
+                                    [100, 130, 120, 135, 10, 139, 140, 139]])
+@pytest.mark.parametrize("R_", [900, 140])
+@pytest.mark.parametrize("listed", [True, False])
+def test_offsets_that_decrease_give_each_row_to_its_owner(values, R_, listed):
+    """An offset is cut to 0..R, and one below an offset before it counts as that one: so each row has at most one owner."""
+    e, K, N = 7, 64, 300
+    x, w = whole(1, -9, 9, R_, K), whole(2, -9, 9, e, N, K)
+    rows = whole(3, 0, R_ - 1, R_, dtype=torch.int32) if listed else None
+    y = torch.full((R_ + 2, N), 9.25, device=DEV)
+    B.matmul_grouped(x, w, torch.tensor(values, dtype=torch.int32, device=DEV), rows, y=y[1:-1])
+    want, reached = torch.full((R_ + 2, N), 9.25, device=DEV, dtype=torch.float64), 0
+    source = x.double() if rows is None else x.double()[rows.long()]
+    for i in range(e):
+        first = max(reached, min(max(values[i], 0), R_))
+        reached = max(first, min(max(values[i + 1], 0), R_))
+        want[1 + first:1 + reached] = source[first:reached] @ w[i].double().t()
+    assert torch.equal(y.double(), want)
+
+
 # ---- what outputs keep alive ----------------------------------------------------------------------------------
 def test_outputs_keep_little_more_than_themselves_alive():
     """New outputs may share a storage, of 1 MiB at most: a scale kept does not keep a matrix of codes."""
