@@ -500,7 +500,8 @@ bl_status bitlinear_kv4_copy_pages(void* pages, size_t page_bytes, int64_t num_p
  *   h, y [T, K] strides ld_h, ld_y, x_q int8 [T, K] stride ld_q with scale fp32 [T]: each may be NULL if not wanted,
  *   but not all.  h and y may be residual, or without rows x, themselves (same stride), else outputs overlap nothing.
  *   K a multiple of 8, 8..32768; strides multiples of 8.
- * fp32 throughout; the codes are those of h before it is rounded to dt, and those of exact arithmetic where y / scale is
+ * fp32 throughout, also for rows whose squares or products with the weights leave its range (they are scaled by powers of
+ * two for it); the codes are those of h before it is rounded to dt, and those of exact arithmetic where y / scale is
  * further than 2^-13 from a border between two codes (with rows: and further than the roundings of the sum of
  * top_k + 1 terms).  A row of zeros has codes and scale 0; a row in which a value is not finite has scale NaN and codes 0.
  * T = 0 does nothing.  No workspace. */

@@ -28,7 +28,7 @@ Choice choose(const MatmulArgs& a, int64_t sms) {
   auto rows_of_tile = [&](int64_t tile) { return mean <= tile ? mean : ceil_div(mean, ceil_div(mean, tile)); };
 
   // Wide: rounds of tiles over the pairs of SMs, 0.27 us a block of K and a little for each row; weights at 5.2 TB/s at most.  So large
-  // tiles, unless smaller ones need no more rounds (1000 x 2048 x 2048: 10.3 us with 128 rows, 11.9 with 256; 509 x 2048 x 8192: 15 and 12).
+  // tiles, unless smaller ones need no more rounds (1000 x 2048 x 2048: 9.5 us with 128 rows, 10.6 with 256; 509 x 2048 x 8192: 15.2 and 12.3).
   Choice c{false, 0, 1, 1, 64};
   double least = 0;
   for (int tile = 64; tile <= 256; tile += 64) {
@@ -39,9 +39,9 @@ Choice choose(const MatmulArgs& a, int64_t sms) {
   }
   if (mean > 256) return c;
   // Narrow: 0.24 us a block of K (listed rows 0.035 more for every four), two CTAs on an SM 1.6 times that each; weights at 6.5 TB/s at
-  // most.  K shared by a cluster: as much less of it for each CTA, and a join that grows with the rows (1 x 4096 x 4096 12.6 us in one
-  // piece, 7.6 in four; 64 x 4096 x 4096 13.0 and 10.5; 40 x 2048 x 8192 9.0 in one, 10.9 in two).  Clusters of eight need GPCs with room
-  // for them: one CTA per SM takes 17 us for 40 x 8192 x 2048, two per SM 9.9.
+  // most.  K shared by a cluster: as much less of it for each CTA, and a join that grows with the rows (1 x 4096 x 4096 11.3 us in one
+  // piece, 8.0 in four; 64 x 4096 x 4096 13.0 and 10.5; 40 x 2048 x 8192 8.8 in one, 10.3 in two).  Clusters of eight need GPCs with room
+  // for them: one CTA per SM takes 16.2 us for 40 x 8192 x 2048, two per SM 9.5.
   for (int tokens = mean <= 16 ? 16 : 32; tokens <= (mean <= 16 ? 16 : 64); tokens *= 2) {
     const int64_t tiles = row_tiles(tokens) * features;
     const int64_t most = (a.offsets ? a.R / tokens + met : ceil_div(a.R, tokens)) * features;      // that there can be
@@ -50,8 +50,8 @@ Choice choose(const MatmulArgs& a, int64_t sms) {
       for (int per_sm = 1; per_sm <= 2; ++per_sm) {
         const int64_t room = splits == 8 && per_sm == 1 ? sms * 3 / 4 : sms * per_sm;
         if (splits > 1 && (most * splits > room || blocks < splits)) continue;
-        // Two CTAs per SM where there are more than SMs (8 lists of 5 rows, 4096 x 4096: 23.7 us, one per SM 27.7), else one (some SMs
-        // would get two and others none: 192 x 4096 x 4096 17.3, one per SM 13.7).
+        // Two CTAs per SM where there are more than SMs (8 lists of 5 rows, 4096 x 4096: 24.8 us, one per SM 25.6), else one (some SMs
+        // would get two and others none: 192 x 4096 x 4096 17.4, one per SM 14.0).
         if (splits == 1 ? per_sm != (tiles > sms ? 2 : 1) : per_sm == 2 && tiles * splits <= sms) continue;
         const double rounds = (double)ceil_div(tiles * splits, room);
         const double block = (a.rows ? 0.24 + 0.035 * (double)ceil_div((int64_t)rows, 4) : 0.24 + 0.0006 * tokens) * (per_sm == 2 ? 1.6 : 1.0);

@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, int 
 }
 
 // Many blocks: one per SM.  They need few registers, and two on an SM while another has none take as long as two (8191 tokens over 128
-// experts 12.2 us, so 8.7): each asks for more than half of the shared memory.
+// experts 13.1 us, so 9.1): each asks for more than half of the shared memory.
 constexpr size_t kAlone = 120 * 1024;
 
 template <typename T, int kPer>
